@@ -304,6 +304,92 @@ szo_status szo_attention(const void* q, const void* k, const void* v, void* o, s
 szo_status szo_attention_paired(const void* q, const void* k, const void* v, void* o, int64_t row0, int32_t B,
                                 int32_t S, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, void* stream);
 
+/* ---- Key/value cache in 8 bits, paged, for batches of sequences of different lengths (the paper measures
+ * generation from 4-bit weights, Section 1's speed figure and the appendix on sparse operations; it does not
+ * say how the cache is kept.  With 4-bit weights a 16-bit cache is the larger part of memory and traffic from
+ * a few thousand cached tokens on).
+ *
+ * Cache.  An element is an e4m3 code times a scale 2^e; one e per (page, key/value head), keys and values
+ * apart.  All buffers are the caller's; zeroed memory is a valid empty cache.
+ *   k_codes, v_codes  uint8 [n_pages][n_kv_heads][page_tokens][head_dim]
+ *   scales            fp32  [n_pages][n_kv_heads][2]   (keys, values), powers of two
+ *   page_tokens 16, 32, 64 or 128; head_dim 64 or 128.
+ * Batch.  Position p of sequence b is slot p % page_tokens of page page_table[b][p / page_tokens].
+ *   page_table  int32 [batch][max_pages]  (entries that no position needs are not read)
+ *   kv_len      int32 [batch]    positions of each sequence, its rows of this call among them
+ *   start       int32 [batch+1]  sequence b has the rows start[b] .. start[b+1]-1 of the row buffers, at most
+ *                                max_new of them; NULL: every sequence has max_new rows, b's from b*max_new on
+ *   rows        rows that the row buffers hold (start[b+1] <= rows); rows outside every sequence are not touched
+ * Row i of n stands at position kv_len - n + i.  Rows at negative positions are padding.  Lengths and tables
+ * are read on the device when the work runs: a captured graph serves changing contents.  A sequence whose
+ * description does not fit (negative or decreasing start, more than max_new rows, kv_len beyond
+ * max_pages*page_tokens) is skipped, its rows left as they were, and a needed page id outside [0, n_pages) is treated
+ * as a page without tokens; the device status word reports both (SZO_ERR_SHAPE, SZO_ERR_INVALID_ARG).
+ * Sequences may share pages (a common prefix) as long as no call writes a shared page.  No call allocates
+ * or needs a workspace. */
+typedef struct {
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  float* scales;
+  int64_t n_pages;
+  int32_t page_tokens, n_kv_heads, head_dim;
+} szo_kv8_cache;
+typedef struct {
+  const int32_t* page_table;
+  const int32_t* kv_len;
+  const int32_t* start;
+  int64_t rows;
+  int32_t batch, max_pages, max_new;
+} szo_kv8_batch;
+/* Stores the rows' keys and values.  k, v: dtype (SZO_F32, SZO_BF16, SZO_F16) [rows][n_kv_heads*head_dim], rows
+ * k_stride / v_stride elements apart (a slice of a fused q/k/v buffer will do; rows 16-byte aligned).  For every
+ * page, head and kind with a = the largest finite magnitude among the new elements (up to 448*2^63):
+ *   e(a) = the smallest integer in [-63, 63] with a <= 448 * 2^e(a)
+ *   a page whose first slot this call writes takes e = e(a); another keeps e = max(its e, e(a)), and where that
+ *   grows, the codes of its earlier positions become RN_e4m3(code * 2^(old e - e))
+ *   code = RN_e4m3(x * 2^-e), ties to even; elements that are not finite, or larger, are stored as NaN.
+ * Slots behind the last position are left as they were.  Padding rows are not stored. */
+szo_status szo_kv8_write(const szo_kv8_cache* cache, const szo_kv8_batch* batch, const void* k, const void* v,
+                         szo_dtype dtype, int64_t k_stride, int64_t v_stride, void* stream);
+/* Reads the rows' positions back: k_out, v_out dtype [rows][n_kv_heads*head_dim], code * 2^e rounded once (exact in
+ * fp32 and bf16).  With kv_len rows per sequence this is the whole cache.  Padding rows become zeros. */
+szo_status szo_kv8_read(const szo_kv8_cache* cache, const szo_kv8_batch* batch, void* k_out, void* v_out, szo_dtype dtype,
+                        int64_t k_stride, int64_t v_stride, void* stream);
+/* Causal softmax attention of the rows over the cache: the query at position p attends to positions 0 .. p of its
+ * sequence (its own among them: write first).  o = softmax(scale * q k^T) v, statistics and sums in fp32; q, o: dtype
+ * [rows][n_heads*head_dim], rows q_stride / o_stride elements apart; grouped-query attention when n_kv_heads <
+ * n_heads; scale finite (1/sqrt(head_dim) for szo_attention's).  A row that attends to nothing (padding) becomes zeros.
+ * A NaN element of the cache reaches the rows that attend to it and no others. */
+szo_status szo_attention_kv8(const szo_kv8_cache* cache, const szo_kv8_batch* batch, const void* q, int64_t q_stride,
+                             void* o, int64_t o_stride, szo_dtype dtype, int32_t n_heads, float scale, void* stream);
+
+/* ---- Log probabilities of given tokens (the quantity that the losses of Section 2 and the candidate comparison of
+ * the classification experiments are made of), with the distribution's entropy and best alternatives.  Row r of
+ * logits (dtype SZO_F32, SZO_BF16 or SZO_F16 [rows][vocab], rows row_stride >= vocab elements apart, any alignment of
+ * rows) is x = scale * logits[r] (scale > 0: one over the temperature), p = softmax(x):
+ *   logp[r][i]   fp32 [rows][n_targets]  x[t] - lse, t = targets[r][i] (int32); 0 where t < 0 (padding); t >= vocab:
+ *                NaN, and the device status word reports SZO_ERR_INVALID_ARG.  n_targets in [0, 64]
+ *   entropy[r]   fp32 [rows] or NULL     - sum p log p (terms with p = 0 count nothing)
+ *   lse[r]       fp32 [rows] or NULL     log sum exp x
+ *   top_ids[r], top_logp[r]  int32, fp32 [rows][n_top], n_top in [0, min(32, vocab)]: the tokens of the largest logits
+ *                in falling order, equal logits by rising index, and their log probabilities
+ * Logits of -inf are masked tokens (log probability -inf); a row with nothing else has lse -inf and entropy 0.  A row
+ * that holds a NaN or +inf has NaN results (its top_ids order NaN before everything).  x and all sums are held in
+ * fp32: an x beyond its range is -inf or +inf and counts as such (the lowest fp32 or bf16 number times a scale above 1). */
+szo_status szo_token_logprobs(const void* logits, szo_dtype dtype, int64_t rows, int64_t vocab, int64_t row_stride,
+                              float scale, const int32_t* targets, int32_t n_targets, int32_t n_top, float* logp,
+                              float* entropy, float* lse, int32_t* top_ids, float* top_logp, void* stream);
+/* Its gradient.  With d_logp [rows][n_targets] and d_entropy [rows] (NULL: zeros; else entropy is needed) the gradients
+ * of the results, and lse and entropy as szo_token_logprobs gave them:
+ *   d_logits[j] = scale * ( sum_i d_logp[i] (1[j = t_i] - p_j) - d_entropy * p_j (log p_j + entropy) )
+ * in fp32, rounded once to dtype; targets outside [0, vocab) count nothing; the same target twice counts twice.
+ * d_logits [rows][vocab], rows d_row_stride elements apart, may be logits itself (equal strides).  A row whose lse is
+ * -inf gets zeros. */
+szo_status szo_token_logprobs_bwd(const void* logits, szo_dtype dtype, int64_t rows, int64_t vocab, int64_t row_stride,
+                                  float scale, const int32_t* targets, int32_t n_targets, const float* lse,
+                                  const float* entropy, const float* d_logp, const float* d_entropy, void* d_logits,
+                                  int64_t d_row_stride, void* stream);
+
 typedef struct szo_model szo_model_t;
 /* layers_host: host array of n_layers entries holding device pointers.  S_all: fp32 [k_total],
  * the trainable sparse values of all linears concatenated in model order (the only mutable

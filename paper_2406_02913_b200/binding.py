@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -37,6 +38,16 @@ class ModelConfig(C.Structure):
                 ("rope_base", C.c_float), ("group", C.c_int32), ("sz_dtype", C.c_int32),
                 ("act_dtype", C.c_int32), ("linear_mode", C.c_int32), ("loss_kind", C.c_int32),
                 ("max_batch", C.c_int32), ("max_seq", C.c_int32)]
+
+
+class Kv8CacheStruct(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("scales", C.c_void_p), ("n_pages", C.c_int64),
+                ("page_tokens", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class Kv8BatchStruct(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("kv_len", C.c_void_p), ("start", C.c_void_p), ("rows", C.c_int64),
+                ("batch", C.c_int32), ("max_pages", C.c_int32), ("max_new", C.c_int32)]
 
 
 class LinearWeights(C.Structure):
@@ -100,6 +111,15 @@ _SIGS = {
                                          C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]),
     "szo_attention": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int32, C.c_int32,
                                   C.c_int32, C.c_int32, C.c_int32, C.c_void_p]),
+    "szo_kv8_write": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_void_p]),
+    "szo_kv8_read": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_void_p]),
+    "szo_attention_kv8": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_int32,
+                                      C.c_float, C.c_void_p]),
+    "szo_token_logprobs": (C.c_int32, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_float, C.c_void_p, C.c_int32,
+                                       C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "szo_token_logprobs_bwd": (C.c_int32, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_float, C.c_void_p,
+                                           C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
+                                           C.c_void_p]),
     "szo_model_create": (C.c_int32, [C.POINTER(C.c_void_p), C.POINTER(ModelConfig),
                                      C.POINTER(ModelWeights), C.POINTER(LayerWeights), C.c_void_p,
                                      C.c_void_p]),
@@ -342,6 +362,186 @@ def szo_attention(q, k, v, B: int, S: int, n_heads: int, n_kv_heads: int, head_d
     _check(lib().szo_attention(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _DT[q.dtype], B, S, n_heads, n_kv_heads,
                                head_dim, _stream()))
     return o
+
+
+# ------------------------------------------------------------------------------ 8-bit key/value cache
+def _here(t, dtype=None, name="tensor"):
+    """t is a CUDA tensor of the current device (the library launches there) and of the given type."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be a CUDA tensor of the current device (got {t.device})")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
+    return t
+
+
+class Kv8Cache:
+    """Paged key/value cache of e4m3 codes with a power-of-two scale per (page, head) (szo_kv8_cache).
+    codes: uint8 CUDA tensor [2, n_pages, n_kv_heads, page_tokens, head_dim] (keys, values); scales: fp32
+    [n_pages, n_kv_heads, 2].  Zeroed tensors are an empty cache; Kv8Cache.empty makes them."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        _here(codes, torch.uint8, "codes")
+        _here(scales, torch.float32, "scales")
+        if codes.dim() != 5 or codes.shape[0] != 2 or tuple(scales.shape) != (codes.shape[1], codes.shape[2], 2):
+            raise ValueError("codes must be [2, n_pages, n_kv_heads, page_tokens, head_dim] and scales [n_pages, n_kv_heads, 2]")
+        if not codes.is_contiguous() or not scales.is_contiguous():
+            raise ValueError("codes and scales must be contiguous")
+        self.codes, self.scales = codes, scales
+        _, self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = codes.shape
+        self.struct = Kv8CacheStruct(codes[0].data_ptr(), codes[1].data_ptr(), scales.data_ptr(), self.n_pages, self.page_tokens,
+                                     self.n_kv_heads, self.head_dim)
+        self.ref = C.addressof(self.struct)
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv_heads: int, page_tokens: int, head_dim: int, device="cuda"):
+        return cls(torch.zeros((2, n_pages, n_kv_heads, page_tokens, head_dim), dtype=torch.uint8, device=device),
+                   torch.zeros((n_pages, n_kv_heads, 2), dtype=torch.float32, device=device))
+
+
+class Kv8Batch:
+    """Which rows of a call stand at which cached positions (szo_kv8_batch): page_table int32 [batch, max_pages],
+    kv_len int32 [batch] (positions of each sequence, the call's rows among them), start int32 [batch + 1] with
+    max_new (rows of each sequence, at most max_new), or None: rows // batch rows each.  The tensors are read
+    when the work runs, so their contents may change between calls."""
+
+    def __init__(self, page_table: torch.Tensor, kv_len: torch.Tensor, rows: int, start: torch.Tensor | None = None,
+                 max_new: int | None = None):
+        batch = kv_len.numel()
+        for name, t in (("page_table", page_table), ("kv_len", kv_len), ("start", start)):
+            if t is not None:
+                _here(t, torch.int32, name)
+                if not t.is_contiguous():
+                    raise ValueError(f"{name} must be contiguous")
+        if page_table.dim() != 2 or page_table.shape[0] != batch or (start is not None and start.numel() != batch + 1):
+            raise ValueError("page_table must be [batch, max_pages], kv_len [batch] and start [batch + 1]")
+        if start is None:
+            if batch and rows % batch:
+                raise ValueError("without start, rows must be a multiple of the batch")
+            max_new = rows // batch if batch else 0
+        elif max_new is None:
+            raise ValueError("start needs max_new, the most rows that a sequence has")
+        self.page_table, self.kv_len, self.start, self.rows = page_table, kv_len, start, rows
+        self.struct = Kv8BatchStruct(page_table.data_ptr() or None, kv_len.data_ptr() or None,
+                                     None if start is None else start.data_ptr(), rows, batch, page_table.shape[1], max_new)
+        self.ref = C.addressof(self.struct)
+
+
+def _row_buffer(t, rows: int, heads: int, head_dim: int, name: str):
+    """Row stride in elements of [rows, heads, head_dim] or [rows, heads * head_dim], rows possibly apart."""
+    _here(t, None, name)
+    inner = t.stride(-1) == 1 and (t.dim() == 2 or t.dim() == 3 and (t.shape[1] == 1 or t.stride(1) == head_dim))
+    if t.shape[0] != rows or t.numel() != rows * heads * head_dim or (rows and not inner):
+        raise ValueError(f"{name} must be [{rows}, {heads}, {head_dim}] or [{rows}, {heads * head_dim}] with contiguous rows")
+    if t.dtype not in _DT:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16 (got {t.dtype})")
+    return t.stride(0) if rows > 1 else heads * head_dim
+
+
+def _kv8_stream(cache, batch):
+    if cache.codes.device != batch.kv_len.device or cache.codes.device.index != torch.cuda.current_device():
+        raise ValueError("cache and batch must be on the current device")
+    return _stream()
+
+
+def szo_kv8_write(cache: Kv8Cache, batch: Kv8Batch, k: torch.Tensor, v: torch.Tensor):
+    """Stores the rows' keys and values ([rows, n_kv_heads, head_dim] or [rows, n_kv_heads * head_dim], fp32, bf16 or fp16)."""
+    st = _kv8_stream(cache, batch)
+    ks = _row_buffer(k, batch.rows, cache.n_kv_heads, cache.head_dim, "k")
+    vs = _row_buffer(v, batch.rows, cache.n_kv_heads, cache.head_dim, "v")
+    if k.dtype != v.dtype:
+        raise ValueError("k and v must have the same type")
+    if batch.rows:
+        _check(lib().szo_kv8_write(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), _DT[k.dtype], ks, vs, st))
+
+
+def szo_kv8_read(cache: Kv8Cache, batch: Kv8Batch, dtype=torch.bfloat16, out=None):
+    """The rows' cached keys and values as (k, v), each [rows, n_kv_heads, head_dim] of dtype (or of `out`)."""
+    st = _kv8_stream(cache, batch)
+    shape = (batch.rows, cache.n_kv_heads, cache.head_dim)
+    k, v = out if out is not None else (torch.empty(shape, dtype=dtype, device=cache.codes.device) for _ in range(2))
+    ks = _row_buffer(k, batch.rows, cache.n_kv_heads, cache.head_dim, "k")
+    vs = _row_buffer(v, batch.rows, cache.n_kv_heads, cache.head_dim, "v")
+    if k.dtype != v.dtype:
+        raise ValueError("k and v must have the same type")
+    if batch.rows:
+        _check(lib().szo_kv8_read(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), _DT[k.dtype], ks, vs, st))
+    return k, v
+
+
+def szo_attention_kv8(cache: Kv8Cache, batch: Kv8Batch, q: torch.Tensor, scale: float | None = None, out=None):
+    """Causal attention of the rows q ([rows, n_heads, head_dim] or [rows, n_heads * head_dim]) over the cache,
+    which already holds their own keys and values.  scale: 1 / sqrt(head_dim) where None.  Returns o like q."""
+    st = _kv8_stream(cache, batch)
+    d = cache.head_dim
+    width = q.numel() // batch.rows if batch.rows else d * cache.n_kv_heads
+    if width % d:
+        raise ValueError(f"q must be [rows, n_heads, {d}] or [rows, n_heads * {d}]")
+    qs = _row_buffer(q, batch.rows, width // d, d, "q")
+    o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    os_ = _row_buffer(o, batch.rows, width // d, d, "out")
+    if o.dtype != q.dtype:
+        raise ValueError("out must have q's type")
+    if batch.rows:
+        _check(lib().szo_attention_kv8(cache.ref, batch.ref, q.data_ptr(), qs, o.data_ptr(), os_, _DT[q.dtype], width // d,
+                                       d ** -0.5 if scale is None else scale, st))
+    return o
+
+
+# ------------------------------------------------------------------------------ log probabilities
+class TokenLogprobs(NamedTuple):
+    logp: torch.Tensor          # fp32 [rows, n_targets]
+    entropy: torch.Tensor       # fp32 [rows]
+    lse: torch.Tensor           # fp32 [rows]
+    top_ids: torch.Tensor       # int32 [rows, n_top]
+    top_logp: torch.Tensor      # fp32 [rows, n_top]
+
+
+def _logit_rows(logits, targets):
+    _here(logits, None, "logits")
+    if logits.dim() != 2 or logits.dtype not in _DT or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be [rows, vocab], float32, bfloat16 or float16, with contiguous rows")
+    rows, vocab = logits.shape
+    if targets is not None:
+        _here(targets, torch.int32, "targets")
+        if targets.dim() != 2 or targets.shape[0] != rows or not targets.is_contiguous():
+            raise ValueError("targets must be a contiguous int32 tensor [rows, n_targets]")
+    return rows, vocab, logits.stride(0) if rows > 1 else vocab, 0 if targets is None else targets.shape[1]
+
+
+def szo_token_logprobs(logits: torch.Tensor, targets: torch.Tensor | None = None, n_top: int = 0, scale: float = 1.0) -> TokenLogprobs:
+    """Log probabilities of targets[r] (int32 [rows, n_targets], negative: none) under softmax(scale * logits[r]), with
+    the entropy, log sum exp and the n_top best alternatives of every row."""
+    rows, vocab, ld, nt = _logit_rows(logits, targets)
+    f = torch.empty(rows * (nt + 2 + n_top) + 16, dtype=torch.float32, device=logits.device)
+    sizes, parts, at = (rows * nt, rows, rows, rows * n_top), [], 0
+    for n in sizes:                                     # one allocation; every part starts on 16 bytes
+        parts.append(f[at:at + n])
+        at += -(-n // 4) * 4
+    logp, entropy, lse, top_logp = parts
+    top_ids = torch.empty((rows, n_top), dtype=torch.int32, device=logits.device)
+    if rows:
+        _check(lib().szo_token_logprobs(logits.data_ptr(), _DT[logits.dtype], rows, vocab, ld, scale, None if nt == 0 else targets.data_ptr(),
+                                        nt, n_top, logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), top_ids.data_ptr(),
+                                        top_logp.data_ptr(), _stream()))
+    return TokenLogprobs(logp.view(rows, nt), entropy, lse, top_ids, top_logp.view(rows, n_top))
+
+
+def szo_token_logprobs_bwd(logits: torch.Tensor, targets: torch.Tensor | None, lse: torch.Tensor, entropy: torch.Tensor | None,
+                           d_logp: torch.Tensor | None, d_entropy: torch.Tensor | None = None, scale: float = 1.0, out=None):
+    """Gradient of sum(d_logp * logp) + sum(d_entropy * entropy) with respect to the logits; `out` may be the logits."""
+    rows, vocab, ld, nt = _logit_rows(logits, targets)
+    for name, t, n in (("lse", lse, rows), ("entropy", entropy, rows), ("d_logp", d_logp, rows * nt), ("d_entropy", d_entropy, rows)):
+        if t is not None and (_here(t, torch.float32, name).numel() != n or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous float32 tensor of {n} values")
+    d = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device) if out is None else out
+    _here(d, logits.dtype, "out")
+    if d.shape != logits.shape or (vocab > 1 and d.stride(1) != 1):
+        raise ValueError("out must have the logits' shape and contiguous rows")
+    p = lambda t: None if t is None or not t.numel() else t.data_ptr()
+    if rows:
+        _check(lib().szo_token_logprobs_bwd(logits.data_ptr(), _DT[logits.dtype], rows, vocab, ld, scale, p(targets), nt, p(lse), p(entropy),
+                                            p(d_logp), p(d_entropy), d.data_ptr(), d.stride(0) if rows > 1 else vocab, _stream()))
+    return d
 
 
 # ------------------------------------------------------------------------------ model

@@ -35,9 +35,19 @@ int32_t* device_status_word() {
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
   std::lock_guard<std::mutex> lock(mu);
   if (!words[dev]) {
+    // The first call on a device may come from inside a stream capture, of this thread or another: the
+    // allocation and the clearing then run outside it (relaxed mode, a stream of their own).
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    cudaThreadExchangeStreamCaptureMode(&mode);
     int32_t* p = nullptr;
-    if (cudaMalloc(&p, sizeof(int32_t)) != cudaSuccess) return nullptr;
-    cudaMemset(p, 0, sizeof(int32_t));
+    cudaStream_t st = nullptr;
+    bool ok = cudaMalloc(&p, sizeof(int32_t)) == cudaSuccess &&
+              cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking) == cudaSuccess &&
+              cudaMemsetAsync(p, 0, sizeof(int32_t), st) == cudaSuccess && cudaStreamSynchronize(st) == cudaSuccess;
+    if (st) cudaStreamDestroy(st);
+    if (!ok && p) cudaFree(p);
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    if (!ok) return nullptr;
     words[dev] = p;
   }
   return words[dev];
