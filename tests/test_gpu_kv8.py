@@ -343,8 +343,9 @@ def test_offsets_beyond_32_bits(B):
     for new in (1, 40):
         q = torch.from_numpy(g.normal(0, 1, (new, 2 * hkv, d))).bfloat16()
         o = B.szo_attention_kv8(cache, B.Kv8Batch(table, kv_len, new), q.cuda()).double().cpu().numpy()
-        want, wide, big, _ = ref.attention(q.double().numpy(), small.values(range(4), n, 0), small.values(range(4), n, 1), n - new, d ** -0.5)
-        assert (np.abs(o - want) <= attention_bound(want, wide, big, n, d, "bf16")).all()
+        size = 2.0 ** small.e[np.arange(n) // page, :, 1]
+        want, wide, big, top = ref.attention(q.double().numpy(), small.values(range(4), n, 0), small.values(range(4), n, 1), n - new, d ** -0.5, size)
+        assert not (np.abs(o - want) > attention_bound(want, wide, big, n, d, "bf16", top[..., None])).any()
 
 
 def test_no_rows_no_sequences(B):
@@ -394,8 +395,10 @@ def test_captured_and_replayed_with_other_lengths_on_two_streams(B):
                 n = int(lens[b])
                 for which, x in enumerate((k, v)):
                     w.ref.write(w.pages[b], n - 1, x[b:b + 1].double().cpu().numpy(), which)
-                want, wide, big, _ = ref.attention(q[b:b + 1].double().cpu().numpy(), w.ref.values(w.pages[b], n, 0), w.ref.values(w.pages[b], n, 1), n - 1, 0.125)
-                assert (np.abs(o[b:b + 1].double().cpu().numpy() - want) <= attention_bound(want, wide, big, n, 64, "bf16")).all()
+                size = 2.0 ** w.ref.e[w.pages[b][np.arange(n) // 16], :, 1]
+                want, wide, big, top = ref.attention(q[b:b + 1].double().cpu().numpy(), w.ref.values(w.pages[b], n, 0), w.ref.values(w.pages[b], n, 1), n - 1,
+                                                     0.125, size)
+                assert not (np.abs(o[b:b + 1].double().cpu().numpy() - want) > attention_bound(want, wide, big, n, 64, "bf16", top[..., None])).any()
             w.check()
 
 
