@@ -325,8 +325,7 @@ szo_status szo_attention_paired(const void* q, const void* k, const void* v, voi
  * description does not fit (negative or decreasing start, more than max_new rows, kv_len beyond
  * max_pages*page_tokens) is skipped, its rows left as they were, and a needed page id outside [0, n_pages) is treated
  * as a page without tokens; the device status word reports both (SZO_ERR_SHAPE, SZO_ERR_INVALID_ARG).
- * Sequences may share pages (a common prefix) as long as no call writes a shared page.  No call allocates
- * or needs a workspace. */
+ * Sequences may share pages (a common prefix) as long as no call writes a shared page. */
 typedef struct {
   uint8_t* k_codes;
   uint8_t* v_codes;
@@ -359,9 +358,13 @@ szo_status szo_kv8_read(const szo_kv8_cache* cache, const szo_kv8_batch* batch, 
  * sequence (its own among them: write first).  o = softmax(scale * q k^T) v, statistics and sums in fp32; q, o: dtype
  * [rows][n_heads*head_dim], rows q_stride / o_stride elements apart; grouped-query attention when n_kv_heads <
  * n_heads; scale finite (1/sqrt(head_dim) for szo_attention's).  A row that attends to nothing (padding) becomes zeros.
- * A NaN element of the cache reaches the rows that attend to it and no others. */
+ * A NaN element of the cache reaches the rows that attend to it and no others.  workspace: at least
+ * szo_attention_kv8_workspace_bytes(cache, batch, n_heads) bytes (0, below a megabyte otherwise: it depends on the shapes
+ * only, not on the lengths), contents irrelevant on entry; calls that may run at the same time need one each. */
+size_t szo_attention_kv8_workspace_bytes(const szo_kv8_cache* cache, const szo_kv8_batch* batch, int32_t n_heads);
 szo_status szo_attention_kv8(const szo_kv8_cache* cache, const szo_kv8_batch* batch, const void* q, int64_t q_stride,
-                             void* o, int64_t o_stride, szo_dtype dtype, int32_t n_heads, float scale, void* stream);
+                             void* o, int64_t o_stride, szo_dtype dtype, int32_t n_heads, float scale, void* workspace,
+                             size_t workspace_bytes, void* stream);
 
 /* ---- Log probabilities of given tokens (the quantity that the losses of Section 2 and the candidate comparison of
  * the classification experiments are made of), with the distribution's entropy and best alternatives.  Row r of

@@ -114,7 +114,8 @@ _SIGS = {
     "szo_kv8_write": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_void_p]),
     "szo_kv8_read": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_void_p]),
     "szo_attention_kv8": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_int32,
-                                      C.c_float, C.c_void_p]),
+                                      C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "szo_attention_kv8_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_void_p, C.c_int32]),
     "szo_token_logprobs": (C.c_int32, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_float, C.c_void_p, C.c_int32,
                                        C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "szo_token_logprobs_bwd": (C.c_int32, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_float, C.c_void_p,
@@ -482,8 +483,10 @@ def szo_attention_kv8(cache: Kv8Cache, batch: Kv8Batch, q: torch.Tensor, scale: 
     if o.dtype != q.dtype:
         raise ValueError("out must have q's type")
     if batch.rows:
+        need = lib().szo_attention_kv8_workspace_bytes(cache.ref, batch.ref, width // d)
+        ws = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else None
         _check(lib().szo_attention_kv8(cache.ref, batch.ref, q.data_ptr(), qs, o.data_ptr(), os_, _DT[q.dtype], width // d,
-                                       d ** -0.5 if scale is None else scale, st))
+                                       d ** -0.5 if scale is None else scale, None if ws is None else ws.data_ptr(), need, st))
     return o
 
 

@@ -4,14 +4,18 @@
 // together, so a cached element is read once for up to 8 kNT rows.  What bounds it is reading the cache, one byte per
 // element; everything else is arranged around keeping enough loads in flight:
 //   * tokens are the M dimension of the products (16 per mma.sync m16n8k16), the query rows its N dimension: scores
-//     S^T = K q^T and outputs O^T = V^T P^T.  Both cache operands then are A fragments, which a thread can load
-//     straight from global memory in 16-byte pieces (the order of the contracted head dimension, and of the output's
-//     rows, is free), with no shared memory and no barrier in the loop; the next step's 4 KB per warp (head_dim 128)
-//     are in flight while this one is multiplied.  tcgen05 would need the converted operands in shared memory and
-//     128 rows of queries to be worth it: the arithmetic here is a fraction of the tensor pipe either way.
-//   * a sequence's positions are divided among the warps of a block and among the blocks of a cluster (up to 16),
-//     whose partial results are joined through distributed shared memory in a fixed order: no workspace, no second
-//     launch, and the same bits every time.
+//     S^T = K q^T and outputs O^T = V^T P^T.  Both cache operands then are A fragments that a thread takes in
+//     16-byte pieces (the order of the contracted head dimension, and of the output's rows, is free).  tcgen05 would
+//     need the converted operands in shared memory and 128 rows of queries to be worth it: the arithmetic here is a
+//     fraction of the tensor pipe either way;
+//   * every warp runs on its own: its share of the positions arrives 32 tokens (8 KB for head_dim 128) at a time by TMA
+//     in a private ring, two units deep, so that 16 KB per warp are in flight whatever the registers hold; no block
+//     barrier in the loop.  The TMA swizzle makes both fragment reads free of bank conflicts;
+//   * a sequence's positions are divided among the warps of a block and among the blocks of a cluster, whose
+//     partial results are joined through distributed shared memory: no workspace and no second launch.  Where one
+//     cluster per sequence and head leaves SMs idle (few sequences and heads, long contexts: seven clusters of 16 such
+//     blocks fit this GPU), blocks of 12 warps, one per SM, write their partial results to a workspace and a second,
+//     chained launch joins them.  Both join in a fixed order: the same bits every time.
 //
 // Numbers.  Codes become fp16 exactly (one cvt per two).  A query row is divided by the power of two of its largest
 // element and is then exact in fp16 for bf16 and fp16 input (elements below 2^-14 of the largest lose bits that fp32
@@ -26,6 +30,7 @@
 #include <cmath>
 
 #include "kv8.cuh"
+#include "tc_common.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -34,8 +39,10 @@ namespace kv8 {
 
 namespace {
 
-constexpr int kWarps = 4, kStep = 16;
-constexpr float kOffset = 14.0f;
+constexpr int kStep = 16, kUnit = 32, kDepth = 2;     // kDepth: units of a warp's ring
+// The largest weight is 2^kOffset when the reference maximum m is set; m follows the running maximum only once that
+// is more than 2^kSlack above it (weights then stay below 2^15), so the outputs are rescaled a few times per sequence.
+constexpr float kOffset = 12.0f, kSlack = 3.0f;
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -62,70 +69,72 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ uint4 load_stream16(const uint8_t* p) {
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
   uint4 r;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a));
   return r;
 }
-__device__ __forceinline__ uint2 load_stream8(const uint8_t* p) {
+__device__ __forceinline__ uint2 lds8(uint32_t a) {
   uint2 r;
-  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(a));
   return r;
-}
-__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) {
-  uint32_t d;
-  asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(sel));
-  return d;
 }
 
-// One step (16 tokens) of a page and head as the thread (g, t) = (lane / 4, lane % 4) of a warp holds it.
-//   keys    tokens g and g + 8, dims [16 t, 16 t + 16) and, for 128, [64 + 16 t, ...): word i of a row feeds k-step i
-//   values  tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9, dims [kPiece g, kPiece (g + 1)), kPiece = HD / 8
-template <int HD> struct Raw {
-  uint32_t k[2][HD / 16];
-  uint32_t v[4][HD / 32];
-};
-template <int HD>
-__device__ __forceinline__ void load_step(Raw<HD>& r, const uint8_t* k, const uint8_t* v, int g, int t) {
+// Shared-memory image of 16 tokens (a TMA box): rows of HD bytes, 16-byte chunks permuted by the TMA swizzle.
+template <int HD> __device__ __forceinline__ uint32_t chunk_at(uint32_t base, int row, int chunk) {
+  return base + row * HD + ((chunk ^ (HD == 128 ? row & 7 : (row >> 1) & 3)) << 4);
+}
+// Keys of 16 tokens as the thread (g, t) = (lane / 4, lane % 4) holds them: tokens g and g + 8, dims [kDims t, kDims (t + 1)),
+// kDims = HD / 4: word i of a row feeds k-step i.  (Chunks 2 t and 2 t + 1 and not t and t + 4: with the swizzle eight
+// neighbouring lanes then read eight different bank groups.)
+template <int HD> __device__ __forceinline__ void load_keys(uint32_t (&k)[2][HD / 16], uint32_t base, int g, int t) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
 #pragma unroll
     for (int j = 0; j < HD / 64; ++j) {
-      const uint4 x = load_stream16(k + (g + 8 * i) * HD + 64 * j + 16 * t);
-      r.k[i][4 * j] = x.x;
-      r.k[i][4 * j + 1] = x.y;
-      r.k[i][4 * j + 2] = x.z;
-      r.k[i][4 * j + 3] = x.w;
+      const uint4 x = lds16(chunk_at<HD>(base, g + 8 * i, HD / 64 * t + j));
+      k[i][4 * j] = x.x;
+      k[i][4 * j + 1] = x.y;
+      k[i][4 * j + 2] = x.z;
+      k[i][4 * j + 3] = x.w;
     }
   }
+}
+// Values of 16 tokens: tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9, dims [kPiece g, kPiece (g + 1)), kPiece = HD / 8
+template <int HD> __device__ __forceinline__ void load_values(uint32_t (&v)[4][HD / 32], uint32_t base, int g, int t) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint8_t* p = v + (2 * t + (i & 1) + 8 * (i >> 1)) * HD + HD / 8 * g;
+    const int row = 2 * t + (i & 1) + 8 * (i >> 1);
     if constexpr (HD == 128) {
-      const uint4 x = load_stream16(p);
-      r.v[i][0] = x.x;
-      r.v[i][1] = x.y;
-      r.v[i][2] = x.z;
-      r.v[i][3] = x.w;
+      const uint4 x = lds16(chunk_at<HD>(base, row, g));
+      v[i][0] = x.x;
+      v[i][1] = x.y;
+      v[i][2] = x.z;
+      v[i][3] = x.w;
     } else {
-      const uint2 x = load_stream8(p);
-      r.v[i][0] = x.x;
-      r.v[i][1] = x.y;
+      const uint2 x = lds8(chunk_at<HD>(base, row, g >> 1) + 8 * (g & 1));
+      v[i][0] = x.x;
+      v[i][1] = x.y;
     }
   }
 }
 
-template <typename T, int HD, int NT>
-__global__ void __launch_bounds__(kWarps * 32)
-kv8_attention_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __restrict__ o, int64_t o_stride, int H, float scale_log2e,
-                     int row_tiles, int nsplit) {
-  constexpr int R = 8 * NT, kK = HD / 16;
+template <int HD> constexpr int kRingBytes = kDepth * kUnit * HD * 2;       // per warp
+
+template <typename T, int HD, int NT, int kWarps>
+__global__ void __launch_bounds__(kWarps * 32, NT == 1 ? (kWarps == 4 ? 3 : 1) : 1)
+kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, View V, const T* __restrict__ q,
+                     int64_t q_stride, T* __restrict__ o, int64_t o_stride, int H, float scale_log2e, int row_tiles, int nsplit, float* __restrict__ ws) {
+  constexpr int R = 8 * NT, kK = HD / 16, kRing = kRingBytes<HD>;
   constexpr bool kSplit = sizeof(T) == 4;
-  extern __shared__ __align__(16) unsigned char smem_kv8[];
-  float* part = reinterpret_cast<float*>(smem_kv8);               // [kWarps][R][HD]; the block's own sum ends up in [0]
-  float* wm = part + kWarps * R * HD;                             // [kWarps][R] maxima, then [R] the block's
-  float* wl = wm + kWarps * R;                                    // the same for sums of weights
-  int* nan_at = reinterpret_cast<int*>(wl + kWarps * R);          // [HD]: first position in the masked steps whose value is NaN
+  static_assert(R * HD * 4 <= kRing, "a warp's partial result takes the place of its ring");
+  extern __shared__ __align__(1024) unsigned char smem_kv8[];
+  __shared__ float wm[kWarps * R], wl[kWarps * R];                // per warp: row maxima, sums of weights; [0, R): the block's
+  __shared__ int nan_at[HD];                                      // first position in the masked steps whose value is NaN
+  __shared__ __align__(8) uint64_t full[kWarps][kDepth];
+  __shared__ int abort_flag;
+  unsigned char* ring0 = smem_kv8 + ((1024u - (tc::smem_u32(smem_kv8) & 1023u)) & 1023u);
+  auto part = [&](int warp) { return reinterpret_cast<float*>(ring0 + warp * kRing); };     // [R][HD]; the block's sum ends up in part(0)
 
   chain_release();
   chain_wait();
@@ -140,10 +149,69 @@ kv8_attention_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __res
   const int r0 = rt * R, n_rows = static_cast<int>(min(static_cast<int64_t>(seq.n) * G - r0, static_cast<int64_t>(R)));
   if (n_rows <= 0) return;                                        // (the same in every block of a cluster)
   for (int i = threadIdx.x; i < HD; i += kWarps * 32) nan_at[i] = 0x7fffffff;
+  if (threadIdx.x == 0) abort_flag = 0;
+  const uint32_t ring = tc::smem_u32(ring0) + w * kRing, bars = tc::smem_u32(&full[w][0]);
+  if (lane == 0) {
+    for (int i = 0; i < kDepth; ++i) tc::mbar_init(bars + 8 * i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
   const int first = seq.len - seq.n;                              // position of the sequence's row 0; negative: padding
   const int pos_lo = first + r0 / G, pos_hi = first + (r0 + n_rows - 1) / G;
 
-  // queries: B fragments of k-step i are row g's dims dim(i, t) .. + 3
+  // this warp's units of two steps; a last unit may have one
+  const int steps = pos_hi < 0 ? 0 : pos_hi / kStep + 1, units = (steps + 1) / 2;
+  int u_lo = static_cast<int>(static_cast<int64_t>(units) * split / nsplit), u_hi = static_cast<int>(static_cast<int64_t>(units) * (split + 1) / nsplit);
+  {
+    const int span = u_hi - u_lo, base = u_lo;
+    u_lo = base + span * w / kWarps;
+    u_hi = base + span * (w + 1) / kWarps;
+  }
+  float acc[NT][HD / 16][4], m[NT][2], l[NT][2];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    m[n][0] = m[n][1] = -INFINITY;
+    l[n][0] = l[n][1] = 0.f;
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) acc[n][i][0] = acc[n][i][1] = acc[n][i][2] = acc[n][i][3] = 0.f;
+  }
+  // Rows (of the tensor maps) and scales of 32 steps (16 units) at a time, one step per lane, loaded a chunk ahead
+  struct Meta {
+    int row;                                                      // -1: no page, or behind this warp's share
+    float ks, fe;                                                 // 2^(keys' exponent), the values' exponent; without a page -inf
+  };
+  auto load_meta = [&](int s) {
+    Meta r{-1, 0.f, -INFINITY};
+    s += lane;
+    if (s < 2 * u_hi && s < steps) {
+      const int page = load_page(V, b, s >> (V.page_shift - 4));
+      if (page >= 0) {
+        const float2 sc = V.scales[static_cast<int64_t>(page) * V.hkv + h];
+        r.row = ((page * V.hkv + h) << V.page_shift) + ((s << 4) & ((1 << V.page_shift) - 1));
+        r.ks = exp2_int(scale_exponent(sc.x));
+        r.fe = static_cast<float>(scale_exponent(sc.y));
+      }
+    }
+    return r;
+  };
+  // A unit into ring slot `slot`: lanes 0-3 issue one copy of 16 tokens each (keys, keys, values, values).  A step without
+  // a page is left out.  Called by the whole warp; row: of the first step in lanes 0 and 2, of the second in lanes 1 and 3.
+  auto issue = [&](int slot, int row) {
+    const uint32_t bar = bars + 8 * slot;
+    const unsigned live = __ballot_sync(0xffffffffu, lane < 4 && row >= 0);
+    if (lane == 0) tc::mbar_expect_tx(bar, __popc(live) * kStep * HD);
+    __syncwarp();
+    if (lane < 4 && row >= 0)
+      tc::tma_load_2d(ring + slot * kUnit * HD * 2 + lane * kStep * HD, lane < 2 ? &map_k : &map_v, 0, row, bar);
+  };
+  Meta mc = load_meta(2 * u_lo);
+#pragma unroll
+  for (int i = 0; i < kDepth; ++i) {
+    const int row = __shfl_sync(0xffffffffu, mc.row, 2 * i + (lane & 1));
+    if (u_lo + i < u_hi) issue(i, row);
+  }
+  Meta mn = load_meta(2 * u_lo + 32);
+  // queries: the B fragments of k-step i are row g's dims (HD / 4) t + 4 i .. + 3
   uint32_t qa[NT][kK][2], qb[kSplit ? NT : 1][kK][2];
   float rs[NT][2];
   int rpos[NT][2];
@@ -152,20 +220,17 @@ kv8_attention_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __res
     const int r = 8 * n + g;
     float x[kK][4], amax = 0.f;
     bool fine = true;
-    const T* qp = q + (seq.row0 + (r0 + r) / G) * q_stride + (h * G + (r0 + r) % G) * static_cast<int64_t>(HD) + 16 * t;
+    const T* qp = q + (seq.row0 + (r0 + r) / G) * q_stride + (h * G + (r0 + r) % G) * static_cast<int64_t>(HD) + HD / 4 * t;
 #pragma unroll
-    for (int j = 0; j < HD / 64; ++j) {
+    for (int i = 0; i < HD / 4; i += Vec<T>::kN) {
+      Vec<T> v = {};
+      if (r < n_rows) v = *reinterpret_cast<const Vec<T>*>(qp + i);
 #pragma unroll
-      for (int i = 0; i < 16; i += Vec<T>::kN) {
-        Vec<T> v = {};
-        if (r < n_rows) v = *reinterpret_cast<const Vec<T>*>(qp + 64 * j + i);
-#pragma unroll
-        for (int u = 0; u < Vec<T>::kN; ++u) {
-          const float y = widen<T>(v.x[u]);
-          x[4 * j + (i + u) / 4][(i + u) % 4] = y;
-          amax = fmaxf(amax, fabsf(y));
-          fine = fine && isfinite(y);
-        }
+      for (int u = 0; u < Vec<T>::kN; ++u) {
+        const float y = widen<T>(v.x[u]);
+        x[(i + u) / 4][(i + u) % 4] = y;
+        amax = fmaxf(amax, fabsf(y));
+        fine = fine && isfinite(y);
       }
     }
 #pragma unroll
@@ -195,147 +260,144 @@ kv8_attention_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __res
   }
   __syncthreads();
 
-  // this warp's steps
-  const int total = pos_hi < 0 ? 0 : pos_hi / kStep + 1;
-  int s_lo = static_cast<int>(static_cast<int64_t>(total) * split / nsplit), s_hi = static_cast<int>(static_cast<int64_t>(total) * (split + 1) / nsplit);
-  {
-    const int span = s_hi - s_lo, base = s_lo;
-    s_lo = base + span * w / kWarps;
-    s_hi = base + span * (w + 1) / kWarps;
-  }
-  float acc[NT][HD / 16][4], m[NT][2], l[NT][2];
+  int slot = 0;
+  uint32_t phase = 0;
+  for (int u = u_lo; u < u_hi; ++u) {
+    const int i = 2 * (u - u_lo) & 31;
+    bool have[2];
+    float ks[2], fe[2], el[2];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    m[n][0] = m[n][1] = -INFINITY;
-    l[n][0] = l[n][1] = 0.f;
-#pragma unroll
-    for (int i = 0; i < HD / 16; ++i) acc[n][i][0] = acc[n][i][1] = acc[n][i][2] = acc[n][i][3] = 0.f;
-  }
-  // Page ids and scales of 32 steps at a time, one step per lane, loaded a chunk ahead
-  const int per_page = V.page_shift - 4;
-  int page_c = -1, page_n = -1;
-  float2 sc_c = make_float2(0.f, 0.f), sc_n = sc_c;
-  auto load_meta = [&](int s, int& page, float2& sc) {
-    page = -1;
-    if (s + lane < s_hi) {
-      page = load_page(V, b, (s + lane) >> per_page);
-      if (page >= 0) sc = V.scales[static_cast<int64_t>(page) * V.hkv + h];
+    for (int a = 0; a < 2; ++a) {
+      ks[a] = __shfl_sync(0xffffffffu, mc.ks, i + a);
+      fe[a] = __shfl_sync(0xffffffffu, mc.fe, i + a);
+      have[a] = fe[a] != -INFINITY;
+      el[a] = have[a] ? exp2_int(-static_cast<int>(fe[a])) : 0.f;
     }
-  };
-  auto fetch = [&](Raw<HD>& r, int page, int s) {
-    if (page < 0) return;
-    const int64_t at = page_offset(V, page, h, HD) + ((s << 4) & ((1 << V.page_shift) - 1)) * HD;
-    load_step<HD>(r, V.k + at, V.v + at, g, t);
-  };
-  load_meta(s_lo, page_c, sc_c);
-  load_meta(s_lo + 32, page_n, sc_n);
-  Raw<HD> cur;
-  int page = __shfl_sync(0xffffffffu, page_c, 0);
-  fetch(cur, page, s_lo);
-#pragma unroll 2
-  for (int s = s_lo; s < s_hi; ++s) {
-    const int i = (s - s_lo) & 31, i1 = (i + 1) & 31;
-    const int ek = scale_exponent(__shfl_sync(0xffffffffu, sc_c.x, i)), ev = scale_exponent(__shfl_sync(0xffffffffu, sc_c.y, i));
-    const bool have = page >= 0;
-    page = __shfl_sync(0xffffffffu, i1 ? page_c : page_n, i1);
-    Raw<HD> next;
-    if (s + 1 < s_hi) fetch(next, page, s + 1);
-    if (i1 == 0) {
-      page_c = page_n;
-      sc_c = sc_n;
-      load_meta(s + 33, page_n, sc_n);
-    }
-    if (have) {
-      float c[NT][4];
+    if (!tc::mbar_wait(bars + 8 * slot, phase, &abort_flag, V.status, 0)) break;
+    const uint32_t at = ring + slot * kUnit * HD * 2;
+    float c[2][NT][4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.f;
-#pragma unroll
-      for (int k = 0; k < kK; ++k) {
-        const uint32_t a0 = decode2(cur.k[0][k]), a1 = decode2(cur.k[1][k]), a2 = decode2(cur.k[0][k] >> 16), a3 = decode2(cur.k[1][k] >> 16);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          mma_f16(c[n], a0, a1, a2, a3, qa[n][k][0], qa[n][k][1]);
-          if constexpr (kSplit) mma_f16(c[n], a0, a1, a2, a3, qb[n][k][0], qb[n][k][1]);
-        }
-      }
-      const bool masked = s * kStep + kStep - 1 > pos_lo;         // some row does not see the whole step
-      const float ks = exp2_int(ek), fe = static_cast<float>(ev), el = exp2_int(-ev);
-      uint32_t pa[NT][2], pb[kSplit ? NT : 1][2];
+    for (int a = 0; a < 2; ++a) {
+      uint32_t kk[2][kK];
+      load_keys<HD>(kk, at + a * kStep * HD, g, t);
+      // (with one tile of rows even and odd k-steps are summed apart: four chains of products instead of two)
+      float odd[NT][4];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float x[4];
+        c[a][n][0] = c[a][n][1] = c[a][n][2] = c[a][n][3] = 0.f;
+        odd[n][0] = odd[n][1] = odd[n][2] = odd[n][3] = 0.f;
+      }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          x[u] = fmaf(c[n][u], rs[n][u & 1] * ks, fe);
-          if (masked && s * kStep + g + 8 * (u >> 1) > rpos[n][u & 1]) x[u] = -INFINITY;
-        }
-        float mx[2] = {fmaxf(x[0], x[2]), fmaxf(x[1], x[3])};
+      for (int k = 0; k < kK; ++k) {
+        const uint32_t a0 = decode2(kk[0][k]), a1 = decode2(kk[1][k]), a2 = decode2(kk[0][k] >> 16), a3 = decode2(kk[1][k] >> 16);
 #pragma unroll
-        for (int off = 4; off <= 16; off <<= 1) {
-          mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], off));
-          mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], off));
-        }
-        const bool grew = mx[0] > m[n][0] || mx[1] > m[n][1];
-        if (__any_sync(0xffffffffu, grew)) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const float mn = fmaxf(m[n][u], mx[u]), corr = mn == -INFINITY ? 1.f : ex2(m[n][u] - mn);
-            m[n][u] = mn;
-            l[n][u] *= corr;
-#pragma unroll
-            for (int j = 0; j < HD / 16; ++j) {
-              acc[n][j][u] *= corr;
-              acc[n][j][u + 2] *= corr;
-            }
-          }
-        }
-        float y[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) y[u] = ex2(x[u] - (m[n][u & 1] == -INFINITY ? 0.f : m[n][u & 1] - kOffset));
-        l[n][0] = fmaf(el, y[0] + y[2], l[n][0]);
-        l[n][1] = fmaf(el, y[1] + y[3], l[n][1]);
-        const uint32_t h0 = pack_f16(y[0], y[1]), h1 = pack_f16(y[2], y[3]);
-        pa[n][0] = transpose8x8(h0);
-        pa[n][1] = transpose8x8(h1);
-        if constexpr (kSplit) {
-          pb[n][0] = transpose8x8(pack_rest(h0, y[0], y[1]));
-          pb[n][1] = transpose8x8(pack_rest(h1, y[2], y[3]));
+        for (int n = 0; n < NT; ++n) {
+          float(&to)[4] = NT == 1 && (k & 1) ? odd[n] : c[a][n];
+          mma_f16(to, a0, a1, a2, a3, qa[n][k][0], qa[n][k][1]);
+          if constexpr (kSplit) mma_f16(to, a0, a1, a2, a3, qb[n][k][0], qb[n][k][1]);
         }
       }
+      if constexpr (NT == 1) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c[a][0][j] += odd[0][j];
+      }
+    }
+    uint32_t vv[2][4][HD / 32];
+    load_values<HD>(vv[0], at + 2 * kStep * HD, g, t);
+    load_values<HD>(vv[1], at + 3 * kStep * HD, g, t);
+    const bool masked = u * kUnit + kUnit - 1 > pos_lo || !have[0] || !have[1];      // some row does not see the whole unit
+    uint32_t pa[NT][4], pb[kSplit ? NT : 1][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float x[2][4];
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[a][j] = fmaf(c[a][n][j], rs[n][j & 1] * ks[a], fe[a]);
+          if (masked && (!have[a] || u * kUnit + a * kStep + g + 8 * (j >> 1) > rpos[n][j & 1])) x[a][j] = -INFINITY;
+        }
+      }
+      float mx[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) mx[j] = fmaxf(fmaxf(x[0][j], x[0][j + 2]), fmaxf(x[1][j], x[1][j + 2]));
+      if (__any_sync(0xffffffffu, mx[0] > m[n][0] + kSlack || mx[1] > m[n][1] + kSlack)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+          for (int off = 4; off <= 16; off <<= 1) mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], off));
+          const float mn = fmaxf(m[n][j], mx[j]), corr = mn == -INFINITY ? 1.f : ex2(m[n][j] - mn);
+          m[n][j] = mn;
+          l[n][j] *= corr;
+#pragma unroll
+          for (int k = 0; k < HD / 16; ++k) {
+            acc[n][k][j] *= corr;
+            acc[n][k][j + 2] *= corr;
+          }
+        }
+      }
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        float y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = ex2(x[a][j] - (m[n][j & 1] == -INFINITY ? 0.f : m[n][j & 1] - kOffset));
+        l[n][0] = fmaf(el[a], y[0] + y[2], l[n][0]);
+        l[n][1] = fmaf(el[a], y[1] + y[3], l[n][1]);
+        const uint32_t h0 = pack_f16(y[0], y[1]), h1 = pack_f16(y[2], y[3]);
+        pa[n][2 * a] = transpose8x8(h0);
+        pa[n][2 * a + 1] = transpose8x8(h1);
+        if constexpr (kSplit) {
+          pb[n][2 * a] = transpose8x8(pack_rest(h0, y[0], y[1]));
+          pb[n][2 * a + 1] = transpose8x8(pack_rest(h1, y[2], y[3]));
+        }
+      }
+    }
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
       if (masked) {
         // 0 * NaN: a NaN value must not reach rows that do not see its token.  It is taken out here, and the rows that do
-        // see it are set to NaN when the block's sums are joined.
+        // see it are set to NaN when the block's sums are joined.  (Without a page the slot holds leftovers: zeros.)
 #pragma unroll
         for (int i2 = 0; i2 < 4; ++i2) {
 #pragma unroll
           for (int j = 0; j < HD / 32; ++j) {
-            uint32_t bad = ((cur.v[i2][j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-            cur.v[i2][j] &= ~((bad >> 7) * 0xffu);
+            if (!have[a]) vv[a][i2][j] = 0;
+            uint32_t bad = ((vv[a][i2][j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+            vv[a][i2][j] &= ~((bad >> 7) * 0xffu);
             while (bad) {
               const int byte = (__ffs(bad) - 1) >> 3;
               bad &= bad - 1;
-              atomicMin(nan_at + HD / 8 * g + 4 * j + byte, s * kStep + 2 * t + (i2 & 1) + 8 * (i2 >> 1));
+              atomicMin(nan_at + HD / 8 * g + 4 * j + byte, u * kUnit + a * kStep + 2 * t + (i2 & 1) + 8 * (i2 >> 1));
             }
           }
         }
       }
 #pragma unroll
       for (int j = 0; j < HD / 32; ++j) {
-        const uint32_t lo0 = prmt(cur.v[0][j], cur.v[1][j], 0x5140), hi0 = prmt(cur.v[0][j], cur.v[1][j], 0x7362);
-        const uint32_t lo1 = prmt(cur.v[2][j], cur.v[3][j], 0x5140), hi1 = prmt(cur.v[2][j], cur.v[3][j], 0x7362);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {                             // dims kPiece g + 4 j + 2 u and + 1 are rows g and g + 8 of tile 2 j + u
-          const uint32_t x0 = u ? hi0 : lo0, x1 = u ? hi1 : lo1;
+        for (int x = 0; x < 2; ++x) {                             // dims kPiece g + 4 j + 2 x and + 1 are rows g and g + 8 of tile 2 j + x
+          const uint32_t x0 = tc::prmt(vv[a][0][j], vv[a][1][j], x ? 0x7362 : 0x5140), x1 = tc::prmt(vv[a][2][j], vv[a][3][j], x ? 0x7362 : 0x5140);
           const uint32_t a0 = decode2(x0), a1 = decode2(x0 >> 16), a2 = decode2(x1), a3 = decode2(x1 >> 16);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            mma_f16(acc[n][2 * j + u], a0, a1, a2, a3, pa[n][0], pa[n][1]);
-            if constexpr (kSplit) mma_f16(acc[n][2 * j + u], a0, a1, a2, a3, pb[n][0], pb[n][1]);
+            mma_f16(acc[n][2 * j + x], a0, a1, a2, a3, pa[n][2 * a], pa[n][2 * a + 1]);
+            if constexpr (kSplit) mma_f16(acc[n][2 * j + x], a0, a1, a2, a3, pb[n][2 * a], pb[n][2 * a + 1]);
           }
         }
       }
     }
-    cur = next;
+    // the slot's next unit (its rows are in this chunk of metadata or the next one)
+    const int i3 = i + 2 * kDepth, src = (i3 & 31) + (lane & 1);
+    const int rc = __shfl_sync(0xffffffffu, mc.row, src), rn = __shfl_sync(0xffffffffu, mn.row, src);
+    if (u + kDepth < u_hi) issue(slot, i3 < 32 ? rc : rn);
+    if (i == 30) {
+      mc = mn;
+      mn = load_meta(2 * u + 34);
+    }
+    if (++slot == kDepth) {
+      slot = 0;
+      phase ^= 1;
+    }
   }
 
   // the block's warps joined in warp order
@@ -352,53 +414,66 @@ kv8_attention_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __res
       }
 #pragma unroll
       for (int j = 0; j < HD / 16; ++j) {
-        float* p = part + (w * R + r) * HD + HD / 8 * g + 2 * j;
+        float* p = part(w) + r * HD + HD / 8 * g + 2 * j;
         *reinterpret_cast<float2*>(p) = make_float2(acc[n][j][u], acc[n][j][u + 2]);
       }
     }
   }
   __syncthreads();
-  float bm[R * HD / (kWarps * 32)];                               // values of this thread: one dim, every (128 / HD)-th row
-  constexpr int kPer = R * HD / (kWarps * 32), kRowStep = kWarps * 32 / HD;
-  const int dim = threadIdx.x % HD, row_a = threadIdx.x / HD;
-  const int nan_pos = nan_at[dim];
-  float rm[kPer], rl[kPer];
+  constexpr int kThreads = kWarps * 32, kPer = (R * HD + kThreads - 1) / kThreads;      // results of this thread: threadIdx.x + i * kThreads
+  float bm[kPer], rm[kPer], rl[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const int r = row_a + i * kRowStep;
-    float mm = -INFINITY, sum = 0.f, ll = 0.f;
+    const int at = threadIdx.x + i * kThreads, r = at / HD, d = at % HD;
+    bm[i] = rl[i] = 0.f;
+    rm[i] = -INFINITY;
+    if (at >= R * HD) continue;
 #pragma unroll
-    for (int x = 0; x < kWarps; ++x) mm = fmaxf(mm, wm[x * R + r]);
+    for (int x = 0; x < kWarps; ++x) rm[i] = fmaxf(rm[i], wm[x * R + r]);
 #pragma unroll
     for (int x = 0; x < kWarps; ++x) {
-      const float f = mm == -INFINITY ? 1.f : ex2(wm[x * R + r] - mm);
-      sum = fmaf(f, part[(x * R + r) * HD + dim], sum);
-      ll = fmaf(f, wl[x * R + r], ll);
+      const float f = rm[i] == -INFINITY ? 1.f : ex2(wm[x * R + r] - rm[i]);
+      bm[i] = fmaf(f, part(x)[at], bm[i]);
+      rl[i] = fmaf(f, wl[x * R + r], rl[i]);
     }
-    if (first + (r0 + r) / G >= nan_pos) sum = __int_as_float(0x7fffffff);
-    bm[i] = sum;
-    rm[i] = mm;
-    rl[i] = ll;
+    if (first + (r0 + r) / G >= nan_at[d]) bm[i] = __int_as_float(0x7fffffff);
   }
   auto store = [&](int r, int d, float sum, float ll) {
     o[(seq.row0 + (r0 + r) / G) * o_stride + (h * G + (r0 + r) % G) * static_cast<int64_t>(HD) + d] =
-        narrow<T>(ll == 0.f ? (sum == 0.f ? 0.f : sum) : sum / ll);                // nothing attended to: zeros
+        narrow<T>(ll == 0.f ? sum : sum / ll);                    // nothing attended to: sum = 0
   };
   if (nsplit == 1) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (row_a + i * kRowStep < n_rows) store(row_a + i * kRowStep, dim, bm[i], rl[i]);
+    for (int i = 0; i < kPer; ++i) {
+      const int at = threadIdx.x + i * kThreads;
+      if (at < n_rows * HD) store(at / HD, at % HD, bm[i], rl[i]);
+    }
+    return;
+  }
+  if (ws != nullptr) {                                            // [item][split]: R * HD sums, R maxima, R sums of weights
+    float* mine = ws + static_cast<int64_t>(blockIdx.x) * (R * (HD + 2));
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int at = threadIdx.x + i * kThreads;
+      if (at >= n_rows * HD) continue;
+      mine[at] = bm[i];
+      if (at % HD == 0) {
+        mine[R * HD + at / HD] = rm[i];
+        mine[R * (HD + 1) + at / HD] = rl[i];
+      }
+    }
     return;
   }
   // the cluster's blocks joined in block order; block i writes the i-th share of the results
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const int r = row_a + i * kRowStep;
-    part[r * HD + dim] = bm[i];
-    if (dim == 0) {
-      wm[r] = rm[i];
-      wl[r] = rl[i];
+    const int at = threadIdx.x + i * kThreads;
+    if (at >= R * HD) continue;
+    part(0)[at] = bm[i];
+    if (at % HD == 0) {
+      wm[at / HD] = rm[i];
+      wl[at / HD] = rl[i];
     }
   }
   cg::cluster_group cluster = cg::this_cluster();
@@ -411,7 +486,7 @@ kv8_attention_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __res
     for (int x = 0; x < nsplit; ++x) mm = fmaxf(mm, cluster.map_shared_rank(wm, x)[r]);
     for (int x = 0; x < nsplit; ++x) {
       const float f = mm == -INFINITY ? 1.f : ex2(cluster.map_shared_rank(wm, x)[r] - mm);
-      sum = fmaf(f, cluster.map_shared_rank(part, x)[at], sum);
+      sum = fmaf(f, cluster.map_shared_rank(part(0), x)[at], sum);
       ll = fmaf(f, cluster.map_shared_rank(wl, x)[r], ll);
     }
     store(r, at % HD, sum, ll);
@@ -419,18 +494,58 @@ kv8_attention_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __res
   cluster.sync();                                                 // nobody leaves while its sums are being read
 }
 
-template <typename T, int HD, int NT>
-szo_status launch_rows(const View& V, const void* q, int64_t q_stride, void* o, int64_t o_stride, int H, float scale, cudaStream_t st) {
+// The row buffers and heads of a call
+struct Rows {
+  const void* q;
+  void* o;
+  int64_t q_stride, o_stride;
+  int H;
+  float scale;
+};
+
+// Joins the partial results in `ws` in split order: a block per (row of a tile, item), a thread per dim.
+template <typename T, int HD>
+__global__ void __launch_bounds__(HD)
+kv8_join_kernel(View V, const float* __restrict__ ws, T* __restrict__ o, int64_t o_stride, int H, int R, int row_tiles, int nsplit) {
+  chain_release();
+  const int r = blockIdx.x % R, d = threadIdx.x, G = H / V.hkv;
+  const unsigned item = blockIdx.x / R;
+  const int rt = item % row_tiles, h = item / row_tiles % V.hkv, b = item / row_tiles / V.hkv;
+  chain_wait();
+  const Seq seq = load_seq(V, b);
+  const int64_t row = static_cast<int64_t>(rt) * R + r;
+  if (row >= static_cast<int64_t>(seq.n) * G) return;
+  const int64_t step = static_cast<int64_t>(R) * (HD + 2);
+  const float* p = ws + item * nsplit * step;
+  float mm = -INFINITY, sum = 0.f, ll = 0.f;
+  for (int x = 0; x < nsplit; ++x) mm = fmaxf(mm, p[x * step + R * HD + r]);
+#pragma unroll 4
+  for (int x = 0; x < nsplit; ++x) {
+    const float f = mm == -INFINITY ? 1.f : ex2(p[x * step + R * HD + r] - mm);
+    sum = fmaf(f, p[x * step + r * HD + d], sum);
+    ll = fmaf(f, p[x * step + R * (HD + 1) + r], ll);
+  }
+  o[(seq.row0 + row / G) * o_stride + (h * G + row % G) * HD + d] = narrow<T>(ll == 0.f ? sum : sum / ll);
+}
+
+// Keys or values as one matrix of bytes, a token and head per row; boxes of `rows` tokens, swizzled over the row
+szo_status codes_map(const uint8_t* codes, const View& V, int hd, int rows, CUtensorMap* map) {
+  return encode_map_2d(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, (V.n_pages * V.hkv) << V.page_shift, hd, 1, rows, hd,
+                       hd == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+}
+
+template <typename T, int HD, int NT, int kWarps>
+szo_status launch_rows(const View& V, const Rows& A, int nsplit, float* ws, cudaStream_t st) {
   constexpr int R = 8 * NT;
-  const size_t smem = static_cast<size_t>(kWarps) * R * (HD + 2) * 4 + HD * 4;
-  const int64_t tiles = ceil_div(static_cast<int64_t>(V.max_new) * (H / V.hkv), R);
-  const int64_t capacity = static_cast<int64_t>(V.max_pages) << V.page_shift;
-  // Blocks per sequence and head: enough for eight per SM, as long as a warp keeps two steps
-  int nsplit = 1;
-  while (nsplit < 16 && tiles * V.batch * V.hkv * nsplit < 148 * 8 && capacity >= static_cast<int64_t>(nsplit) * 2 * kWarps * kStep * 2) nsplit *= 2;
-  unsigned blocks;
+  const size_t smem = static_cast<size_t>(kWarps) * kRingBytes<HD> + 1024;
+  const int64_t tiles = ceil_div(static_cast<int64_t>(V.max_new) * (A.H / V.hkv), R);
+  unsigned blocks, joins;
   SZO_TRY(grid_items(tiles * nsplit, V, &blocks));
-  auto kern = kv8_attention_kernel<T, HD, NT>;
+  SZO_TRY(grid_items(tiles * R, V, &joins));
+  CUtensorMap map_k, map_v;
+  SZO_TRY(codes_map(V.k, V, HD, kStep, &map_k));
+  SZO_TRY(codes_map(V.v, V, HD, kStep, &map_v));
+  auto kern = kv8_attention_kernel<T, HD, NT, kWarps>;
   SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
   SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   cudaLaunchConfig_t cfg = {};
@@ -443,18 +558,49 @@ szo_status launch_rows(const View& V, const void* q, int64_t q_stride, void* o, 
   attr[0].val.clusterDim.x = nsplit;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = nsplit > 1 ? 1 : 0;
-  SZO_CHECK_CUDA(cudaLaunchKernelEx(&cfg, kern, V, static_cast<const T*>(q), q_stride, static_cast<T*>(o), o_stride, H,
-                                    scale * 1.4426950408889634f, static_cast<int>(tiles), nsplit));
+  cfg.numAttrs = nsplit > 1 && ws == nullptr ? 1 : 0;
+  SZO_CHECK_CUDA(cudaLaunchKernelEx(&cfg, kern, map_k, map_v, V, static_cast<const T*>(A.q), A.q_stride, static_cast<T*>(A.o), A.o_stride, A.H,
+                                    A.scale * 1.4426950408889634f, static_cast<int>(tiles), nsplit, ws));
+  count_launch();
+  if (ws == nullptr) return SZO_OK;
+  SZO_CHECK_CUDA(launch_maybe_chained(kv8_join_kernel<T, HD>, dim3(joins), dim3(HD), 0, st, true, V, ws, static_cast<T*>(A.o), A.o_stride, A.H, R,
+                                      static_cast<int>(tiles), nsplit));
   count_launch();
   return SZO_OK;
 }
 
-template <typename T, int HD>
-szo_status launch_attention(const View& V, const void* q, int64_t q_stride, void* o, int64_t o_stride, int H, float scale, cudaStream_t st) {
+// How the positions are cut: blocks of 4 warps, three per SM, joined in clusters of up to 16, or (`wide`) of 12, one per SM,
+// joined by the second launch.  A cut stops at one unit per warp of what the page table could hold (the lengths are on
+// the device).
+struct Plan {
+  int rows, nsplit;
+  bool wide;
+};
+Plan plan(const View& V, int H) {
   const int64_t rows = static_cast<int64_t>(V.max_new) * (H / V.hkv);
-  if (rows <= 8) return launch_rows<T, HD, 1>(V, q, q_stride, o, o_stride, H, scale, st);
-  return launch_rows<T, HD, 2>(V, q, q_stride, o, o_stride, H, scale, st);
+  Plan p{rows <= 8 ? 8 : 16, 1, false};
+  const int64_t items = ceil_div(rows, p.rows) * V.batch * V.hkv;
+  const int64_t units = ceil_div(static_cast<int64_t>(V.max_pages) << V.page_shift, kUnit);
+  if (p.rows == 8 && items * 16 <= 148 * 2 && units >= 12 * 16 * 2) {
+    p.wide = true;
+    p.nsplit = static_cast<int>(148 / items);
+    return p;
+  }
+  while (p.nsplit < 16 && items * p.nsplit < 148 * 2 && units >= 2 * p.nsplit * 4) p.nsplit *= 2;
+  return p;
+}
+
+template <typename T, int HD>
+szo_status launch_attention(const View& V, const Rows& A, float* ws, cudaStream_t st) {
+  const Plan p = plan(V, A.H);
+  if (p.wide) return launch_rows<T, HD, 1, 12>(V, A, p.nsplit, ws, st);
+  return p.rows == 8 ? launch_rows<T, HD, 1, 4>(V, A, p.nsplit, nullptr, st) : launch_rows<T, HD, 2, 4>(V, A, p.nsplit, nullptr, st);
+}
+
+size_t workspace_bytes(const View& V, int H, int hd) {
+  if (V.batch == 0 || V.max_new == 0 || V.rows == 0) return 0;
+  const Plan p = plan(V, H);
+  return p.wide ? static_cast<size_t>(148) * p.rows * (hd + 2) * sizeof(float) : 0;
 }
 
 }  // namespace
@@ -463,8 +609,17 @@ szo_status launch_attention(const View& V, const void* q, int64_t q_stride, void
 
 using namespace szo;
 
-extern "C" szo_status szo_attention_kv8(const szo_kv8_cache* cache, const szo_kv8_batch* batch, const void* q, int64_t q_stride,
-                                        void* o, int64_t o_stride, szo_dtype dtype, int32_t n_heads, float scale, void* stream) {
+extern "C" {
+
+size_t szo_attention_kv8_workspace_bytes(const szo_kv8_cache* cache, const szo_kv8_batch* batch, int32_t n_heads) {
+  kv8::View V;
+  if (kv8::make_view(cache, batch, &V) != SZO_OK || n_heads <= 0 || n_heads % cache->n_kv_heads != 0) return 0;
+  return kv8::workspace_bytes(V, n_heads, cache->head_dim);
+}
+
+szo_status szo_attention_kv8(const szo_kv8_cache* cache, const szo_kv8_batch* batch, const void* q, int64_t q_stride, void* o,
+                             int64_t o_stride, szo_dtype dtype, int32_t n_heads, float scale, void* workspace, size_t workspace_bytes,
+                             void* stream) {
   kv8::View V;
   SZO_TRY(kv8::make_view(cache, batch, &V));
   SZO_REQUIRE(q && o, SZO_ERR_INVALID_ARG, "NULL q or o");
@@ -473,19 +628,23 @@ extern "C" szo_status szo_attention_kv8(const szo_kv8_cache* cache, const szo_kv
   SZO_REQUIRE(std::isfinite(scale), SZO_ERR_INVALID_ARG, "scale must be finite");
   const int64_t width = static_cast<int64_t>(n_heads) * cache->head_dim, vec = dtype == SZO_F32 ? 4 : 8;
   SZO_REQUIRE(q_stride >= width && o_stride >= width, SZO_ERR_SHAPE, "row strides must be at least n_heads * head_dim");
-  SZO_REQUIRE(aligned16(q) && aligned16(o) && q_stride % vec == 0 && o_stride % vec == 0, SZO_ERR_ALIGNMENT,
-              "row buffers and rows must be 16-byte aligned");
+  SZO_REQUIRE(aligned16(q) && aligned16(o) && aligned16(workspace) && q_stride % vec == 0 && o_stride % vec == 0, SZO_ERR_ALIGNMENT,
+              "buffers and rows must be 16-byte aligned");
   if (V.batch == 0 || V.max_new == 0 || V.rows == 0) return SZO_OK;
   SZO_REQUIRE(static_cast<int64_t>(V.max_new) * n_heads <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows and heads");
+  SZO_REQUIRE(cache->n_pages <= 0x7fffffff / cache->n_kv_heads / cache->page_tokens, SZO_ERR_SHAPE,
+              "n_pages * n_kv_heads * page_tokens must be below 2^31");
+  const size_t need = kv8::workspace_bytes(V, n_heads, cache->head_dim);
+  SZO_REQUIRE(need == 0 || (workspace && workspace_bytes >= need), SZO_ERR_WORKSPACE, "workspace: %zu bytes needed, %zu given", need,
+              workspace ? workspace_bytes : size_t(0));
   SZO_TRY(kv8::set_status_word(&V));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const kv8::Rows A{q, o, q_stride, o_stride, n_heads, scale};
+  float* ws = static_cast<float*>(workspace);
   const bool wide = cache->head_dim == 128;
-  if (dtype == SZO_F32)
-    return wide ? kv8::launch_attention<float, 128>(V, q, q_stride, o, o_stride, n_heads, scale, st)
-                : kv8::launch_attention<float, 64>(V, q, q_stride, o, o_stride, n_heads, scale, st);
-  if (dtype == SZO_BF16)
-    return wide ? kv8::launch_attention<__nv_bfloat16, 128>(V, q, q_stride, o, o_stride, n_heads, scale, st)
-                : kv8::launch_attention<__nv_bfloat16, 64>(V, q, q_stride, o, o_stride, n_heads, scale, st);
-  return wide ? kv8::launch_attention<__half, 128>(V, q, q_stride, o, o_stride, n_heads, scale, st)
-              : kv8::launch_attention<__half, 64>(V, q, q_stride, o, o_stride, n_heads, scale, st);
+  if (dtype == SZO_F32) return wide ? kv8::launch_attention<float, 128>(V, A, ws, st) : kv8::launch_attention<float, 64>(V, A, ws, st);
+  if (dtype == SZO_BF16) return wide ? kv8::launch_attention<__nv_bfloat16, 128>(V, A, ws, st) : kv8::launch_attention<__nv_bfloat16, 64>(V, A, ws, st);
+  return wide ? kv8::launch_attention<__half, 128>(V, A, ws, st) : kv8::launch_attention<__half, 64>(V, A, ws, st);
 }
+
+}  // extern "C"

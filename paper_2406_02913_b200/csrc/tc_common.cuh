@@ -258,6 +258,10 @@ __device__ __forceinline__ uint4 dequant_word(uint32_t w, float2 p) {
 
 }  // namespace tc
 
+// Tensor map of a row-major matrix [rows, cols], box [box_rows x box_cols], zero fill (gemm_tc.cu).
+szo_status encode_map_2d(CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t rows, int64_t cols, int elem_bytes,
+                         int box_rows, int box_cols, CUtensorMapSwizzle swizzle);
+
 // Two-CTA pair-tile kernel (gemm_tc2.cu): tmap_x has a [128 x 64] box; P.m_tiles counts
 // 256-token tiles, P.n_tiles the 256-row tiles of all P.nsub matrices; n_pairs clusters are launched.
 // dequant == false: dense bf16 weight through mw (one matrix only).

@@ -402,11 +402,22 @@ def test_captured_and_replayed_with_other_lengths_on_two_streams(B):
             w.check()
 
 
+@pytest.mark.parametrize("d,hkv,group,page", [(128, 2, 4, 16), (64, 1, 7, 128), (64, 8, 1, 32)])
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+def test_long_contexts_of_few_sequences(B, dt, d, hkv, group, page):
+    """Page tables long enough for the form that joins its blocks' results in a second launch."""
+    lens = [13001, 31]
+    w = World(B, lens, hkv, page, d, seed=d + group)
+    fill(B, w, lens)
+    run_attention(B, w, lens, [1, 1], hkv * group, dt)
+    run_attention(B, w, [12999, 20], [8 // group, 0], hkv * group, dt)
+
+
 def test_same_call_same_bits(B):
-    w = World(B, [3000, 900], 2, 32, 128, seed=21)
-    fill(B, w, [3000, 900])
+    w = World(B, [14000, 900], 2, 32, 128, seed=21)
+    fill(B, w, [14000, 900])
     for dt, news in (("bf16", [1, 1]), ("f32", [3, 2]), ("f16", [200, 150])):
-        batch, _, rows = w.batch([3000, 900], news)
+        batch, _, rows = w.batch([14000, 900], news)
         q = torch.randn(rows, 8, 128, device="cuda").to(DT[dt])
         first = B.szo_attention_kv8(w.cache, batch, q)
         for _ in range(5):

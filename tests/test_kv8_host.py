@@ -44,7 +44,7 @@ def test_cache_and_batch_are_checked_before_any_launch(B, cache, batch, code):
     L = B.lib()
     assert L.szo_kv8_write(c, b, 16, 16, 1, 128, 128, None) == code
     assert L.szo_kv8_read(c, b, 16, 16, 1, 128, 128, None) == code
-    assert L.szo_attention_kv8(c, b, 16, 256, 16, 256, 1, 4, 0.125, None) == code
+    assert L.szo_attention_kv8(c, b, 16, 256, 16, 256, 1, 4, 0.125, None, 0, None) == code
     assert L.szo_last_error()
 
 
@@ -61,13 +61,31 @@ def test_row_buffers_are_checked(B):
         assert f(c, b, 16, 16, 0, 128, 130, None) == ALIGN
         assert f(c, e, 16, 16, 1, 128, 128, None) == OK                       # nothing to do, nothing launched
     a = L.szo_attention_kv8
-    assert a(c, b, None, 256, 16, 256, 1, 4, 0.125, None) == ARG
-    assert a(c, b, 16, 256, 16, 256, 7, 4, 0.125, None) == UNSUP
-    assert a(c, b, 16, 256, 16, 256, 1, 3, 0.125, None) == SHAPE              # 3 query heads on 2 key/value heads
-    assert a(c, b, 16, 248, 16, 256, 1, 4, 0.125, None) == SHAPE
-    assert a(c, b, 16, 260, 16, 256, 1, 4, 0.125, None) == ALIGN
-    assert a(c, b, 16, 256, 16, 256, 1, 4, float("nan"), None) == ARG and a(c, b, 16, 256, 16, 256, 1, 4, float("inf"), None) == ARG
-    assert a(c, e, 16, 256, 16, 256, 1, 4, 0.125, None) == OK
+    assert a(c, b, None, 256, 16, 256, 1, 4, 0.125, None, 0, None) == ARG
+    assert a(c, b, 16, 256, 16, 256, 7, 4, 0.125, None, 0, None) == UNSUP
+    assert a(c, b, 16, 256, 16, 256, 1, 3, 0.125, None, 0, None) == SHAPE              # 3 query heads on 2 key/value heads
+    assert a(c, b, 16, 248, 16, 256, 1, 4, 0.125, None, 0, None) == SHAPE
+    assert a(c, b, 16, 260, 16, 256, 1, 4, 0.125, None, 0, None) == ALIGN
+    assert a(c, b, 16, 256, 16, 256, 1, 4, float("nan"), None, 0, None) == ARG and a(c, b, 16, 256, 16, 256, 1, 4, float("inf"), None, 0, None) == ARG
+    assert a(c, e, 16, 256, 16, 256, 1, 4, 0.125, None, 0, None) == OK
+
+
+def test_attention_workspace(B):
+    """One sequence with a long page table needs one; whether it does is a matter of shapes alone."""
+    L = B.lib()
+    c_, b_ = _cache(B, n_pages=10000), _batch(B, max_pages=8192, batch=1, rows=1)
+    c, b = C.addressof(c_), C.addressof(b_)
+    need = L.szo_attention_kv8_workspace_bytes(c, b, 4)
+    assert 0 < need < 1 << 20
+    a = L.szo_attention_kv8
+    assert a(c, b, 16, 256, 16, 256, 1, 4, 0.125, None, need, None) == -5
+    assert a(c, b, 16, 256, 16, 256, 1, 4, 0.125, 16, need - 1, None) == -5
+    assert a(c, b, 16, 256, 16, 256, 1, 4, 0.125, 24, need, None) == ALIGN
+    s_, e_ = _batch(B), _batch(B, batch=0, rows=0)
+    assert L.szo_attention_kv8_workspace_bytes(c, C.addressof(s_), 4) == 0 and L.szo_attention_kv8_workspace_bytes(c, C.addressof(e_), 4) == 0
+    assert L.szo_attention_kv8_workspace_bytes(None, b, 4) == 0 and L.szo_attention_kv8_workspace_bytes(c, b, 3) == 0
+    big_ = _cache(B, n_pages=1 << 28)
+    assert a(C.addressof(big_), C.addressof(s_), 16, 256, 16, 256, 1, 4, 0.125, None, 0, None) == SHAPE      # 2^33 tokens
 
 
 def test_logprob_arguments_are_checked(B):
