@@ -369,7 +369,7 @@ szo_status szo_attention_kv8(const szo_kv8_cache* cache, const szo_kv8_batch* ba
 /* ---- Log probabilities of given tokens (the quantity that the losses of Section 2 and the candidate comparison of
  * the classification experiments are made of), with the distribution's entropy and best alternatives.  Row r of
  * logits (dtype SZO_F32, SZO_BF16 or SZO_F16 [rows][vocab], rows row_stride >= vocab elements apart, any alignment of
- * rows) is x = scale * logits[r] (scale > 0: one over the temperature), p = softmax(x):
+ * rows) is x = scale * logits[r] (scale in [1e-30, 1e30]: one over the temperature), p = softmax(x):
  *   logp[r][i]   fp32 [rows][n_targets]  x[t] - lse, t = targets[r][i] (int32); 0 where t < 0 (padding); t >= vocab:
  *                NaN, and the device status word reports SZO_ERR_INVALID_ARG.  n_targets in [0, 64]
  *   entropy[r]   fp32 [rows] or NULL     - sum p log p (terms with p = 0 count nothing)
