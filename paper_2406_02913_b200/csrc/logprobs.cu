@@ -3,7 +3,8 @@
 //
 // Forward: one pass over a row.  Every thread keeps a reference maximum m, s = sum e^(x-m), t = sum e^(x-m) (x-m) and
 // its best (logit, index); what bounds it is reading the logits, next to it the exponentials (16 per cycle and SM: 0.72 of
-// the time that 16-bit logits take to arrive), so sums run as packed pairs and m moves only when it is exceeded by e^8.
+// the time that 16-bit logits take to arrive) and the instructions around them (4.5 per logit), so maxima and sums run
+// as packed pairs, the scale and log2 e are one factor of one packed fma, and m moves only when it is exceeded by e^8.
 // lse = m + log s and H = log s - t / s come out of the same pass.  Few rows are cut over the blocks of a cluster and
 // joined through distributed shared memory.
 //
@@ -13,6 +14,7 @@
 #include <cooperative_groups.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "common.cuh"
 
@@ -21,8 +23,9 @@ namespace cg = cooperative_groups;
 namespace szo {
 namespace {
 
-constexpr int kMaxTop = 32, kMaxTargets = 64, kThreads = 256, kMaxCand = 2048, kMaxCluster = 8;
-constexpr float kLog2e = 1.4426950408889634f, kSlack = 8.0f;
+// (a thread per target and per entry of the cluster's joined list: kThreads >= kMaxTargets, kMaxCluster * kMaxTop)
+constexpr int kMaxTop = 32, kMaxTargets = 64, kThreads = 256, kMaxCand = 2048, kMaxCluster = 8, kUnroll = 4;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f, kSlack = 8.0f, kBigRef = 65536.0f;
 
 template <typename T> __device__ __forceinline__ float widen(T x);
 template <> __device__ __forceinline__ float widen<float>(float x) { return x; }
@@ -51,16 +54,13 @@ template <typename T> struct Row {
   __device__ __forceinline__ bool whole(int v) const { return v * Vec<T>::kN >= off && (v + 1) * Vec<T>::kN <= off + n; }
   __device__ __forceinline__ bool inside(int v, int i) const { return v * Vec<T>::kN + i >= off && v * Vec<T>::kN + i < off + n; }
   __device__ __forceinline__ int index(int v, int i) const { return v * Vec<T>::kN + i - off; }
-  template <typename U> __device__ __forceinline__ void load(int v, U (&x)[Vec<T>::kN], float outside) const {
-    if (whole(v)) {
-      const Vec<T> r = *reinterpret_cast<const Vec<T>*>(base + static_cast<int64_t>(v) * Vec<T>::kN);
+  using E = typename std::remove_const<T>::type;
+  __device__ __forceinline__ Vec<E> vec(int v) const { return *reinterpret_cast<const Vec<E>*>(base + static_cast<int64_t>(v) * Vec<T>::kN); }
+  __device__ __forceinline__ Vec<E> edge(int v) const {           // element by element, -inf outside
+    Vec<E> r;
 #pragma unroll
-      for (int i = 0; i < Vec<T>::kN; ++i) x[i] = widen<typename std::remove_const<T>::type>(r.x[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < Vec<T>::kN; ++i)
-        x[i] = inside(v, i) ? widen<typename std::remove_const<T>::type>(base[static_cast<int64_t>(v) * Vec<T>::kN + i]) : outside;
-    }
+    for (int i = 0; i < Vec<T>::kN; ++i) r.x[i] = inside(v, i) ? base[static_cast<int64_t>(v) * Vec<T>::kN + i] : narrow<E>(-INFINITY);
+    return r;
   }
 };
 
@@ -101,18 +101,44 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   return r;
 }
 
+// Elements 2 i and 2 i + 1 of a vector as a pair of fp32, and two fp32 rounded into them
+__device__ __forceinline__ uint64_t widen2(const Vec<float>& v, int i) { return pair(v.x[2 * i], v.x[2 * i + 1]); }
+__device__ __forceinline__ uint64_t widen2(const Vec<__nv_bfloat16>& v, int i) {
+  const uint32_t w = reinterpret_cast<const uint32_t*>(v.x)[i];
+  return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ uint64_t widen2(const Vec<__half>& v, int i) {
+  const float2 f = __half22float2(reinterpret_cast<const __half2*>(v.x)[i]);
+  return pair(f.x, f.y);
+}
+__device__ __forceinline__ void narrow2(Vec<float>& v, int i, float2 f) {
+  v.x[2 * i] = f.x;
+  v.x[2 * i + 1] = f.y;
+}
+__device__ __forceinline__ void narrow2(Vec<__nv_bfloat16>& v, int i, float2 f) { reinterpret_cast<__nv_bfloat162*>(v.x)[i] = __floats2bfloat162_rn(f.x, f.y); }
+__device__ __forceinline__ void narrow2(Vec<__half>& v, int i, float2 f) { reinterpret_cast<__half2*>(v.x)[i] = __floats2half2_rn(f.x, f.y); }
+
 // Softmax statistics of a part of a row relative to m; a part that holds NaN or +inf has s = NaN.
 struct Stat {
   float m, s, t;
 };
-__device__ __forceinline__ Stat merge(const Stat& a, const Stat& b) {
-  Stat r;
-  r.m = fmaxf(a.m, b.m);
-  const float da = a.m - r.m, db = b.m - r.m;
-  const float fa = a.m == -INFINITY ? 0.f : expf(da), fb = b.m == -INFINITY ? 0.f : expf(db);
-  r.s = fa * a.s + fb * b.s;
-  r.t = (fa == 0.f ? 0.f : fa * fmaf(da, a.s, a.t)) + (fb == 0.f ? 0.f : fb * fmaf(db, b.s, b.t));
-  return r;
+// Joins the statistics of 2^k neighbouring lanes, in every one of them: one exponential per lane
+template <int kLanes> __device__ __forceinline__ Stat join_lanes(Stat a) {
+  float m = a.m;
+#pragma unroll
+  for (int o = kLanes / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (a.m != -INFINITY) {                                         // (else s is 0, or NaN where only NaN was seen)
+    const float d = fmaxf(a.m - m, -120.f), f = expf(d);
+    a.t = f * fmaf(d, a.s, a.t);
+    a.s *= f;
+  }
+#pragma unroll
+  for (int o = kLanes / 2; o; o >>= 1) {
+    a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+    a.t += __shfl_xor_sync(0xffffffffu, a.t, o);
+  }
+  a.m = m;
+  return a;
 }
 // Order of alternatives: larger logit first, then lower index; NaN before everything, -0 = +0.  Never 0.
 __device__ __forceinline__ uint64_t order_key(float x, uint32_t idx) {
@@ -127,16 +153,105 @@ struct Out {
   int32_t* top_ids;
 };
 
+// Largest element (NaN if there is one) and the elements kept at or above `low`, packed for 16-bit types
+__device__ __forceinline__ float largest(const Vec<float>& r) { return max_nan(max_nan(r.x[0], r.x[1]), max_nan(r.x[2], r.x[3])); }
+__device__ __forceinline__ Vec<float> at_least(const Vec<float>& r, float low) {
+  Vec<float> o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o.x[i] = fmaxf(r.x[i], low);
+  return o;
+}
+template <typename T2, typename T> __device__ __forceinline__ float largest16(const Vec<T>& r) {
+  const T2* p = reinterpret_cast<const T2*>(r.x);
+  const T2 hi = __hmax2_nan(__hmax2_nan(p[0], p[1]), __hmax2_nan(p[2], p[3]));
+  return max_nan(widen<T>(hi.x), widen<T>(hi.y));
+}
+template <typename T2, typename T> __device__ __forceinline__ Vec<T> at_least16(const Vec<T>& r, T low) {
+  Vec<T> o;
+  T2 l;
+  l.x = l.y = low;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) reinterpret_cast<T2*>(o.x)[i] = __hmax2(reinterpret_cast<const T2*>(r.x)[i], l);
+  return o;
+}
+__device__ __forceinline__ float largest(const Vec<__nv_bfloat16>& r) { return largest16<__nv_bfloat162>(r); }
+__device__ __forceinline__ float largest(const Vec<__half>& r) { return largest16<__half2>(r); }
+__device__ __forceinline__ Vec<__nv_bfloat16> at_least(const Vec<__nv_bfloat16>& r, __nv_bfloat16 low) { return at_least16<__nv_bfloat162>(r, low); }
+__device__ __forceinline__ Vec<__half> at_least(const Vec<__half>& r, __half low) { return at_least16<__half2>(r, low); }
+// A logit that stands for -inf: far below what counts, with a finite product
+template <typename T> __device__ __forceinline__ T floor_of(float c) { return narrow<T>(-1e37f / c); }
+template <> __device__ __forceinline__ __half floor_of<__half>(float c) { return narrow<__half>(fmaxf(-1e37f / c, -65504.f)); }
+
+// One thread's statistics.  With c = scale log2 e, the reference logit g and ref = RN(g c):
+//   s = sum 2^y, t = sum 2^y y,  y = x c - ref = (x - g) c + eps,  eps = g c - ref (the rounding of ref, known exactly)
+// one fma per element and free of rounding in the exponent.  Masked tokens are raised to a floor first (2^y is 0 all the
+// same, and y stays finite).  Where the floor is too near (fp16) or ref so large that its rounding counts, y is formed as
+// (RN(x scale) - RN(g scale)) log2 e + eps, kept above -160 (2^-160 is 0).
+template <typename T> struct Running {
+  float ref = 0.f, eps = 0.f, z = -INFINITY;                      // z = RN(g scale); -inf: nothing yet
+  uint64_t s2 = 0, t2 = 0;
+  bool bad = false;                                               // NaN or +inf seen
+  template <int kU> __device__ __forceinline__ void take(const Vec<T> (&r)[kU], float mx, float scale, float c, T low, float low_y) {
+    constexpr int kN = Vec<T>::kN;
+    const float top = __fmul_rn(mx, scale);
+    if (!(top < INFINITY)) bad = true;
+    if (!(top > -INFINITY)) return;                               // nothing but masked tokens (or NaN)
+    if (top > z + kSlack) {
+      const float ref_n = __fmul_rn(mx, c), eps_n = fabsf(ref_n) < kBigRef ? fmaf(mx, c, -ref_n) : 0.f;
+      // every earlier term by 2^d, its y by + d
+      const float d = z == -INFINITY ? 0.f : fmaxf((z - top) * kLog2e + (eps_n - eps), -160.f), f = ex2(d);
+      t2 = mul2(pair(f, f), fma2(pair(d, d), s2, t2));
+      s2 = mul2(pair(f, f), s2);
+      ref = ref_n;
+      eps = eps_n;
+      z = top;
+    }
+    if (fabsf(ref) < kBigRef && ref > low_y) {
+      const uint64_t c2 = pair(c, c), r2 = pair(-ref, -ref);
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const Vec<T> q = at_least(r[u], low);
+#pragma unroll
+        for (int i = 0; i < kN; i += 2) {
+          const uint64_t y = fma2(widen2(q, i / 2), c2, r2);
+          const float2 b = unpair(y);
+          const uint64_t e = pair(ex2(b.x), ex2(b.y));
+          s2 = add2(s2, e);
+          t2 = fma2(e, y, t2);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+#pragma unroll
+        for (int i = 0; i < kN; i += 2) {
+          float y[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) y[k] = fmaxf(fmaf(__fmul_rn(widen<T>(r[u].x[i + k]), scale) - z, kLog2e, eps), -160.f);
+          const uint64_t e = pair(ex2(y[0]), ex2(y[1]));
+          s2 = add2(s2, e);
+          t2 = fma2(e, pair(y[0], y[1]), t2);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ Stat stat() const {                  // relative to z, in natural units
+    const float2 s = unpair(s2), t = unpair(t2);
+    const float f = ex2(-eps), sum = s.x + s.y, ts = fmaf(-eps, sum, t.x + t.y);
+    return Stat{z, bad ? __int_as_float(0x7fffffff) : f * sum, f * ts * kLn2};
+  }
+};
+
 // Block = a row, or the rank-th of `parts` shares of its vectors; a cluster = a row.
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 4)
+template <typename T, bool kTop>
+__global__ void __launch_bounds__(kThreads, kTop ? 4 : 5)
 token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float scale, const int32_t* __restrict__ targets,
                       int n_targets, int n_top, Out out, int32_t* status, int parts) {
-  constexpr int kN = Vec<T>::kN, kW = kThreads / 32, kUnroll = 4;
+  constexpr int kN = Vec<T>::kN, kW = kThreads / 32;
   __shared__ Stat part[kW];
   __shared__ Stat mine;
   __shared__ uint64_t keys[kThreads];                             // best of every thread; later the cluster's lists
-  __shared__ uint64_t cand[kMaxCand];
+  __shared__ uint64_t cand[kTop ? kMaxCand : 1];
   __shared__ uint64_t top[kMaxTop];
   __shared__ uint64_t bound;
   __shared__ int n_cand;
@@ -145,72 +260,63 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
   const Row<const T> R(logits + row * ld, vocab);
   const int v_lo = static_cast<int>(static_cast<int64_t>(R.vecs) * rank / parts), v_hi = static_cast<int>(static_cast<int64_t>(R.vecs) * (rank + 1) / parts);
 
-  float m = -INFINITY, best = -INFINITY;
-  uint64_t s2 = 0, t2 = 0, key = 0;
-  bool bad = false;
-  const uint64_t log2e2 = pair(kLog2e, kLog2e);
-  auto take = [&](const float (&x)[kN], int v) {
-    float top_x = x[0];
+  // the targets' logits (one per thread) are fetched with the first vectors
+  int target = -1;
+  float target_x = 0.f;
+  if (rank == 0 && tid < n_targets) {
+    target = targets[row * n_targets + tid];
+    if (target >= 0 && target < vocab) target_x = widen<T>(logits[row * ld + target]);
+  }
+  Running<T> run;
+  float best = -INFINITY;
+  uint64_t key = 0;
+  const float c = scale * kLog2e;
+  const T low = floor_of<T>(c);
+  const float low_y = fmaf(widen<T>(low), c, 200.f);              // the floor counts as -inf for references above this
+  auto take = [&](const Vec<T>(&r)[kUnroll], int v, int count = kUnroll) {
+    float mx = largest(r[0]);
 #pragma unroll
-    for (int i = 1; i < kN; ++i) top_x = max_nan(top_x, x[i]);
-    if (n_top > 0 && (key == 0 || !(top_x <= best))) {            // (vectors come in rising order: equal logits keep the earlier key)
+    for (int u = 1; u < kUnroll; ++u) mx = max_nan(mx, largest(r[u]));
+    if (kTop && (key == 0 || !(mx <= best))) {               // (vectors come in rising order: equal logits keep the earlier key)
+#pragma unroll 1
+      for (int at = v; at < min(v + count * kThreads, v_hi); at += kThreads) {       // (seldom: from L1 or L2 again)
+        const Vec<T> x = R.whole(at) ? R.vec(at) : R.edge(at);
 #pragma unroll
-      for (int i = 0; i < kN; ++i) {
-        if (!R.inside(v, i)) continue;
-        const uint64_t k = order_key(x[i], R.index(v, i));
-        if (k > key) key = k;
+        for (int i = 0; i < kN; ++i) {
+          const uint64_t k = R.inside(at, i) ? order_key(widen<T>(x.x[i]), R.index(at, i)) : 0;
+          if (k > key) key = k;
+        }
       }
-      best = top_x;
+      best = mx;
     }
-    const float z = __fmul_rn(top_x, scale);
-    if (!(z < INFINITY)) bad = true;
-    if (!(z > -INFINITY)) return;                                 // nothing but masked tokens (or NaN)
-    if (z > m + kSlack || m == -INFINITY) {
-      const float d = fmaxf(m - z, -120.f), f = ex2(d * kLog2e);       // every earlier term by e^d, its (x-m) by + d
-      const uint64_t f2 = pair(f, f), d2 = pair(d, d);
-      t2 = mul2(f2, fma2(d2, s2, t2));
-      s2 = mul2(f2, s2);
-      m = z;
-    }
-    const uint64_t ref = pair(-m, -m);
-#pragma unroll
-    for (int i = 0; i < kN; i += 2) {
-      // x * scale is rounded as in m (a product fused with the subtraction would leave its rounding error, which is huge
-      // near the end of fp32's range), by single products: the assembler fuses a packed product with a packed sum
-      const float2 a = unpair(add2(pair(__fmul_rn(x[i], scale), __fmul_rn(x[i + 1], scale)), ref));
-      const uint64_t y = pair(fmaxf(a.x, -120.f), fmaxf(a.y, -120.f));         // e^-120 is 0 in fp32, and 0 * -120 too
-      const float2 b = unpair(mul2(y, log2e2));
-      const uint64_t e = pair(ex2(b.x), ex2(b.y));
-      s2 = add2(s2, e);
-      t2 = fma2(e, y, t2);
-    }
+    run.take(r, mx, scale, c, low, low_y);
   };
   int v = v_lo + tid;
-  auto take_one = [&]() {
-    float x[kN];
-    R.load(v, x, -INFINITY);
-    take(x, v);
-    v += kThreads;
-  };
-  if (v < v_hi && !R.whole(v)) take_one();
-  for (; v + (kUnroll - 1) * kThreads < v_hi && R.whole(v + (kUnroll - 1) * kThreads); v += kUnroll * kThreads) {      // all loads first
+  {
     Vec<T> r[kUnroll];
+    if (v == 0 && v < v_hi && !R.whole(0)) {                      // a row that starts inside a vector (or a single partial one)
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) r[u] = *reinterpret_cast<const Vec<T>*>(R.base + static_cast<int64_t>(v + u * kThreads) * kN);
+      for (int u = 0; u < kUnroll; ++u) r[u] = R.edge(u ? R.vecs : 0);               // (behind the row: -inf throughout)
+      take(r, 0, 1);
+      v = kThreads;
+    }
+    const int v_whole = v_hi - (rank == parts - 1 && !R.whole(R.vecs - 1));
+    for (; v + (kUnroll - 1) * kThreads < v_whole; v += kUnroll * kThreads) {        // all loads first
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      float x[kN];
+      for (int u = 0; u < kUnroll; ++u) r[u] = R.vec(v + u * kThreads);
+      take(r, v);
+    }
+    if (v < v_hi) {                                               // what is left; -inf where there is nothing
 #pragma unroll
-      for (int i = 0; i < kN; ++i) x[i] = widen<T>(r[u].x[i]);
-      take(x, v + u * kThreads);
+      for (int u = 0; u < kUnroll; ++u) {
+        const int at = v + u * kThreads;
+        if (at < v_whole) r[u] = R.vec(at);
+        else r[u] = R.edge(at < v_hi ? at : R.vecs);
+      }
+      take(r, v);
     }
   }
-  while (v < v_hi) take_one();
-  const float2 sp = unpair(s2), tp = unpair(t2);
-  Stat st{m, bad ? __int_as_float(0x7fffffff) : sp.x + sp.y, tp.x + tp.y};
-#pragma unroll
-  for (int o = 16; o; o >>= 1)
-    st = merge(st, Stat{__shfl_xor_sync(~0u, st.m, o), __shfl_xor_sync(~0u, st.s, o), __shfl_xor_sync(~0u, st.t, o)});
+  Stat st = join_lanes<32>(run.stat());
   if (lane == 0) part[w] = st;
   if (tid == 0) {
     n_cand = 0;
@@ -219,10 +325,9 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
   if (tid < kMaxTop) top[tid] = 0;
   keys[tid] = key;
   __syncthreads();
-  st = part[0];
-  for (int i = 1; i < kW; ++i) st = merge(st, part[i]);
+  st = join_lanes<kW>(part[lane % kW]);                           // (every warp: all threads know the row's)
 
-  if (n_top > 0) {
+  if constexpr (kTop) {
     if (key != 0) {
       int above = 0;
 #pragma unroll 8
@@ -233,11 +338,10 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
     if (key >= bound) {
 #pragma unroll 4
       for (v = v_lo + tid; v < v_hi; v += kThreads) {
-        float x[kN];
-        R.load(v, x, -INFINITY);
+        const Vec<T> x = R.whole(v) ? R.vec(v) : R.edge(v);
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
-          const uint64_t k = R.inside(v, i) ? order_key(x[i], R.index(v, i)) : 0;
+          const uint64_t k = R.inside(v, i) ? order_key(widen<T>(x.x[i]), R.index(v, i)) : 0;
           if (k >= bound) {
             const int at = atomicAdd(&n_cand, 1);
             if (at < kMaxCand) cand[at] = k;
@@ -247,8 +351,8 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
     }
     __syncthreads();
     if (n_cand <= kMaxCand) {
-      for (int c = tid; c < n_cand; c += kThreads) {
-        const uint64_t k = cand[c];
+      for (int j = tid; j < n_cand; j += kThreads) {
+        const uint64_t k = cand[j];
         int above = 0;
         for (int i = 0; i < n_cand; ++i) above += cand[i] > k;
         if (above < n_top) top[above] = k;
@@ -258,12 +362,11 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
       for (int r = 0; r < n_top; ++r) {
         uint64_t k = 0;
         for (v = v_lo + tid; v < v_hi; v += kThreads) {
-          float x[kN];
-          R.load(v, x, -INFINITY);
+          const Vec<T> x = R.whole(v) ? R.vec(v) : R.edge(v);
 #pragma unroll
           for (int i = 0; i < kN; ++i) {
-            const uint64_t c = R.inside(v, i) ? order_key(x[i], R.index(v, i)) : 0;
-            if (c < last && c > k) k = c;
+            const uint64_t ck = R.inside(v, i) ? order_key(widen<T>(x.x[i]), R.index(v, i)) : 0;
+            if (ck < last && ck > k) k = ck;
           }
         }
         __syncthreads();
@@ -282,7 +385,7 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
     if (rank == 0) {
-      for (int i = 1; i < parts; ++i) st = merge(st, *cluster.map_shared_rank(&mine, i));
+      st = join_lanes<kMaxCluster>(lane % kMaxCluster < parts ? *cluster.map_shared_rank(&mine, lane % kMaxCluster) : Stat{-INFINITY, 0.f, 0.f});
       if (n_top > 0) {
         const int n = parts * n_top;                              // at most kThreads
         uint64_t k = 0;
@@ -310,10 +413,9 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
     if (out.lse) out.lse[row] = lse;
     if (out.entropy) out.entropy[row] = lse == -INFINITY ? 0.f : logf(st.s) - st.t / st.s;
   }
-  for (int i = tid; i < n_targets; i += kThreads) {
-    const int t = targets[row * n_targets + i];
-    if (t >= vocab) atomicExch(status, static_cast<int32_t>(SZO_ERR_INVALID_ARG));
-    out.logp[row * n_targets + i] = t < 0 ? 0.f : t >= vocab ? __int_as_float(0x7fffffff) : value(widen<T>(x[t]));
+  if (tid < n_targets) {
+    if (target >= vocab) atomicExch(status, static_cast<int32_t>(SZO_ERR_INVALID_ARG));
+    out.logp[row * n_targets + tid] = target < 0 ? 0.f : target >= vocab ? __int_as_float(0x7fffffff) : value(target_x);
   }
   if (tid < n_top) {
     const uint32_t id = key_index(top[tid]);
@@ -323,78 +425,120 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
 }
 
 // d_logits[j] = scale * ( sum_i d_logp[i] (1[j = t_i] - p_j) - d_entropy p_j (log p_j + H) ): a stream of one read and one
-// write.  Block = kChunk vectors of a row, all loads first; the block's own targets, mostly none, are picked out before.
-constexpr int kBwdUnroll = 4, kChunk = kThreads * kBwdUnroll;
+// write.  Block = one of `parts` shares of a row's vectors: four vectors per thread are on their way while four are worked
+// on; the row's targets are sorted out once, while the first are.
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 4)
 token_logprobs_bwd_kernel(const T* logits, int64_t ld, int vocab, float scale, const int32_t* __restrict__ targets, int n_targets,
                           const float* __restrict__ lse_in, const float* __restrict__ entropy, const float* __restrict__ d_logp,
-                          const float* __restrict__ d_entropy, T* d_logits, int64_t dld, int chunks) {
+                          const float* __restrict__ d_entropy, T* d_logits, int64_t dld, int parts) {
   constexpr int kN = Vec<T>::kN;
   __shared__ int own_t[kMaxTargets];
   __shared__ float own_g[kMaxTargets];
+  __shared__ float sum_s;
   __shared__ int n_own;
-  const int64_t row = blockIdx.x / chunks;
-  const int v0 = blockIdx.x % chunks * kChunk, tid = threadIdx.x;
+  const int64_t row = blockIdx.x / parts;
+  const int rank = blockIdx.x % parts, tid = threadIdx.x;
   const Row<const T> X(logits + row * ld, vocab);
   const Row<T> D(d_logits + row * dld, vocab);
-  Vec<T> r[kBwdUnroll];
+  const int v_lo = static_cast<int>(static_cast<int64_t>(X.vecs) * rank / parts), v_hi = static_cast<int>(static_cast<int64_t>(X.vecs) * (rank + 1) / parts);
   const bool same = X.off == D.off;                               // else element by element (row strides that differ modulo 16 bytes)
+  Vec<T> r[kUnroll], next[kUnroll];
+  auto load4 = [&](Vec<T>(&x)[kUnroll], int v) {
 #pragma unroll
-  for (int u = 0; u < kBwdUnroll; ++u) {
-    const int v = v0 + u * kThreads + tid;
-    if (v < X.vecs && X.whole(v)) r[u] = *reinterpret_cast<const Vec<T>*>(X.base + static_cast<int64_t>(v) * kN);
-  }
+    for (int u = 0; u < kUnroll; ++u)
+      if (v + u * kThreads < v_hi && X.whole(v + u * kThreads)) x[u] = X.vec(v + u * kThreads);
+  };
+  int v = v_lo + tid;
+  load4(r, v);
   const float lse = lse_in[row], gh = d_entropy ? d_entropy[row] : 0.f, ent = d_entropy ? entropy[row] : 0.f;
-  float sum = 0.f;
-  for (int i = 0; i < n_targets; ++i) {
-    const int t = targets[row * n_targets + i];
-    if (t >= 0 && t < vocab) sum += d_logp[row * n_targets + i];
-  }
-  if (tid == 0) {                                                 // in order: the same target twice adds up the same way every time
-    n_own = 0;
-    for (int i = 0; i < n_targets; ++i) {
-      const int t = targets[row * n_targets + i];
-      if (t < 0 || t >= vocab || t + X.off < v0 * kN || t + X.off >= (v0 + kChunk) * kN) continue;
-      int at = 0;
-      while (at < n_own && own_t[at] != t) ++at;
-      own_g[at] = at < n_own ? own_g[at] + d_logp[row * n_targets + i] : d_logp[row * n_targets + i];
-      own_t[at] = t;
-      if (at == n_own) ++n_own;
+  if (tid < 32) {                                                 // in order: the same target twice adds up the same way every time
+    int n = 0;
+    float sum = 0.f;
+    for (int i0 = 0; i0 < n_targets; i0 += 32) {
+      const int i = i0 + tid;
+      const int t = i < n_targets ? targets[row * n_targets + i] : -1;
+      const float g = i < n_targets ? d_logp[row * n_targets + i] : 0.f;
+      for (int k = 0; k < min(32, n_targets - i0); ++k) {
+        const int tk = __shfl_sync(0xffffffffu, t, k);
+        const float gk = __shfl_sync(0xffffffffu, g, k);
+        if (tk < 0 || tk >= vocab) continue;
+        sum += gk;
+        const int at = tk + X.off;
+        if (at < v_lo * kN || at >= v_hi * kN) continue;
+        if (tid == 0) {
+          int j = 0;
+          while (j < n && own_t[j] != tk) ++j;
+          own_g[j] = j < n ? own_g[j] + gk : gk;
+          own_t[j] = tk;
+          n = j < n ? n : n + 1;
+        }
+      }
+    }
+    if (tid == 0) {
+      n_own = n;
+      sum_s = sum;
     }
   }
   __syncthreads();
-  const float poison = isnan(lse) ? lse : 0.f;
-  const bool empty = lse == -INFINITY;
-  const float a = -sum - gh * ent;                                // -p (sum + gh H) - gh p log p
+  const int n = n_own;
+  // With c = scale log2 e, ref = RN(lse log2 e) and y = x c - ref, one fma: p = 2^(y + delta), log p = (y + delta) ln 2 with
+  // delta = ref - lse log2 e, so that scale times the formula without its targets is 2^y (A + B y).  Masked logits are raised
+  // to a floor as in the forward pass; where the floor is too near (fp16) or ref too large, the plain form.
+  const float c = scale * kLog2e, ref = lse * kLog2e, delta = -fmaf(lse, kLog2e, -ref), F = exp2f(delta);
+  const float a = -sum_s - gh * ent;                              // p (a - gh log p)
+  const float B = -gh * kLn2 * F * scale, A = fmaf(B, delta, a * F * scale);
+  const T low = floor_of<T>(c);
+  const bool fast = fabsf(lse) < kBigRef && ref > fmaf(widen<T>(low), c, 200.f);
+  const uint64_t c2 = pair(c, c), r2 = pair(-ref, -ref), A2 = pair(A, A), B2 = pair(B, B);
+  for (; v < v_hi; v += kUnroll * kThreads) {
+    load4(next, v + kUnroll * kThreads);
 #pragma unroll
-  for (int u = 0; u < kBwdUnroll; ++u) {
-    const int v = v0 + u * kThreads + tid;
-    if (v >= X.vecs) continue;
-    const bool whole = X.whole(v);
-    float g[kN];
+    for (int u = 0; u < kUnroll; ++u) {
+      const int at = v + u * kThreads;
+      if (at >= v_hi) break;
+      const bool whole = X.whole(at);
+      if (!whole) r[u] = X.edge(at);
+      float2 g[kN / 2];
+      if (fast) {
+        const Vec<T> q = at_least(r[u], low);
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const float x = whole ? widen<T>(r[u].x[i]) : X.inside(v, i) ? widen<T>(X.base[static_cast<int64_t>(v) * kN + i]) : 0.f;
-      const float lp = fmaxf(__fmul_rn(x, scale) - lse, -120.f), p = ex2(lp * kLog2e);        // e^-120 is 0 in fp32
-      g[i] = fmaf(p, fmaf(-gh, lp, a), poison);
+        for (int i = 0; i < kN / 2; ++i) {
+          const uint64_t y = fma2(widen2(q, i), c2, r2);
+          const float2 f = unpair(y);
+          g[i] = unpair(mul2(pair(ex2(f.x), ex2(f.y)), fma2(B2, y, A2)));
+        }
+      } else {
+        auto plain = [&](float x) {
+          const float lp = fmaxf(__fmul_rn(x, scale) - lse, -120.f);
+          return lse == -INFINITY ? 0.f : isnan(lse) ? lse : scale * ex2(lp * kLog2e) * fmaf(-gh, lp, a);
+        };
+#pragma unroll
+        for (int i = 0; i < kN / 2; ++i) g[i] = make_float2(plain(widen<T>(r[u].x[2 * i])), plain(widen<T>(r[u].x[2 * i + 1])));
+      }
+      for (int k = 0; k < n; ++k) {
+        const int j = own_t[k] + X.off - at * kN;
+        if (j >= 0 && j < kN && lse != -INFINITY) {
+#pragma unroll
+          for (int i = 0; i < kN / 2; ++i) {
+            if (j == 2 * i) g[i].x = fmaf(scale, own_g[k], g[i].x);
+            if (j == 2 * i + 1) g[i].y = fmaf(scale, own_g[k], g[i].y);
+          }
+        }
+      }
+      Vec<T> o;
+#pragma unroll
+      for (int i = 0; i < kN / 2; ++i) narrow2(o, i, g[i]);
+      if (whole && same) {
+        *reinterpret_cast<Vec<T>*>(D.base + static_cast<int64_t>(at) * kN) = o;
+      } else {
+#pragma unroll
+        for (int i = 0; i < kN; ++i)
+          if (X.inside(at, i)) d_logits[row * dld + X.index(at, i)] = o.x[i];
+      }
     }
-    for (int k = 0; k < n_own; ++k) {
-      const int at = own_t[k] + X.off - v * kN;
 #pragma unroll
-      for (int i = 0; i < kN; ++i)
-        if (at == i) g[i] += own_g[k];
-    }
-    Vec<T> o;
-#pragma unroll
-    for (int i = 0; i < kN; ++i) o.x[i] = narrow<T>(empty ? 0.f : g[i] * scale);
-    if (whole && same) {
-      *reinterpret_cast<Vec<T>*>(D.base + static_cast<int64_t>(v) * kN) = o;
-    } else {
-#pragma unroll
-      for (int i = 0; i < kN; ++i)
-        if (X.inside(v, i)) d_logits[row * dld + X.index(v, i)] = o.x[i];
-    }
+    for (int u = 0; u < kUnroll; ++u) r[u] = next[u];
   }
 }
 
@@ -448,8 +592,9 @@ szo_status szo_token_logprobs(const void* logits, szo_dtype dtype, int64_t rows,
   cfg.attrs = attr;
   cfg.numAttrs = parts > 1 ? 1 : 0;
 #define SZO_LOGP(T)                                                                                                              \
-  SZO_CHECK_CUDA(cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T>, static_cast<const T*>(logits), row_stride, static_cast<int>(vocab), \
-                                    scale, targets, n_targets, n_top, out, status, parts))
+  SZO_CHECK_CUDA(cudaLaunchKernelEx(&cfg, n_top > 0 ? token_logprobs_kernel<T, true> : token_logprobs_kernel<T, false>,              \
+                                    static_cast<const T*>(logits), row_stride, static_cast<int>(vocab), scale, targets, n_targets, n_top, \
+                                    out, status, parts))
   if (dtype == SZO_F32) SZO_LOGP(float);
   else if (dtype == SZO_BF16) SZO_LOGP(__nv_bfloat16);
   else SZO_LOGP(__half);
@@ -472,13 +617,15 @@ szo_status szo_token_logprobs_bwd(const void* logits, szo_dtype dtype, int64_t r
               "buffers must be 16-byte aligned");
   if (rows == 0) return SZO_OK;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // vectors of a row, one more for a row that does not start on 16 bytes
-  const int64_t chunks = ceil_div(ceil_div(vocab, 16 / static_cast<int64_t>(dtype_size(dtype))) + 1, kChunk);
-  SZO_REQUIRE(rows * chunks <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows for one launch");
+  // A row is cut while that leaves SMs without their four blocks and each thread its four vectors
+  const int64_t vecs = ceil_div(vocab, 16 / static_cast<int64_t>(dtype_size(dtype)));
+  int parts = 1;
+  while (rows * parts < 148 * 4 && vecs >= static_cast<int64_t>(parts) * 2 * kThreads * kUnroll) parts *= 2;
+  SZO_REQUIRE(rows * parts <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows for one launch");
 #define SZO_LOGP_BWD(T)                                                                                                     \
-  token_logprobs_bwd_kernel<T><<<static_cast<unsigned>(rows * chunks), kThreads, 0, st>>>(static_cast<const T*>(logits), row_stride, \
+  token_logprobs_bwd_kernel<T><<<static_cast<unsigned>(rows * parts), kThreads, 0, st>>>(static_cast<const T*>(logits), row_stride, \
       static_cast<int>(vocab), scale, targets, n_targets, lse, entropy, d_logp, d_entropy, static_cast<T*>(d_logits), d_row_stride,  \
-      static_cast<int>(chunks))
+      parts)
   if (dtype == SZO_F32) SZO_LOGP_BWD(float);
   else if (dtype == SZO_BF16) SZO_LOGP_BWD(__nv_bfloat16);
   else SZO_LOGP_BWD(__half);
