@@ -29,8 +29,7 @@
 
 #include <cmath>
 
-#include "kv8.cuh"
-#include "tc_common.cuh"
+#include "kv8_attention.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -39,7 +38,7 @@ namespace kv8 {
 
 namespace {
 
-constexpr int kStep = 16, kUnit = 32, kDepth = 2;     // kDepth: units of a warp's ring
+constexpr int kUnit = 32, kDepth = 2;     // kDepth: units of a warp's ring
 // The largest weight is 2^kOffset when the reference maximum m is set; m follows the running maximum only once that
 // is more than 2^kSlack above it (weights then stay below 2^15), so the outputs are rescaled a few times per sequence.
 constexpr float kOffset = 12.0f, kSlack = 3.0f;
@@ -55,19 +54,10 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 // what pack_f16 lost of (lo, hi), again as fp16
 __device__ __forceinline__ uint32_t pack_rest(uint32_t packed, float lo, float hi) {
   const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&packed));
   return pack_f16(lo - f.x, hi - f.y);
-}
-__device__ __forceinline__ float ex2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
 }
 __device__ __forceinline__ uint4 lds16(uint32_t a) {
   uint4 r;
@@ -273,7 +263,7 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
       have[a] = fe[a] != -INFINITY;
       el[a] = have[a] ? exp2_int(-static_cast<int>(fe[a])) : 0.f;
     }
-    if (!tc::mbar_wait(bars + 8 * slot, phase, &abort_flag, V.status, 0)) break;
+    if (!__all_sync(0xffffffffu, tc::mbar_wait(bars + 8 * slot, phase, &abort_flag, V.status, 0))) break;
     const uint32_t at = ring + slot * kUnit * HD * 2;
     float c[2][NT][4];
 #pragma unroll
@@ -494,15 +484,6 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   cluster.sync();                                                 // nobody leaves while its sums are being read
 }
 
-// The row buffers and heads of a call
-struct Rows {
-  const void* q;
-  void* o;
-  int64_t q_stride, o_stride;
-  int H;
-  float scale;
-};
-
 // Joins the partial results in `ws` in split order: a block per (row of a tile, item), a thread per dim.
 template <typename T, int HD>
 __global__ void __launch_bounds__(HD)
@@ -592,6 +573,8 @@ Plan plan(const View& V, int H) {
 
 template <typename T, int HD>
 szo_status launch_attention(const View& V, const Rows& A, float* ws, cudaStream_t st) {
+  if constexpr (sizeof(T) == 2)
+    if (static_cast<int64_t>(V.max_new) * (A.H / V.hkv) > 64) return launch_attention_tc<T, HD>(V, A, st);
   const Plan p = plan(V, A.H);
   if (p.wide) return launch_rows<T, HD, 1, 12>(V, A, p.nsplit, ws, st);
   return p.rows == 8 ? launch_rows<T, HD, 1, 4>(V, A, p.nsplit, nullptr, st) : launch_rows<T, HD, 2, 4>(V, A, p.nsplit, nullptr, st);

@@ -1,0 +1,546 @@
+// Attention over the 8-bit paged cache for many query rows per key/value head (prompts, chunks of prompts) on the
+// 5th-generation tensor cores.
+//
+// A block takes 256 query rows (new tokens x heads of one key/value head) of a sequence as two row tiles of 128 and
+// walks over the cached positions 128 at a time.  Per step and row tile: S = Q K^T (128 x 128), softmax weights P,
+// O += P V, all accumulated in TMEM (S and O of both row tiles fill its 512 columns; P, fp16, takes the place of S and
+// is the A operand of the second product from there).  The bound is the tensor pipe (2 x 2 x 128 x 128 x 128 multiply-
+// adds per step), with three more close behind it: the exponentials (16 per cycle and SM: as long as the products),
+// shared memory (operands of the products and the converted tiles, 128 bytes per cycle) and the issue slots of the
+// softmax.  Hence the split into warps that only meet at mbarriers:
+//   warps 0-3, 4-7   softmax of row tile 0 and 1, one row per thread (a TMEM lane): no shuffles.  While one tile's weights
+//                    are formed, the tensor cores work for the other
+//   warps 8-11       bring the e4m3 codes of the next 128 positions from global memory to registers, turn them into fp16
+//                    (exact) and store them in the swizzled layout that the products read.  Through registers and not by
+//                    TMA: a staged copy would cost another pass of shared memory each way
+//   warp 12          one thread issues every product
+// Numbers are those of the kernel for few rows: queries divided by a power of two per row, weights relative to each
+// token's contribution (logit + exponent of its page's value scale), sums of weights divided by that scale again.
+// The reference maximum follows the running maximum once that is 2^8 above it, so O is rescaled in TMEM a few times
+// per row; weights stay between 2^-24 and 2^15.
+#include <cmath>
+
+#include "kv8_attention.cuh"
+
+namespace szo {
+namespace kv8 {
+
+namespace {
+
+constexpr int kTile = 128;                     // rows of a row tile, positions of a step
+constexpr int kConv = 4, kMmaWarp = 8 + kConv, kTcThreads = (kMmaWarp + 1) * 32;      // (13 warps: 128 registers per thread)
+constexpr float kTcOffset = 7.0f, kTcSlack = 8.0f;
+constexpr uint32_t kTmemCols = 512;
+
+__device__ __forceinline__ void tmem_alloc(uint32_t result_smem, uint32_t ncols) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(result_smem), "r"(ncols) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+}
+// D += A B, A and B in shared memory
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// D += A B, A in TMEM
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Arrives on the barrier when the products issued so far are done
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+        "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
+        "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]),
+        "=r"(v[31])
+      : "r"(addr)
+      : "memory");
+}
+// Waits for this thread's TMEM loads; v is an operand so that its uses stay behind
+__device__ __forceinline__ void tmem_load_wait(uint32_t (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                 "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]),
+                 "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]),
+                 "+r"(v[28])
+               :
+               : "memory");
+  asm volatile("" : "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
+}
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(v[0]),
+      "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]),
+      "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+      "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(v[0]),
+      "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]),
+      "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t p) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// fp16 operand tiles in shared memory: 128 rows in blocks of 64 columns (one 128-byte row each), 128-byte swizzle.
+__device__ __forceinline__ uint32_t tile_chunk(uint32_t base, int row, int chunk) {      // 16-byte chunk (8 columns) of a row
+  return base + (chunk >> 3) * (kTile * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+}
+__device__ __forceinline__ void sts16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+// Descriptor of such a tile as an operand whose rows are the contracted dimension (columns of the result contiguous):
+// blocks of 64 columns kTile * 128 bytes apart, groups of 8 rows 1024 bytes apart
+__device__ __forceinline__ uint64_t make_desc_rows_contracted(uint32_t smem_addr) {
+  return static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>((kTile * 128) >> 4) << 16) |
+         (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// Instruction descriptors, kind::f16, fp16 x fp16 with fp32 sums; bit 16: B's rows are the contracted dimension
+constexpr uint32_t make_idesc_f16(int M, int N, bool b_rows_contracted) {
+  return (1u << 4) | (b_rows_contracted ? 1u << 16 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kTcThreads, 1)
+kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __restrict__ o, int64_t o_stride, int H, float scale, int row_tiles) {
+  constexpr int kBytes = kTile * HD * 2;                          // of an operand tile
+  constexpr int kLanes = HD / 16, kRowsPass = kConv * 32 / kLanes, kPass = kTile / kRowsPass;
+  extern __shared__ __align__(1024) unsigned char smem_tc[];
+  struct alignas(16) Step {
+    float ks, fe, el;                                             // 2^(keys' exponent), values' exponent, its inverse power; no page: 0, -inf, 0
+    float pad;
+  };
+  __shared__ Step meta[4][kTile / kStep];
+  __shared__ int nan_at[HD];
+  __shared__ __align__(8) uint64_t bars[20];
+  __shared__ uint32_t tmem_ptr;
+  __shared__ int abort_flag;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int64_t others = static_cast<int64_t>(V.batch) * V.hkv;
+  const int rt = row_tiles - 1 - static_cast<int>(blockIdx.x / others);          // the longest rows first
+  const int h = static_cast<int>(blockIdx.x % others) % V.hkv, b = static_cast<int>(blockIdx.x % others) / V.hkv, G = H / V.hkv;
+  const Seq seq = load_seq(V, b);
+  const int64_t r0 = static_cast<int64_t>(rt) * 2 * kTile, left = static_cast<int64_t>(seq.n) * G - r0;
+  if (left <= 0) return;
+  const int n_rows = static_cast<int>(left < 2 * kTile ? left : 2 * kTile);
+  const int first = seq.len - seq.n;                              // position of the sequence's row 0; negative: padding
+  auto pos_of = [&](int r) { return first + static_cast<int>((r0 + r) / G); };
+  int n_kv[2], lo[2];                                             // steps of each row tile; position of its first row
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int rows = n_rows - kTile * i < kTile ? n_rows - kTile * i : kTile;
+    lo[i] = pos_of(kTile * i);
+    const int hi = rows > 0 ? pos_of(kTile * i + rows - 1) : -1;
+    n_kv[i] = hi < 0 ? 0 : hi / kTile + 1;
+  }
+  const int n = n_kv[1] > n_kv[0] ? n_kv[1] : n_kv[0];
+  const int n_steps = (pos_of(n_rows - 1) < 0 ? -1 : pos_of(n_rows - 1) / kStep) + 1;      // of 16 positions
+
+  const uint32_t base = (tc::smem_u32(smem_tc) + 1023u) & ~1023u;
+  auto v_tile = [&](int s) { return base + s * kBytes; };
+  auto k_tile = [&](int s) { return base + (2 + s) * kBytes; };
+  auto q_tile = [&](int i) { return base + (4 + i) * kBytes; };
+  auto bar = [&](int i) { return tc::smem_u32(&bars[i]); };
+  const int kSFull = 0, kPFull = 2, kODone = 4, kKFull = 6, kKEmpty = 8, kVFull = 10, kVEmpty = 12, kQFull = 14, kDrain = 15, kMeta = 16;
+  if (tid == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(bar(kSFull + i), 1);
+      tc::mbar_init(bar(kPFull + i), 4);
+      tc::mbar_init(bar(kODone + i), 1);
+      tc::mbar_init(bar(kKFull + i), kConv);
+      tc::mbar_init(bar(kKEmpty + i), 1);
+      tc::mbar_init(bar(kVFull + i), kConv);
+      tc::mbar_init(bar(kVEmpty + i), 1);
+    }
+    tc::mbar_init(bar(kQFull), 8);
+    tc::mbar_init(bar(kDrain), 1);
+    for (int i = 0; i < 4; ++i) tc::mbar_init(bar(kMeta + i), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  for (int i = tid; i < HD; i += kTcThreads) nan_at[i] = 0x7fffffff;
+  if (warp == kMmaWarp) tmem_alloc(tc::smem_u32(&tmem_ptr), kTmemCols);
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = tmem_ptr;
+  auto wait = [&](int i, int phase, unsigned backoff) { return tc::mbar_wait(bar(i), phase & 1, &abort_flag, V.status, backoff); };
+  auto wait_warp = [&](int i, int phase, unsigned backoff) { return __all_sync(0xffffffffu, wait(i, phase, backoff)) != 0; };
+
+  if (warp < 8) {
+    // ------------------------------------------------------------------ softmax: thread = row
+    const int i = warp >> 2, r = tid;                             // row tile, row of the block
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_addr = tmem + lanes + i * kTile, o_addr = tmem + lanes + 2 * kTile + i * kTile;
+    const int rpos = pos_of(r < n_rows ? r : n_rows - 1);         // (rows that are not there: anything, they are not stored)
+    const int64_t q_off = (seq.row0 + (r0 + r) / G), head = h * G + (r0 + r) % G;
+    float rs;
+    {
+      const T* qp = q + q_off * q_stride + head * HD;
+      float amax = 0.f;
+      bool fine = true;
+      if (r < n_rows) {
+#pragma unroll 4
+        for (int c = 0; c < HD / 8; ++c) {
+          const Vec<T> x = *reinterpret_cast<const Vec<T>*>(qp + 8 * c);
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const float y = widen<T>(x.x[u]);
+            amax = fmaxf(amax, fabsf(y));
+            fine = fine && isfinite(y);
+          }
+        }
+      }
+      const int e = min(max((__float_as_int(amax) >> 23) - 127, -126), 126);
+      const float inv = scale < 0.f ? -exp2_int(-e) : exp2_int(-e);
+      rs = fine ? exp2_int(e) * (fabsf(scale) * 1.4426950408889634f) : __int_as_float(0x7fffffff);
+#pragma unroll 4
+      for (int c = 0; c < HD / 8; ++c) {
+        Vec<T> x = {};
+        if (r < n_rows) x = *reinterpret_cast<const Vec<T>*>(qp + 8 * c);
+        uint32_t p[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) p[u] = pack_f16(widen<T>(x.x[2 * u]) * inv, widen<T>(x.x[2 * u + 1]) * inv);
+        sts16(tile_chunk(q_tile(i), r & (kTile - 1), c), p[0], p[1], p[2], p[3]);
+      }
+      tc::fence_async_smem();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(bar(kQFull));
+    }
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    for (int j = 0; j < n_kv[i] && ok; ++j) {
+      if (!(ok = wait_warp(kMeta + (j & 3), j >> 2, 20) && wait_warp(kSFull + i, j, 20))) break;
+      tc::tc_fence_after();
+      const Step* st = meta[j & 3];
+      const int limit = rpos - j * kTile;                         // columns up to this one are seen
+      const bool masked = j * kTile + kTile - 1 > lo[i];
+      uint32_t va[32], vb[32];
+      float mx = -INFINITY;
+      auto peak = [&](uint32_t(&v)[32], int c) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const float ks = st[2 * c + s].ks, fe = st[2 * c + s].fe;
+          float t = -INFINITY;
+          if (masked) {
+#pragma unroll
+            for (int u = 0; u < 16; ++u) t = fmaxf(t, 32 * c + 16 * s + u > limit ? -INFINITY : __uint_as_float(v[16 * s + u]));
+          } else {
+#pragma unroll
+            for (int u = 0; u < 16; ++u) t = fmaxf(t, __uint_as_float(v[16 * s + u]));
+          }
+          // (nothing seen: t = -inf, which a zero factor must not turn into NaN)
+          mx = fmaxf(mx, t == -INFINITY ? -INFINITY : fmaf(t, rs * ks, fe));
+        }
+      };
+      tmem_load32(s_addr, va);
+#pragma unroll
+      for (int c = 0; c < 4; c += 2) {
+        tmem_load_wait(va);
+        tmem_load32(s_addr + 32 * (c + 1), vb);
+        peak(va, c);
+        tmem_load_wait(vb);
+        tmem_load32(s_addr + 32 * ((c + 2) & 3), va);             // (the last one: chunk 0 again, for the weights)
+        peak(vb, c + 1);
+      }
+      const bool need = mx > m + kTcSlack || (m == -INFINITY && mx > -INFINITY);
+      if (__any_sync(0xffffffffu, need)) {
+        const float m_new = need ? mx : m, corr = need ? ex2(m - m_new) : 1.f;       // (mx > m there; ex2(-inf) = 0)
+        if (j > 0) {
+          tmem_load_wait(va);
+          if (!(ok = wait_warp(kODone + i, j - 1, 0))) break;
+          tc::tc_fence_after();
+#pragma unroll
+          for (int c = 0; c < HD / 32; ++c) {
+            tmem_load32(o_addr + 32 * c, vb);
+            tmem_load_wait(vb);
+#pragma unroll
+            for (int u = 0; u < 32; ++u) vb[u] = __float_as_uint(__uint_as_float(vb[u]) * corr);
+            tmem_store32(o_addr + 32 * c, vb);
+          }
+          l *= corr;
+        }
+        m = m_new;
+      }
+      const float ref = (m == -INFINITY ? 0.f : m) - kTcOffset;
+      auto weigh = [&](uint32_t(&v)[32], int c) {
+        uint32_t p[16];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const Step x = st[2 * c + s];
+          const float f = rs * x.ks, d = x.fe - ref;
+          const uint64_t f2 = pair(f, f), d2 = pair(d, d);
+          uint64_t sum = 0;
+#pragma unroll
+          for (int u = 0; u < 16; u += 2) {
+            float2 y = unpair(fma2(pair(__uint_as_float(v[16 * s + u]), __uint_as_float(v[16 * s + u + 1])), f2, d2));
+            if (masked) {
+              if (32 * c + 16 * s + u > limit) y.x = -INFINITY;
+              if (32 * c + 16 * s + u + 1 > limit) y.y = -INFINITY;
+            }
+            y = make_float2(ex2(y.x), ex2(y.y));
+            sum = add2(sum, pair(y.x, y.y));
+            p[8 * s + u / 2] = pack_f16(y.x, y.y);
+          }
+          const float2 t = unpair(sum);
+          l = fmaf(x.el, t.x + t.y, l);
+        }
+        tmem_store16(s_addr + 16 * c, p);                         // over columns that this thread has read
+      };
+#pragma unroll
+      for (int c = 0; c < 4; c += 2) {
+        tmem_load_wait(va);
+        tmem_load32(s_addr + 32 * (c + 1), vb);
+        weigh(va, c);
+        tmem_load_wait(vb);
+        if (c == 0) tmem_load32(s_addr + 64, va);
+        weigh(vb, c + 1);
+      }
+      tmem_store_wait();
+      tc::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(bar(kPFull + i));
+    }
+    if (ok && n_kv[i] > 0) wait_warp(kODone + i, n_kv[i] - 1, 20);
+    __syncthreads();                                              // (nan_at is complete; see the other warps' ends)
+    tc::tc_fence_after();
+    T* op = o + q_off * o_stride + head * HD;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll 1
+    for (int c = 0; c < HD / 32; ++c) {
+      uint32_t v[32];
+      if (n_kv[i] > 0) {
+        tmem_load32(o_addr + 32 * c, v);
+        tmem_load_wait(v);
+      }
+      if (r >= n_rows) continue;
+#pragma unroll
+      for (int u = 0; u < 32; u += 8) {
+        Vec<T> x;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          float y = l == 0.f ? 0.f : __uint_as_float(v[u + k]) * inv;             // nothing attended to: zeros
+          if (rpos >= nan_at[32 * c + u + k]) y = __int_as_float(0x7fffffff);
+          x.x[k] = narrow<T>(y);
+        }
+        *reinterpret_cast<Vec<T>*>(op + 32 * c + u) = x;
+      }
+    }
+    tc::tc_fence_before();
+  } else if (warp < kMmaWarp) {
+    // ------------------------------------------------------------------ codes to fp16 operand tiles
+    const int w = warp - 8, piece = lane % kLanes, row_a = w * (32 / kLanes) + lane / kLanes;
+    uint4 kr[kPass], vr[kPass];
+    int pg[kPass];
+    auto pages = [&](int j) {                                     // pages of this thread's rows of step j
+#pragma unroll
+      for (int p = 0; p < kPass; ++p) {
+        const int step = (j * kTile + p * kRowsPass + row_a) / kStep;
+        pg[p] = j < n && step < n_steps ? load_page(V, b, (step * kStep) >> V.page_shift) : -1;
+      }
+    };
+    auto fetch = [&](uint4(&x)[kPass], const uint8_t* codes, int j) {
+#pragma unroll
+      for (int p = 0; p < kPass; ++p) {
+        x[p] = make_uint4(0u, 0u, 0u, 0u);
+        const int pos = j * kTile + p * kRowsPass + row_a;
+        if (pg[p] >= 0)
+          x[p] = __ldg(reinterpret_cast<const uint4*>(codes + page_offset(V, pg[p], h, HD) + (pos & ((1 << V.page_shift) - 1)) * HD + 16 * piece));
+      }
+    };
+    auto put = [&](uint32_t tile, const uint4(&x)[kPass]) {
+#pragma unroll
+      for (int p = 0; p < kPass; ++p) {
+        const int row = p * kRowsPass + row_a;
+        const uint32_t a = tile_chunk(tile, row, 2 * piece), c = tile_chunk(tile, row, 2 * piece + 1);
+        const uint32_t h0 = decode2(x[p].x), h1 = decode2(x[p].x >> 16), h2 = decode2(x[p].y), h3 = decode2(x[p].y >> 16);
+        const uint32_t h4 = decode2(x[p].z), h5 = decode2(x[p].z >> 16), h6 = decode2(x[p].w), h7 = decode2(x[p].w >> 16);
+        if (piece & 4) {                                          // (the second block's lanes in the other order: no bank is hit twice)
+          sts16(c, h4, h5, h6, h7);
+          sts16(a, h0, h1, h2, h3);
+        } else {
+          sts16(a, h0, h1, h2, h3);
+          sts16(c, h4, h5, h6, h7);
+        }
+      }
+      tc::fence_async_smem();
+      __syncwarp();
+    };
+    // scales of the step's pages, a step ahead: lane s < 8 of the first warp
+    auto load_scales = [&](int j) {
+      Step x{0.f, -INFINITY, 0.f, 0.f};
+      const int step = j * (kTile / kStep) + lane;
+      if (w == 0 && lane < kTile / kStep && j < n && step < n_steps) {
+        const int page = load_page(V, b, (step * kStep) >> V.page_shift);
+        if (page >= 0) {
+          const float2 sc = V.scales[static_cast<int64_t>(page) * V.hkv + h];
+          const int ev = scale_exponent(sc.y);
+          x = Step{exp2_int(scale_exponent(sc.x)), static_cast<float>(ev), exp2_int(-ev), 0.f};
+        }
+      }
+      return x;
+    };
+    if (n > 0) {
+      pages(0);
+      fetch(kr, V.k, 0);
+      fetch(vr, V.v, 0);
+      Step sc = load_scales(0);
+      pages(1);
+      for (int j = 0; j < n; ++j) {
+        const int s = j & 1;
+        if (j >= 2 && !wait_warp(kKEmpty + s, (j >> 1) - 1, 20)) break;
+        if (w == 0) {                                             // (the readers of step j - 4 are done: the products of step j - 2 are)
+          if (lane < kTile / kStep) meta[j & 3][lane] = sc;
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(bar(kMeta + (j & 3)));
+        }
+        put(k_tile(s), kr);
+        if (lane == 0) tc::mbar_arrive(bar(kKFull + s));
+        fetch(kr, V.k, j + 1);
+        sc = load_scales(j + 1);
+        if (j >= 2 && !wait_warp(kVEmpty + s, (j >> 1) - 1, 20)) break;
+        if (j * kTile + kTile - 1 > lo[0]) {
+          // 0 * NaN: where rows do not see the whole step a NaN value is taken out, and the rows that do see it are set to NaN
+          // at the end
+#pragma unroll
+          for (int p = 0; p < kPass; ++p) {
+            uint32_t* x = reinterpret_cast<uint32_t*>(&vr[p]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint32_t bad = ((x[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+              x[k] &= ~((bad >> 7) * 0xffu);
+              while (bad) {
+                const int byte = (__ffs(bad) - 1) >> 3;
+                bad &= bad - 1;
+                atomicMin(nan_at + 16 * piece + 4 * k + byte, j * kTile + p * kRowsPass + row_a);
+              }
+            }
+          }
+        }
+        put(v_tile(s), vr);
+        if (lane == 0) tc::mbar_arrive(bar(kVFull + s));
+        fetch(vr, V.v, j + 1);
+        pages(j + 2);
+      }
+    }
+    __syncthreads();
+  } else {
+    // ------------------------------------------------------------------ one thread issues the products
+    if (lane == 0 && n > 0) {
+      constexpr uint32_t kIdS = make_idesc_f16(kTile, kTile, false), kIdO = make_idesc_f16(kTile, HD, true);
+      auto scores = [&](int i, int s) {
+        const uint64_t a = tc::make_desc_sw128(q_tile(i)), bd = tc::make_desc_sw128(k_tile(s));
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+          const int off = ((k >> 2) * (kTile * 128) + (k & 3) * 32) >> 4;
+          mma_ss(tmem + i * kTile, a + off, bd + off, kIdS, k > 0);
+        }
+        mma_commit(bar(kSFull + i));
+      };
+      auto values = [&](int i, int s, int j) {
+        const uint64_t bd = make_desc_rows_contracted(v_tile(s));
+#pragma unroll
+        for (int k = 0; k < kTile / 16; ++k)
+          mma_ts(tmem + 2 * kTile + i * kTile, tmem + i * kTile + 8 * k, bd + (k * 2048 >> 4), kIdO, j > 0 || k > 0);
+        mma_commit(bar(kODone + i));
+      };
+      bool ok = wait(kQFull, 0, 0) && wait(kKFull, 0, 0);
+      if (ok) {
+        tc::tc_fence_after();
+        if (n_kv[0] > 0) scores(0, 0);
+        if (n_kv[1] > 0) scores(1, 0);
+        mma_commit(bar(kKEmpty));
+      }
+      for (int j = 0; j < n && ok; ++j) {
+        const int s = j & 1, s1 = s ^ 1;
+        if (j + 1 < n && !(ok = wait(kKFull + s1, (j + 1) >> 1, 0))) break;
+        if (!(ok = wait(kVFull + s, j >> 1, 0))) break;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (j < n_kv[i]) {
+            if (!(ok = wait(kPFull + i, j, 0))) break;
+            tc::tc_fence_after();
+            values(i, s, j);
+          }
+          if (i == 1) mma_commit(bar(kVEmpty + s));
+          if (j + 1 < n_kv[i]) scores(i, s1);
+          if (i == 1 && j + 1 < n) mma_commit(bar(kKEmpty + s1));
+        }
+      }
+      mma_commit(bar(kDrain));                                    // nothing is in flight when the TMEM goes
+      wait(kDrain, 0, 20);
+    }
+    __syncwarp();
+    __syncthreads();
+  }
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc::tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+}  // namespace
+
+template <typename T, int HD>
+szo_status launch_attention_tc(const View& V, const Rows& A, cudaStream_t st) {
+  const int64_t tiles = ceil_div(static_cast<int64_t>(V.max_new) * (A.H / V.hkv), 2 * kTile);
+  unsigned blocks;
+  SZO_TRY(grid_items(tiles, V, &blocks));
+  const int smem = 6 * kTile * HD * 2 + 1024;
+  auto kern = kv8_attention_tc_kernel<T, HD>;
+  SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  kern<<<blocks, kTcThreads, smem, st>>>(V, static_cast<const T*>(A.q), A.q_stride, static_cast<T*>(A.o), A.o_stride, A.H, A.scale,
+                                         static_cast<int>(tiles));
+  count_launch();
+  SZO_CHECK_LAUNCH("kv8_attention_tc_kernel");
+  return SZO_OK;
+}
+template szo_status launch_attention_tc<__nv_bfloat16, 64>(const View&, const Rows&, cudaStream_t);
+template szo_status launch_attention_tc<__nv_bfloat16, 128>(const View&, const Rows&, cudaStream_t);
+template szo_status launch_attention_tc<__half, 64>(const View&, const Rows&, cudaStream_t);
+template szo_status launch_attention_tc<__half, 128>(const View&, const Rows&, cudaStream_t);
+
+}  // namespace kv8
+}  // namespace szo
