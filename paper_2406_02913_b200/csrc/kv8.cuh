@@ -57,11 +57,12 @@ __device__ __forceinline__ Seq load_seq(const View& V, int b) {
   }
   return s;
 }
+__device__ __forceinline__ void report_page(const View& V) { atomicExch(V.status, static_cast<int32_t>(SZO_ERR_INVALID_ARG)); }
 // Page id of the j-th page of sequence b, or -1 (reported) where the table holds none
 __device__ __forceinline__ int load_page(const View& V, int b, int j) {
   const int p = V.table[static_cast<int64_t>(b) * V.max_pages + j];
   if (static_cast<uint32_t>(p) >= static_cast<uint64_t>(V.n_pages)) {
-    atomicExch(V.status, static_cast<int32_t>(SZO_ERR_INVALID_ARG));
+    report_page(V);
     return -1;
   }
   return p;

@@ -19,6 +19,7 @@
 // The reference maximum follows the running maximum once that is 2^8 above it, so O is rescaled in TMEM a few times
 // per row; weights stay between 2^-24 and 2^15.
 #include <cmath>
+#include <type_traits>
 
 #include "kv8_attention.cuh"
 
@@ -30,6 +31,7 @@ namespace {
 constexpr int kTile = 128;                     // rows of a row tile, positions of a step
 constexpr int kConv = 4, kMmaWarp = 8 + kConv, kTcThreads = (kMmaWarp + 1) * 32;      // (13 warps: 128 registers per thread)
 constexpr float kTcOffset = 7.0f, kTcSlack = 8.0f;
+constexpr float kTiny = 1e-37f;                // factors of scores are kept above it: a zero would make NaN of a masked -inf
 constexpr uint32_t kTmemCols = 512;
 
 __device__ __forceinline__ void tmem_alloc(uint32_t result_smem, uint32_t ncols) {
@@ -122,6 +124,12 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 // fp16 operand tiles in shared memory: 128 rows in blocks of 64 columns (one 128-byte row each), 128-byte swizzle.
 __device__ __forceinline__ uint32_t tile_chunk(uint32_t base, int row, int chunk) {      // 16-byte chunk (8 columns) of a row
   return base + (chunk >> 3) * (kTile * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
@@ -147,7 +155,7 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
   constexpr int kLanes = HD / 16, kRowsPass = kConv * 32 / kLanes, kPass = kTile / kRowsPass;
   extern __shared__ __align__(1024) unsigned char smem_tc[];
   struct alignas(16) Step {
-    float ks, fe, el;                                             // 2^(keys' exponent), values' exponent, its inverse power; no page: 0, -inf, 0
+    float ks, fe, el;                                             // 2^(keys' exponent), values' exponent, its inverse power; no page: 1, -inf, 0
     float pad;
   };
   __shared__ Step meta[4][kTile / kStep];
@@ -215,7 +223,7 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
     const uint32_t s_addr = tmem + lanes + i * kTile, o_addr = tmem + lanes + 2 * kTile + i * kTile;
     const int rpos = pos_of(r < n_rows ? r : n_rows - 1);         // (rows that are not there: anything, they are not stored)
     const int64_t q_off = (seq.row0 + (r0 + r) / G), head = h * G + (r0 + r) % G;
-    float rs;
+    float rs, poison;
     {
       const T* qp = q + q_off * q_stride + head * HD;
       float amax = 0.f;
@@ -234,7 +242,8 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
       }
       const int e = min(max((__float_as_int(amax) >> 23) - 127, -126), 126);
       const float inv = scale < 0.f ? -exp2_int(-e) : exp2_int(-e);
-      rs = fine ? exp2_int(e) * (fabsf(scale) * 1.4426950408889634f) : __int_as_float(0x7fffffff);
+      rs = exp2_int(e) * (fabsf(scale) * 1.4426950408889634f);
+      poison = fine ? 0.f : __int_as_float(0x7fffffff);           // a row that holds NaN or an infinity is NaN
 #pragma unroll 4
       for (int c = 0; c < HD / 8; ++c) {
         Vec<T> x = {};
@@ -257,25 +266,32 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
       const int limit = rpos - j * kTile;                         // columns up to this one are seen
       const bool masked = j * kTile + kTile - 1 > lo[i];
       uint32_t va[32], vb[32];
+      if (masked) {                                               // what a row does not see becomes -inf in S itself: one form of the rest
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          tmem_load32(s_addr + 32 * c, va);
+          tmem_load_wait(va);
+#pragma unroll
+          for (int u = 0; u < 32; ++u)
+            if (32 * c + u > limit) va[u] = 0xff800000u;
+          tmem_store32(s_addr + 32 * c, va);
+        }
+        tmem_store_wait();
+      }
       float mx = -INFINITY;
-      auto peak = [&](uint32_t(&v)[32], int c) {
+      auto peak = [&](const uint32_t(&v)[32], int c) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-          const float ks = st[2 * c + s].ks, fe = st[2 * c + s].fe;
+          const float2 kf = *reinterpret_cast<const float2*>(&st[2 * c + s]);
           float t = -INFINITY;
-          if (masked) {
 #pragma unroll
-            for (int u = 0; u < 16; ++u) t = fmaxf(t, 32 * c + 16 * s + u > limit ? -INFINITY : __uint_as_float(v[16 * s + u]));
-          } else {
-#pragma unroll
-            for (int u = 0; u < 16; ++u) t = fmaxf(t, __uint_as_float(v[16 * s + u]));
-          }
-          // (nothing seen: t = -inf, which a zero factor must not turn into NaN)
-          mx = fmaxf(mx, t == -INFINITY ? -INFINITY : fmaf(t, rs * ks, fe));
+          for (int u = 0; u < 16; u += 2) t = max3(t, __uint_as_float(v[16 * s + u]), __uint_as_float(v[16 * s + u + 1]));
+          mx = fmaxf(mx, fmaf(t, fmaxf(rs * kf.x, kTiny), kf.y));
         }
       };
+      // (loops and not four copies, here and below: instruction fetch is what straight code would wait for)
       tmem_load32(s_addr, va);
-#pragma unroll
+#pragma unroll 1
       for (int c = 0; c < 4; c += 2) {
         tmem_load_wait(va);
         tmem_load32(s_addr + 32 * (c + 1), vb);
@@ -303,32 +319,28 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
         }
         m = m_new;
       }
-      const float ref = (m == -INFINITY ? 0.f : m) - kTcOffset;
-      auto weigh = [&](uint32_t(&v)[32], int c) {
+      const float ref = (m == -INFINITY ? 0.f : m) - kTcOffset + poison;
+      auto weigh = [&](const uint32_t(&v)[32], int c) {
         uint32_t p[16];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-          const Step x = st[2 * c + s];
-          const float f = rs * x.ks, d = x.fe - ref;
+          const float4 x = *reinterpret_cast<const float4*>(&st[2 * c + s]);
+          const float f = fmaxf(rs * x.x, kTiny), d = x.y - ref;
           const uint64_t f2 = pair(f, f), d2 = pair(d, d);
           uint64_t sum = 0;
 #pragma unroll
           for (int u = 0; u < 16; u += 2) {
             float2 y = unpair(fma2(pair(__uint_as_float(v[16 * s + u]), __uint_as_float(v[16 * s + u + 1])), f2, d2));
-            if (masked) {
-              if (32 * c + 16 * s + u > limit) y.x = -INFINITY;
-              if (32 * c + 16 * s + u + 1 > limit) y.y = -INFINITY;
-            }
             y = make_float2(ex2(y.x), ex2(y.y));
             sum = add2(sum, pair(y.x, y.y));
             p[8 * s + u / 2] = pack_f16(y.x, y.y);
           }
           const float2 t = unpair(sum);
-          l = fmaf(x.el, t.x + t.y, l);
+          l = fmaf(x.z, t.x + t.y, l);
         }
         tmem_store16(s_addr + 16 * c, p);                         // over columns that this thread has read
       };
-#pragma unroll
+#pragma unroll 1
       for (int c = 0; c < 4; c += 2) {
         tmem_load_wait(va);
         tmem_load32(s_addr + 32 * (c + 1), vb);
@@ -372,73 +384,81 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
     // ------------------------------------------------------------------ codes to fp16 operand tiles
     const int w = warp - 8, piece = lane % kLanes, row_a = w * (32 / kLanes) + lane / kLanes;
     uint4 kr[kPass], vr[kPass];
-    int pg[kPass];
+    int pg[kPass];                                                // entries of the page table as they come
+    int at[kPass];                                                // row of k and v of this thread's codes; -1: none
+    const int32_t* table = V.table + static_cast<int64_t>(b) * V.max_pages;
+    auto entry = [&](int step) { return step < n_steps ? __ldg(table + (step >> (V.page_shift - 4))) : -1; };
     auto pages = [&](int j) {                                     // pages of this thread's rows of step j
 #pragma unroll
+      for (int p = 0; p < kPass; ++p) pg[p] = entry((j * kTile + p * kRowsPass + row_a) / kStep);
+    };
+    auto places = [&](int j) {
+#pragma unroll
       for (int p = 0; p < kPass; ++p) {
-        const int step = (j * kTile + p * kRowsPass + row_a) / kStep;
-        pg[p] = j < n && step < n_steps ? load_page(V, b, (step * kStep) >> V.page_shift) : -1;
+        const int pos = j * kTile + p * kRowsPass + row_a, slot = pos & ((1 << V.page_shift) - 1);
+        const bool there = pos / kStep < n_steps;
+        if (there && static_cast<uint32_t>(pg[p]) >= static_cast<uint64_t>(V.n_pages)) report_page(V);
+        at[p] = there && static_cast<uint32_t>(pg[p]) < static_cast<uint64_t>(V.n_pages) ? ((pg[p] * V.hkv + h) << V.page_shift) + slot : -1;
       }
     };
-    auto fetch = [&](uint4(&x)[kPass], const uint8_t* codes, int j) {
+    auto fetch = [&](uint4(&x)[kPass], const uint8_t* codes) {
 #pragma unroll
       for (int p = 0; p < kPass; ++p) {
         x[p] = make_uint4(0u, 0u, 0u, 0u);
-        const int pos = j * kTile + p * kRowsPass + row_a;
-        if (pg[p] >= 0)
-          x[p] = __ldg(reinterpret_cast<const uint4*>(codes + page_offset(V, pg[p], h, HD) + (pos & ((1 << V.page_shift) - 1)) * HD + 16 * piece));
+        if (at[p] >= 0) x[p] = __ldg(reinterpret_cast<const uint4*>(codes + static_cast<int64_t>(at[p]) * HD + 16 * piece));
       }
     };
+    // (kRowsPass is a multiple of 8: every pass is the same place of the swizzle, kRowsPass rows further)
+    static_assert(kRowsPass % 8 == 0, "");
+    const bool other = (piece & 4) != 0;                          // the second block's lanes store in the other order: no bank is hit twice
+    const uint32_t place0 = tile_chunk(0, row_a, 2 * piece + (other ? 1 : 0)), place1 = tile_chunk(0, row_a, 2 * piece + (other ? 0 : 1));
     auto put = [&](uint32_t tile, const uint4(&x)[kPass]) {
+      const uint32_t p0 = tile + place0, p1 = tile + place1;
 #pragma unroll
       for (int p = 0; p < kPass; ++p) {
-        const int row = p * kRowsPass + row_a;
-        const uint32_t a = tile_chunk(tile, row, 2 * piece), c = tile_chunk(tile, row, 2 * piece + 1);
-        const uint32_t h0 = decode2(x[p].x), h1 = decode2(x[p].x >> 16), h2 = decode2(x[p].y), h3 = decode2(x[p].y >> 16);
-        const uint32_t h4 = decode2(x[p].z), h5 = decode2(x[p].z >> 16), h6 = decode2(x[p].w), h7 = decode2(x[p].w >> 16);
-        if (piece & 4) {                                          // (the second block's lanes in the other order: no bank is hit twice)
-          sts16(c, h4, h5, h6, h7);
-          sts16(a, h0, h1, h2, h3);
-        } else {
-          sts16(a, h0, h1, h2, h3);
-          sts16(c, h4, h5, h6, h7);
-        }
+        const uint32_t w0 = other ? x[p].z : x[p].x, w1 = other ? x[p].w : x[p].y, w2 = other ? x[p].x : x[p].z, w3 = other ? x[p].y : x[p].w;
+        sts16(p0 + p * kRowsPass * 128, decode2(w0), decode2(w0 >> 16), decode2(w1), decode2(w1 >> 16));
+        sts16(p1 + p * kRowsPass * 128, decode2(w2), decode2(w2 >> 16), decode2(w3), decode2(w3 >> 16));
       }
       tc::fence_async_smem();
       __syncwarp();
     };
-    // scales of the step's pages, a step ahead: lane s < 8 of the first warp
-    auto load_scales = [&](int j) {
-      Step x{0.f, -INFINITY, 0.f, 0.f};
-      const int step = j * (kTile / kStep) + lane;
-      if (w == 0 && lane < kTile / kStep && j < n && step < n_steps) {
-        const int page = load_page(V, b, (step * kStep) >> V.page_shift);
-        if (page >= 0) {
-          const float2 sc = V.scales[static_cast<int64_t>(page) * V.hkv + h];
-          const int ev = scale_exponent(sc.y);
-          x = Step{exp2_int(scale_exponent(sc.x)), static_cast<float>(ev), exp2_int(-ev), 0.f};
-        }
-      }
-      return x;
+    // Scales of the steps of 16 positions, lane s < 8 of the first warp: page ids two steps ahead, scales one
+    const bool scaler = w == 0 && lane < kTile / kStep;
+    int spage = -1;
+    float2 sc;
+    auto scale_page = [&](int j) { spage = scaler ? entry(j * (kTile / kStep) + lane) : -1; };
+    bool have = false;
+    auto load_scales = [&]() {
+      have = static_cast<uint32_t>(spage) < static_cast<uint64_t>(V.n_pages);
+      if (have) sc = __ldg(V.scales + static_cast<int64_t>(spage) * V.hkv + h);
     };
     if (n > 0) {
       pages(0);
-      fetch(kr, V.k, 0);
-      fetch(vr, V.v, 0);
-      Step sc = load_scales(0);
+      places(0);
+      fetch(kr, V.k);
+      fetch(vr, V.v);
+      scale_page(0);
+      load_scales();
+      scale_page(1);
       pages(1);
       for (int j = 0; j < n; ++j) {
         const int s = j & 1;
         if (j >= 2 && !wait_warp(kKEmpty + s, (j >> 1) - 1, 20)) break;
         if (w == 0) {                                             // (the readers of step j - 4 are done: the products of step j - 2 are)
-          if (lane < kTile / kStep) meta[j & 3][lane] = sc;
+          if (scaler) {
+            const int ev = scale_exponent(sc.y);
+            meta[j & 3][lane] = have ? Step{exp2_int(scale_exponent(sc.x)), static_cast<float>(ev), exp2_int(-ev), 0.f} : Step{1.f, -INFINITY, 0.f, 0.f};
+          }
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(bar(kMeta + (j & 3)));
         }
         put(k_tile(s), kr);
         if (lane == 0) tc::mbar_arrive(bar(kKFull + s));
-        fetch(kr, V.k, j + 1);
-        sc = load_scales(j + 1);
+        places(j + 1);
+        fetch(kr, V.k);
+        load_scales();
+        scale_page(j + 2);
         if (j >= 2 && !wait_warp(kVEmpty + s, (j >> 1) - 1, 20)) break;
         if (j * kTile + kTile - 1 > lo[0]) {
           // 0 * NaN: where rows do not see the whole step a NaN value is taken out, and the rows that do see it are set to NaN
@@ -460,7 +480,7 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
         }
         put(v_tile(s), vr);
         if (lane == 0) tc::mbar_arrive(bar(kVFull + s));
-        fetch(vr, V.v, j + 1);
+        fetch(vr, V.v);
         pages(j + 2);
       }
     }
