@@ -283,10 +283,13 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           const float2 kf = *reinterpret_cast<const float2*>(&st[2 * c + s]);
-          float t = -INFINITY;
+          float t[4];
 #pragma unroll
-          for (int u = 0; u < 16; u += 2) t = max3(t, __uint_as_float(v[16 * s + u]), __uint_as_float(v[16 * s + u + 1]));
-          mx = fmaxf(mx, fmaf(t, fmaxf(rs * kf.x, kTiny), kf.y));
+          for (int u = 0; u < 4; ++u) t[u] = max3(__uint_as_float(v[16 * s + 3 * u]), __uint_as_float(v[16 * s + 3 * u + 1]), __uint_as_float(v[16 * s + 3 * u + 2]));
+          t[0] = max3(t[0], __uint_as_float(v[16 * s + 12]), __uint_as_float(v[16 * s + 13]));
+          t[1] = max3(t[1], __uint_as_float(v[16 * s + 14]), __uint_as_float(v[16 * s + 15]));
+          t[0] = fmaxf(max3(t[0], t[1], t[2]), t[3]);
+          mx = fmaxf(mx, fmaf(t[0], fmaxf(rs * kf.x, kTiny), kf.y));
         }
       };
       // (loops and not four copies, here and below: instruction fetch is what straight code would wait for)
@@ -384,28 +387,29 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
     // ------------------------------------------------------------------ codes to fp16 operand tiles
     const int w = warp - 8, piece = lane % kLanes, row_a = w * (32 / kLanes) + lane / kLanes;
     uint4 kr[kPass], vr[kPass];
-    int pg[kPass];                                                // entries of the page table as they come
-    int at[kPass];                                                // row of k and v of this thread's codes; -1: none
+    // Lane s < 8 keeps the page of the s-th 16 positions: the table's entry two steps ahead, the row in k and v (-1: no page)
+    // and, in the first warp, the scales one step ahead
     const int32_t* table = V.table + static_cast<int64_t>(b) * V.max_pages;
-    auto entry = [&](int step) { return step < n_steps ? __ldg(table + (step >> (V.page_shift - 4))) : -1; };
-    auto pages = [&](int j) {                                     // pages of this thread's rows of step j
-#pragma unroll
-      for (int p = 0; p < kPass; ++p) pg[p] = entry((j * kTile + p * kRowsPass + row_a) / kStep);
+    const bool scaler = w == 0 && lane < kTile / kStep;
+    int entry = -1, place = -1;
+    float2 sc = make_float2(0.f, 0.f);
+    auto load_entry = [&](int j) {
+      const int step = j * (kTile / kStep) + lane;
+      entry = lane < kTile / kStep && step < n_steps ? __ldg(table + (step >> (V.page_shift - 4))) : -2;
     };
-    auto places = [&](int j) {
-#pragma unroll
-      for (int p = 0; p < kPass; ++p) {
-        const int pos = j * kTile + p * kRowsPass + row_a, slot = pos & ((1 << V.page_shift) - 1);
-        const bool there = pos / kStep < n_steps;
-        if (there && static_cast<uint32_t>(pg[p]) >= static_cast<uint64_t>(V.n_pages)) report_page(V);
-        at[p] = there && static_cast<uint32_t>(pg[p]) < static_cast<uint64_t>(V.n_pages) ? ((pg[p] * V.hkv + h) << V.page_shift) + slot : -1;
-      }
+    auto take_entry = [&](int j) {
+      const bool there = static_cast<uint32_t>(entry) < static_cast<uint64_t>(V.n_pages);
+      if (entry != -2 && !there) report_page(V);
+      place = there ? ((entry * V.hkv + h) << V.page_shift) + ((j * kTile + lane * kStep) & ((1 << V.page_shift) - 1)) : -1;
+      if (scaler && there) sc = __ldg(V.scales + static_cast<int64_t>(entry) * V.hkv + h);
     };
     auto fetch = [&](uint4(&x)[kPass], const uint8_t* codes) {
+      const uint8_t* mine = codes + (row_a % kStep) * HD + 16 * piece;
 #pragma unroll
       for (int p = 0; p < kPass; ++p) {
+        const int row = __shfl_sync(0xffffffffu, place, p * (kRowsPass / kStep) + row_a / kStep);
         x[p] = make_uint4(0u, 0u, 0u, 0u);
-        if (at[p] >= 0) x[p] = __ldg(reinterpret_cast<const uint4*>(codes + static_cast<int64_t>(at[p]) * HD + 16 * piece));
+        if (row >= 0) x[p] = __ldg(reinterpret_cast<const uint4*>(mine + static_cast<int64_t>(row) * HD));
       }
     };
     // (kRowsPass is a multiple of 8: every pass is the same place of the swizzle, kRowsPass rows further)
@@ -423,42 +427,28 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
       tc::fence_async_smem();
       __syncwarp();
     };
-    // Scales of the steps of 16 positions, lane s < 8 of the first warp: page ids two steps ahead, scales one
-    const bool scaler = w == 0 && lane < kTile / kStep;
-    int spage = -1;
-    float2 sc;
-    auto scale_page = [&](int j) { spage = scaler ? entry(j * (kTile / kStep) + lane) : -1; };
-    bool have = false;
-    auto load_scales = [&]() {
-      have = static_cast<uint32_t>(spage) < static_cast<uint64_t>(V.n_pages);
-      if (have) sc = __ldg(V.scales + static_cast<int64_t>(spage) * V.hkv + h);
-    };
     if (n > 0) {
-      pages(0);
-      places(0);
+      load_entry(0);
+      take_entry(0);
+      load_entry(1);
       fetch(kr, V.k);
       fetch(vr, V.v);
-      scale_page(0);
-      load_scales();
-      scale_page(1);
-      pages(1);
       for (int j = 0; j < n; ++j) {
         const int s = j & 1;
         if (j >= 2 && !wait_warp(kKEmpty + s, (j >> 1) - 1, 20)) break;
         if (w == 0) {                                             // (the readers of step j - 4 are done: the products of step j - 2 are)
           if (scaler) {
             const int ev = scale_exponent(sc.y);
-            meta[j & 3][lane] = have ? Step{exp2_int(scale_exponent(sc.x)), static_cast<float>(ev), exp2_int(-ev), 0.f} : Step{1.f, -INFINITY, 0.f, 0.f};
+            meta[j & 3][lane] = place >= 0 ? Step{exp2_int(scale_exponent(sc.x)), static_cast<float>(ev), exp2_int(-ev), 0.f} : Step{1.f, -INFINITY, 0.f, 0.f};
           }
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(bar(kMeta + (j & 3)));
         }
         put(k_tile(s), kr);
         if (lane == 0) tc::mbar_arrive(bar(kKFull + s));
-        places(j + 1);
+        take_entry(j + 1);
+        load_entry(j + 2);
         fetch(kr, V.k);
-        load_scales();
-        scale_page(j + 2);
         if (j >= 2 && !wait_warp(kVEmpty + s, (j >> 1) - 1, 20)) break;
         if (j * kTile + kTile - 1 > lo[0]) {
           // 0 * NaN: where rows do not see the whole step a NaN value is taken out, and the rows that do see it are set to NaN
@@ -481,7 +471,6 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
         put(v_tile(s), vr);
         if (lane == 0) tc::mbar_arrive(bar(kVFull + s));
         fetch(vr, V.v);
-        pages(j + 2);
       }
     }
     __syncthreads();
