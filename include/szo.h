@@ -359,7 +359,7 @@ szo_status szo_kv8_read(const szo_kv8_cache* cache, const szo_kv8_batch* batch, 
  * [rows][n_heads*head_dim], rows q_stride / o_stride elements apart; grouped-query attention when n_kv_heads <
  * n_heads; scale finite (1/sqrt(head_dim) for szo_attention's).  A row that attends to nothing (padding) becomes zeros.
  * A NaN element of the cache reaches the rows that attend to it and no others.  workspace: at least
- * szo_attention_kv8_workspace_bytes(cache, batch, n_heads) bytes (0, below a megabyte otherwise: it depends on the shapes
+ * szo_attention_kv8_workspace_bytes(cache, batch, n_heads) bytes (0, up to 20 MB otherwise: it depends on the shapes
  * only, not on the lengths), contents irrelevant on entry; calls that may run at the same time need one each. */
 size_t szo_attention_kv8_workspace_bytes(const szo_kv8_cache* cache, const szo_kv8_batch* batch, int32_t n_heads);
 szo_status szo_attention_kv8(const szo_kv8_cache* cache, const szo_kv8_batch* batch, const void* q, int64_t q_stride,

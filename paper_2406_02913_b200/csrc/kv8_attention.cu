@@ -484,20 +484,23 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   cluster.sync();                                                 // nobody leaves while its sums are being read
 }
 
-// Joins the partial results in `ws` in split order: a block per (row of a tile, item), a thread per dim.
+// A block per (row of a tile, item), a thread per dim; shares in order.
 template <typename T, int HD>
 __global__ void __launch_bounds__(HD)
-kv8_join_kernel(View V, const float* __restrict__ ws, T* __restrict__ o, int64_t o_stride, int H, int R, int row_tiles, int nsplit) {
+kv8_join_kernel(View V, const float* __restrict__ ws, T* __restrict__ o, int64_t o_stride, int H, int R, int row_tiles, int nsplit,
+                bool long_first, unsigned item0) {
   chain_release();
   const int r = blockIdx.x % R, d = threadIdx.x, G = H / V.hkv;
-  const unsigned item = blockIdx.x / R;
-  const int rt = item % row_tiles, h = item / row_tiles % V.hkv, b = item / row_tiles / V.hkv;
+  const unsigned item = item0 + blockIdx.x / R, others = static_cast<unsigned>(V.batch) * V.hkv;
+  const int rt = long_first ? row_tiles - 1 - static_cast<int>(item / others) : item % row_tiles;
+  const unsigned bh = long_first ? item % others : item / row_tiles;
+  const int h = bh % V.hkv, b = bh / V.hkv;
   chain_wait();
   const Seq seq = load_seq(V, b);
   const int64_t row = static_cast<int64_t>(rt) * R + r;
   if (row >= static_cast<int64_t>(seq.n) * G) return;
   const int64_t step = static_cast<int64_t>(R) * (HD + 2);
-  const float* p = ws + item * nsplit * step;
+  const float* p = ws + static_cast<int64_t>(blockIdx.x / R) * nsplit * step;
   float mm = -INFINITY, sum = 0.f, ll = 0.f;
   for (int x = 0; x < nsplit; ++x) mm = fmaxf(mm, p[x * step + R * HD + r]);
 #pragma unroll 4
@@ -520,9 +523,8 @@ szo_status launch_rows(const View& V, const Rows& A, int nsplit, float* ws, cuda
   constexpr int R = 8 * NT;
   const size_t smem = static_cast<size_t>(kWarps) * kRingBytes<HD> + 1024;
   const int64_t tiles = ceil_div(static_cast<int64_t>(V.max_new) * (A.H / V.hkv), R);
-  unsigned blocks, joins;
+  unsigned blocks;
   SZO_TRY(grid_items(tiles * nsplit, V, &blocks));
-  SZO_TRY(grid_items(tiles * R, V, &joins));
   CUtensorMap map_k, map_v;
   SZO_TRY(codes_map(V.k, V, HD, kStep, &map_k));
   SZO_TRY(codes_map(V.v, V, HD, kStep, &map_v));
@@ -544,10 +546,7 @@ szo_status launch_rows(const View& V, const Rows& A, int nsplit, float* ws, cuda
                                     A.scale * 1.4426950408889634f, static_cast<int>(tiles), nsplit, ws));
   count_launch();
   if (ws == nullptr) return SZO_OK;
-  SZO_CHECK_CUDA(launch_maybe_chained(kv8_join_kernel<T, HD>, dim3(joins), dim3(HD), 0, st, true, V, ws, static_cast<T*>(A.o), A.o_stride, A.H, R,
-                                      static_cast<int>(tiles), nsplit));
-  count_launch();
-  return SZO_OK;
+  return launch_join<T, HD>(V, A, ws, R, static_cast<int>(tiles), nsplit, false, 0, tiles * V.batch * V.hkv, st);
 }
 
 // How the positions are cut: blocks of 4 warps, three per SM, joined in clusters of up to 16, or (`wide`) of 12, one per SM,
@@ -571,10 +570,13 @@ Plan plan(const View& V, int H) {
   return p;
 }
 
+// More rows per key/value head than this go to the tensor-core kernel (in 16-bit types)
+bool many_rows(const View& V, int H) { return static_cast<int64_t>(V.max_new) * (H / V.hkv) > 64; }
+
 template <typename T, int HD>
 szo_status launch_attention(const View& V, const Rows& A, float* ws, cudaStream_t st) {
   if constexpr (sizeof(T) == 2)
-    if (static_cast<int64_t>(V.max_new) * (A.H / V.hkv) > 64) return launch_attention_tc<T, HD>(V, A, st);
+    if (many_rows(V, A.H)) return launch_attention_tc<T, HD>(V, A, ws, st);
   const Plan p = plan(V, A.H);
   if (p.wide) return launch_rows<T, HD, 1, 12>(V, A, p.nsplit, ws, st);
   return p.rows == 8 ? launch_rows<T, HD, 1, 4>(V, A, p.nsplit, nullptr, st) : launch_rows<T, HD, 2, 4>(V, A, p.nsplit, nullptr, st);
@@ -582,11 +584,32 @@ szo_status launch_attention(const View& V, const Rows& A, float* ws, cudaStream_
 
 size_t workspace_bytes(const View& V, int H, int hd) {
   if (V.batch == 0 || V.max_new == 0 || V.rows == 0) return 0;
+  if (many_rows(V, H)) return workspace_bytes_tc(V, H, hd);         // (fp32 needs none then)
   const Plan p = plan(V, H);
   return p.wide ? static_cast<size_t>(148) * p.rows * (hd + 2) * sizeof(float) : 0;
 }
 
 }  // namespace
+
+template <typename T, int HD>
+szo_status launch_join(const View& V, const Rows& A, const float* ws, int R, int row_tiles, int nsplit, bool long_first, int64_t item0,
+                       int64_t n_items, cudaStream_t st) {
+  SZO_REQUIRE(n_items * R <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows for one launch");
+  SZO_CHECK_CUDA(launch_maybe_chained(kv8_join_kernel<T, HD>, dim3(static_cast<unsigned>(n_items * R)), dim3(HD), 0, st, true, V, ws,
+                                      static_cast<T*>(A.o), A.o_stride, A.H, R, row_tiles, nsplit, long_first, static_cast<unsigned>(item0)));
+  count_launch();
+  return SZO_OK;
+}
+#define SZO_KV8_JOIN(T, HD) \
+  template szo_status launch_join<T, HD>(const View&, const Rows&, const float*, int, int, int, bool, int64_t, int64_t, cudaStream_t)
+SZO_KV8_JOIN(float, 64);
+SZO_KV8_JOIN(float, 128);
+SZO_KV8_JOIN(__nv_bfloat16, 64);
+SZO_KV8_JOIN(__nv_bfloat16, 128);
+SZO_KV8_JOIN(__half, 64);
+SZO_KV8_JOIN(__half, 128);
+#undef SZO_KV8_JOIN
+
 }  // namespace kv8
 }  // namespace szo
 

@@ -18,7 +18,14 @@ struct Rows {
   float scale;
 };
 
-template <typename T, int HD> szo_status launch_attention_tc(const View& V, const Rows& A, cudaStream_t st);
+// Many query rows per key/value head (kv8_attention_tc.cu); 16-bit types only
+template <typename T, int HD> szo_status launch_attention_tc(const View& V, const Rows& A, float* ws, cudaStream_t st);
+size_t workspace_bytes_tc(const View& V, int H, int hd);
+// Joins the partial results of n_items items from item0 on, cut into nsplit shares each (kv8_attention.cu).  ws: per item and
+// share R * HD sums, R maxima (base 2), R sums of weights.  long_first: items are counted as kv8_attention_tc.cu does.
+template <typename T, int HD>
+szo_status launch_join(const View& V, const Rows& A, const float* ws, int R, int row_tiles, int nsplit, bool long_first, int64_t item0,
+                       int64_t n_items, cudaStream_t st);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {

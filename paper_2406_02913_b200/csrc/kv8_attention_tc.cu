@@ -148,9 +148,15 @@ constexpr uint32_t make_idesc_f16(int M, int N, bool b_rows_contracted) {
   return (1u << 4) | (b_rows_contracted ? 1u << 16 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 
+// Items (row tile, sequence, head) from `whole` on are cut into `nsplit` shares of their positions, a block each
+struct TcSplit {
+  unsigned whole;
+  int nsplit;
+};
+
 template <typename T, int HD>
 __global__ void __launch_bounds__(kTcThreads, 1)
-kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __restrict__ o, int64_t o_stride, int H, float scale, int row_tiles) {
+kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __restrict__ o, int64_t o_stride, int H, float scale, int row_tiles, TcSplit part, float* __restrict__ ws) {
   constexpr int kBytes = kTile * HD * 2;                          // of an operand tile
   constexpr int kLanes = HD / 16, kRowsPass = kConv * 32 / kLanes, kPass = kTile / kRowsPass;
   extern __shared__ __align__(1024) unsigned char smem_tc[];
@@ -166,8 +172,11 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int64_t others = static_cast<int64_t>(V.batch) * V.hkv;
-  const int rt = row_tiles - 1 - static_cast<int>(blockIdx.x / others);          // the longest rows first
-  const int h = static_cast<int>(blockIdx.x % others) % V.hkv, b = static_cast<int>(blockIdx.x % others) / V.hkv, G = H / V.hkv;
+  const bool cut = blockIdx.x >= part.whole;
+  const unsigned item = cut ? part.whole + (blockIdx.x - part.whole) / part.nsplit : blockIdx.x;
+  const int split = cut ? (blockIdx.x - part.whole) % part.nsplit : 0, nsplit = cut ? part.nsplit : 1;
+  const int rt = row_tiles - 1 - static_cast<int>(item / others);                // the longest rows first
+  const int h = static_cast<int>(item % others) % V.hkv, b = static_cast<int>(item % others) / V.hkv, G = H / V.hkv;
   const Seq seq = load_seq(V, b);
   const int64_t r0 = static_cast<int64_t>(rt) * 2 * kTile, left = static_cast<int64_t>(seq.n) * G - r0;
   if (left <= 0) return;
@@ -182,7 +191,12 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
     const int hi = rows > 0 ? pos_of(kTile * i + rows - 1) : -1;
     n_kv[i] = hi < 0 ? 0 : hi / kTile + 1;
   }
-  const int n = n_kv[1] > n_kv[0] ? n_kv[1] : n_kv[0];
+  // this block's steps [j0, j0 + n), counted from j0 from here on
+  const int n_all = n_kv[1] > n_kv[0] ? n_kv[1] : n_kv[0];
+  const int j0 = static_cast<int>(static_cast<int64_t>(n_all) * split / nsplit), n = static_cast<int>(static_cast<int64_t>(n_all) * (split + 1) / nsplit) - j0;
+  const int p0 = j0 * kTile;                                      // position of the first column of step 0
+#pragma unroll
+  for (int i = 0; i < 2; ++i) n_kv[i] = min(max(n_kv[i] - j0, 0), n);
   const int n_steps = (pos_of(n_rows - 1) < 0 ? -1 : pos_of(n_rows - 1) / kStep) + 1;      // of 16 positions
 
   const uint32_t base = (tc::smem_u32(smem_tc) + 1023u) & ~1023u;
@@ -263,8 +277,8 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
       if (!(ok = wait_warp(kMeta + (j & 3), j >> 2, 20) && wait_warp(kSFull + i, j, 20))) break;
       tc::tc_fence_after();
       const Step* st = meta[j & 3];
-      const int limit = rpos - j * kTile;                         // columns up to this one are seen
-      const bool masked = j * kTile + kTile - 1 > lo[i];
+      const int limit = rpos - p0 - j * kTile;                         // columns up to this one are seen
+      const bool masked = p0 + j * kTile + kTile - 1 > lo[i];
       uint32_t va[32], vb[32];
       if (masked) {                                               // what a row does not see becomes -inf in S itself: one form of the rest
 #pragma unroll 1
@@ -361,7 +375,8 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
     __syncthreads();                                              // (nan_at is complete; see the other warps' ends)
     tc::tc_fence_after();
     T* op = o + q_off * o_stride + head * HD;
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    float* wp = ws + static_cast<int64_t>(blockIdx.x - part.whole) * (2 * kTile * (HD + 2));       // (a share's: sums, maxima, sums of weights)
+    const float inv = cut ? 1.f : l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll 1
     for (int c = 0; c < HD / 32; ++c) {
       uint32_t v[32];
@@ -371,16 +386,26 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
       }
       if (r >= n_rows) continue;
 #pragma unroll
+      for (int u = 0; u < 32; ++u) {
+        v[u] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(v[u]) * inv);      // nothing attended to: zeros
+        if (rpos >= nan_at[32 * c + u]) v[u] = 0x7fffffffu;
+      }
+      if (cut) {
+#pragma unroll
+        for (int u = 0; u < 32; u += 4) *reinterpret_cast<uint4*>(wp + r * HD + 32 * c + u) = make_uint4(v[u], v[u + 1], v[u + 2], v[u + 3]);
+        continue;
+      }
+#pragma unroll
       for (int u = 0; u < 32; u += 8) {
         Vec<T> x;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          float y = l == 0.f ? 0.f : __uint_as_float(v[u + k]) * inv;             // nothing attended to: zeros
-          if (rpos >= nan_at[32 * c + u + k]) y = __int_as_float(0x7fffffff);
-          x.x[k] = narrow<T>(y);
-        }
+        for (int k = 0; k < 8; ++k) x.x[k] = narrow<T>(__uint_as_float(v[u + k]));
         *reinterpret_cast<Vec<T>*>(op + 32 * c + u) = x;
       }
+    }
+    if (cut && r < n_rows) {
+      wp[2 * kTile * HD + r] = m;
+      wp[2 * kTile * (HD + 1) + r] = l;
     }
     tc::tc_fence_before();
   } else if (warp < kMmaWarp) {
@@ -394,13 +419,13 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
     int entry = -1, place = -1;
     float2 sc = make_float2(0.f, 0.f);
     auto load_entry = [&](int j) {
-      const int step = j * (kTile / kStep) + lane;
+      const int step = (j0 + j) * (kTile / kStep) + lane;
       entry = lane < kTile / kStep && step < n_steps ? __ldg(table + (step >> (V.page_shift - 4))) : -2;
     };
     auto take_entry = [&](int j) {
       const bool there = static_cast<uint32_t>(entry) < static_cast<uint64_t>(V.n_pages);
       if (entry != -2 && !there) report_page(V);
-      place = there ? ((entry * V.hkv + h) << V.page_shift) + ((j * kTile + lane * kStep) & ((1 << V.page_shift) - 1)) : -1;
+      place = there ? ((entry * V.hkv + h) << V.page_shift) + ((p0 + j * kTile + lane * kStep) & ((1 << V.page_shift) - 1)) : -1;
       if (scaler && there) sc = __ldg(V.scales + static_cast<int64_t>(entry) * V.hkv + h);
     };
     auto fetch = [&](uint4(&x)[kPass], const uint8_t* codes) {
@@ -450,7 +475,7 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
         load_entry(j + 2);
         fetch(kr, V.k);
         if (j >= 2 && !wait_warp(kVEmpty + s, (j >> 1) - 1, 20)) break;
-        if (j * kTile + kTile - 1 > lo[0]) {
+        if (p0 + j * kTile + kTile - 1 > lo[0]) {
           // 0 * NaN: where rows do not see the whole step a NaN value is taken out, and the rows that do see it are set to NaN
           // at the end
 #pragma unroll
@@ -463,7 +488,7 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
               while (bad) {
                 const int byte = (__ffs(bad) - 1) >> 3;
                 bad &= bad - 1;
-                atomicMin(nan_at + 16 * piece + 4 * k + byte, j * kTile + p * kRowsPass + row_a);
+                atomicMin(nan_at + 16 * piece + 4 * k + byte, p0 + j * kTile + p * kRowsPass + row_a);
               }
             }
           }
@@ -532,24 +557,48 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
 
 }  // namespace
 
+// The blocks of the last, partial round of SMs (all, where there are fewer than SMs) are cut along the positions as far as
+// SMs are idle, four steps of 128 positions each at least (of what the page table could hold) and not for contexts so short
+// that the joining launch would cost more.
+struct TcCut {
+  int64_t tiles, items, whole;
+  int nsplit;
+};
+static TcCut tc_plan(const View& V, int H) {
+  TcCut p;
+  p.tiles = ceil_div(static_cast<int64_t>(V.max_new) * (H / V.hkv), 2 * kTile);
+  p.items = p.tiles * V.batch * V.hkv;
+  const int64_t tail = p.items % 148, steps = (static_cast<int64_t>(V.max_pages) << V.page_shift) / kTile;
+  p.nsplit = 1;
+  while (p.nsplit < 8 && tail > 0 && tail * (p.nsplit + 1) <= 148 && steps >= 4 * (p.nsplit + 1) && steps >= 16) ++p.nsplit;
+  p.whole = p.nsplit > 1 ? p.items - tail : p.items;
+  return p;
+}
+
+size_t workspace_bytes_tc(const View& V, int H, int hd) {
+  const TcCut p = tc_plan(V, H);
+  return static_cast<size_t>(p.items - p.whole) * p.nsplit * 2 * kTile * (hd + 2) * sizeof(float);
+}
+
 template <typename T, int HD>
-szo_status launch_attention_tc(const View& V, const Rows& A, cudaStream_t st) {
-  const int64_t tiles = ceil_div(static_cast<int64_t>(V.max_new) * (A.H / V.hkv), 2 * kTile);
-  unsigned blocks;
-  SZO_TRY(grid_items(tiles, V, &blocks));
+szo_status launch_attention_tc(const View& V, const Rows& A, float* ws, cudaStream_t st) {
+  const TcCut p = tc_plan(V, A.H);
+  SZO_REQUIRE(p.items <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows, heads and sequences for one launch");
   const int smem = 6 * kTile * HD * 2 + 1024;
   auto kern = kv8_attention_tc_kernel<T, HD>;
   SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  const unsigned blocks = static_cast<unsigned>(p.whole + (p.items - p.whole) * p.nsplit);
   kern<<<blocks, kTcThreads, smem, st>>>(V, static_cast<const T*>(A.q), A.q_stride, static_cast<T*>(A.o), A.o_stride, A.H, A.scale,
-                                         static_cast<int>(tiles));
+                                         static_cast<int>(p.tiles), TcSplit{static_cast<unsigned>(p.whole), p.nsplit}, ws);
   count_launch();
   SZO_CHECK_LAUNCH("kv8_attention_tc_kernel");
-  return SZO_OK;
+  if (p.whole == p.items) return SZO_OK;
+  return launch_join<T, HD>(V, A, ws, 2 * kTile, static_cast<int>(p.tiles), p.nsplit, true, p.whole, p.items - p.whole, st);
 }
-template szo_status launch_attention_tc<__nv_bfloat16, 64>(const View&, const Rows&, cudaStream_t);
-template szo_status launch_attention_tc<__nv_bfloat16, 128>(const View&, const Rows&, cudaStream_t);
-template szo_status launch_attention_tc<__half, 64>(const View&, const Rows&, cudaStream_t);
-template szo_status launch_attention_tc<__half, 128>(const View&, const Rows&, cudaStream_t);
+template szo_status launch_attention_tc<__nv_bfloat16, 64>(const View&, const Rows&, float*, cudaStream_t);
+template szo_status launch_attention_tc<__nv_bfloat16, 128>(const View&, const Rows&, float*, cudaStream_t);
+template szo_status launch_attention_tc<__half, 64>(const View&, const Rows&, float*, cudaStream_t);
+template szo_status launch_attention_tc<__half, 128>(const View&, const Rows&, float*, cudaStream_t);
 
 }  // namespace kv8
 }  // namespace szo

@@ -413,6 +413,18 @@ def test_long_contexts_of_few_sequences(B, dt, d, hkv, group, page):
     run_attention(B, w, [12999, 20], [8 // group, 0], hkv * group, dt)
 
 
+@pytest.mark.parametrize("d,hkv,group,page", [(128, 1, 4, 32), (64, 2, 3, 64)])
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+def test_chunks_of_few_sequences_with_long_contexts(B, dt, d, hkv, group, page):
+    """Few blocks of query rows: their positions are cut and joined."""
+    lens = [2900, 700]
+    w = World(B, lens, hkv, page, d, seed=d + group)
+    fill(B, w, lens)
+    run_attention(B, w, lens, [130, 60], hkv * group, dt)
+    run_attention(B, w, [2100, 30], [97, 100], hkv * group, dt)           # (and padding rows in a cut sequence)
+    assert B.device_status() == 0
+
+
 def test_same_call_same_bits(B):
     w = World(B, [14000, 900], 2, 32, 128, seed=21)
     fill(B, w, [14000, 900])
