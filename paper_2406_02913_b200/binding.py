@@ -366,9 +366,14 @@ def szo_attention(q, k, v, B: int, S: int, n_heads: int, n_kv_heads: int, head_d
 
 
 # ------------------------------------------------------------------------------ 8-bit key/value cache
+_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _here(t, dtype=None, name="tensor"):
     """t is a CUDA tensor of the current device (the library launches there) and of the given type."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if t.get_device() != (_device() if t.is_cuda else -2):
         raise ValueError(f"{name} must be a CUDA tensor of the current device (got {t.device})")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
@@ -392,6 +397,7 @@ class Kv8Cache:
         self.struct = Kv8CacheStruct(codes[0].data_ptr(), codes[1].data_ptr(), scales.data_ptr(), self.n_pages, self.page_tokens,
                                      self.n_kv_heads, self.head_dim)
         self.ref = C.addressof(self.struct)
+        self.device = codes.get_device()
 
     @classmethod
     def empty(cls, n_pages: int, n_kv_heads: int, page_tokens: int, head_dim: int, device="cuda"):
@@ -425,46 +431,56 @@ class Kv8Batch:
         self.struct = Kv8BatchStruct(page_table.data_ptr() or None, kv_len.data_ptr() or None,
                                      None if start is None else start.data_ptr(), rows, batch, page_table.shape[1], max_new)
         self.ref = C.addressof(self.struct)
+        self.device = kv_len.get_device()
 
 
-def _row_buffer(t, rows: int, heads: int, head_dim: int, name: str):
+def _row_buffer(t, device: int, rows: int, heads: int, head_dim: int, name: str):
     """Row stride in elements of [rows, heads, head_dim] or [rows, heads * head_dim], rows possibly apart."""
-    _here(t, None, name)
-    inner = t.stride(-1) == 1 and (t.dim() == 2 or t.dim() == 3 and (t.shape[1] == 1 or t.stride(1) == head_dim))
-    if t.shape[0] != rows or t.numel() != rows * heads * head_dim or (rows and not inner):
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 3:
+        ok = shape == (rows, heads, head_dim) and stride[2] == 1 and (stride[1] == head_dim or heads == 1)
+    else:
+        ok = shape == (rows, heads * head_dim) and stride[1] == 1
+    if not ok and not (rows == 0 and shape[:1] == (0,)):
         raise ValueError(f"{name} must be [{rows}, {heads}, {head_dim}] or [{rows}, {heads * head_dim}] with contiguous rows")
     if t.dtype not in _DT:
         raise ValueError(f"{name} must be float32, bfloat16 or float16 (got {t.dtype})")
-    return t.stride(0) if rows > 1 else heads * head_dim
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on the cache's device (got {t.device})")
+    return stride[0] if rows > 1 else heads * head_dim
 
 
 def _kv8_stream(cache, batch):
-    if cache.codes.device != batch.kv_len.device or cache.codes.device.index != torch.cuda.current_device():
+    device = cache.device
+    if batch.device != device or _device() != device:
         raise ValueError("cache and batch must be on the current device")
-    return _stream()
+    return _raw_stream(device)
 
 
 def szo_kv8_write(cache: Kv8Cache, batch: Kv8Batch, k: torch.Tensor, v: torch.Tensor):
     """Stores the rows' keys and values ([rows, n_kv_heads, head_dim] or [rows, n_kv_heads * head_dim], fp32, bf16 or fp16)."""
-    st = _kv8_stream(cache, batch)
-    ks = _row_buffer(k, batch.rows, cache.n_kv_heads, cache.head_dim, "k")
-    vs = _row_buffer(v, batch.rows, cache.n_kv_heads, cache.head_dim, "v")
+    st, rows = _kv8_stream(cache, batch), batch.rows
+    ks = _row_buffer(k, cache.device, rows, cache.n_kv_heads, cache.head_dim, "k")
+    vs = _row_buffer(v, cache.device, rows, cache.n_kv_heads, cache.head_dim, "v")
     if k.dtype != v.dtype:
         raise ValueError("k and v must have the same type")
-    if batch.rows:
+    if rows:
         _check(lib().szo_kv8_write(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), _DT[k.dtype], ks, vs, st))
 
 
 def szo_kv8_read(cache: Kv8Cache, batch: Kv8Batch, dtype=torch.bfloat16, out=None):
     """The rows' cached keys and values as (k, v), each [rows, n_kv_heads, head_dim] of dtype (or of `out`)."""
-    st = _kv8_stream(cache, batch)
-    shape = (batch.rows, cache.n_kv_heads, cache.head_dim)
-    k, v = out if out is not None else (torch.empty(shape, dtype=dtype, device=cache.codes.device) for _ in range(2))
-    ks = _row_buffer(k, batch.rows, cache.n_kv_heads, cache.head_dim, "k")
-    vs = _row_buffer(v, batch.rows, cache.n_kv_heads, cache.head_dim, "v")
+    st, rows = _kv8_stream(cache, batch), batch.rows
+    if out is None:
+        # (one allocation, two whole tensors of it)
+        k, v = torch.empty((2, rows, cache.n_kv_heads, cache.head_dim), dtype=dtype, device=cache.codes.device).unbind(0)
+    else:
+        k, v = out
+    ks = _row_buffer(k, cache.device, rows, cache.n_kv_heads, cache.head_dim, "k")
+    vs = _row_buffer(v, cache.device, rows, cache.n_kv_heads, cache.head_dim, "v")
     if k.dtype != v.dtype:
         raise ValueError("k and v must have the same type")
-    if batch.rows:
+    if rows:
         _check(lib().szo_kv8_read(cache.ref, batch.ref, k.data_ptr(), v.data_ptr(), _DT[k.dtype], ks, vs, st))
     return k, v
 
@@ -472,21 +488,19 @@ def szo_kv8_read(cache: Kv8Cache, batch: Kv8Batch, dtype=torch.bfloat16, out=Non
 def szo_attention_kv8(cache: Kv8Cache, batch: Kv8Batch, q: torch.Tensor, scale: float | None = None, out=None):
     """Causal attention of the rows q ([rows, n_heads, head_dim] or [rows, n_heads * head_dim]) over the cache,
     which already holds their own keys and values.  scale: 1 / sqrt(head_dim) where None.  Returns o like q."""
-    st = _kv8_stream(cache, batch)
-    d = cache.head_dim
-    width = q.numel() // batch.rows if batch.rows else d * cache.n_kv_heads
-    if width % d:
-        raise ValueError(f"q must be [rows, n_heads, {d}] or [rows, n_heads * {d}]")
-    qs = _row_buffer(q, batch.rows, width // d, d, "q")
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-    os_ = _row_buffer(o, batch.rows, width // d, d, "out")
+    st, rows, d = _kv8_stream(cache, batch), batch.rows, cache.head_dim
+    heads = (q.numel() // (rows * d)) if rows else cache.n_kv_heads
+    qs = _row_buffer(q, cache.device, rows, heads, d, "q")
+    o = torch.empty_like(q) if out is None else out
+    os_ = _row_buffer(o, cache.device, rows, heads, d, "out")
     if o.dtype != q.dtype:
         raise ValueError("out must have q's type")
-    if batch.rows:
-        need = lib().szo_attention_kv8_workspace_bytes(cache.ref, batch.ref, width // d)
-        ws = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else None
-        _check(lib().szo_attention_kv8(cache.ref, batch.ref, q.data_ptr(), qs, o.data_ptr(), os_, _DT[q.dtype], width // d,
-                                       d ** -0.5 if scale is None else scale, None if ws is None else ws.data_ptr(), need, st))
+    if rows:
+        L = lib()
+        need = L.szo_attention_kv8_workspace_bytes(cache.ref, batch.ref, heads)
+        ws = torch.empty((need,), dtype=torch.uint8, device=cache.codes.device) if need else None
+        _check(L.szo_attention_kv8(cache.ref, batch.ref, q.data_ptr(), qs, o.data_ptr(), os_, _DT[q.dtype], heads,
+                                   d ** -0.5 if scale is None else scale, None if ws is None else ws.data_ptr(), need, st))
     return o
 
 
@@ -500,50 +514,63 @@ class TokenLogprobs(NamedTuple):
 
 
 def _logit_rows(logits, targets):
-    _here(logits, None, "logits")
-    if logits.dim() != 2 or logits.dtype not in _DT or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    """rows, vocab, row stride, targets per row and the device of checked arguments."""
+    shape, stride, device = logits.shape, logits.stride(), logits.get_device()
+    if len(shape) != 2 or logits.dtype not in _DT or (shape[1] > 1 and stride[1] != 1):
         raise ValueError("logits must be [rows, vocab], float32, bfloat16 or float16, with contiguous rows")
-    rows, vocab = logits.shape
+    if not logits.is_cuda or device != _device():
+        raise ValueError(f"logits must be a CUDA tensor of the current device (got {logits.device})")
+    rows, vocab = shape
+    nt = 0
     if targets is not None:
-        _here(targets, torch.int32, "targets")
-        if targets.dim() != 2 or targets.shape[0] != rows or not targets.is_contiguous():
-            raise ValueError("targets must be a contiguous int32 tensor [rows, n_targets]")
-    return rows, vocab, logits.stride(0) if rows > 1 else vocab, 0 if targets is None else targets.shape[1]
+        if targets.dtype != torch.int32 or targets.dim() != 2 or targets.shape[0] != rows or not targets.is_contiguous() or targets.get_device() != device:
+            raise ValueError("targets must be a contiguous int32 tensor [rows, n_targets] on the logits' device")
+        nt = targets.shape[1]
+    return rows, vocab, stride[0] if rows > 1 else vocab, nt, device
 
 
 def szo_token_logprobs(logits: torch.Tensor, targets: torch.Tensor | None = None, n_top: int = 0, scale: float = 1.0) -> TokenLogprobs:
     """Log probabilities of targets[r] (int32 [rows, n_targets], negative: none) under softmax(scale * logits[r]), with
     the entropy, log sum exp and the n_top best alternatives of every row."""
-    rows, vocab, ld, nt = _logit_rows(logits, targets)
-    f = torch.empty(rows * (nt + 2 + n_top) + 16, dtype=torch.float32, device=logits.device)
-    sizes, parts, at = (rows * nt, rows, rows, rows * n_top), [], 0
-    for n in sizes:                                     # one allocation; every part starts on 16 bytes
-        parts.append(f[at:at + n])
-        at += -(-n // 4) * 4
-    logp, entropy, lse, top_logp = parts
-    top_ids = torch.empty((rows, n_top), dtype=torch.int32, device=logits.device)
+    rows, vocab, ld, nt, device = _logit_rows(logits, targets)
+    # one allocation for the results; every part starts on 16 bytes
+    r4, t4, a4 = (rows + 3) & ~3, (rows * nt + 3) & ~3, (rows * n_top + 3) & ~3
+    f = torch.empty(2 * r4 + t4 + 2 * a4, dtype=torch.float32, device=logits.device)
+    lse, entropy, logp, top_logp, top_ids = f.split_with_sizes((r4, r4, t4, a4, a4))
+    if r4 != rows:
+        lse, entropy = lse[:rows], entropy[:rows]
+    logp = (logp if t4 == rows * nt else logp[:rows * nt]).view(rows, nt)
+    if a4 != rows * n_top:
+        top_logp, top_ids = top_logp[:rows * n_top], top_ids[:rows * n_top]
+    top_logp, top_ids = top_logp.view(rows, n_top), top_ids.view(torch.int32).view(rows, n_top)
     if rows:
-        _check(lib().szo_token_logprobs(logits.data_ptr(), _DT[logits.dtype], rows, vocab, ld, scale, None if nt == 0 else targets.data_ptr(),
-                                        nt, n_top, logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), top_ids.data_ptr(),
-                                        top_logp.data_ptr(), _stream()))
-    return TokenLogprobs(logp.view(rows, nt), entropy, lse, top_ids, top_logp.view(rows, n_top))
+        _check(lib().szo_token_logprobs(logits.data_ptr(), _DT[logits.dtype], rows, vocab, ld, scale, targets.data_ptr() if nt else None,
+                                        nt, n_top, logp.data_ptr() if nt else None, entropy.data_ptr(), lse.data_ptr(),
+                                        top_ids.data_ptr() if n_top else None, top_logp.data_ptr() if n_top else None, _raw_stream(device)))
+    return TokenLogprobs(logp, entropy, lse, top_ids, top_logp)
 
 
 def szo_token_logprobs_bwd(logits: torch.Tensor, targets: torch.Tensor | None, lse: torch.Tensor, entropy: torch.Tensor | None,
                            d_logp: torch.Tensor | None, d_entropy: torch.Tensor | None = None, scale: float = 1.0, out=None):
     """Gradient of sum(d_logp * logp) + sum(d_entropy * entropy) with respect to the logits; `out` may be the logits."""
-    rows, vocab, ld, nt = _logit_rows(logits, targets)
-    for name, t, n in (("lse", lse, rows), ("entropy", entropy, rows), ("d_logp", d_logp, rows * nt), ("d_entropy", d_entropy, rows)):
-        if t is not None and (_here(t, torch.float32, name).numel() != n or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous float32 tensor of {n} values")
-    d = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device) if out is None else out
-    _here(d, logits.dtype, "out")
-    if d.shape != logits.shape or (vocab > 1 and d.stride(1) != 1):
-        raise ValueError("out must have the logits' shape and contiguous rows")
-    p = lambda t: None if t is None or not t.numel() else t.data_ptr()
+    rows, vocab, ld, nt, device = _logit_rows(logits, targets)
+
+    def ptr(t, n, name):
+        if t is None:
+            return None
+        if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+            raise ValueError(f"{name} must be a contiguous float32 tensor of {n} values on the logits' device")
+        return t.data_ptr() if n else None
+    p = ptr(lse, rows, "lse"), ptr(entropy, rows, "entropy"), ptr(d_logp, rows * nt, "d_logp"), ptr(d_entropy, rows, "d_entropy")
+    if out is None:
+        d, dld = torch.empty_like(logits, memory_format=torch.contiguous_format), vocab
+    else:
+        d, dld = out, out.stride(0) if rows > 1 else vocab
+        if d.shape != logits.shape or d.dtype != logits.dtype or d.get_device() != device or (vocab > 1 and d.stride(1) != 1):
+            raise ValueError("out must have the logits' shape, type and device and contiguous rows")
     if rows:
-        _check(lib().szo_token_logprobs_bwd(logits.data_ptr(), _DT[logits.dtype], rows, vocab, ld, scale, p(targets), nt, p(lse), p(entropy),
-                                            p(d_logp), p(d_entropy), d.data_ptr(), d.stride(0) if rows > 1 else vocab, _stream()))
+        _check(lib().szo_token_logprobs_bwd(logits.data_ptr(), _DT[logits.dtype], rows, vocab, ld, scale, targets.data_ptr() if nt else None,
+                                            nt, *p, d.data_ptr(), dld, _raw_stream(device)))
     return d
 
 
