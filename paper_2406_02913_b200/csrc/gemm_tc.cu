@@ -499,7 +499,7 @@ szo_status linear_fwd_tc_materialised(const szo_linear* const* plans, int n, con
                                       const float* const* S_pert, void* const* y, int y_dtype, void* ws,
                                       size_t ws_bytes, cudaStream_t st, const float* const* S_second,
                                       __nv_bfloat16* W_resident, __nv_bfloat16* saved_resident, bool relu,
-                                      const PairedArgs* paired) {
+                                      const PairedArgs* paired, bool resident_ext) {
   const szo_linear* p0 = plans[0];
   const bool resident = W_resident != nullptr;
   SZO_REQUIRE(paired == nullptr || (S_second == nullptr && !relu), SZO_ERR_INVALID_ARG,
@@ -518,7 +518,8 @@ szo_status linear_fwd_tc_materialised(const szo_linear* const* plans, int n, con
   }
   // dense form of the paired sparse product: eps * Zbar beside W, rows 2 K wide
   const bool ext = paired != nullptr && paired->dense && nnz_all > 0;
-  const int64_t ld = p0->K * (ext ? 2 : 1);
+  // (a lone forward of a paired model reads the first half of the wide resident rows)
+  const int64_t ld = p0->K * (ext || resident_ext ? 2 : 1);
   // resident form: the weight and the dense values at the masked positions live in the caller's buffers
   const size_t w_bytes = resident ? 0 : round_up(static_cast<size_t>(rows) * ld * sizeof(__nv_bfloat16), 256);
   const size_t saved_bytes = resident ? 0 : round_up(nnz_all * sizeof(__nv_bfloat16), 256);

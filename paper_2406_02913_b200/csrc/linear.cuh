@@ -130,7 +130,7 @@ szo_status linear_fwd_tc_materialised(const szo_linear* const* plans, int n, con
                                       size_t ws_bytes, cudaStream_t st, const float* const* S_second = nullptr,
                                       __nv_bfloat16* W_resident = nullptr, __nv_bfloat16* saved_resident = nullptr,
                                       bool relu = false,    // relu: y = max(y, 0) applied in the epilogue
-                                      const PairedArgs* paired = nullptr);
+                                      const PairedArgs* paired = nullptr, bool resident_ext = false);
 // Resident form for dense bf16 plans (G == 0): W_resident [sum Npad, K] and saved_resident [sum nnz]
 // are filled once by tc_resident_init and passed to linear_fwd_tc_materialised, which then skips the
 // weight pass and writes every masked entry as RN_bf16(saved + S); ws is only the K-split scratch.

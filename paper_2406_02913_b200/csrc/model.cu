@@ -1091,7 +1091,8 @@ szo_status run_loss_t(szo_model* m, const int32_t* tokens, const int32_t* labels
     }
     const szo_status rc = mat ? linear_fwd_tc_materialised(plans, n, x, M, spert, outs, act, m->ws, m->ws_bytes, st,
                                                            nsets == 2 ? spert2 : nullptr, res ? m->res_W[t0] : nullptr,
-                                                           res ? m->res_saved[t0] : nullptr, relu_applied != nullptr)
+                                                           res ? m->res_saved[t0] : nullptr, relu_applied != nullptr, nullptr,
+                                                           res && m->paired && tc_paired_dense_cross(plans, n))
                               : linear_fwd_tc_group(plans, n, x, M, recs, outs, act, m->ws, m->ws_bytes, st);
     if (mat && relu_applied != nullptr) *relu_applied = true;
     if (m->timing) {
