@@ -475,6 +475,18 @@ szo_status szo_model_zo_step_host(szo_model_t* m, const int32_t* tokens_host,
 szo_status szo_model_enable_decode(szo_model_t* m, void* stream);
 szo_status szo_model_decode_step(szo_model_t* m, const int32_t* tokens, int32_t B, int32_t T, int32_t pos0,
                                  const float* S_vals, float* logits_dev, void* stream);
+/* Token generation with the 8-bit paged cache instead (szo_kv8_write, szo_attention_kv8): e4m3 codes and scales for
+ * max_batch sequences of max_seq positions (a little over half of a bf16 cache's memory), pages of page_tokens
+ * (16, 32, 64 or 128).  szo_model_decode_step then works as described above; its results carry the cache's rounding
+ * (a key or value is off by at most 2^-4 of its size).  Once, and not together with szo_model_enable_decode. */
+szo_status szo_model_enable_decode_kv8(szo_model_t* m, int32_t page_tokens, void* stream);
+/* Log probabilities of given tokens at every position of B sequences of S tokens (the terms that the next-token loss
+ * sums, and those of any other candidates): one forward as for szo_model_loss, then szo_token_logprobs on the fp32
+ * logits of all B*S positions.  targets int32 [B*S][n_targets]; outputs as for szo_token_logprobs with rows = B*S (row
+ * b*S+s is the distribution of the token after position s).  Needs loss_kind 0. */
+szo_status szo_model_token_logprobs(szo_model_t* m, const int32_t* tokens, int32_t B, int32_t S, const int32_t* targets,
+                                    int32_t n_targets, int32_t n_top, const float* S_vals, float* logp, float* entropy,
+                                    float* lse, int32_t* top_ids, float* top_logp, void* stream);
 /* Number of kernel launches the last szo_model_zo_step on this model enqueued. */
 int64_t szo_model_last_launches(const szo_model_t* m);
 /* Measurement aid (no counterpart in the paper): when enabled, the model brackets every

@@ -142,6 +142,9 @@ _SIGS = {
                                            C.c_int32, C.c_uint64, C.c_uint64, C.c_float, C.c_float,
                                            C.c_void_p, C.c_void_p]),
     "szo_model_enable_decode": (C.c_int32, [C.c_void_p, C.c_void_p]),
+    "szo_model_enable_decode_kv8": (C.c_int32, [C.c_void_p, C.c_int32, C.c_void_p]),
+    "szo_model_token_logprobs": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p,
+                                             C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "szo_model_decode_step": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                                           C.c_void_p, C.c_void_p]),
     "szo_model_last_launches": (C.c_int64, [C.c_void_p]),
@@ -684,8 +687,31 @@ class Model:
                                             seed, step, eps, lr, C.cast(out, C.c_void_p), _stream()))
         return out[0], out[1], out[2]
 
-    def enable_decode(self):
-        _check(lib().szo_model_enable_decode(self.h, _stream()))
+    def enable_decode(self, kv8_page_tokens: int | None = None):
+        """Allocates the key/value cache of decode_step: in the activations' type, or (kv8_page_tokens 16, 32, 64 or
+        128) in 8 bits with pages of that many positions."""
+        if kv8_page_tokens is None:
+            _check(lib().szo_model_enable_decode(self.h, _stream()))
+        else:
+            _check(lib().szo_model_enable_decode_kv8(self.h, kv8_page_tokens, _stream()))
+
+    def token_logprobs(self, tokens, targets=None, n_top: int = 0, S_vals=None) -> TokenLogprobs:
+        """Log probabilities under the model's next-token distributions: tokens int32 [B, S]; targets int32
+        [B * S, n_targets] (negative: none) or None: the tokens that follow (none after the last of a sequence)."""
+        B, S = tokens.shape
+        if targets is None:
+            targets = torch.full_like(tokens, -1)
+            targets[:, :-1] = tokens[:, 1:]
+            targets = targets.view(B * S, 1)
+        if targets.dtype != torch.int32 or targets.dim() != 2 or targets.shape[0] != B * S:
+            raise ValueError("targets must be int32 [B * S, n_targets]")
+        new = lambda n, dt=torch.float32: torch.empty((B * S, n), dtype=dt, device=tokens.device)
+        nt = targets.shape[1]
+        r = TokenLogprobs(new(nt), new(1).view(-1), new(1).view(-1), new(n_top, torch.int32), new(n_top))
+        p = lambda t: _ptr(t) if t.numel() else None
+        _check(lib().szo_model_token_logprobs(self.h, _ptr(tokens), B, S, p(targets), nt, n_top, _ptr(S_vals), p(r.logp), _ptr(r.entropy),
+                                              _ptr(r.lse), p(r.top_ids), p(r.top_logp), _stream()))
+        return r
 
     def decode_step(self, tokens, pos0: int, logits=None, S_vals=None) -> torch.Tensor:
         """tokens int32 [B, T] following pos0 cached positions; returns fp32 logits [B, vocab] of the last one."""

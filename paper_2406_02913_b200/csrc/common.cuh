@@ -127,4 +127,9 @@ szo_status launch_flash_attention_bf16(const void* q, const void* k, const void*
 szo_status launch_flash_attention_pair_bf16(const void* q, const void* k, const void* v, void* o, int64_t row0, int B,
                                             int S, int H, int Hkv, int hd, cudaStream_t st);
 
+// The argument checks of szo_token_logprobs (logprobs.cu), for a caller that has work to do before it
+szo_status check_token_logprobs(const void* logits, szo_dtype dtype, int64_t rows, int64_t vocab, int64_t row_stride, float scale,
+                                const int32_t* targets, int32_t n_targets, int32_t n_top, const float* logp, const float* entropy,
+                                const float* lse, const int32_t* top_ids, const float* top_logp);
+
 }  // namespace szo

@@ -556,6 +556,19 @@ szo_status check_logits(const void* logits, szo_dtype dt, int64_t rows, int64_t 
 }
 
 }  // namespace
+
+szo_status check_token_logprobs(const void* logits, szo_dtype dtype, int64_t rows, int64_t vocab, int64_t row_stride, float scale,
+                                const int32_t* targets, int32_t n_targets, int32_t n_top, const float* logp, const float* entropy,
+                                const float* lse, const int32_t* top_ids, const float* top_logp) {
+  SZO_TRY(check_logits(logits, dtype, rows, vocab, row_stride, scale, targets, n_targets));
+  SZO_REQUIRE(n_top >= 0 && n_top <= kMaxTop && n_top <= vocab, SZO_ERR_UNSUPPORTED, "n_top must be in [0, min(%d, vocab)]", kMaxTop);
+  SZO_REQUIRE(rows == 0 || n_targets == 0 || logp, SZO_ERR_INVALID_ARG, "logp is NULL");
+  SZO_REQUIRE(rows == 0 || n_top == 0 || (top_ids && top_logp), SZO_ERR_INVALID_ARG, "top_ids or top_logp is NULL");
+  SZO_REQUIRE(aligned16(logp) && aligned16(entropy) && aligned16(lse) && aligned16(top_ids) && aligned16(top_logp), SZO_ERR_ALIGNMENT,
+              "buffers must be 16-byte aligned");
+  return SZO_OK;
+}
+
 }  // namespace szo
 
 using namespace szo;
@@ -565,12 +578,7 @@ extern "C" {
 szo_status szo_token_logprobs(const void* logits, szo_dtype dtype, int64_t rows, int64_t vocab, int64_t row_stride, float scale,
                               const int32_t* targets, int32_t n_targets, int32_t n_top, float* logp, float* entropy, float* lse,
                               int32_t* top_ids, float* top_logp, void* stream) {
-  SZO_TRY(check_logits(logits, dtype, rows, vocab, row_stride, scale, targets, n_targets));
-  SZO_REQUIRE(n_top >= 0 && n_top <= kMaxTop && n_top <= vocab, SZO_ERR_UNSUPPORTED, "n_top must be in [0, min(%d, vocab)]", kMaxTop);
-  SZO_REQUIRE(rows == 0 || n_targets == 0 || logp, SZO_ERR_INVALID_ARG, "logp is NULL");
-  SZO_REQUIRE(rows == 0 || n_top == 0 || (top_ids && top_logp), SZO_ERR_INVALID_ARG, "top_ids or top_logp is NULL");
-  SZO_REQUIRE(aligned16(logp) && aligned16(entropy) && aligned16(lse) && aligned16(top_ids) && aligned16(top_logp), SZO_ERR_ALIGNMENT,
-              "buffers must be 16-byte aligned");
+  SZO_TRY(check_token_logprobs(logits, dtype, rows, vocab, row_stride, scale, targets, n_targets, n_top, logp, entropy, lse, top_ids, top_logp));
   if (rows == 0) return SZO_OK;
   int32_t* status = device_status_word();
   SZO_REQUIRE(status != nullptr, SZO_ERR_CUDA, "no device status word (no CUDA device?)");

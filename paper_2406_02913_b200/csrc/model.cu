@@ -887,6 +887,14 @@ cls2_pair_kernel(const float* __restrict__ a_last, int B, const __nv_bfloat16* _
 }
 
 __global__ void set_i32_kernel(int32_t* p, int32_t v) { *p = v; }
+__global__ void fill_i32_kernel(int32_t* p, int64_t n, int32_t v) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+  if (i < n) p[i] = v;
+}
+__global__ void iota_i32_kernel(int32_t* p, int64_t n) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+  if (i < n) p[i] = static_cast<int32_t>(i);
+}
 
 // *out = (sum of v[0..n)) / denom, fixed order, fp64.
 __global__ void __launch_bounds__(1024) mean_f64_kernel(const double* __restrict__ v, int64_t n, double denom,
@@ -970,6 +978,13 @@ struct szo_model {
   double* d_scalars = nullptr;
   int64_t last_launches = 0;
   void *kcache = nullptr, *vcache = nullptr;     // [n_layers][max_batch][max_seq][n_kv_heads * head_dim], act dtype
+  // 8-bit cache (szo_model_enable_decode_kv8): sequence b owns the pages b * kv8_pages .. of every layer
+  uint8_t* kv8_codes = nullptr;                  // [n_layers][keys, values][max_batch * kv8_pages][n_kv_heads][kv8_page][head_dim]
+  float* kv8_scales = nullptr;                   // [n_layers][max_batch * kv8_pages][n_kv_heads][2]
+  int32_t *kv8_table = nullptr, *kv8_len = nullptr;    // [max_batch][kv8_pages]; [max_batch], set by every call
+  void* kv8_ws = nullptr;
+  size_t kv8_ws_bytes = 0;
+  int kv8_page = 0, kv8_pages = 0;
   float* h2 = nullptr;                           // [2][d_model]: second copy of the residual stream of a one- or two-row token step
   int sparse_dt = SZO_F32;                       // storage format of the sparse values (szo_model_set_sparse_storage)
   void* S16_out = nullptr;                       // caller-owned mirror of the stored form, or NULL
@@ -1019,10 +1034,18 @@ unsigned blocks_for(int64_t n, int t) { return static_cast<unsigned>(ceil_div(n,
 // two sets of sparse values.  Every activation buffer then holds 2 M rows (set 0 first), the
 // elementwise, norm and attention kernels run once over both sets, and each linear group makes one
 // weight pass for both (materialised form only).
+// score != nullptr: instead of the loss, the log probabilities of score's targets at every position.
+struct ScoreArgs {
+  const int32_t* targets;
+  int n_targets, n_top;
+  float *logp, *entropy, *lse;
+  int32_t* top_ids;
+  float* top_logp;
+};
 template <typename T>
 szo_status run_loss_t(szo_model* m, const int32_t* tokens, const int32_t* labels, const int32_t* cand, int B,
                       int S, const float* Sv, double* loss_dev, cudaStream_t st, const float* Sv2 = nullptr,
-                      double* loss_dev2 = nullptr) {
+                      double* loss_dev2 = nullptr, const ScoreArgs* score = nullptr) {
   const szo_model_config& c = m->cfg;
   const int64_t M = static_cast<int64_t>(B) * S;
   const int nsets = Sv2 != nullptr ? 2 : 1;
@@ -1170,6 +1193,11 @@ szo_status run_loss_t(szo_model* m, const int32_t* tokens, const int32_t* labels
     const int mode = lmode == SZO_MODE_FP32_VALIDATE ? SZO_MODE_FP32_VALIDATE : SZO_MODE_SPARSE_ADD;
     SZO_TRY(szo_linear_fwd(m->lm_head_plan, a, static_cast<szo_dtype>(act), Mr, nullptr, m->logits, SZO_F32, mode,
                            m->ws, m->ws_bytes, st));
+    if (score != nullptr) {
+      SZO_CHECK_LAUNCH("model kernels");
+      return szo_token_logprobs(m->logits, SZO_F32, M, c.vocab, c.vocab, 1.0f, score->targets, score->n_targets, score->n_top, score->logp,
+                                score->entropy, score->lse, score->top_ids, score->top_logp, st);
+    }
     for (int set = 0; set < nsets; ++set) {
       ce_rows_kernel<<<static_cast<unsigned>(M), 256, 0, st>>>(m->logits + set * M * c.vocab, tokens, S, c.vocab,
                                                               m->tok_loss + set * M);
@@ -1413,7 +1441,20 @@ szo_status run_decode_t(szo_model* m, const int32_t* tokens, int B, int Tn, cons
     T* vc = static_cast<T*>(m->vcache) + l * layer_cache;
     dim3 grid(static_cast<unsigned>(Tn), H, B);
     const float scale = 1.0f / sqrtf(static_cast<float>(hd));
-    if (Tn <= 16) {
+    if (m->kv8_codes != nullptr) {
+      if (!opt) {
+        const int64_t n_rot = M * (H + Hkv) * ((hd / 2) / Vec16<T>::kN);
+        SZO_CHECK_CUDA(launch_maybe_chained(rope_kernel<T>, dim3(blocks_for(n_rot, 256)), dim3(256), 0, st, chained, q, k, m->rope_tab, M,
+                                            Tn, H, Hkv, hd, 0, pos_dev));
+        count_launch();
+      }
+      const int64_t pages = static_cast<int64_t>(c.max_batch) * m->kv8_pages, bytes = pages * m->kv8_page * dkv;
+      uint8_t* codes = m->kv8_codes + l * 2 * bytes;
+      const szo_kv8_cache cache{codes, codes + bytes, m->kv8_scales + l * pages * Hkv * 2, pages, m->kv8_page, Hkv, hd};
+      const szo_kv8_batch batch{m->kv8_table, m->kv8_len, nullptr, M, B, m->kv8_pages, Tn};
+      SZO_TRY(szo_kv8_write(&cache, &batch, k, v, static_cast<szo_dtype>(act), dkv, dkv, st));
+      SZO_TRY(szo_attention_kv8(&cache, &batch, q, d, o, d, static_cast<szo_dtype>(act), H, scale, m->kv8_ws, m->kv8_ws_bytes, st));
+    } else if (Tn <= 16) {
       // rotation, cache append and attention in one launch
       const float2* tab = opt ? nullptr : m->rope_tab;
       auto attn = hd == 64 ? attn_decode_fused_kernel<T, 64> : attn_decode_fused_kernel<T, 128>;
@@ -1897,14 +1938,9 @@ szo_status szo_model_zo_step_host(szo_model_t* m, const int32_t* tokens_host, co
   return SZO_OK;
 }
 
-szo_status szo_model_enable_decode(szo_model_t* m, void* stream) {
-  SZO_REQUIRE(m != nullptr, SZO_ERR_INVALID_ARG, "model is NULL");
-  if (m->kcache != nullptr) return SZO_OK;
+// What token generation needs besides its cache: buffers that a captured step can keep, the LM head, the workspace
+static szo_status enable_decode_common(szo_model* m, cudaStream_t st) {
   const szo_model_config& c = m->cfg;
-  const size_t e = c.act_dtype == SZO_F32 ? 4 : 2;
-  const size_t bytes = static_cast<size_t>(c.n_layers) * c.max_batch * c.max_seq * c.n_kv_heads * (c.d_model / c.n_heads) * e;
-  SZO_TRY(dev_alloc(m, reinterpret_cast<char**>(&m->kcache), bytes));
-  SZO_TRY(dev_alloc(m, reinterpret_cast<char**>(&m->vcache), bytes));
   SZO_TRY(dev_alloc(m, &m->d_pos, sizeof(int32_t)));
   SZO_TRY(dev_alloc(m, &m->h2, 2 * static_cast<size_t>(c.d_model) * sizeof(float)));
   SZO_TRY(dev_alloc(m, &m->dec_tokens, static_cast<size_t>(m->Mmax) * sizeof(int32_t)));
@@ -1914,7 +1950,6 @@ szo_status szo_model_enable_decode(szo_model_t* m, void* stream) {
     const char* env = getenv("SZO_DECODE_GRAPH");
     m->dec_use_graph = !(env != nullptr && env[0] == '0');
   }
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (m->lm_head_plan == nullptr) {
     SZO_TRY(szo_linear_create(&m->decode_head, c.vocab, c.d_model, 0, m->top.lm_head, nullptr, nullptr, SZO_BF16, nullptr,
                               0, nullptr, st));
@@ -1940,10 +1975,72 @@ szo_status szo_model_enable_decode(szo_model_t* m, void* stream) {
   return SZO_OK;
 }
 
+szo_status szo_model_enable_decode(szo_model_t* m, void* stream) {
+  SZO_REQUIRE(m != nullptr, SZO_ERR_INVALID_ARG, "model is NULL");
+  SZO_REQUIRE(m->kv8_codes == nullptr, SZO_ERR_INVALID_ARG, "token generation is already enabled, with an 8-bit cache");
+  if (m->kcache != nullptr) return SZO_OK;
+  const szo_model_config& c = m->cfg;
+  const size_t e = c.act_dtype == SZO_F32 ? 4 : 2;
+  const size_t bytes = static_cast<size_t>(c.n_layers) * c.max_batch * c.max_seq * c.n_kv_heads * (c.d_model / c.n_heads) * e;
+  SZO_TRY(dev_alloc(m, reinterpret_cast<char**>(&m->kcache), bytes));
+  SZO_TRY(dev_alloc(m, reinterpret_cast<char**>(&m->vcache), bytes));
+  return enable_decode_common(m, static_cast<cudaStream_t>(stream));
+}
+
+szo_status szo_model_enable_decode_kv8(szo_model_t* m, int32_t page_tokens, void* stream) {
+  SZO_REQUIRE(m != nullptr, SZO_ERR_INVALID_ARG, "model is NULL");
+  SZO_REQUIRE(page_tokens == 16 || page_tokens == 32 || page_tokens == 64 || page_tokens == 128, SZO_ERR_UNSUPPORTED,
+              "page_tokens must be 16, 32, 64 or 128 (got %d)", page_tokens);
+  SZO_REQUIRE(m->kcache == nullptr, SZO_ERR_INVALID_ARG, "token generation is already enabled, with a 16- or 32-bit cache");
+  SZO_REQUIRE(m->kv8_codes == nullptr || m->kv8_page == page_tokens, SZO_ERR_INVALID_ARG, "token generation is already enabled, with pages of %d",
+              m->kv8_page);
+  if (m->kv8_codes != nullptr) return SZO_OK;
+  const szo_model_config& c = m->cfg;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int hd = c.d_model / c.n_heads;
+  const int64_t per_seq = ceil_div(c.max_seq, page_tokens), pages = per_seq * c.max_batch;
+  SZO_REQUIRE(pages < (int64_t(1) << 31) / page_tokens / c.n_kv_heads, SZO_ERR_SHAPE, "max_batch * max_seq is too large for the 8-bit cache");
+  const size_t bytes = static_cast<size_t>(c.n_layers) * 2 * pages * page_tokens * c.n_kv_heads * hd;
+  const size_t scales = static_cast<size_t>(c.n_layers) * pages * c.n_kv_heads * 2 * sizeof(float);
+  // the most that szo_attention_kv8 asks for at these shapes: one partial tile of 256 rows per SM
+  const size_t ws = static_cast<size_t>(148) * 256 * (hd + 2) * sizeof(float);
+  uint8_t* codes = nullptr;
+  SZO_TRY(dev_alloc(m, &codes, bytes));
+  SZO_TRY(dev_alloc(m, &m->kv8_scales, scales));
+  SZO_TRY(dev_alloc(m, &m->kv8_table, static_cast<size_t>(pages) * sizeof(int32_t)));
+  SZO_TRY(dev_alloc(m, &m->kv8_len, static_cast<size_t>(c.max_batch) * sizeof(int32_t)));
+  SZO_TRY(dev_alloc(m, reinterpret_cast<char**>(&m->kv8_ws), ws));
+  SZO_CHECK_CUDA(cudaMemsetAsync(codes, 0, bytes, st));
+  SZO_CHECK_CUDA(cudaMemsetAsync(m->kv8_scales, 0, scales, st));
+  iota_i32_kernel<<<blocks_for(pages, 256), 256, 0, st>>>(m->kv8_table, pages);
+  SZO_CHECK_LAUNCH("iota_i32_kernel");
+  SZO_TRY(enable_decode_common(m, st));
+  m->kv8_ws_bytes = ws;
+  m->kv8_page = page_tokens;
+  m->kv8_pages = static_cast<int>(per_seq);
+  m->kv8_codes = codes;
+  return SZO_OK;
+}
+
+szo_status szo_model_token_logprobs(szo_model_t* m, const int32_t* tokens, int32_t B, int32_t S, const int32_t* targets, int32_t n_targets,
+                                    int32_t n_top, const float* S_vals, float* logp, float* entropy, float* lse, int32_t* top_ids,
+                                    float* top_logp, void* stream) {
+  SZO_REQUIRE(m != nullptr, SZO_ERR_INVALID_ARG, "model is NULL");
+  SZO_REQUIRE(m->cfg.loss_kind == 0, SZO_ERR_UNSUPPORTED, "needs a model of the next-token loss (loss_kind 0)");
+  SZO_TRY(check_batch(m, tokens, nullptr, nullptr, B, S));
+  SZO_TRY(check_token_logprobs(m->logits, SZO_F32, static_cast<int64_t>(B) * S, m->cfg.vocab, m->cfg.vocab, 1.0f, targets, n_targets, n_top,
+                               logp, entropy, lse, top_ids, top_logp));
+  const ScoreArgs score{targets, n_targets, n_top, logp, entropy, lse, top_ids, top_logp};
+  const float* Sv = S_vals ? S_vals : m->S_all;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (m->cfg.act_dtype == SZO_F32) return run_loss_t<float>(m, tokens, nullptr, nullptr, B, S, Sv, nullptr, st, nullptr, nullptr, &score);
+  return run_loss_t<__nv_bfloat16>(m, tokens, nullptr, nullptr, B, S, Sv, nullptr, st, nullptr, nullptr, &score);
+}
+
 szo_status szo_model_decode_step(szo_model_t* m, const int32_t* tokens, int32_t B, int32_t T, int32_t pos0,
                                  const float* S_vals, float* logits_dev, void* stream) {
   SZO_REQUIRE(m != nullptr && tokens != nullptr && logits_dev != nullptr, SZO_ERR_INVALID_ARG, "NULL argument");
-  SZO_REQUIRE(m->kcache != nullptr, SZO_ERR_INVALID_ARG, "call szo_model_enable_decode first");
+  SZO_REQUIRE(m->kcache != nullptr || m->kv8_codes != nullptr, SZO_ERR_INVALID_ARG, "call szo_model_enable_decode first");
   SZO_REQUIRE(B >= 1 && B <= m->cfg.max_batch && T >= 1 && pos0 >= 0 && pos0 + T <= m->cfg.max_seq, SZO_ERR_SHAPE,
               "need 1 <= B <= %d, T >= 1 and pos0 + T <= %d (got B=%d, T=%d, pos0=%d)", m->cfg.max_batch, m->cfg.max_seq, B,
               T, pos0);
@@ -1957,6 +2054,10 @@ szo_status szo_model_decode_step(szo_model_t* m, const int32_t* tokens, int32_t 
   };
   set_i32_kernel<<<1, 1, 0, st>>>(m->d_pos, pos0);
   count_launch();
+  if (m->kv8_codes != nullptr) {
+    fill_i32_kernel<<<blocks_for(B, 256), 256, 0, st>>>(m->kv8_len, B, pos0 + T);
+    count_launch();
+  }
   // A token step is several hundred short launches: on a stream that can be captured it is recorded once
   // per (B, T, sparse values) as a CUDA graph and replayed (the position comes from device memory, the
   // tokens and logits pass through buffers of the model); the legacy default stream runs it launch by launch.

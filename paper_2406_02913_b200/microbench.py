@@ -317,7 +317,7 @@ def step_case(name, Bn, S, loss, steps, eps, lr, profile_range=False, form="pair
     model.close()
 
 
-def decode_case(name, Bn, prompt, gen):
+def decode_case(name, Bn, prompt, gen, kv8_page=0):
     """Token generation with a KV cache (szo_model_decode_step): a prompt of `prompt` tokens in one
     call, then `gen` calls of one token per sequence, timed with CUDA events over the generation loop.
     Every step streams all linear weights once, so the roofline is the weight bytes over the HBM
@@ -326,7 +326,7 @@ def decode_case(name, Bn, prompt, gen):
     tensors, S_all = wl.device_decoder_tensors(shape, seed=0)
     model = B.Model(shape, wl.linear_names(shape), tensors, S_all, act_dtype=B.SZO_BF16, linear_mode=B.MODE_SPARSE_ADD,
                     loss_kind=B.LOSS_LM, max_batch=Bn, max_seq=prompt + gen)
-    model.enable_decode()
+    model.enable_decode(kv8_page or None)
     g = torch.Generator(device="cuda")
     g.manual_seed(1)
     toks = torch.randint(0, shape["vocab"], (Bn, prompt), generator=g, device="cuda", dtype=torch.int32)
@@ -361,7 +361,7 @@ def decode_case(name, Bn, prompt, gen):
     weight_bytes = weight_bytes * shape["n_layers"] + 2 * shape["vocab"] * shape["d_model"]
     hbm = peaks()[0]
     per_step_ms = ms_gen / gen
-    print(json.dumps({"case": "decode", "model": name, "batch": Bn, "prompt": prompt, "generated": gen,
+    print(json.dumps({"case": "decode", "model": name, "batch": Bn, "prompt": prompt, "generated": gen, "cache": f"e4m3, pages of {kv8_page}" if kv8_page else "bf16",
                       "prompt_ms": e0.elapsed_time(e1), "ms_per_token_step": per_step_ms,
                       "tokens_per_s": Bn * gen / ms_gen * 1e3, "weight_bytes_per_step": weight_bytes,
                       "roofline_ms_per_step": weight_bytes / hbm / 1e6, "frac_of_hbm": weight_bytes / hbm / 1e6 / per_step_ms,
@@ -374,6 +374,7 @@ def main():
     ap.add_argument("what", choices=["linear", "paired", "steady", "sparse", "sweep", "attention", "step", "decode"])
     ap.add_argument("--prompt", type=int, default=16)
     ap.add_argument("--gen", type=int, default=128)
+    ap.add_argument("--kv8-page", type=int, default=0, help="decode: 8-bit cache with pages of this many tokens (0: bf16 cache)")
     ap.add_argument("--model", default="mistral_7b", choices=sorted(wl.MODEL_SHAPES))
     ap.add_argument("--batch", type=int, default=8)
     ap.add_argument("--seq", type=int, default=512)
@@ -398,7 +399,7 @@ def main():
     if a.what == "linear":
         linear_case(a.M, a.N, a.K, a.G, a.mode, a.rho, a.reps)
     elif a.what == "decode":
-        decode_case(a.model, a.batch, a.prompt, a.gen)
+        decode_case(a.model, a.batch, a.prompt, a.gen, a.kv8_page)
     elif a.what == "paired":
         paired_case(a.M, a.N, a.K, a.G, a.rho, a.reps)
     elif a.what == "steady":
