@@ -42,6 +42,7 @@ constexpr int kUnit = 32, kDepth = 2;     // kDepth: units of a warp's ring
 // The largest weight is 2^kOffset when the reference maximum m is set; m follows the running maximum only once that
 // is more than 2^kSlack above it (weights then stay below 2^15), so the outputs are rescaled a few times per sequence.
 constexpr float kOffset = 12.0f, kSlack = 3.0f;
+constexpr int kWideUnits = 12 * 16 * 2;        // see plan()
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -468,9 +469,9 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   }
   cg::cluster_group cluster = cg::this_cluster();
   cluster.sync();
-  const int share = R * HD / nsplit;
+  const int from = R * HD * split / nsplit, share = R * HD * (split + 1) / nsplit - from;
   for (int i = threadIdx.x; i < share; i += kWarps * 32) {
-    const int at = split * share + i, r = at / HD;
+    const int at = from + i, r = at / HD;
     if (r >= n_rows) continue;
     float mm = -INFINITY, sum = 0.f, ll = 0.f;
     for (int x = 0; x < nsplit; ++x) mm = fmaxf(mm, cluster.map_shared_rank(wm, x)[r]);
@@ -484,13 +485,15 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   cluster.sync();                                                 // nobody leaves while its sums are being read
 }
 
-// A block per (row of a tile, item), a thread per dim; shares in order.
-template <typename T, int HD>
-__global__ void __launch_bounds__(HD)
+// A block per (row of a tile, item): kGroups groups of a thread per dim take every kGroups-th share, the groups' results are
+// joined in order.
+template <typename T, int HD, int kGroups>
+__global__ void __launch_bounds__(HD * kGroups)
 kv8_join_kernel(View V, const float* __restrict__ ws, T* __restrict__ o, int64_t o_stride, int H, int R, int row_tiles, int nsplit,
                 bool long_first, unsigned item0) {
+  __shared__ float sums[kGroups][HD], ms[kGroups], ls[kGroups];
   chain_release();
-  const int r = blockIdx.x % R, d = threadIdx.x, G = H / V.hkv;
+  const int r = blockIdx.x % R, d = threadIdx.x % HD, grp = threadIdx.x / HD, G = H / V.hkv;
   const unsigned item = item0 + blockIdx.x / R, others = static_cast<unsigned>(V.batch) * V.hkv;
   const int rt = long_first ? row_tiles - 1 - static_cast<int>(item / others) : item % row_tiles;
   const unsigned bh = long_first ? item % others : item / row_tiles;
@@ -502,12 +505,32 @@ kv8_join_kernel(View V, const float* __restrict__ ws, T* __restrict__ o, int64_t
   const int64_t step = static_cast<int64_t>(R) * (HD + 2);
   const float* p = ws + static_cast<int64_t>(blockIdx.x / R) * nsplit * step;
   float mm = -INFINITY, sum = 0.f, ll = 0.f;
-  for (int x = 0; x < nsplit; ++x) mm = fmaxf(mm, p[x * step + R * HD + r]);
-#pragma unroll 4
-  for (int x = 0; x < nsplit; ++x) {
+#pragma unroll 8
+  for (int x = grp; x < nsplit; x += kGroups) mm = fmaxf(mm, p[x * step + R * HD + r]);
+#pragma unroll 8
+  for (int x = grp; x < nsplit; x += kGroups) {
     const float f = mm == -INFINITY ? 1.f : ex2(p[x * step + R * HD + r] - mm);
     sum = fmaf(f, p[x * step + r * HD + d], sum);
     ll = fmaf(f, p[x * step + R * (HD + 1) + r], ll);
+  }
+  if constexpr (kGroups > 1) {
+    sums[grp][d] = sum;
+    if (d == 0) {
+      ms[grp] = mm;
+      ls[grp] = ll;
+    }
+    __syncthreads();
+    if (grp != 0) return;
+    mm = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k) mm = fmaxf(mm, ms[k]);
+    sum = ll = 0.f;
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k) {
+      const float f = mm == -INFINITY ? 1.f : ex2(ms[k] - mm);
+      sum = fmaf(f, sums[k][d], sum);
+      ll = fmaf(f, ls[k], ll);
+    }
   }
   o[(seq.row0 + row / G) * o_stride + (h * G + row % G) * HD + d] = narrow<T>(ll == 0.f ? sum : sum / ll);
 }
@@ -550,8 +573,12 @@ szo_status launch_rows(const View& V, const Rows& A, int nsplit, float* ws, cuda
 }
 
 // How the positions are cut: blocks of 4 warps, three per SM, joined in clusters of up to 16, or (`wide`) of 12, one per SM,
-// joined by the second launch.  A cut stops at one unit per warp of what the page table could hold (the lengths are on
-// the device).
+// joined by the second launch.  The lengths are on the device, so the rule goes by the number of (sequence, head, row tile)
+// items alone: as many blocks as stay at two per SM; a second, partial round of blocks costs more than the idle third (8
+// sequences of 4096 positions and 8 heads: clusters of 4 / 8 16.5 / 22.6 us; 16 sequences: 2 / 4 30.6 / 40.1).  Between one
+// and two items per SM one block per item is best for equal lengths and worst for unequal ones, clusters of 3 near the best
+// for both (32 sequences, 8 heads, 1 / 2 / 3 blocks: 4096 positions each 48 / 69 / 57 us, 513 to 8192 67 / 56 / 59 us).
+// A cut stops at one unit per warp of what the page table could hold.
 struct Plan {
   int rows, nsplit;
   bool wide;
@@ -561,12 +588,13 @@ Plan plan(const View& V, int H) {
   Plan p{rows <= 8 ? 8 : 16, 1, false};
   const int64_t items = ceil_div(rows, p.rows) * V.batch * V.hkv;
   const int64_t units = ceil_div(static_cast<int64_t>(V.max_pages) << V.page_shift, kUnit);
-  if (p.rows == 8 && items * 16 <= 148 * 2 && units >= 12 * 16 * 2) {
+  if (p.rows == 8 && items * 16 <= 148 * 2 && units >= kWideUnits) {
     p.wide = true;
     p.nsplit = static_cast<int>(148 / items);
     return p;
   }
-  while (p.nsplit < 16 && items * p.nsplit < 148 * 2 && units >= 2 * p.nsplit * 4) p.nsplit *= 2;
+  while (p.nsplit < 16 && items * p.nsplit * 2 <= 148 * 2 && units >= 2 * p.nsplit * 4) p.nsplit *= 2;
+  if (p.nsplit == 1 && items > 148 && items <= 148 * 2 && units >= 3 * 4) p.nsplit = 3;
   return p;
 }
 
@@ -595,8 +623,12 @@ template <typename T, int HD>
 szo_status launch_join(const View& V, const Rows& A, const float* ws, int R, int row_tiles, int nsplit, bool long_first, int64_t item0,
                        int64_t n_items, cudaStream_t st) {
   SZO_REQUIRE(n_items * R <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows for one launch");
-  SZO_CHECK_CUDA(launch_maybe_chained(kv8_join_kernel<T, HD>, dim3(static_cast<unsigned>(n_items * R)), dim3(HD), 0, st, true, V, ws,
-                                      static_cast<T*>(A.o), A.o_stride, A.H, R, row_tiles, nsplit, long_first, static_cast<unsigned>(item0)));
+  const dim3 grid(static_cast<unsigned>(n_items * R));
+  auto run = [&](auto kern, int threads) {
+    return launch_maybe_chained(kern, grid, dim3(threads), 0, st, true, V, ws, static_cast<T*>(A.o), A.o_stride, A.H, R, row_tiles, nsplit, long_first,
+                                static_cast<unsigned>(item0));
+  };
+  SZO_CHECK_CUDA(nsplit > 8 ? run(kv8_join_kernel<T, HD, 8>, 8 * HD) : run(kv8_join_kernel<T, HD, 1>, HD));
   count_launch();
   return SZO_OK;
 }

@@ -76,7 +76,7 @@ def test_attention_workspace(B):
     c_, b_ = _cache(B, n_pages=10000), _batch(B, max_pages=8192, batch=1, rows=1)
     c, b = C.addressof(c_), C.addressof(b_)
     need = L.szo_attention_kv8_workspace_bytes(c, b, 4)
-    assert 0 < need < 1 << 20
+    assert 0 < need < 20 << 20
     a = L.szo_attention_kv8
     assert a(c, b, 16, 256, 16, 256, 1, 4, 0.125, None, need, None) == -5
     assert a(c, b, 16, 256, 16, 256, 1, 4, 0.125, 16, need - 1, None) == -5
