@@ -166,22 +166,22 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
 #pragma unroll
     for (int i = 0; i < HD / 16; ++i) acc[n][i][0] = acc[n][i][1] = acc[n][i][2] = acc[n][i][3] = 0.f;
   }
-  // Rows (of the tensor maps) and scales of 32 steps (16 units) at a time, one step per lane, loaded a chunk ahead
+  // Rows (of the tensor maps) and scales of 32 steps (16 units) at a time, one step per lane: table entries are loaded two
+  // chunks ahead, scales one, so that nothing waits for either
   struct Meta {
     int row;                                                      // -1: no page, or behind this warp's share
-    float ks, fe;                                                 // 2^(keys' exponent), the values' exponent; without a page -inf
+    float2 sc;                                                    // as stored
   };
-  auto load_meta = [&](int s) {
-    Meta r{-1, 0.f, -INFINITY};
-    s += lane;
-    if (s < 2 * u_hi && s < steps) {
-      const int page = load_page(V, b, s >> (V.page_shift - 4));
-      if (page >= 0) {
-        const float2 sc = V.scales[static_cast<int64_t>(page) * V.hkv + h];
-        r.row = ((page * V.hkv + h) << V.page_shift) + ((s << 4) & ((1 << V.page_shift) - 1));
-        r.ks = exp2_int(scale_exponent(sc.x));
-        r.fe = static_cast<float>(scale_exponent(sc.y));
-      }
+  const int32_t* table = V.table + static_cast<int64_t>(b) * V.max_pages;
+  const int s_end = min(2 * u_hi, steps);
+  auto load_entry = [&](int s) { return s + lane < s_end ? __ldg(table + ((s + lane) >> (V.page_shift - 4))) : -2; };
+  auto load_meta = [&](int entry, int s) {
+    Meta r{-1, make_float2(0.f, 0.f)};
+    if (static_cast<uint32_t>(entry) < static_cast<uint64_t>(V.n_pages)) {
+      r.row = ((entry * V.hkv + h) << V.page_shift) + (((s + lane) << 4) & ((1 << V.page_shift) - 1));
+      r.sc = __ldg(V.scales + static_cast<int64_t>(entry) * V.hkv + h);
+    } else if (entry != -2) {
+      report_page(V);
     }
     return r;
   };
@@ -195,13 +195,20 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     if (lane < 4 && row >= 0)
       tc::tma_load_2d(ring + slot * kUnit * HD * 2 + lane * kStep * HD, lane < 2 ? &map_k : &map_v, 0, row, bar);
   };
-  Meta mc = load_meta(2 * u_lo);
+  int entry = load_entry(2 * u_lo), entry_n = load_entry(2 * u_lo + 32);
+  Meta mc = load_meta(entry, 2 * u_lo);
 #pragma unroll
   for (int i = 0; i < kDepth; ++i) {
     const int row = __shfl_sync(0xffffffffu, mc.row, 2 * i + (lane & 1));
     if (u_lo + i < u_hi) issue(i, row);
   }
-  Meta mn = load_meta(2 * u_lo + 32);
+  Meta mn = load_meta(entry_n, 2 * u_lo + 32);
+  entry_n = load_entry(2 * u_lo + 64);
+  float ks_c, fe_c;                                               // this chunk's: 2^(keys' exponent), the values' exponent; no page: -inf
+  auto take_scales = [&]() {
+    ks_c = exp2_int(scale_exponent(mc.sc.x));
+    fe_c = mc.row >= 0 ? static_cast<float>(scale_exponent(mc.sc.y)) : -INFINITY;
+  };
   // queries: the B fragments of k-step i are row g's dims (HD / 4) t + 4 i .. + 3
   uint32_t qa[NT][kK][2], qb[kSplit ? NT : 1][kK][2];
   float rs[NT][2];
@@ -251,6 +258,7 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   }
   __syncthreads();
 
+  take_scales();
   int slot = 0;
   uint32_t phase = 0;
   for (int u = u_lo; u < u_hi; ++u) {
@@ -259,8 +267,8 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     float ks[2], fe[2], el[2];
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
-      ks[a] = __shfl_sync(0xffffffffu, mc.ks, i + a);
-      fe[a] = __shfl_sync(0xffffffffu, mc.fe, i + a);
+      ks[a] = __shfl_sync(0xffffffffu, ks_c, i + a);
+      fe[a] = __shfl_sync(0xffffffffu, fe_c, i + a);
       have[a] = fe[a] != -INFINITY;
       el[a] = have[a] ? exp2_int(-static_cast<int>(fe[a])) : 0.f;
     }
@@ -383,7 +391,9 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     if (u + kDepth < u_hi) issue(slot, i3 < 32 ? rc : rn);
     if (i == 30) {
       mc = mn;
-      mn = load_meta(2 * u + 34);
+      take_scales();
+      mn = load_meta(entry_n, 2 * u + 34);
+      entry_n = load_entry(2 * u + 66);
     }
     if (++slot == kDepth) {
       slot = 0;
