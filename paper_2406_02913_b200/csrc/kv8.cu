@@ -54,9 +54,46 @@ template <typename T, int HD> struct Slots {
   static constexpr int kN = Vec<T>::kN, kLR = HD / kN, kRows = 32 / kLR, kLoads = 16 / kRows;
 };
 
+// Bits of |x| of both 16-bit halves
+__device__ __forceinline__ uint32_t magnitudes(uint32_t w) { return w & 0x7fff7fffu; }
+// Largest magnitude of a vector: of the finite elements within the format's range, and whether there are others.  For 16-bit
+// types the order of magnitudes is that of their bits, two at a time.
+__device__ __forceinline__ float largest(const Vec<float>& v, bool& others) {
+  float a = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float m = fabsf(v.x[i]);
+    others = others || !(m <= kLargest);
+    a = fmaxf(a, m <= kLargest ? m : 0.f);
+  }
+  return a;
+}
+template <typename T> __device__ __forceinline__ float largest(const Vec<T>& v, bool& others) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(v.x);
+  const uint32_t m = __vmaxu2(__vmaxu2(magnitudes(w[0]), magnitudes(w[1])), __vmaxu2(magnitudes(w[2]), magnitudes(w[3])));
+  const uint16_t top = static_cast<uint16_t>(max(m & 0xffffu, m >> 16));
+  const float a = widen<T>(*reinterpret_cast<const T*>(&top));
+  if (a <= kLargest) return a;
+  others = true;
+  float b = 0.f;
+#pragma unroll
+  for (int i = 0; i < Vec<T>::kN; ++i) {
+    const float x = fabsf(widen<T>(v.x[i]));
+    b = fmaxf(b, x <= kLargest ? x : 0.f);
+  }
+  return b;
+}
+// Elements 2 i, 2 i + 1 in fp32
+__device__ __forceinline__ float2 widen2(const Vec<float>& v, int i) { return make_float2(v.x[2 * i], v.x[2 * i + 1]); }
+__device__ __forceinline__ float2 widen2(const Vec<__half>& v, int i) { return __half22float2(reinterpret_cast<const __half2*>(v.x)[i]); }
+__device__ __forceinline__ float2 widen2(const Vec<__nv_bfloat16>& v, int i) {
+  const uint32_t w = reinterpret_cast<const uint32_t*>(v.x)[i];
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
 // Block = (touched page, head, sequence); warps 2 i and 2 i + 1 take slots [16 i, 16 i + 16) of keys and values.
 template <typename T, int HD>
-__global__ void __launch_bounds__(512)
+__global__ void __launch_bounds__(512, sizeof(T) == 2 ? 2 : 1)
 kv8_write_kernel(View V, const T* __restrict__ k, const T* __restrict__ v, int64_t k_stride, int64_t v_stride, int per_seq) {
   using S = Slots<T, HD>;
   __shared__ float amax[2][8];
@@ -80,19 +117,16 @@ kv8_write_kernel(View V, const T* __restrict__ k, const T* __restrict__ v, int64
 
   const int r0 = sub * 16 + lane / S::kLR, c0 = lane % S::kLR * S::kN;
   Vec<T> x[S::kLoads];
-  float a = 0.f;
 #pragma unroll
   for (int i = 0; i < S::kLoads; ++i) {
     const int pos = base + r0 + i * S::kRows;
-    if (pos >= pos0 && pos < seq.len) {
-      x[i] = *reinterpret_cast<const Vec<T>*>(rows + pos * stride + c0);
-#pragma unroll
-      for (int u = 0; u < S::kN; ++u) {
-        const float m = fabsf(widen<T>(x[i].x[u]));
-        a = fmaxf(a, m <= kLargest ? m : 0.f);                    // non-finite elements do not set the scale
-      }
-    }
+    x[i] = Vec<T>{};
+    if (pos >= pos0 && pos < seq.len) x[i] = *reinterpret_cast<const Vec<T>*>(rows + pos * stride + c0);
   }
+  float a = 0.f;
+  bool others = false;                                            // elements that are not finite, or too large: they do not set the scale
+#pragma unroll
+  for (int i = 0; i < S::kLoads; ++i) a = fmaxf(a, largest(x[i], others));
 #pragma unroll
   for (int o = 16; o; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
   if (lane == 0) amax[which][sub] = a;
@@ -111,13 +145,13 @@ kv8_write_kernel(View V, const T* __restrict__ k, const T* __restrict__ v, int64
     if (pos >= pos0 && pos < seq.len) {
 #pragma unroll
       for (int u = 0; u < S::kN; u += 4) {
-        float f[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const float y = widen<T>(x[i].x[u + t]);
-          f[t] = fabsf(y) <= kLargest ? y * inv : __int_as_float(0x7fffffff);
+        float2 lo = widen2(x[i], u / 2), hi = widen2(x[i], u / 2 + 1);
+        if (others) {
+          const float nan = __int_as_float(0x7fffffff);
+          lo = make_float2(fabsf(lo.x) <= kLargest ? lo.x : nan, fabsf(lo.y) <= kLargest ? lo.y : nan);
+          hi = make_float2(fabsf(hi.x) <= kLargest ? hi.x : nan, fabsf(hi.y) <= kLargest ? hi.y : nan);
         }
-        out[u / 4] = encode2(f[0], f[1]) | encode2(f[2], f[3]) << 16;
+        out[u / 4] = encode2(lo.x * inv, lo.y * inv) | encode2(hi.x * inv, hi.y * inv) << 16;
       }
     } else if (rescale && pos < pos0) {
 #pragma unroll
@@ -161,22 +195,26 @@ kv8_read_kernel(View V, T* __restrict__ k, T* __restrict__ v, int64_t k_stride, 
   const uint8_t* codes = (which ? V.v : V.k) + page_offset(V, page < 0 ? 0 : page, h, HD);
   const float2 sc = V.scales[static_cast<int64_t>(page < 0 ? 0 : page) * V.hkv + h];
   const float scale = exp2_int(scale_exponent(which ? sc.y : sc.x));
+  uint32_t word[S::kLoads][S::kN / 4];
+#pragma unroll
+  for (int i = 0; i < S::kLoads; ++i) {                           // (all loads first; a page is whole, so slots behind the last position may be read)
+    const uint8_t* p = codes + (r0 + i * S::kRows) * HD + c0;
+    if constexpr (S::kN == 8) {
+      const uint2 t = *reinterpret_cast<const uint2*>(p);
+      word[i][0] = t.x;
+      word[i][1] = t.y;
+    } else {
+      word[i][0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+  }
 #pragma unroll
   for (int i = 0; i < S::kLoads; ++i) {
-    const int slot = r0 + i * S::kRows, pos = base + slot;
+    const int pos = base + r0 + i * S::kRows;
     if (pos < first || pos >= seq.len) continue;
     Vec<T> out;
-    uint32_t word[S::kN / 4];
-    if constexpr (S::kN == 8) {
-      const uint2 t = *reinterpret_cast<const uint2*>(codes + slot * HD + c0);
-      word[0] = t.x;
-      word[1] = t.y;
-    } else {
-      word[0] = *reinterpret_cast<const uint32_t*>(codes + slot * HD + c0);
-    }
 #pragma unroll
     for (int u = 0; u < S::kN; u += 4) {
-      const float2 lo = decode2f(word[u / 4]), hi = decode2f(word[u / 4] >> 16);
+      const float2 lo = decode2f(word[i][u / 4]), hi = decode2f(word[i][u / 4] >> 16);
       out.x[u] = narrow<T>(lo.x * scale);
       out.x[u + 1] = narrow<T>(lo.y * scale);
       out.x[u + 2] = narrow<T>(hi.x * scale);
