@@ -8,12 +8,13 @@
 // adds per step), with three more close behind it: the exponentials (16 per cycle and SM: as long as the products),
 // shared memory (operands of the products and the converted tiles, 128 bytes per cycle) and the issue slots of the
 // softmax.  Hence the split into warps that only meet at mbarriers:
-//   warps 0-3, 4-7   softmax of row tile 0 and 1, one row per thread (a TMEM lane): no shuffles.  While one tile's weights
-//                    are formed, the tensor cores work for the other
-//   warps 8-11       bring the e4m3 codes of the next 128 positions from global memory to registers, turn them into fp16
-//                    (exact) and store them in the swizzled layout that the products read.  Through registers and not by
-//                    TMA: a staged copy would cost another pass of shared memory each way
-//   warp 12          one thread issues every product
+//   warps 0-7, 8-15  softmax of row tile 0 and 1, two threads per row (a TMEM lane), 64 columns each: no shuffles, one
+//                    exchange of maxima per step.  While one tile's weights are formed, the tensor cores work for the other
+//   warps 16-19      turn the e4m3 codes into fp16 (exact) and store them in the swizzled layout that the products read
+//   warp 20          one thread issues every product
+//   warp 21          brings the codes by TMA, 64 positions of keys or values per slot of a small ring, and the pages' scales
+//                    (with the converting warps loading for themselves the latency of a step's loads showed: they have
+//                    no registers for a second set)
 // Numbers are those of the kernel for few rows: queries divided by a power of two per row, weights relative to each
 // token's contribution (logit + exponent of its page's value scale), sums of weights divided by that scale again.
 // The reference maximum follows the running maximum once that is 2^8 above it, so O is rescaled in TMEM a few times
@@ -29,7 +30,8 @@ namespace kv8 {
 namespace {
 
 constexpr int kTile = 128;                     // rows of a row tile, positions of a step
-constexpr int kConv = 4, kMmaWarp = 8 + kConv, kTcThreads = (kMmaWarp + 1) * 32;      // (13 warps: 128 registers per thread)
+constexpr int kSoft = 16, kConv = 4, kMmaWarp = kSoft + kConv, kLoadWarp = kMmaWarp + 1, kTcThreads = (kLoadWarp + 1) * 32;      // (22 warps: 80 registers)
+constexpr int kRawTokens = 64, kRawSlots = 3;  // ring of codes as they come: half a step of keys or values per slot
 constexpr float kTcOffset = 7.0f, kTcSlack = 8.0f;
 constexpr float kTiny = 1e-37f;                // factors of scores are kept above it: a zero would make NaN of a masked -inf
 constexpr uint32_t kTmemCols = 512;
@@ -134,6 +136,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 __device__ __forceinline__ uint32_t tile_chunk(uint32_t base, int row, int chunk) {      // 16-byte chunk (8 columns) of a row
   return base + (chunk >> 3) * (kTile * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
 }
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
+  uint4 r;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a) : "memory");
+  return r;
+}
 __device__ __forceinline__ void sts16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
@@ -156,9 +163,9 @@ struct TcSplit {
 
 template <typename T, int HD>
 __global__ void __launch_bounds__(kTcThreads, 1)
-kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __restrict__ o, int64_t o_stride, int H, float scale, int row_tiles, TcSplit part, float* __restrict__ ws) {
+kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, View V, const T* __restrict__ q, int64_t q_stride, T* __restrict__ o, int64_t o_stride, int H, float scale, int row_tiles, TcSplit part, float* __restrict__ ws) {
   constexpr int kBytes = kTile * HD * 2;                          // of an operand tile
-  constexpr int kLanes = HD / 16, kRowsPass = kConv * 32 / kLanes, kPass = kTile / kRowsPass;
+  constexpr int kLanes = HD / 16, kRowsPass = kConv * 32 / kLanes;
   extern __shared__ __align__(1024) unsigned char smem_tc[];
   struct alignas(16) Step {
     float ks, fe, el;                                             // 2^(keys' exponent), values' exponent, its inverse power; no page: 1, -inf, 0
@@ -166,7 +173,8 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
   };
   __shared__ Step meta[4][kTile / kStep];
   __shared__ int nan_at[HD];
-  __shared__ __align__(8) uint64_t bars[20];
+  __shared__ float peaks[2][2][2][kTile];                         // [step parity][row tile][half][row]; in the end sums of weights
+  __shared__ __align__(8) uint64_t bars[20 + 2 * kRawSlots];
   __shared__ uint32_t tmem_ptr;
   __shared__ int abort_flag;
 
@@ -203,22 +211,27 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
   auto v_tile = [&](int s) { return base + s * kBytes; };
   auto k_tile = [&](int s) { return base + (2 + s) * kBytes; };
   auto q_tile = [&](int i) { return base + (4 + i) * kBytes; };
+  auto raw_slot = [&](int s) { return base + 6 * kBytes + s * kRawTokens * HD; };
   auto bar = [&](int i) { return tc::smem_u32(&bars[i]); };
-  const int kSFull = 0, kPFull = 2, kODone = 4, kKFull = 6, kKEmpty = 8, kVFull = 10, kVEmpty = 12, kQFull = 14, kDrain = 15, kMeta = 16;
+  const int kSFull = 0, kPFull = 2, kODone = 4, kKFull = 6, kKEmpty = 8, kVFull = 10, kVEmpty = 12, kQFull = 14, kDrain = 15, kMeta = 16, kRawFull = 20, kRawEmpty = 20 + kRawSlots;
   if (tid == 0) {
     abort_flag = 0;
     for (int i = 0; i < 2; ++i) {
       tc::mbar_init(bar(kSFull + i), 1);
-      tc::mbar_init(bar(kPFull + i), 4);
+      tc::mbar_init(bar(kPFull + i), kSoft / 2);
       tc::mbar_init(bar(kODone + i), 1);
       tc::mbar_init(bar(kKFull + i), kConv);
       tc::mbar_init(bar(kKEmpty + i), 1);
       tc::mbar_init(bar(kVFull + i), kConv);
       tc::mbar_init(bar(kVEmpty + i), 1);
     }
-    tc::mbar_init(bar(kQFull), 8);
+    tc::mbar_init(bar(kQFull), kSoft);
     tc::mbar_init(bar(kDrain), 1);
     for (int i = 0; i < 4; ++i) tc::mbar_init(bar(kMeta + i), 1);
+    for (int i = 0; i < kRawSlots; ++i) {
+      tc::mbar_init(bar(kRawFull + i), 1);
+      tc::mbar_init(bar(kRawEmpty + i), kConv);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   for (int i = tid; i < HD; i += kTcThreads) nan_at[i] = 0x7fffffff;
@@ -230,11 +243,11 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
   auto wait = [&](int i, int phase, unsigned backoff) { return tc::mbar_wait(bar(i), phase & 1, &abort_flag, V.status, backoff); };
   auto wait_warp = [&](int i, int phase, unsigned backoff) { return __all_sync(0xffffffffu, wait(i, phase, backoff)) != 0; };
 
-  if (warp < 8) {
-    // ------------------------------------------------------------------ softmax: thread = row
-    const int i = warp >> 2, r = tid;                             // row tile, row of the block
+  if (warp < kSoft) {
+    // ------------------------------------------------------------------ softmax: two threads per row, 64 columns each
+    const int i = warp >> 3, half = (warp >> 2) & 1, rr = (warp & 3) * 32 + lane, r = i * kTile + rr;      // row tile, columns, row of it, of the block
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_addr = tmem + lanes + i * kTile, o_addr = tmem + lanes + 2 * kTile + i * kTile;
+    const uint32_t s_addr = tmem + lanes + i * kTile + half * (kTile / 2), o_addr = tmem + lanes + 2 * kTile + i * kTile + half * (HD / 2);
     const int rpos = pos_of(r < n_rows ? r : n_rows - 1);         // (rows that are not there: anything, they are not stored)
     const int64_t q_off = (seq.row0 + (r0 + r) / G), head = h * G + (r0 + r) % G;
     float rs, poison;
@@ -259,41 +272,45 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
       rs = exp2_int(e) * (fabsf(scale) * 1.4426950408889634f);
       poison = fine ? 0.f : __int_as_float(0x7fffffff);           // a row that holds NaN or an infinity is NaN
 #pragma unroll 4
-      for (int c = 0; c < HD / 8; ++c) {
+      for (int c = half * (HD / 16); c < (half + 1) * (HD / 16); ++c) {
         Vec<T> x = {};
         if (r < n_rows) x = *reinterpret_cast<const Vec<T>*>(qp + 8 * c);
         uint32_t p[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) p[u] = pack_f16(widen<T>(x.x[2 * u]) * inv, widen<T>(x.x[2 * u + 1]) * inv);
-        sts16(tile_chunk(q_tile(i), r & (kTile - 1), c), p[0], p[1], p[2], p[3]);
+        sts16(tile_chunk(q_tile(i), rr, c), p[0], p[1], p[2], p[3]);
       }
       tc::fence_async_smem();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(bar(kQFull));
     }
     float m = -INFINITY, l = 0.f;
-    bool ok = true;
-    for (int j = 0; j < n_kv[i] && ok; ++j) {
-      if (!(ok = wait_warp(kMeta + (j & 3), j >> 2, 20) && wait_warp(kSFull + i, j, 20))) break;
+    // (a wait that gave up changes nothing here: every warp of a row tile meets the others as often, whatever it read)
+    for (int j = 0; j < n_kv[i]; ++j) {
+      wait_warp(kMeta + (j & 3), j >> 2, 20);
+      wait_warp(kSFull + i, j, 20);
       tc::tc_fence_after();
-      const Step* st = meta[j & 3];
-      const int limit = rpos - p0 - j * kTile;                         // columns up to this one are seen
-      const bool masked = p0 + j * kTile + kTile - 1 > lo[i];
-      uint32_t va[32], vb[32];
-      if (masked) {                                               // what a row does not see becomes -inf in S itself: one form of the rest
+      const Step* st = &meta[j & 3][half * (kTile / kStep / 2)];
+      const int limit = rpos - p0 - j * kTile - half * (kTile / 2);       // columns up to this one are seen
+      uint32_t v[32];
+      if (p0 + j * kTile + kTile - 1 > lo[i]) {                   // what a row does not see becomes -inf in S itself: one form of the rest
 #pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
-          tmem_load32(s_addr + 32 * c, va);
-          tmem_load_wait(va);
+        for (int c = 0; c < 2; ++c) {
+          tmem_load32(s_addr + 32 * c, v);
+          tmem_load_wait(v);
 #pragma unroll
           for (int u = 0; u < 32; ++u)
-            if (32 * c + u > limit) va[u] = 0xff800000u;
-          tmem_store32(s_addr + 32 * c, va);
+            if (32 * c + u > limit) v[u] = 0xff800000u;
+          tmem_store32(s_addr + 32 * c, v);
         }
         tmem_store_wait();
       }
+      // (loops and not copies, here and below: instruction fetch is what straight code would wait for)
       float mx = -INFINITY;
-      auto peak = [&](const uint32_t(&v)[32], int c) {
+#pragma unroll 1
+      for (int c = 0; c < 2; ++c) {
+        tmem_load32(s_addr + 32 * c, v);
+        tmem_load_wait(v);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
           const float2 kf = *reinterpret_cast<const float2*>(&st[2 * c + s]);
@@ -305,39 +322,34 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
           t[0] = fmaxf(max3(t[0], t[1], t[2]), t[3]);
           mx = fmaxf(mx, fmaf(t[0], fmaxf(rs * kf.x, kTiny), kf.y));
         }
-      };
-      // (loops and not four copies, here and below: instruction fetch is what straight code would wait for)
-      tmem_load32(s_addr, va);
-#pragma unroll 1
-      for (int c = 0; c < 4; c += 2) {
-        tmem_load_wait(va);
-        tmem_load32(s_addr + 32 * (c + 1), vb);
-        peak(va, c);
-        tmem_load_wait(vb);
-        tmem_load32(s_addr + 32 * ((c + 2) & 3), va);             // (the last one: chunk 0 again, for the weights)
-        peak(vb, c + 1);
       }
+      // the row's other half
+      peaks[j & 1][i][half][rr] = mx;
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + i), "r"(kSoft / 2 * 32) : "memory");
+      mx = fmaxf(mx, peaks[j & 1][i][half ^ 1][rr]);
       const bool need = mx > m + kTcSlack || (m == -INFINITY && mx > -INFINITY);
       if (__any_sync(0xffffffffu, need)) {
         const float m_new = need ? mx : m, corr = need ? ex2(m - m_new) : 1.f;       // (mx > m there; ex2(-inf) = 0)
         if (j > 0) {
-          tmem_load_wait(va);
-          if (!(ok = wait_warp(kODone + i, j - 1, 0))) break;
+          wait_warp(kODone + i, j - 1, 0);
           tc::tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < HD / 64; ++c) {
+            tmem_load32(o_addr + 32 * c, v);
+            tmem_load_wait(v);
 #pragma unroll
-          for (int c = 0; c < HD / 32; ++c) {
-            tmem_load32(o_addr + 32 * c, vb);
-            tmem_load_wait(vb);
-#pragma unroll
-            for (int u = 0; u < 32; ++u) vb[u] = __float_as_uint(__uint_as_float(vb[u]) * corr);
-            tmem_store32(o_addr + 32 * c, vb);
+            for (int u = 0; u < 32; ++u) v[u] = __float_as_uint(__uint_as_float(v[u]) * corr);
+            tmem_store32(o_addr + 32 * c, v);
           }
           l *= corr;
         }
         m = m_new;
       }
       const float ref = (m == -INFINITY ? 0.f : m) - kTcOffset + poison;
-      auto weigh = [&](const uint32_t(&v)[32], int c) {
+#pragma unroll 1
+      for (int c = 0; c < 2; ++c) {
+        tmem_load32(s_addr + 32 * c, v);
+        tmem_load_wait(v);
         uint32_t p[16];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -356,29 +368,24 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
           l = fmaf(x.z, t.x + t.y, l);
         }
         tmem_store16(s_addr + 16 * c, p);                         // over columns that this thread has read
-      };
-#pragma unroll 1
-      for (int c = 0; c < 4; c += 2) {
-        tmem_load_wait(va);
-        tmem_load32(s_addr + 32 * (c + 1), vb);
-        weigh(va, c);
-        tmem_load_wait(vb);
-        if (c == 0) tmem_load32(s_addr + 64, va);
-        weigh(vb, c + 1);
       }
       tmem_store_wait();
       tc::tc_fence_before();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(bar(kPFull + i));
     }
-    if (ok && n_kv[i] > 0) wait_warp(kODone + i, n_kv[i] - 1, 20);
+    if (n_kv[i] > 0) wait_warp(kODone + i, n_kv[i] - 1, 20);
     __syncthreads();                                              // (nan_at is complete; see the other warps' ends)
+    peaks[0][i][half][rr] = l;
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + i), "r"(kSoft / 2 * 32) : "memory");
+    l = peaks[0][i][0][rr] + peaks[0][i][1][rr];
     tc::tc_fence_after();
-    T* op = o + q_off * o_stride + head * HD;
+    const int d0 = half * (HD / 2);                               // this thread's share of the row's dims
+    T* op = o + q_off * o_stride + head * HD + d0;
     float* wp = ws + static_cast<int64_t>(blockIdx.x - part.whole) * (2 * kTile * (HD + 2));       // (a share's: sums, maxima, sums of weights)
     const float inv = cut ? 1.f : l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll 1
-    for (int c = 0; c < HD / 32; ++c) {
+    for (int c = 0; c < HD / 64; ++c) {
       uint32_t v[32];
       if (n_kv[i] > 0) {
         tmem_load32(o_addr + 32 * c, v);
@@ -388,11 +395,12 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
 #pragma unroll
       for (int u = 0; u < 32; ++u) {
         v[u] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(v[u]) * inv);      // nothing attended to: zeros
-        if (rpos >= nan_at[32 * c + u]) v[u] = 0x7fffffffu;
+        if (rpos >= nan_at[d0 + 32 * c + u]) v[u] = 0x7fffffffu;
       }
       if (cut) {
 #pragma unroll
-        for (int u = 0; u < 32; u += 4) *reinterpret_cast<uint4*>(wp + r * HD + 32 * c + u) = make_uint4(v[u], v[u + 1], v[u + 2], v[u + 3]);
+        for (int u = 0; u < 32; u += 4)
+          *reinterpret_cast<uint4*>(wp + r * HD + d0 + 32 * c + u) = make_uint4(v[u], v[u + 1], v[u + 2], v[u + 3]);
         continue;
       }
 #pragma unroll
@@ -403,100 +411,120 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
         *reinterpret_cast<Vec<T>*>(op + 32 * c + u) = x;
       }
     }
-    if (cut && r < n_rows) {
+    if (cut && r < n_rows && half == 0) {
       wp[2 * kTile * HD + r] = m;
       wp[2 * kTile * (HD + 1) + r] = l;
     }
     tc::tc_fence_before();
   } else if (warp < kMmaWarp) {
     // ------------------------------------------------------------------ codes to fp16 operand tiles
-    const int w = warp - 8, piece = lane % kLanes, row_a = w * (32 / kLanes) + lane / kLanes;
-    uint4 kr[kPass], vr[kPass];
-    // Lane s < 8 keeps the page of the s-th 16 positions: the table's entry two steps ahead, the row in k and v (-1: no page)
-    // and, in the first warp, the scales one step ahead
+    const int w = warp - kSoft, piece = lane % kLanes, row_a = w * (32 / kLanes) + lane / kLanes;
+    // (kRowsPass is a multiple of 8: every pass is the same place of the swizzle, kRowsPass rows further)
+    static_assert(kRowsPass % 8 == 0 && kRawTokens % kRowsPass == 0, "");
+    const bool other = (piece & 4) != 0;                          // the second block's lanes store in the other order: no bank is hit twice
+    const uint32_t place0 = tile_chunk(0, row_a, 2 * piece + (other ? 1 : 0)), place1 = tile_chunk(0, row_a, 2 * piece + (other ? 0 : 1));
+    int raw = 0;
+    uint32_t raw_phase = 0;
+    // a tile of step j, a slot of the ring after the other
+    auto convert = [&](uint32_t tile, int j, bool values) {
+      const bool partial = values && p0 + j * kTile + kTile - 1 > lo[0];
+#pragma unroll 1
+      for (int hf = 0; hf < kTile / kRawTokens; ++hf) {
+        if (!wait_warp(kRawFull + raw, raw_phase, 20)) return false;
+        const uint32_t src = raw_slot(raw) + row_a * HD + 16 * piece, dst = tile + hf * kRawTokens * 128;
+#pragma unroll
+        for (int p = 0; p < kRawTokens / kRowsPass; ++p) {
+          uint4 x = lds16(src + p * kRowsPass * HD);
+          const int row = hf * kRawTokens + p * kRowsPass + row_a;
+          if (meta[j & 3][row / kStep].fe == -INFINITY) x = make_uint4(0u, 0u, 0u, 0u);         // no page: the slot holds leftovers
+          if (partial) {
+            // 0 * NaN: where rows do not see the whole step a NaN value is taken out, and the rows that do see it are set to NaN
+            // at the end
+            uint32_t* y = reinterpret_cast<uint32_t*>(&x);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint32_t bad = ((y[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+              y[k] &= ~((bad >> 7) * 0xffu);
+              while (bad) {
+                const int byte = (__ffs(bad) - 1) >> 3;
+                bad &= bad - 1;
+                atomicMin(nan_at + 16 * piece + 4 * k + byte, p0 + j * kTile + row);
+              }
+            }
+          }
+          const uint32_t w0 = other ? x.z : x.x, w1 = other ? x.w : x.y, w2 = other ? x.x : x.z, w3 = other ? x.y : x.w;
+          sts16(dst + place0 + p * kRowsPass * 128, decode2(w0), decode2(w0 >> 16), decode2(w1), decode2(w1 >> 16));
+          sts16(dst + place1 + p * kRowsPass * 128, decode2(w2), decode2(w2 >> 16), decode2(w3), decode2(w3 >> 16));
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(bar(kRawEmpty + raw));
+        if (++raw == kRawSlots) {
+          raw = 0;
+          raw_phase ^= 1;
+        }
+      }
+      tc::fence_async_smem();
+      __syncwarp();
+      return true;
+    };
+    for (int j = 0; j < n; ++j) {
+      const int s = j & 1;
+      if (j >= 2 && !wait_warp(kKEmpty + s, (j >> 1) - 1, 20)) break;
+      if (!convert(k_tile(s), j, false)) break;
+      if (lane == 0) tc::mbar_arrive(bar(kKFull + s));
+      if (j >= 2 && !wait_warp(kVEmpty + s, (j >> 1) - 1, 20)) break;
+      if (!convert(v_tile(s), j, true)) break;
+      if (lane == 0) tc::mbar_arrive(bar(kVFull + s));
+    }
+    __syncthreads();
+  } else if (warp == kLoadWarp) {
+    // ------------------------------------------------------------------ codes and scales from global memory
+    // Lane s < 8 keeps the page of the s-th 16 positions of a step: the table's entry two steps ahead, its row in the tensor
+    // maps (-1: no page) and its scales one step ahead
     const int32_t* table = V.table + static_cast<int64_t>(b) * V.max_pages;
-    const bool scaler = w == 0 && lane < kTile / kStep;
-    int entry = -1, place = -1;
-    float2 sc = make_float2(0.f, 0.f);
     auto load_entry = [&](int j) {
       const int step = (j0 + j) * (kTile / kStep) + lane;
-      entry = lane < kTile / kStep && step < n_steps ? __ldg(table + (step >> (V.page_shift - 4))) : -2;
+      return lane < kTile / kStep && step < n_steps ? __ldg(table + (step >> (V.page_shift - 4))) : -2;
     };
+    int entry = load_entry(0), place = -1, raw = 0;
+    uint32_t raw_phase = 1;
+    float2 sc = make_float2(0.f, 0.f);
     auto take_entry = [&](int j) {
       const bool there = static_cast<uint32_t>(entry) < static_cast<uint64_t>(V.n_pages);
       if (entry != -2 && !there) report_page(V);
       place = there ? ((entry * V.hkv + h) << V.page_shift) + ((p0 + j * kTile + lane * kStep) & ((1 << V.page_shift) - 1)) : -1;
-      if (scaler && there) sc = __ldg(V.scales + static_cast<int64_t>(entry) * V.hkv + h);
+      if (there) sc = __ldg(V.scales + static_cast<int64_t>(entry) * V.hkv + h);
     };
-    auto fetch = [&](uint4(&x)[kPass], const uint8_t* codes) {
-      const uint8_t* mine = codes + (row_a % kStep) * HD + 16 * piece;
-#pragma unroll
-      for (int p = 0; p < kPass; ++p) {
-        const int row = __shfl_sync(0xffffffffu, place, p * (kRowsPass / kStep) + row_a / kStep);
-        x[p] = make_uint4(0u, 0u, 0u, 0u);
-        if (row >= 0) x[p] = __ldg(reinterpret_cast<const uint4*>(mine + static_cast<int64_t>(row) * HD));
-      }
-    };
-    // (kRowsPass is a multiple of 8: every pass is the same place of the swizzle, kRowsPass rows further)
-    static_assert(kRowsPass % 8 == 0, "");
-    const bool other = (piece & 4) != 0;                          // the second block's lanes store in the other order: no bank is hit twice
-    const uint32_t place0 = tile_chunk(0, row_a, 2 * piece + (other ? 1 : 0)), place1 = tile_chunk(0, row_a, 2 * piece + (other ? 0 : 1));
-    auto put = [&](uint32_t tile, const uint4(&x)[kPass]) {
-      const uint32_t p0 = tile + place0, p1 = tile + place1;
-#pragma unroll
-      for (int p = 0; p < kPass; ++p) {
-        const uint32_t w0 = other ? x[p].z : x[p].x, w1 = other ? x[p].w : x[p].y, w2 = other ? x[p].x : x[p].z, w3 = other ? x[p].y : x[p].w;
-        sts16(p0 + p * kRowsPass * 128, decode2(w0), decode2(w0 >> 16), decode2(w1), decode2(w1 >> 16));
-        sts16(p1 + p * kRowsPass * 128, decode2(w2), decode2(w2 >> 16), decode2(w3), decode2(w3 >> 16));
-      }
-      tc::fence_async_smem();
-      __syncwarp();
-    };
-    if (n > 0) {
-      load_entry(0);
-      take_entry(0);
-      load_entry(1);
-      fetch(kr, V.k);
-      fetch(vr, V.v);
-      for (int j = 0; j < n; ++j) {
-        const int s = j & 1;
-        if (j >= 2 && !wait_warp(kKEmpty + s, (j >> 1) - 1, 20)) break;
-        if (w == 0) {                                             // (the readers of step j - 4 are done: the products of step j - 2 are)
-          if (scaler) {
+    take_entry(0);
+    entry = load_entry(1);
+    for (int j = 0; j < n; ++j) {
+      bool ok = true;
+#pragma unroll 1
+      for (int part4 = 0; part4 < 2 * (kTile / kRawTokens) && ok; ++part4) {      // keys, keys, values, values
+        constexpr int kBoxes = kRawTokens / kStep;
+        if (!(ok = wait_warp(kRawEmpty + raw, raw_phase, 20))) break;
+        if (part4 == 0) {                                         // (the readers of step j - 4's scales are done: see the ring's bound)
+          if (lane < kTile / kStep) {
             const int ev = scale_exponent(sc.y);
             meta[j & 3][lane] = place >= 0 ? Step{exp2_int(scale_exponent(sc.x)), static_cast<float>(ev), exp2_int(-ev), 0.f} : Step{1.f, -INFINITY, 0.f, 0.f};
           }
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(bar(kMeta + (j & 3)));
         }
-        put(k_tile(s), kr);
-        if (lane == 0) tc::mbar_arrive(bar(kKFull + s));
-        take_entry(j + 1);
-        load_entry(j + 2);
-        fetch(kr, V.k);
-        if (j >= 2 && !wait_warp(kVEmpty + s, (j >> 1) - 1, 20)) break;
-        if (p0 + j * kTile + kTile - 1 > lo[0]) {
-          // 0 * NaN: where rows do not see the whole step a NaN value is taken out, and the rows that do see it are set to NaN
-          // at the end
-#pragma unroll
-          for (int p = 0; p < kPass; ++p) {
-            uint32_t* x = reinterpret_cast<uint32_t*>(&vr[p]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              uint32_t bad = ((x[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-              x[k] &= ~((bad >> 7) * 0xffu);
-              while (bad) {
-                const int byte = (__ffs(bad) - 1) >> 3;
-                bad &= bad - 1;
-                atomicMin(nan_at + 16 * piece + 4 * k + byte, p0 + j * kTile + p * kRowsPass + row_a);
-              }
-            }
-          }
+        const bool values = part4 >= kTile / kRawTokens;
+        const int row = __shfl_sync(0xffffffffu, place, part4 % (kTile / kRawTokens) * kBoxes + lane % kBoxes);
+        const unsigned live = __ballot_sync(0xffffffffu, lane < kBoxes && row >= 0);
+        if (lane == 0) tc::mbar_expect_tx(bar(kRawFull + raw), __popc(live) * kStep * HD);
+        __syncwarp();
+        if (lane < kBoxes && row >= 0) tc::tma_load_2d(raw_slot(raw) + lane * kStep * HD, values ? &map_v : &map_k, 0, row, bar(kRawFull + raw));
+        if (++raw == kRawSlots) {
+          raw = 0;
+          raw_phase ^= 1;
         }
-        put(v_tile(s), vr);
-        if (lane == 0) tc::mbar_arrive(bar(kVFull + s));
-        fetch(vr, V.v);
       }
+      if (!ok) break;
+      take_entry(j + 1);
+      entry = load_entry(j + 2);
     }
     __syncthreads();
   } else {
@@ -516,7 +544,7 @@ kv8_attention_tc_kernel(View V, const T* __restrict__ q, int64_t q_stride, T* __
         const uint64_t bd = make_desc_rows_contracted(v_tile(s));
 #pragma unroll
         for (int k = 0; k < kTile / 16; ++k)
-          mma_ts(tmem + 2 * kTile + i * kTile, tmem + i * kTile + 8 * k, bd + (k * 2048 >> 4), kIdO, j > 0 || k > 0);
+          mma_ts(tmem + 2 * kTile + i * kTile, tmem + i * kTile + (k >> 2) * (kTile / 2) + 8 * (k & 3), bd + (k * 2048 >> 4), kIdO, j > 0 || k > 0);
         mma_commit(bar(kODone + i));
       };
       bool ok = wait(kQFull, 0, 0) && wait(kKFull, 0, 0);
@@ -584,11 +612,15 @@ template <typename T, int HD>
 szo_status launch_attention_tc(const View& V, const Rows& A, float* ws, cudaStream_t st) {
   const TcCut p = tc_plan(V, A.H);
   SZO_REQUIRE(p.items <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows, heads and sequences for one launch");
-  const int smem = 6 * kTile * HD * 2 + 1024;
+  const int smem = 6 * kTile * HD * 2 + kRawSlots * kRawTokens * HD + 1024;
+  CUtensorMap map_k, map_v;
+  const int64_t rows = (V.n_pages * V.hkv) << V.page_shift;
+  SZO_TRY(encode_map_2d(&map_k, CU_TENSOR_MAP_DATA_TYPE_UINT8, V.k, rows, HD, 1, kStep, HD, CU_TENSOR_MAP_SWIZZLE_NONE));
+  SZO_TRY(encode_map_2d(&map_v, CU_TENSOR_MAP_DATA_TYPE_UINT8, V.v, rows, HD, 1, kStep, HD, CU_TENSOR_MAP_SWIZZLE_NONE));
   auto kern = kv8_attention_tc_kernel<T, HD>;
   SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   const unsigned blocks = static_cast<unsigned>(p.whole + (p.items - p.whole) * p.nsplit);
-  kern<<<blocks, kTcThreads, smem, st>>>(V, static_cast<const T*>(A.q), A.q_stride, static_cast<T*>(A.o), A.o_stride, A.H, A.scale,
+  kern<<<blocks, kTcThreads, smem, st>>>(map_k, map_v, V, static_cast<const T*>(A.q), A.q_stride, static_cast<T*>(A.o), A.o_stride, A.H, A.scale,
                                          static_cast<int>(p.tiles), TcSplit{static_cast<unsigned>(p.whole), p.nsplit}, ws);
   count_launch();
   SZO_CHECK_LAUNCH("kv8_attention_tc_kernel");
