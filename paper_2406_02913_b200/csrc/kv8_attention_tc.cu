@@ -136,9 +136,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 __device__ __forceinline__ uint32_t tile_chunk(uint32_t base, int row, int chunk) {      // 16-byte chunk (8 columns) of a row
   return base + (chunk >> 3) * (kTile * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
 }
-__device__ __forceinline__ uint4 lds16(uint32_t a) {
-  uint4 r;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a) : "memory");
+__device__ __forceinline__ uint2 lds8(uint32_t a) {
+  uint2 r;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(a) : "memory");
   return r;
 }
 __device__ __forceinline__ void sts16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
@@ -421,7 +421,9 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     const int w = warp - kSoft, piece = lane % kLanes, row_a = w * (32 / kLanes) + lane / kLanes;
     // (kRowsPass is a multiple of 8: every pass is the same place of the swizzle, kRowsPass rows further)
     static_assert(kRowsPass % 8 == 0 && kRawTokens % kRowsPass == 0, "");
-    const bool other = (piece & 4) != 0;                          // the second block's lanes store in the other order: no bank is hit twice
+    // (the second block's lanes take their upper 8 codes first: no bank is stored to twice)
+    const bool other = (piece & 4) != 0;
+    const int half0 = other ? 8 : 0;
     const uint32_t place0 = tile_chunk(0, row_a, 2 * piece + (other ? 1 : 0)), place1 = tile_chunk(0, row_a, 2 * piece + (other ? 0 : 1));
     int raw = 0;
     uint32_t raw_phase = 0;
@@ -434,27 +436,26 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         const uint32_t src = raw_slot(raw) + row_a * HD + 16 * piece, dst = tile + hf * kRawTokens * 128;
 #pragma unroll
         for (int p = 0; p < kRawTokens / kRowsPass; ++p) {
-          uint4 x = lds16(src + p * kRowsPass * HD);
-          const int row = hf * kRawTokens + p * kRowsPass + row_a;
-          if (meta[j & 3][row / kStep].fe == -INFINITY) x = make_uint4(0u, 0u, 0u, 0u);         // no page: the slot holds leftovers
+          uint2 x = lds8(src + half0 + p * kRowsPass * HD), y = lds8(src + (8 - half0) + p * kRowsPass * HD);
           if (partial) {
             // 0 * NaN: where rows do not see the whole step a NaN value is taken out, and the rows that do see it are set to NaN
             // at the end
-            uint32_t* y = reinterpret_cast<uint32_t*>(&x);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              uint32_t bad = ((y[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-              y[k] &= ~((bad >> 7) * 0xffu);
+            auto clear = [&](uint32_t& z, int byte0) {
+              uint32_t bad = ((z & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+              z &= ~((bad >> 7) * 0xffu);
               while (bad) {
                 const int byte = (__ffs(bad) - 1) >> 3;
                 bad &= bad - 1;
-                atomicMin(nan_at + 16 * piece + 4 * k + byte, p0 + j * kTile + row);
+                atomicMin(nan_at + 16 * piece + byte0 + byte, p0 + j * kTile + hf * kRawTokens + p * kRowsPass + row_a);
               }
-            }
+            };
+            clear(x.x, half0);
+            clear(x.y, half0 + 4);
+            clear(y.x, 8 - half0);
+            clear(y.y, 12 - half0);
           }
-          const uint32_t w0 = other ? x.z : x.x, w1 = other ? x.w : x.y, w2 = other ? x.x : x.z, w3 = other ? x.y : x.w;
-          sts16(dst + place0 + p * kRowsPass * 128, decode2(w0), decode2(w0 >> 16), decode2(w1), decode2(w1 >> 16));
-          sts16(dst + place1 + p * kRowsPass * 128, decode2(w2), decode2(w2 >> 16), decode2(w3), decode2(w3 >> 16));
+          sts16(dst + place0 + p * kRowsPass * 128, decode2(x.x), decode2(x.x >> 16), decode2(x.y), decode2(x.y >> 16));
+          sts16(dst + place1 + p * kRowsPass * 128, decode2(y.x), decode2(y.x >> 16), decode2(y.y), decode2(y.y >> 16));
         }
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(bar(kRawEmpty + raw));
@@ -514,6 +515,11 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         const bool values = part4 >= kTile / kRawTokens;
         const int row = __shfl_sync(0xffffffffu, place, part4 % (kTile / kRawTokens) * kBoxes + lane % kBoxes);
         const unsigned live = __ballot_sync(0xffffffffu, lane < kBoxes && row >= 0);
+        if (live != (1u << kBoxes) - 1) {                         // positions without a page (or behind the last) are zeros
+          for (int i = lane; i < kRawTokens * HD / 16; i += 32) sts16(raw_slot(raw) + 16 * i, 0u, 0u, 0u, 0u);
+          tc::fence_async_smem();
+          __syncwarp();
+        }
         if (lane == 0) tc::mbar_expect_tx(bar(kRawFull + raw), __popc(live) * kStep * HD);
         __syncwarp();
         if (lane < kBoxes && row >= 0) tc::tma_load_2d(raw_slot(raw) + lane * kStep * HD, values ? &map_v : &map_k, 0, row, bar(kRawFull + raw));
