@@ -28,6 +28,7 @@
 #include <cooperative_groups.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "kv8_attention.cuh"
 
@@ -495,37 +496,45 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   cluster.sync();                                                 // nobody leaves while its sums are being read
 }
 
-// A block per (row of a tile, item): kGroups groups of a thread per dim take every kGroups-th share, the groups' results are
-// joined in order.
+// Joins the shares' partial results in the workspace: HD / 4 threads per row, four dims each.  With many shares (kGroups =
+// 16) a block is one row, every group of threads taking every 16th share, and the groups' results are joined in order;
+// with few, a block is four rows, since what it waits for is its chain of loads.  `rows`: rows of a tile that can be there.
+template <int kGroups> constexpr int kJoinRows = kGroups == 1 ? 4 : 1;
 template <typename T, int HD, int kGroups>
-__global__ void __launch_bounds__(HD * kGroups)
-kv8_join_kernel(View V, const float* __restrict__ ws, T* __restrict__ o, int64_t o_stride, int H, int R, int row_tiles, int nsplit,
+__global__ void __launch_bounds__(HD / 4 * kGroups * kJoinRows<kGroups>)
+kv8_join_kernel(View V, const float* __restrict__ ws, T* __restrict__ o, int64_t o_stride, int H, int R, int rows, int row_tiles, int nsplit,
                 bool long_first, unsigned item0) {
-  __shared__ float sums[kGroups][HD], ms[kGroups], ls[kGroups];
+  constexpr int kLanes = HD / 4;
+  __shared__ float4 sums[kGroups][kLanes];
+  __shared__ float ms[kGroups], ls[kGroups];
   chain_release();
-  const int r = blockIdx.x % R, d = threadIdx.x % HD, grp = threadIdx.x / HD, G = H / V.hkv;
-  const unsigned item = item0 + blockIdx.x / R, others = static_cast<unsigned>(V.batch) * V.hkv;
+  const int groups = (rows + kJoinRows<kGroups> - 1) / kJoinRows<kGroups>, part = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  const int grp = kGroups > 1 ? part : 0, r = static_cast<int>(blockIdx.x % groups) * kJoinRows<kGroups> + (kGroups > 1 ? 0 : part), G = H / V.hkv;
+  const unsigned item = item0 + blockIdx.x / groups, others = static_cast<unsigned>(V.batch) * V.hkv;
   const int rt = long_first ? row_tiles - 1 - static_cast<int>(item / others) : item % row_tiles;
   const unsigned bh = long_first ? item % others : item / row_tiles;
   const int h = bh % V.hkv, b = bh / V.hkv;
-  chain_wait();
-  const Seq seq = load_seq(V, b);
+  const Seq seq = load_seq(V, b);                                 // (before the wait: the launch before this one was not chained to its own predecessor)
   const int64_t row = static_cast<int64_t>(rt) * R + r;
-  if (row >= static_cast<int64_t>(seq.n) * G) return;
+  chain_wait();
+  if (r >= rows || row >= static_cast<int64_t>(seq.n) * G) return;      // (with groups: the whole block)
   const int64_t step = static_cast<int64_t>(R) * (HD + 2);
-  const float* p = ws + static_cast<int64_t>(blockIdx.x / R) * nsplit * step;
-  float mm = -INFINITY, sum = 0.f, ll = 0.f;
+  const float* p = ws + static_cast<int64_t>(blockIdx.x / groups) * nsplit * step;
+  float mm = -INFINITY, ll = 0.f;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](float f, const float4& x, float l) {
+    sum = make_float4(fmaf(f, x.x, sum.x), fmaf(f, x.y, sum.y), fmaf(f, x.z, sum.z), fmaf(f, x.w, sum.w));
+    ll = fmaf(f, l, ll);
+  };
 #pragma unroll 8
   for (int x = grp; x < nsplit; x += kGroups) mm = fmaxf(mm, p[x * step + R * HD + r]);
-#pragma unroll 8
-  for (int x = grp; x < nsplit; x += kGroups) {
-    const float f = mm == -INFINITY ? 1.f : ex2(p[x * step + R * HD + r] - mm);
-    sum = fmaf(f, p[x * step + r * HD + d], sum);
-    ll = fmaf(f, p[x * step + R * (HD + 1) + r], ll);
-  }
+#pragma unroll 4
+  for (int x = grp; x < nsplit; x += kGroups)
+    add(mm == -INFINITY ? 1.f : ex2(p[x * step + R * HD + r] - mm), *reinterpret_cast<const float4*>(p + x * step + r * HD + 4 * lane),
+        p[x * step + R * (HD + 1) + r]);
   if constexpr (kGroups > 1) {
-    sums[grp][d] = sum;
-    if (d == 0) {
+    sums[grp][lane] = sum;
+    if (lane == 0) {
       ms[grp] = mm;
       ls[grp] = ll;
     }
@@ -534,15 +543,18 @@ kv8_join_kernel(View V, const float* __restrict__ ws, T* __restrict__ o, int64_t
     mm = -INFINITY;
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) mm = fmaxf(mm, ms[k]);
-    sum = ll = 0.f;
+    sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    ll = 0.f;
 #pragma unroll
-    for (int k = 0; k < kGroups; ++k) {
-      const float f = mm == -INFINITY ? 1.f : ex2(ms[k] - mm);
-      sum = fmaf(f, sums[k][d], sum);
-      ll = fmaf(f, ls[k], ll);
-    }
+    for (int k = 0; k < kGroups; ++k) add(mm == -INFINITY ? 1.f : ex2(ms[k] - mm), sums[k][lane], ls[k]);
   }
-  o[(seq.row0 + row / G) * o_stride + (h * G + row % G) * HD + d] = narrow<T>(ll == 0.f ? sum : sum / ll);
+  T y[4];
+  y[0] = narrow<T>(ll == 0.f ? sum.x : sum.x / ll);
+  y[1] = narrow<T>(ll == 0.f ? sum.y : sum.y / ll);
+  y[2] = narrow<T>(ll == 0.f ? sum.z : sum.z / ll);
+  y[3] = narrow<T>(ll == 0.f ? sum.w : sum.w / ll);
+  struct alignas(4 * sizeof(T)) Four { T x[4]; };
+  *reinterpret_cast<Four*>(o + (seq.row0 + row / G) * o_stride + (h * G + row % G) * HD + 4 * lane) = Four{{y[0], y[1], y[2], y[3]}};
 }
 
 // Keys or values as one matrix of bytes, a token and head per row; boxes of `rows` tokens, swizzled over the row
@@ -608,8 +620,16 @@ Plan plan(const View& V, int H) {
   return p;
 }
 
-// More rows per key/value head than this go to the tensor-core kernel (in 16-bit types)
-bool many_rows(const View& V, int H) { return static_cast<int64_t>(V.max_new) * (H / V.hkv) > 64; }
+// Whether a call of 16-bit type goes to the kernel for many rows.  That one takes 256 rows at a time and waits longer before
+// its first product, this one reads the cache again for every 16 rows.  Measured with 8 key/value heads of 128 (this kernel /
+// that one, us; the cut of the positions included): 32 rows per head, 1 sequence of 1024 / 8 of 4096 / 32 of 4096 positions
+// 10.8 / 20.4, 37 / 51, 109 / 163; 64 rows, 1 of 1024 / 1 of 8192 / 1 of 65536 12 / 21, 22 / 26, 99 / 90 and, where the 16-row
+// tiles fill the SMs, 8 of 4096 / 32 of 4096 / 64 of 513 87 / 52, 196 / 165, 117 / 81; 96 rows, 1 of 1024 / 1 of 65536 14 / 21,
+// 184 / 92.
+bool many_rows(const View& V, int H) {
+  const int64_t rows = static_cast<int64_t>(V.max_new) * (H / V.hkv);
+  return rows > 32 && ceil_div(rows, 16) * V.batch * V.hkv > 32;
+}
 
 template <typename T, int HD>
 szo_status launch_attention(const View& V, const Rows& A, float* ws, cudaStream_t st) {
@@ -633,12 +653,14 @@ template <typename T, int HD>
 szo_status launch_join(const View& V, const Rows& A, const float* ws, int R, int row_tiles, int nsplit, bool long_first, int64_t item0,
                        int64_t n_items, cudaStream_t st) {
   SZO_REQUIRE(n_items * R <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows for one launch");
-  const dim3 grid(static_cast<unsigned>(n_items * R));
-  auto run = [&](auto kern, int threads) {
-    return launch_maybe_chained(kern, grid, dim3(threads), 0, st, true, V, ws, static_cast<T*>(A.o), A.o_stride, A.H, R, row_tiles, nsplit, long_first,
-                                static_cast<unsigned>(item0));
+  const int rows = row_tiles > 1 ? R : static_cast<int>(static_cast<int64_t>(V.max_new) * (A.H / V.hkv));
+  auto run = [&](auto kern, auto groups) {
+    constexpr int kG = decltype(groups)::value, kRows = kJoinRows<kG>;
+    return launch_maybe_chained(kern, dim3(static_cast<unsigned>(n_items * ceil_div(rows, kRows))), dim3(HD / 4 * kG * kRows), 0, st, true, V, ws,
+                                static_cast<T*>(A.o), A.o_stride, A.H, R, rows, row_tiles, nsplit, long_first, static_cast<unsigned>(item0));
   };
-  SZO_CHECK_CUDA(nsplit > 8 ? run(kv8_join_kernel<T, HD, 8>, 8 * HD) : run(kv8_join_kernel<T, HD, 1>, HD));
+  SZO_CHECK_CUDA(nsplit > 16 ? run(kv8_join_kernel<T, HD, 16>, std::integral_constant<int, 16>{})
+                             : run(kv8_join_kernel<T, HD, 1>, std::integral_constant<int, 1>{}));
   count_launch();
   return SZO_OK;
 }

@@ -249,41 +249,45 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_addr = tmem + lanes + i * kTile + half * (kTile / 2), o_addr = tmem + lanes + 2 * kTile + i * kTile + half * (HD / 2);
     const int rpos = pos_of(r < n_rows ? r : n_rows - 1);         // (rows that are not there: anything, they are not stored)
-    const int64_t q_off = (seq.row0 + (r0 + r) / G), head = h * G + (r0 + r) % G;
-    float rs, poison;
+    // The queries: a warp brings 16 rows, a row's dims over kQLanes lanes, all loads before the first use
     {
-      const T* qp = q + q_off * q_stride + head * HD;
-      float amax = 0.f;
-      bool fine = true;
-      if (r < n_rows) {
-#pragma unroll 4
-        for (int c = 0; c < HD / 8; ++c) {
-          const Vec<T> x = *reinterpret_cast<const Vec<T>*>(qp + 8 * c);
+      constexpr int kQLanes = HD / 8, kQRows = 32 / kQLanes, kPasses = 16 / kQRows;
+      const int row0 = (warp & 3) * 32 + half * 16 + lane / kQLanes, c = lane % kQLanes;
+      Vec<T> x[kPasses];
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const float y = widen<T>(x.x[u]);
-            amax = fmaxf(amax, fabsf(y));
-            fine = fine && isfinite(y);
-          }
-        }
+      for (int k = 0; k < kPasses; ++k) {
+        const int qr = i * kTile + row0 + k * kQRows;
+        const unsigned at = static_cast<unsigned>(r0) + qr;
+        x[k] = {};
+        if (qr < n_rows)
+          x[k] = *reinterpret_cast<const Vec<T>*>(q + (seq.row0 + at / static_cast<unsigned>(G)) * q_stride +
+                                                  (h * G + at % static_cast<unsigned>(G)) * static_cast<int64_t>(HD) + 8 * c);
       }
-      const int e = min(max((__float_as_int(amax) >> 23) - 127, -126), 126);
-      const float inv = scale < 0.f ? -exp2_int(-e) : exp2_int(-e);
-      rs = exp2_int(e) * (fabsf(scale) * 1.4426950408889634f);
-      poison = fine ? 0.f : __int_as_float(0x7fffffff);           // a row that holds NaN or an infinity is NaN
-#pragma unroll 4
-      for (int c = half * (HD / 16); c < (half + 1) * (HD / 16); ++c) {
-        Vec<T> x = {};
-        if (r < n_rows) x = *reinterpret_cast<const Vec<T>*>(qp + 8 * c);
+#pragma unroll
+      for (int k = 0; k < kPasses; ++k) {
+        int top = 0;                                              // the largest magnitude's bits: NaN above infinity above the rest
+#pragma unroll
+        for (int u = 0; u < 8; ++u) top = max(top, __float_as_int(widen<T>(x[k].x[u])) & 0x7fffffff);
+#pragma unroll
+        for (int s = 1; s < kQLanes; s *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+        const int e = min(max((top >> 23) - 127, -126), 126);
+        const float inv = scale < 0.f ? -exp2_int(-e) : exp2_int(-e);
         uint32_t p[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) p[u] = pack_f16(widen<T>(x.x[2 * u]) * inv, widen<T>(x.x[2 * u + 1]) * inv);
-        sts16(tile_chunk(q_tile(i), rr, c), p[0], p[1], p[2], p[3]);
+        for (int u = 0; u < 4; ++u) p[u] = pack_f16(widen<T>(x[k].x[2 * u]) * inv, widen<T>(x[k].x[2 * u + 1]) * inv);
+        const int row = row0 + k * kQRows;
+        sts16(tile_chunk(q_tile(i), row, c), p[0], p[1], p[2], p[3]);
+        if (c == 0) {
+          peaks[1][i][0][row] = exp2_int(e) * (fabsf(scale) * 1.4426950408889634f);
+          peaks[1][i][1][row] = top < 0x7f800000 ? 0.f : __int_as_float(0x7fffffff);      // a row that holds NaN or an infinity is NaN
+        }
       }
       tc::fence_async_smem();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(bar(kQFull));
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + i), "r"(kSoft / 2 * 32) : "memory");
     }
+    const float rs = peaks[1][i][0][rr], poison = peaks[1][i][1][rr];
     float m = -INFINITY, l = 0.f;
     // (a wait that gave up changes nothing here: every warp of a row tile meets the others as often, whatever it read)
     for (int j = 0; j < n_kv[i]; ++j) {
@@ -381,9 +385,31 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     l = peaks[0][i][0][rr] + peaks[0][i][1][rr];
     tc::tc_fence_after();
     const int d0 = half * (HD / 2);                               // this thread's share of the row's dims
-    T* op = o + q_off * o_stride + head * HD + d0;
     float* wp = ws + static_cast<int64_t>(blockIdx.x - part.whole) * (2 * kTile * (HD + 2));       // (a share's: sums, maxima, sums of weights)
     const float inv = cut ? 1.f : l == 0.f ? 0.f : 1.0f / l;
+    const unsigned at = static_cast<unsigned>(r0) + r;
+    const int64_t mine = cut ? static_cast<int64_t>(r) * HD + d0
+                             : (seq.row0 + at / static_cast<unsigned>(G)) * o_stride + (h * G + at % static_cast<unsigned>(G)) * static_cast<int64_t>(HD) + d0;
+    // Rows go out through shared memory (all of its tiles are done with), 32 rows of at most 128 bytes per warp: whole
+    // lines per store, where a thread that stored its own row would touch 32 lines with each
+    const uint32_t stage = base + warp * 4096;
+    auto put = [&](int chunk, uint32_t x, uint32_t y, uint32_t z, uint32_t w) { sts16(stage + lane * 128 + ((chunk ^ (lane & 7)) << 4), x, y, z, w); };
+    auto flush = [&](auto chunks, auto* to) {                     // `chunks` 16-byte pieces of every row to to[its offset]
+      constexpr int kC = decltype(chunks)::value;
+      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < kC; ++k) {
+        const int row = k * (32 / kC) + lane / kC, chunk = lane % kC;
+        const int64_t off = __shfl_sync(0xffffffffu, mine, row);
+        uint32_t x[4];
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
+                     : "r"(stage + row * 128 + ((chunk ^ (row & 7)) << 4))
+                     : "memory");
+        if (r - lane + row < n_rows) *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(to + off) + 16 * chunk) = make_uint4(x[0], x[1], x[2], x[3]);
+      }
+      __syncwarp();
+    };
 #pragma unroll 1
     for (int c = 0; c < HD / 64; ++c) {
       uint32_t v[32];
@@ -391,7 +417,6 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         tmem_load32(o_addr + 32 * c, v);
         tmem_load_wait(v);
       }
-      if (r >= n_rows) continue;
 #pragma unroll
       for (int u = 0; u < 32; ++u) {
         v[u] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(v[u]) * inv);      // nothing attended to: zeros
@@ -399,18 +424,20 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       }
       if (cut) {
 #pragma unroll
-        for (int u = 0; u < 32; u += 4)
-          *reinterpret_cast<uint4*>(wp + r * HD + d0 + 32 * c + u) = make_uint4(v[u], v[u + 1], v[u + 2], v[u + 3]);
-        continue;
-      }
+        for (int u = 0; u < 8; ++u) put(u, v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+        flush(std::integral_constant<int, 8>{}, wp + 32 * c);
+      } else {
 #pragma unroll
-      for (int u = 0; u < 32; u += 8) {
-        Vec<T> x;
+        for (int u = 0; u < 4; ++u) {
+          Vec<T> x;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x.x[k] = narrow<T>(__uint_as_float(v[u + k]));
-        *reinterpret_cast<Vec<T>*>(op + 32 * c + u) = x;
+          for (int k = 0; k < 8; ++k) x.x[k] = narrow<T>(__uint_as_float(v[8 * u + k]));
+          const uint4 y = *reinterpret_cast<const uint4*>(&x);
+          put(4 * c + u, y.x, y.y, y.z, y.w);
+        }
       }
     }
+    if (!cut) flush(std::integral_constant<int, HD / 16>{}, o);
     if (cut && r < n_rows && half == 0) {
       wp[2 * kTile * HD + r] = m;
       wp[2 * kTile * (HD + 1) + r] = l;
@@ -592,8 +619,9 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 }  // namespace
 
 // The blocks of the last, partial round of SMs (all, where there are fewer than SMs) are cut along the positions as far as
-// SMs are idle, four steps of 128 positions each at least (of what the page table could hold) and not for contexts so short
-// that the joining launch would cost more.
+// SMs are idle: into shares of 2 steps of 128 positions at least (of what the page table could hold) where there is no full
+// round (1 sequence of 1024 positions, 256 rows per head, 8 heads: 24 us, uncut 34; 65536 positions in 16 shares 107 us, in 8
+// 187), of 8 steps behind full ones (8 sequences of 1024, 512 blocks: cut 137 us, uncut 127).
 struct TcCut {
   int64_t tiles, items, whole;
   int nsplit;
@@ -604,7 +632,7 @@ static TcCut tc_plan(const View& V, int H) {
   p.items = p.tiles * V.batch * V.hkv;
   const int64_t tail = p.items % 148, steps = (static_cast<int64_t>(V.max_pages) << V.page_shift) / kTile;
   p.nsplit = 1;
-  while (p.nsplit < 8 && tail > 0 && tail * (p.nsplit + 1) <= 148 && steps >= 4 * (p.nsplit + 1) && steps >= 16) ++p.nsplit;
+  while (p.nsplit < 16 && tail > 0 && tail * (p.nsplit + 1) <= 148 && steps >= (p.items < 148 ? 2 : 8) * (p.nsplit + 1)) ++p.nsplit;
   p.whole = p.nsplit > 1 ? p.items - tail : p.items;
   return p;
 }
