@@ -600,7 +600,9 @@ szo_status launch_rows(const View& V, const Rows& A, int nsplit, float* ws, cuda
 // sequences of 4096 positions and 8 heads: clusters of 4 / 8 16.5 / 22.6 us; 16 sequences: 2 / 4 30.6 / 40.1).  Between one
 // and two items per SM one block per item is best for equal lengths and worst for unequal ones, clusters of 3 near the best
 // for both (32 sequences, 8 heads, 1 / 2 / 3 blocks: 4096 positions each 48 / 69 / 57 us, 513 to 8192 67 / 56 / 59 us).
-// A cut stops at one unit per warp of what the page table could hold.
+// Blocks of 16 rows hold more registers and fewer clusters of 16 fit at once: beyond 8 items they go in clusters of 8 (32 rows,
+// 8 heads, one sequence of 2048 / 8192 positions: 12.6 / 21.1 us, in clusters of 16 21.5 / 30.6; 8 items of 12 rows at 8192
+// positions in 16 / 8: 15.7 / 17.8).  A cut stops at one unit per warp of what the page table could hold.
 struct Plan {
   int rows, nsplit;
   bool wide;
@@ -615,7 +617,8 @@ Plan plan(const View& V, int H) {
     p.nsplit = static_cast<int>(148 / items);
     return p;
   }
-  while (p.nsplit < 16 && items * p.nsplit * 2 <= 148 * 2 && units >= 2 * p.nsplit * 4) p.nsplit *= 2;
+  const int most = p.rows == 8 || items <= 8 ? 16 : 8;
+  while (p.nsplit < most && items * p.nsplit * 2 <= 148 * 2 && units >= 2 * p.nsplit * 4) p.nsplit *= 2;
   if (p.nsplit == 1 && items > 148 && items <= 148 * 2 && units >= 3 * 4) p.nsplit = 3;
   return p;
 }
