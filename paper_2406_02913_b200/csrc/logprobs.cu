@@ -8,9 +8,11 @@
 // lse = m + log s and H = log s - t / s come out of the same pass.  Few rows are cut over the blocks of a cluster and
 // joined through distributed shared memory.
 //
-// Best alternatives: the n-th largest of the threads' best keys is a lower bound of the row's n-th largest key, and
-// only the (at most n) threads whose best reaches it can hold a candidate: those alone read their part again, from L2.
-// Keys are (logit, index) in one 64-bit number, all different, so ties need no care and the result no order of arrival.
+// Best alternatives: the n-th largest of 64 groups' largest logits is a lower bound of the row's n-th largest, and only
+// the threads whose largest reaches it can hold a candidate: their parts alone are read again, from L2, by the whole
+// block.  Candidates are ranked as (logit, index) in one 64-bit number, all different, so ties need no care and the result no order of arrival.
+// Only where too many logits or threads reach the bound (masked rows, whose logits are equal) every thread looks for its
+// best such number first, and the n-th largest of those leaves few.
 #include <cooperative_groups.h>
 
 #include <cmath>
@@ -24,7 +26,7 @@ namespace szo {
 namespace {
 
 // (a thread per target and per entry of the cluster's joined list: kThreads >= kMaxTargets, kMaxCluster * kMaxTop)
-constexpr int kMaxTop = 32, kMaxTargets = 64, kThreads = 256, kMaxCand = 2048, kMaxCluster = 8, kUnroll = 4;
+constexpr int kMaxTop = 32, kMaxTargets = 64, kThreads = 256, kMaxCand = 512, kMaxCluster = 8, kUnroll = 4;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f, kSlack = 8.0f, kBigRef = 65536.0f;
 
 template <typename T> __device__ __forceinline__ float widen(T x);
@@ -140,13 +142,18 @@ template <int kLanes> __device__ __forceinline__ Stat join_lanes(Stat a) {
   a.m = m;
   return a;
 }
-// Order of alternatives: larger logit first, then lower index; NaN before everything, -0 = +0.  Never 0.
+// Order of alternatives: larger logit first, then lower index; NaN before everything, -0 = +0.  Never 0 nor ~0.
 __device__ __forceinline__ uint64_t order_key(float x, uint32_t idx) {
   uint32_t u = isnan(x) ? 0x7fffffffu : __float_as_uint(x + 0.0f);
   u = u & 0x80000000u ? ~u : u | 0x80000000u;
-  return static_cast<uint64_t>(u) << 32 | (0xffffffffu - idx);
+  return static_cast<uint64_t>(u) << 32 | (0xfffffffeu - idx);
 }
-__device__ __forceinline__ uint32_t key_index(uint64_t k) { return 0xffffffffu - static_cast<uint32_t>(k); }
+// The same order of logits alone, as signed numbers
+__device__ __forceinline__ int order_of(float x) {
+  const int u = isnan(x) ? 0x7fffffff : __float_as_int(x + 0.0f);
+  return u >= 0 ? u : u ^ 0x7fffffff;
+}
+__device__ __forceinline__ uint32_t key_index(uint64_t k) { return 0xfffffffeu - static_cast<uint32_t>(k); }
 
 struct Out {
   float *logp, *entropy, *lse, *top_logp;
@@ -250,11 +257,13 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
   constexpr int kN = Vec<T>::kN, kW = kThreads / 32;
   __shared__ Stat part[kW];
   __shared__ Stat mine;
-  __shared__ uint64_t keys[kThreads];                             // best of every thread; later the cluster's lists
+  __shared__ uint64_t keys[kThreads];                             // best of every thread; the cluster's lists
+  __shared__ __align__(16) int groups[kThreads / 4];              // largest of every four threads
   __shared__ uint64_t cand[kTop ? kMaxCand : 1];
   __shared__ uint64_t top[kMaxTop];
   __shared__ uint64_t bound;
-  __shared__ int n_cand;
+  __shared__ int n_cand, n_who, low_bound;
+  __shared__ unsigned char who[kTop ? kThreads : 1];              // threads whose largest reaches the bound
   const int64_t row = blockIdx.x / parts;
   const int rank = blockIdx.x % parts, tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const Row<const T> R(logits + row * ld, vocab);
@@ -269,26 +278,14 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
   }
   Running<T> run;
   float best = -INFINITY;
-  uint64_t key = 0;
   const float c = scale * kLog2e;
   const T low = floor_of<T>(c);
   const float low_y = fmaf(widen<T>(low), c, 200.f);              // the floor counts as -inf for references above this
-  auto take = [&](const Vec<T>(&r)[kUnroll], int v, int count = kUnroll) {
+  auto take = [&](const Vec<T>(&r)[kUnroll]) {
     float mx = largest(r[0]);
 #pragma unroll
     for (int u = 1; u < kUnroll; ++u) mx = max_nan(mx, largest(r[u]));
-    if (kTop && (key == 0 || !(mx <= best))) {               // (vectors come in rising order: equal logits keep the earlier key)
-#pragma unroll 1
-      for (int at = v; at < min(v + count * kThreads, v_hi); at += kThreads) {       // (seldom: from L1 or L2 again)
-        const Vec<T> x = R.whole(at) ? R.vec(at) : R.edge(at);
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-          const uint64_t k = R.inside(at, i) ? order_key(widen<T>(x.x[i]), R.index(at, i)) : 0;
-          if (k > key) key = k;
-        }
-      }
-      best = mx;
-    }
+    if (kTop) best = max_nan(best, mx);
     run.take(r, mx, scale, c, low, low_y);
   };
   int v = v_lo + tid;
@@ -297,14 +294,14 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
     if (v == 0 && v < v_hi && !R.whole(0)) {                      // a row that starts inside a vector (or a single partial one)
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) r[u] = R.edge(u ? R.vecs : 0);               // (behind the row: -inf throughout)
-      take(r, 0, 1);
+      take(r);
       v = kThreads;
     }
     const int v_whole = v_hi - (rank == parts - 1 && !R.whole(R.vecs - 1));
     for (; v + (kUnroll - 1) * kThreads < v_whole; v += kUnroll * kThreads) {        // all loads first
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) r[u] = R.vec(v + u * kThreads);
-      take(r, v);
+      take(r);
     }
     if (v < v_hi) {                                               // what is left; -inf where there is nothing
 #pragma unroll
@@ -313,43 +310,102 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
         if (at < v_whole) r[u] = R.vec(at);
         else r[u] = R.edge(at < v_hi ? at : R.vecs);
       }
-      take(r, v);
+      take(r);
     }
   }
   Stat st = join_lanes<32>(run.stat());
   if (lane == 0) part[w] = st;
   if (tid == 0) {
-    n_cand = 0;
+    n_cand = n_who = 0;
     bound = 1;
   }
-  if (tid < kMaxTop) top[tid] = 0;
-  keys[tid] = key;
+  if constexpr (kTop) {
+    if (tid < kMaxTop) top[tid] = 0;
+    int g = order_of(best);
+    g = max(g, __shfl_xor_sync(0xffffffffu, g, 1));
+    g = max(g, __shfl_xor_sync(0xffffffffu, g, 2));
+    if (tid % 4 == 0) groups[tid / 4] = g;
+  }
   __syncthreads();
   st = join_lanes<kW>(part[lane % kW]);                           // (every warp: all threads know the row's)
 
   if constexpr (kTop) {
-    if (key != 0) {
-      int above = 0;
-#pragma unroll 8
-      for (int i = 0; i < kThreads; ++i) above += keys[i] > key;
-      if (above == n_top - 1) bound = key;
-    }
-    __syncthreads();
-    if (key >= bound) {
+    // this thread's vectors, in the order of their indexes
+    auto each = [&](auto f) {
 #pragma unroll 4
-      for (v = v_lo + tid; v < v_hi; v += kThreads) {
+      for (int v = v_lo + tid; v < v_hi; v += kThreads) {
         const Vec<T> x = R.whole(v) ? R.vec(v) : R.edge(v);
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-          const uint64_t k = R.inside(v, i) ? order_key(widen<T>(x.x[i]), R.index(v, i)) : 0;
-          if (k >= bound) {
-            const int at = atomicAdd(&n_cand, 1);
-            if (at < kMaxCand) cand[at] = k;
-          }
-        }
+        f(x, v);
       }
+    };
+    auto key_at = [&](const Vec<T>& x, int v, int i) { return R.inside(v, i) ? order_key(widen<T>(x.x[i]), R.index(v, i)) : 0; };
+    auto at_most = [&](const Vec<T>& x, int v) { return order_key(largest(x), max(R.index(v, 0), 0)); };      // a vector's keys are not above this
+    if (w < 2) {                                                  // the n-th largest group (equal ones: in order)
+      static_assert(kThreads / 4 == 64 && kMaxTop <= 64, "");
+      const int g = groups[tid];
+      int above = 0;
+#pragma unroll 4
+      for (int i = 0; i < 16; ++i) {
+        const int4 x = reinterpret_cast<const int4*>(groups)[i];
+        above += x.x > g || (x.x == g && 4 * i < tid);
+        above += x.y > g || (x.y == g && 4 * i + 1 < tid);
+        above += x.z > g || (x.z == g && 4 * i + 2 < tid);
+        above += x.w > g || (x.w == g && 4 * i + 3 < tid);
+      }
+      if (above == n_top - 1) low_bound = g;
     }
     __syncthreads();
+    const int lb = low_bound;
+    if (order_of(best) >= lb) who[atomicAdd(&n_who, 1)] = tid;
+    __syncthreads();
+    const int threads = n_who, rounds = (v_hi - v_lo + kThreads - 1) / kThreads;
+    const int work = threads > kThreads / 2 ? 0 : threads * rounds;
+#pragma unroll 4
+    for (int i = tid; i < work; i += kThreads) {                  // their vectors, by all threads: few loads one after the other
+      const int v = v_lo + who[i % threads] + i / threads * kThreads;
+      if (v >= v_hi) continue;
+      const Vec<T> x = R.whole(v) ? R.vec(v) : R.edge(v);
+      if (order_of(largest(x)) < lb) continue;
+#pragma unroll
+      for (int k = 0; k < kN; ++k)
+        if (order_of(widen<T>(x.x[k])) >= lb && R.inside(v, k) && *const_cast<volatile int*>(&n_cand) <= kMaxCand) {
+          const int at = atomicAdd(&n_cand, 1);
+          if (at < kMaxCand) cand[at] = order_key(widen<T>(x.x[k]), R.index(v, k));
+        }
+    }
+    __syncthreads();
+    if (n_cand > kMaxCand || threads > kThreads / 2) {            // (the block)
+      uint64_t key = 0;
+      each([&](const Vec<T>& x, int v) {
+        if (at_most(x, v) <= key) return;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) key = max(key, key_at(x, v, i));
+      });
+      __syncthreads();                                            // (all have seen n_cand)
+      keys[tid] = key;
+      if (tid == 0) n_cand = 0;
+      __syncthreads();
+      if (key != 0) {
+        int above = 0;
+#pragma unroll 8
+        for (int i = 0; i < kThreads; ++i) above += keys[i] > key;
+        if (above == n_top - 1) bound = key;
+      }
+      __syncthreads();
+      if (key >= bound)
+        each([&](const Vec<T>& x, int v) {
+          if (at_most(x, v) < bound) return;
+#pragma unroll
+          for (int i = 0; i < kN; ++i) {
+            const uint64_t k = key_at(x, v, i);
+            if (k >= bound) {
+              const int at = atomicAdd(&n_cand, 1);
+              if (at < kMaxCand) cand[at] = k;
+            }
+          }
+        });
+      __syncthreads();
+    }
     if (n_cand <= kMaxCand) {
       for (int j = tid; j < n_cand; j += kThreads) {
         const uint64_t k = cand[j];
@@ -361,14 +417,14 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
       uint64_t last = ~0ull;
       for (int r = 0; r < n_top; ++r) {
         uint64_t k = 0;
-        for (v = v_lo + tid; v < v_hi; v += kThreads) {
-          const Vec<T> x = R.whole(v) ? R.vec(v) : R.edge(v);
+        each([&](const Vec<T>& x, int v) {
+          if (at_most(x, v) <= k) return;
 #pragma unroll
           for (int i = 0; i < kN; ++i) {
-            const uint64_t ck = R.inside(v, i) ? order_key(widen<T>(x.x[i]), R.index(v, i)) : 0;
+            const uint64_t ck = key_at(x, v, i);
             if (ck < last && ck > k) k = ck;
           }
-        }
+        });
         __syncthreads();
         keys[tid] = k;
         __syncthreads();

@@ -122,6 +122,24 @@ def test_masks_ties_and_non_finite_rows(B, dt):
     assert B.device_status() == 0
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+def test_best_tokens_where_the_largest_logits_crowd(B, dt):
+    g = np.random.default_rng(8)
+    V = 120001
+    x = values(g, 5, V, dt)
+    vec = 4 if dt == "f32" else 8
+    crowd = (np.arange(V) // vec) % 256 < 31             # all with a few of a block's threads
+    x[0, crowd] += 50
+    x[1, crowd] = 50.0
+    x[2, : V - 700] = float("-inf")                      # a mask that leaves some, all at one end
+    x[3] = float("-inf")
+    x[3, [5, 70000, V - 1]] = torch.tensor([1.0, 1.0, 2.0]).to(DT[dt])     # fewer than are asked for
+    x[4, crowd] = float("nan")
+    for top in (1, 31, 32):
+        check(B, x, None, top, 1.0)
+    check(B, x.repeat(80, 1), None, 32, 1.0)             # (a block per row)
+
+
 def test_targets_beyond_the_vocabulary_are_reported(B):
     x = torch.randn(2, 100)
     r = B.szo_token_logprobs(x.cuda(), torch.tensor([[100, 5], [-5, 2 ** 31 - 1]], dtype=torch.int32, device="cuda"))
