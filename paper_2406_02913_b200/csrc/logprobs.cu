@@ -281,20 +281,20 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
   const float c = scale * kLog2e;
   const T low = floor_of<T>(c);
   const float low_y = fmaf(widen<T>(low), c, 200.f);              // the floor counts as -inf for references above this
-  auto take = [&](const Vec<T>(&r)[kUnroll]) {
+  auto take = [&](const auto& r) {
     float mx = largest(r[0]);
 #pragma unroll
-    for (int u = 1; u < kUnroll; ++u) mx = max_nan(mx, largest(r[u]));
+    for (int u = 1; u < static_cast<int>(sizeof(r) / sizeof(r[0])); ++u) mx = max_nan(mx, largest(r[u]));
     if (kTop) best = max_nan(best, mx);
     run.take(r, mx, scale, c, low, low_y);
   };
   int v = v_lo + tid;
   {
     Vec<T> r[kUnroll];
+    Vec<T> one[1];
     if (v == 0 && v < v_hi && !R.whole(0)) {                      // a row that starts inside a vector (or a single partial one)
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) r[u] = R.edge(u ? R.vecs : 0);               // (behind the row: -inf throughout)
-      take(r);
+      one[0] = R.edge(0);
+      take(one);
       v = kThreads;
     }
     const int v_whole = v_hi - (rank == parts - 1 && !R.whole(R.vecs - 1));
@@ -303,14 +303,9 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
       for (int u = 0; u < kUnroll; ++u) r[u] = R.vec(v + u * kThreads);
       take(r);
     }
-    if (v < v_hi) {                                               // what is left; -inf where there is nothing
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int at = v + u * kThreads;
-        if (at < v_whole) r[u] = R.vec(at);
-        else r[u] = R.edge(at < v_hi ? at : R.vecs);
-      }
-      take(r);
+    for (; v < v_hi; v += kThreads) {                             // what is left
+      one[0] = v < v_whole ? R.vec(v) : R.edge(v);
+      take(one);
     }
   }
   Stat st = join_lanes<32>(run.stat());
