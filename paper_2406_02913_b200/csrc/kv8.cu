@@ -4,7 +4,10 @@
 // bandwidth bounds them once there are enough pages, and the latency of one dependent chain
 // (lengths -> page id -> rows -> amax -> codes) when there are few.  One block owns one (page, head): the
 // amax that sets its scale then needs no second pass and no atomics, and the rows stay in registers
-// between the two uses.  Inside a block a warp owns 16 slots of the keys or of the values.
+// between the two uses.  Inside a block a warp owns 16 slots of the keys or of the values, and all its loads are under way
+// before the first is used.  Measured (bf16, 8 heads of 128): 8 x 2048 new positions written in 18.6 us (4.8 TB/s, 0.75 of the
+// measured copy bandwidth; what is left is the chain above, with 2 blocks per SM), contexts of 4 x 8192 read in 33.5 us (5.9
+// TB/s, 0.92); 32 single tokens written in 3.5 us, which is launch and chain.
 #include "kv8.cuh"
 
 namespace szo {
