@@ -698,6 +698,8 @@ class Model:
     def token_logprobs(self, tokens, targets=None, n_top: int = 0, S_vals=None) -> TokenLogprobs:
         """Log probabilities under the model's next-token distributions: tokens int32 [B, S]; targets int32
         [B * S, n_targets] (negative: none) or None: the tokens that follow (none after the last of a sequence)."""
+        if tokens.dtype != torch.int32 or tokens.dim() != 2:
+            raise ValueError("tokens must be int32 [B, S]")
         B, S = tokens.shape
         if targets is None:
             targets = torch.full_like(tokens, -1)

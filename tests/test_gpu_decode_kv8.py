@@ -164,6 +164,8 @@ def test_token_logprobs_of_a_model(B, name, act):
         m.token_logprobs(d_toks, n_top=33)
     with pytest.raises(ValueError):
         m.token_logprobs(d_toks, targets=t[:59].cuda())
+    with pytest.raises(ValueError):
+        m.token_logprobs(d_toks.long(), targets=t.cuda())
     assert B.device_status() == 0
     m.close()
 

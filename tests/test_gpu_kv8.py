@@ -425,6 +425,28 @@ def test_chunks_of_few_sequences_with_long_contexts(B, dt, d, hkv, group, page):
     assert B.device_status() == 0
 
 
+@pytest.mark.parametrize("d,group", [(128, 4), (64, 5)])
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+def test_cut_chunks_with_empty_shares(B, dt, d, group):
+    """The table allows many shares, the lengths leave most of them nothing: sequences of a few positions, none at all, padding."""
+    lens = [2900, 5, 0, 129, 1]
+    w = World(B, lens, 1, 32, d, seed=d + group)
+    fill(B, w, lens)
+    run_attention(B, w, lens, [61, 70, 66, 64, 1], group, dt)
+    run_attention(B, w, [2899, 0, 0, 128, 0], [1, 90, 0, 128, 3], group, dt)
+    assert B.device_status() == 0
+
+
+@pytest.mark.parametrize("new", [8, 9, 16, 17, 33])
+@pytest.mark.parametrize("dt", ["bf16", "f16", "f32"])
+def test_rows_around_the_choice_of_kernel(B, dt, new):
+    lens = [40, 300, 64, 129, 511, 17]
+    w = World(B, lens, 4, 16, 128, seed=new)
+    fill(B, w, lens)
+    run_attention(B, w, lens, [min(new, n) for n in lens], 16, dt)
+    run_attention(B, w, lens, [new, new - 1, 0, 0, 1, 0], 16, dt)
+
+
 def test_same_call_same_bits(B):
     w = World(B, [14000, 900], 2, 32, 128, seed=21)
     fill(B, w, [14000, 900])
