@@ -15,10 +15,11 @@
 //   warp 21          brings the codes by TMA, 64 positions of keys or values per slot of a small ring, and the pages' scales
 //                    (with the converting warps loading for themselves the latency of a step's loads showed: they have
 //                    no registers for a second set)
-// Measured: 2 sequences of 2048 new tokens at 8192 positions, 32 heads over 8 of 128, 548 us (839 TFLOP/s, 0.50 of the measured
-// burst rate of dense products, 0.60 of the sustained one).  With the softmax taken out of a copy 405 us, with the conversion 487,
-// with both 388: what is left is the chain products -> softmax -> products of two row tiles, and shared memory, which the
-// products with both operands there (128 x 128 x 16: 8 KB per 64 cycles) use fully while they run.
+// Measured: 2 sequences of 2048 new tokens at 8192 positions, 32 heads over 8 of 128, 528 us (872 TFLOP/s, 0.52 of the measured
+// burst rate of dense products, 0.63 of the sustained one).  A step of 128 positions takes 4500 cycles against 2048 for its
+// products: a row tile's scores wait 1400 for both tiles' products, its maxima take 700, their exchange 270, its weights 1850
+// (2048 for both tiles by the exponentials' rate), and the next products wait for them.  Copying and converting (1900 and
+// 3100 cycles a step, on their own warps) hide behind that.
 // Numbers are those of the kernel for few rows: queries divided by a power of two per row, weights relative to each
 // token's contribution (logit + exponent of its page's value scale), sums of weights divided by that scale again.
 // The reference maximum follows the running maximum once that is 2^8 above it, so O is rescaled in TMEM a few times
@@ -158,6 +159,8 @@ __device__ __forceinline__ uint64_t make_desc_rows_contracted(uint32_t smem_addr
 constexpr uint32_t make_idesc_f16(int M, int N, bool b_rows_contracted) {
   return (1u << 4) | (b_rows_contracted ? 1u << 16 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
+
+__host__ __device__ __forceinline__ int box_tokens(const View& V) { return V.page_shift < 6 ? 1 << V.page_shift : kRawTokens; }
 
 // Items (row tile, sequence, head) from `whole` on are cut into `nsplit` shares of their positions, a block each
 struct TcSplit {
@@ -513,6 +516,9 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     // ------------------------------------------------------------------ codes and scales from global memory
     // Lane s < 8 keeps the page of the s-th 16 positions of a step: the table's entry two steps ahead, its row in the tensor
     // maps (-1: no page) and its scales one step ahead
+    // A box of the maps is a page's tokens or 64 of them (32 sequences of 12 tokens at 4096 positions, pages of
+    // 32: 158 us, in boxes of 16 163)
+    const int box = box_tokens(V), boxes = kRawTokens / box;
     const int32_t* table = V.table + static_cast<int64_t>(b) * V.max_pages;
     auto load_entry = [&](int j) {
       const int step = (j0 + j) * (kTile / kStep) + lane;
@@ -533,7 +539,6 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       bool ok = true;
 #pragma unroll 1
       for (int part4 = 0; part4 < 2 * (kTile / kRawTokens) && ok; ++part4) {      // keys, keys, values, values
-        constexpr int kBoxes = kRawTokens / kStep;
         if (!(ok = wait_warp(kRawEmpty + raw, raw_phase, 20))) break;
         if (part4 == 0) {                                         // (the readers of step j - 4's scales are done: see the ring's bound)
           if (lane < kTile / kStep) {
@@ -544,16 +549,16 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
           if (lane == 0) tc::mbar_arrive(bar(kMeta + (j & 3)));
         }
         const bool values = part4 >= kTile / kRawTokens;
-        const int row = __shfl_sync(0xffffffffu, place, part4 % (kTile / kRawTokens) * kBoxes + lane % kBoxes);
-        const unsigned live = __ballot_sync(0xffffffffu, lane < kBoxes && row >= 0);
-        if (live != (1u << kBoxes) - 1) {                         // positions without a page (or behind the last) are zeros
+        const int row = __shfl_sync(0xffffffffu, place, part4 % (kTile / kRawTokens) * (kRawTokens / kStep) + (lane % boxes) * (box / kStep));
+        const unsigned live = __ballot_sync(0xffffffffu, lane < boxes && row >= 0);
+        if (live != (1u << boxes) - 1) {                          // positions without a page (or in a box behind the last) are zeros
           for (int i = lane; i < kRawTokens * HD / 16; i += 32) sts16(raw_slot(raw) + 16 * i, 0u, 0u, 0u, 0u);
           tc::fence_async_smem();
           __syncwarp();
         }
-        if (lane == 0) tc::mbar_expect_tx(bar(kRawFull + raw), __popc(live) * kStep * HD);
+        if (lane == 0) tc::mbar_expect_tx(bar(kRawFull + raw), __popc(live) * box * HD);
         __syncwarp();
-        if (lane < kBoxes && row >= 0) tc::tma_load_2d(raw_slot(raw) + lane * kStep * HD, values ? &map_v : &map_k, 0, row, bar(kRawFull + raw));
+        if (lane < boxes && row >= 0) tc::tma_load_2d(raw_slot(raw) + lane * box * HD, values ? &map_v : &map_k, 0, row, bar(kRawFull + raw));
         if (++raw == kRawSlots) {
           raw = 0;
           raw_phase ^= 1;
@@ -566,7 +571,10 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     __syncthreads();
   } else {
     // ------------------------------------------------------------------ one thread issues the products
-    if (lane == 0 && n > 0) {
+    // (elected and not lane 0: the compiler then knows that one thread is left, and issues in half the instructions)
+    uint32_t elected;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(elected));
+    if (elected && n > 0) {
       constexpr uint32_t kIdS = make_idesc_f16(kTile, kTile, false), kIdO = make_idesc_f16(kTile, HD, true);
       auto scores = [&](int i, int s) {
         const uint64_t a = tc::make_desc_sw128(q_tile(i)), bd = tc::make_desc_sw128(k_tile(s));
@@ -653,8 +661,8 @@ szo_status launch_attention_tc(const View& V, const Rows& A, float* ws, cudaStre
   const int smem = 6 * kTile * HD * 2 + kRawSlots * kRawTokens * HD + 1024;
   CUtensorMap map_k, map_v;
   const int64_t rows = (V.n_pages * V.hkv) << V.page_shift;
-  SZO_TRY(encode_map_2d(&map_k, CU_TENSOR_MAP_DATA_TYPE_UINT8, V.k, rows, HD, 1, kStep, HD, CU_TENSOR_MAP_SWIZZLE_NONE));
-  SZO_TRY(encode_map_2d(&map_v, CU_TENSOR_MAP_DATA_TYPE_UINT8, V.v, rows, HD, 1, kStep, HD, CU_TENSOR_MAP_SWIZZLE_NONE));
+  SZO_TRY(encode_map_2d(&map_k, CU_TENSOR_MAP_DATA_TYPE_UINT8, V.k, rows, HD, 1, box_tokens(V), HD, CU_TENSOR_MAP_SWIZZLE_NONE));
+  SZO_TRY(encode_map_2d(&map_v, CU_TENSOR_MAP_DATA_TYPE_UINT8, V.v, rows, HD, 1, box_tokens(V), HD, CU_TENSOR_MAP_SWIZZLE_NONE));
   auto kern = kv8_attention_tc_kernel<T, HD>;
   SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   const unsigned blocks = static_cast<unsigned>(p.whole + (p.items - p.whole) * p.nsplit);
