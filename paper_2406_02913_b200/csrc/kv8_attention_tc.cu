@@ -15,7 +15,7 @@
 //   warp 21          brings the codes by TMA, 64 positions of keys or values per slot of a small ring, and the pages' scales
 //                    (with the converting warps loading for themselves the latency of a step's loads showed: they have
 //                    no registers for a second set)
-// Measured: 2 sequences of 2048 new tokens at 8192 positions, 32 heads over 8 of 128, 528 us (872 TFLOP/s, 0.52 of the measured
+// Measured: 2 sequences of 2048 new tokens at 8192 positions, 32 heads over 8 of 128, 526 us (875 TFLOP/s, 0.52 of the measured
 // burst rate of dense products, 0.63 of the sustained one).  A step of 128 positions takes 4500 cycles against 2048 for its
 // products: a row tile's scores wait 1400 for both tiles' products, its maxima take 700, their exchange 270, its weights 1850
 // (2048 for both tiles by the exponentials' rate), and the next products wait for them.  Copying and converting (1900 and
@@ -193,11 +193,12 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   const int rt = row_tiles - 1 - static_cast<int>(item / others);                // the longest rows first
   const int h = static_cast<int>(item % others) % V.hkv, b = static_cast<int>(item % others) / V.hkv, G = H / V.hkv;
   const Seq seq = load_seq(V, b);
-  const int64_t r0 = static_cast<int64_t>(rt) * 2 * kTile, left = static_cast<int64_t>(seq.n) * G - r0;
+  const unsigned r0 = static_cast<unsigned>(rt) * 2 * kTile;                     // (rows and heads of a call stay below 2^31)
+  const int64_t left = static_cast<int64_t>(seq.n) * G - r0;
   if (left <= 0) return;
   const int n_rows = static_cast<int>(left < 2 * kTile ? left : 2 * kTile);
   const int first = seq.len - seq.n;                              // position of the sequence's row 0; negative: padding
-  auto pos_of = [&](int r) { return first + static_cast<int>((r0 + r) / G); };
+  auto pos_of = [&](int r) { return first + static_cast<int>((r0 + r) / static_cast<unsigned>(G)); };
   int n_kv[2], lo[2];                                             // steps of each row tile; position of its first row
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -264,7 +265,7 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 #pragma unroll
       for (int k = 0; k < kPasses; ++k) {
         const int qr = i * kTile + row0 + k * kQRows;
-        const unsigned at = static_cast<unsigned>(r0) + qr;
+        const unsigned at = r0 + qr;
         x[k] = {};
         if (qr < n_rows)
           x[k] = *reinterpret_cast<const Vec<T>*>(q + (seq.row0 + at / static_cast<unsigned>(G)) * q_stride +
@@ -292,10 +293,11 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       tc::fence_async_smem();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(bar(kQFull));
-      asm volatile("bar.sync %0, %1;" ::"r"(1 + i), "r"(kSoft / 2 * 32) : "memory");
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + 4 * i + (warp & 3)), "r"(64) : "memory");
     }
     const float rs = peaks[1][i][0][rr], poison = peaks[1][i][1][rr];
     float m = -INFINITY, l = 0.f;
+    const int limit0 = rpos - p0 - half * (kTile / 2), masked_from = (lo[i] - p0) / kTile;      // (a negative quotient: 0 or below, all masked)
     // (a wait that gave up changes nothing here: every warp of a row tile meets the others as often, whatever it read)
     for (int j = 0; j < n_kv[i]; ++j) {
       wait_warp(kMeta + (j & 3), j >> 2, 20);
@@ -309,9 +311,10 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         for (int c = 0; c < 2; ++c) {
           tmem_load32(s_addr + 32 * c, v);
           tmem_load_wait(v);
+          const int limit = limit0 - j * kTile - 32 * c;          // columns up to this one are seen
 #pragma unroll
           for (int u = 0; u < 32; ++u)
-            if (32 * c + u > limit) v[u] = 0xff800000u;
+            if (u > limit) v[u] = 0xff800000u;
           tmem_store32(s_addr + 32 * c, v);
         }
         tmem_store_wait();
@@ -336,7 +339,7 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       }
       // the row's other half
       peaks[j & 1][i][half][rr] = mx;
-      asm volatile("bar.sync %0, %1;" ::"r"(1 + i), "r"(kSoft / 2 * 32) : "memory");
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + 4 * i + (warp & 3)), "r"(64) : "memory");
       mx = fmaxf(mx, peaks[j & 1][i][half ^ 1][rr]);
       const bool need = mx > m + kTcSlack || (m == -INFINITY && mx > -INFINITY);
       if (__any_sync(0xffffffffu, need)) {
@@ -388,13 +391,13 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     if (n_kv[i] > 0) wait_warp(kODone + i, n_kv[i] - 1, 20);
     __syncthreads();                                              // (nan_at is complete; see the other warps' ends)
     peaks[0][i][half][rr] = l;
-    asm volatile("bar.sync %0, %1;" ::"r"(1 + i), "r"(kSoft / 2 * 32) : "memory");
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + 4 * i + (warp & 3)), "r"(64) : "memory");
     l = peaks[0][i][0][rr] + peaks[0][i][1][rr];
     tc::tc_fence_after();
     const int d0 = half * (HD / 2);                               // this thread's share of the row's dims
     float* wp = ws + static_cast<int64_t>(blockIdx.x - part.whole) * (2 * kTile * (HD + 2));       // (a share's: sums, maxima, sums of weights)
     const float inv = cut ? 1.f : l == 0.f ? 0.f : 1.0f / l;
-    const unsigned at = static_cast<unsigned>(r0) + r;
+    const unsigned at = r0 + r;
     const int64_t mine = cut ? static_cast<int64_t>(r) * HD + d0
                              : (seq.row0 + at / static_cast<unsigned>(G)) * o_stride + (h * G + at % static_cast<unsigned>(G)) * static_cast<int64_t>(HD) + d0;
     // Rows go out through shared memory (all of its tiles are done with), 32 rows of at most 128 bytes per warp: whole
