@@ -631,8 +631,8 @@ Plan plan(const View& V, int H) {
 // Whether a call of 16-bit type goes to the kernel for many rows.  That one takes 256 rows at a time and waits longer before
 // its first product, this one reads the cache again for every 16 rows.  Measured with 8 key/value heads of 128 (this kernel /
 // that one, us; the cut of the positions included): 32 rows per head, 1 sequence of 1024 / 8 of 4096 / 32 of 4096 positions
-// 10.8 / 20.4, 37 / 51, 109 / 163; 64 rows, 1 of 1024 / 1 of 8192 / 1 of 65536 12 / 21, 22 / 26, 99 / 90 and, where the 16-row
-// tiles fill the SMs, 8 of 4096 / 32 of 4096 / 64 of 513 87 / 52, 196 / 165, 117 / 81; 96 rows, 1 of 1024 / 1 of 65536 14 / 21,
+// 10.9 / 18.7, 37 / 49, 109 / 157; 64 rows, 1 of 1024 / 1 of 8192 / 1 of 65536 12 / 20, 22 / 25, 99 / 89 and, where the 16-row
+// tiles fill the SMs, 8 of 4096 / 32 of 4096 / 64 of 513 86 / 51, 196 / 161, 117 / 88; 96 rows, 1 of 1024 / 1 of 65536 14 / 20,
 // 184 / 92.
 bool many_rows(const View& V, int H) {
   const int64_t rows = static_cast<int64_t>(V.max_new) * (H / V.hkv);

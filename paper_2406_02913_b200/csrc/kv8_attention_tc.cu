@@ -635,8 +635,8 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
 
 // The blocks of the last, partial round of SMs (all, where there are fewer than SMs) are cut along the positions as far as
 // SMs are idle: into shares of 2 steps of 128 positions at least (of what the page table could hold) where there is no full
-// round (1 sequence of 1024 positions, 256 rows per head, 8 heads: 24 us, uncut 34; 65536 positions in 16 shares 107 us, in 8
-// 187), of 8 steps behind full ones (8 sequences of 1024, 512 blocks: cut 137 us, uncut 127).
+// round (1 sequence of 1024 positions, 256 rows per head, 8 heads: 23 us, uncut 32; 65536 positions in 16 shares 106 us, in 8
+// 177, uncut 1145), of 8 steps behind full ones (8 sequences of 1024, 512 blocks: cut 127 us, uncut 117).
 struct TcCut {
   int64_t tiles, items, whole;
   int nsplit;
