@@ -539,13 +539,9 @@ def szo_token_logprobs(logits: torch.Tensor, targets: torch.Tensor | None = None
     # one allocation for the results; every part starts on 16 bytes
     r4, t4, a4 = (rows + 3) & ~3, (rows * nt + 3) & ~3, (rows * n_top + 3) & ~3
     f = torch.empty(2 * r4 + t4 + 2 * a4, dtype=torch.float32, device=logits.device)
-    lse, entropy, logp, top_logp, top_ids = f.split_with_sizes((r4, r4, t4, a4, a4))
-    if r4 != rows:
-        lse, entropy = lse[:rows], entropy[:rows]
-    logp = (logp if t4 == rows * nt else logp[:rows * nt]).view(rows, nt)
-    if a4 != rows * n_top:
-        top_logp, top_ids = top_logp[:rows * n_top], top_ids[:rows * n_top]
-    top_logp, top_ids = top_logp.view(rows, n_top), top_ids.view(torch.int32).view(rows, n_top)
+    part, at = f.as_strided, 2 * r4 + t4
+    lse, entropy, logp = part((rows,), (1,), 0), part((rows,), (1,), r4), part((rows, nt), (nt, 1), 2 * r4)
+    top_logp, top_ids = part((rows, n_top), (n_top, 1), at), f.view(torch.int32).as_strided((rows, n_top), (n_top, 1), at + a4)
     if rows:
         _check(lib().szo_token_logprobs(logits.data_ptr(), _DT[logits.dtype], rows, vocab, ld, scale, targets.data_ptr() if nt else None,
                                         nt, n_top, logp.data_ptr() if nt else None, entropy.data_ptr(), lse.data_ptr(),
