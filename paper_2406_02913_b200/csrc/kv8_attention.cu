@@ -16,8 +16,8 @@
 //     cluster per sequence and head leaves SMs idle (few sequences and heads, long contexts: seven clusters of 16 such
 //     blocks fit this GPU), blocks of 12 warps, one per SM, write their partial results to a workspace and a second,
 //     chained launch joins them.  Both join in a fixed order: the same bits every time.
-// Measured (bf16, 32 heads over 8 of 128): one sequence of 131071 positions 51.8 us (5.2 TB/s, 0.80 of the measured copy
-// bandwidth), 32 of 513 to 8192 58.3 us (4.9 TB/s; the longest sequence's blocks are the last), 64 of 2048 with 40 heads over 40
+// Measured (bf16, 32 heads over 8 of 128): one sequence of 131071 positions 50.1 us (5.4 TB/s, 0.83 of the measured copy
+// bandwidth), 32 of 513 to 8192 57.2 us (5.0 TB/s; the longest sequence's blocks are the last), 64 of 2048 with 40 heads over 40
 // 195 us (6.9 TB/s: reads alone, faster than the copy), one of 1024 6.9 us (launch, two trips to memory, join).
 //
 // Numbers.  Codes become fp16 exactly (one cvt per two).  A query row is divided by the power of two of its largest
@@ -114,6 +114,8 @@ template <int HD> __device__ __forceinline__ void load_values(uint32_t (&v)[4][H
   }
 }
 
+__host__ __device__ __forceinline__ int box_tokens(const View& V) { return V.page_shift < 5 ? kStep : kUnit; }
+
 template <int HD> constexpr int kRingBytes = kDepth * kUnit * HD * 2;       // per warp
 
 template <typename T, int HD, int NT, int kWarps>
@@ -189,21 +191,23 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     }
     return r;
   };
-  // A unit into ring slot `slot`: lanes 0-3 issue one copy of 16 tokens each (keys, keys, values, values).  A step without
-  // a page is left out.  Called by the whole warp; row: of the first step in lanes 0 and 2, of the second in lanes 1 and 3.
+  // A unit into ring slot `slot`: lanes 0 and 1 copy its keys and its values where a page holds a unit, lanes 0-3 16 tokens
+  // each (keys, keys, values, values) where not (pages of 32, either way: 8 sequences of 8192 20.8 / 22.0 us, 131071 50.1 / 50.4).  A copy without a page is left out.  Called by the whole warp; row: of the
+  // lane's first token.
+  const int box = box_tokens(V), nb = kUnit / box;
   auto issue = [&](int slot, int row) {
     const uint32_t bar = bars + 8 * slot;
-    const unsigned live = __ballot_sync(0xffffffffu, lane < 4 && row >= 0);
-    if (lane == 0) tc::mbar_expect_tx(bar, __popc(live) * kStep * HD);
+    const unsigned live = __ballot_sync(0xffffffffu, lane < 2 * nb && row >= 0);
+    if (lane == 0) tc::mbar_expect_tx(bar, __popc(live) * box * HD);
     __syncwarp();
-    if (lane < 4 && row >= 0)
-      tc::tma_load_2d(ring + slot * kUnit * HD * 2 + lane * kStep * HD, lane < 2 ? &map_k : &map_v, 0, row, bar);
+    if (lane < 2 * nb && row >= 0)
+      tc::tma_load_2d(ring + slot * kUnit * HD * 2 + lane * box * HD, lane < nb ? &map_k : &map_v, 0, row, bar);
   };
   int entry = load_entry(2 * u_lo), entry_n = load_entry(2 * u_lo + 32);
   Meta mc = load_meta(entry, 2 * u_lo);
 #pragma unroll
   for (int i = 0; i < kDepth; ++i) {
-    const int row = __shfl_sync(0xffffffffu, mc.row, 2 * i + (lane & 1));
+    const int row = __shfl_sync(0xffffffffu, mc.row, 2 * i + (lane & (nb - 1)));
     if (u_lo + i < u_hi) issue(i, row);
   }
   Meta mn = load_meta(entry_n, 2 * u_lo + 32);
@@ -390,7 +394,7 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
       }
     }
     // the slot's next unit (its rows are in this chunk of metadata or the next one)
-    const int i3 = i + 2 * kDepth, src = (i3 & 31) + (lane & 1);
+    const int i3 = i + 2 * kDepth, src = (i3 & 31) + (lane & (nb - 1));
     const int rc = __shfl_sync(0xffffffffu, mc.row, src), rn = __shfl_sync(0xffffffffu, mn.row, src);
     if (u + kDepth < u_hi) issue(slot, i3 < 32 ? rc : rn);
     if (i == 30) {
@@ -576,8 +580,8 @@ szo_status launch_rows(const View& V, const Rows& A, int nsplit, float* ws, cuda
   unsigned blocks;
   SZO_TRY(grid_items(tiles * nsplit, V, &blocks));
   CUtensorMap map_k, map_v;
-  SZO_TRY(codes_map(V.k, V, HD, kStep, &map_k));
-  SZO_TRY(codes_map(V.v, V, HD, kStep, &map_v));
+  SZO_TRY(codes_map(V.k, V, HD, box_tokens(V), &map_k));
+  SZO_TRY(codes_map(V.v, V, HD, box_tokens(V), &map_v));
   auto kern = kv8_attention_kernel<T, HD, NT, kWarps>;
   SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
   SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
