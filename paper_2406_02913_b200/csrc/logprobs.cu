@@ -188,9 +188,11 @@ __device__ __forceinline__ float largest(const Vec<__nv_bfloat16>& r) { return l
 __device__ __forceinline__ float largest(const Vec<__half>& r) { return largest16<__half2>(r); }
 __device__ __forceinline__ Vec<__nv_bfloat16> at_least(const Vec<__nv_bfloat16>& r, __nv_bfloat16 low) { return at_least16<__nv_bfloat162>(r, low); }
 __device__ __forceinline__ Vec<__half> at_least(const Vec<__half>& r, __half low) { return at_least16<__half2>(r, low); }
-// A logit that stands for -inf: far below what counts, with a finite product
-template <typename T> __device__ __forceinline__ T floor_of(float c) { return narrow<T>(-1e37f / c); }
-template <> __device__ __forceinline__ __half floor_of<__half>(float c) { return narrow<__half>(fmaxf(-1e37f / c, -65504.f)); }
+// A logit that stands for -inf: its product with c is about -2^20, far below every reference that is used with it (those are
+// above -kBigRef), so 2^y is 0, and small enough to stay finite itself for every c >= 1e-30 log2 e and in the products with y
+constexpr float kFloor = -1048576.0f;
+template <typename T> __device__ __forceinline__ T floor_of(float c) { return narrow<T>(kFloor / c); }
+template <> __device__ __forceinline__ __half floor_of<__half>(float c) { return narrow<__half>(fmaxf(kFloor / c, -65504.f)); }
 
 // One thread's statistics.  With c = scale log2 e, the reference logit g and ref = RN(g c):
 //   s = sum 2^y, t = sum 2^y y,  y = x c - ref = (x - g) c + eps,  eps = g c - ref (the rounding of ref, known exactly)

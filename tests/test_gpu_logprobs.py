@@ -264,3 +264,73 @@ def test_binding_refusals(B):
                 lambda: B.szo_token_logprobs_bwd(x, t, x[:, 0].contiguous(), None, x[:, 0].contiguous(), x[:, 0].contiguous())):
         with pytest.raises(B.SzoError):
             bad()
+
+
+def masked_rows(g, V, dt):
+    """Rows as masks make them: half masked, none, everything, all but one, half at the type's lowest value, all but two."""
+    x = values(g, 6, V, dt)
+    x[0, g.random(V) < 0.5] = float("-inf")
+    x[2] = float("-inf")
+    x[3] = float("-inf")
+    x[3, V // 2] = 0.5
+    x[4, g.random(V) < 0.5] = torch.finfo(DT[dt]).min
+    x[5, 2:] = float("-inf")
+    return x
+
+
+def f32(v):
+    return float(np.float32(v))                          # (the scale that the kernel gets)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("scale", [1e-30, 1e-3, 0.02, 0.021, 50.0, 100.0, 1e4, 1e30])
+@pytest.mark.parametrize("V,pad", [(1003, 0), (40003, 2)])
+def test_masked_rows_at_every_scale(B, dt, scale, V, pad):
+    """Odd widths too: the ends of a row that is no whole number of vectors are filled up with -inf."""
+    g = np.random.default_rng(V)
+    x = masked_rows(g, V, dt)
+    store = torch.full((6, V + pad), float("nan"), dtype=DT[dt], device="cuda")
+    store[:, :V] = x.cuda()
+    t = torch.from_numpy(g.integers(-1, V, (6, 3)).astype(np.int32))
+    t[3, 0] = V // 2
+    for top in (0, 5):
+        check(B, x, t, top, f32(scale), store[:, :V])
+    check(B, x.repeat(60, 1), t.repeat(60, 1), 0, f32(scale))          # (a block per row)
+
+
+GRADIENTS = {"wide": [(1e-30, None), (1e-30, 1.0), (1e-3, None), (0.02, 1.0), (0.021, 1.0), (1.0, 100.0), (1.0, 1e4), (1.0, 1e6),
+                      (50.0, 1.0), (50.0, 100.0), (100.0, 1e6), (1e4, 1.0), (1e30, None)],
+             "f16": [(1e-30, None), (1e-3, None), (0.02, 1.0), (0.02, 1e4), (1.0, 100.0), (50.0, 1.0), (50.0, None)]}      # (results within fp16)
+
+
+@pytest.mark.parametrize("dt,scale,size", [(d, *c) for d in ("f32", "bf16", "f16") for c in GRADIENTS["f16" if d == "f16" else "wide"]])
+@pytest.mark.parametrize("V,pad", [(1003, 0), (40003, 2)])
+def test_gradient_of_masked_rows_at_every_scale_and_weight(B, dt, scale, size, V, pad):
+    """A masked token's gradient is 0 (its target's share apart), whatever the scale and the weight of the entropy.  On top of
+    grad_bound: a probability below the fp32 range (2^-126) counts as 0, so its term is off by at most that much (twice: what
+    is below it is 2^y, of which p is 2^y times a number next to 1)."""
+    g = np.random.default_rng(V + 1)
+    scale = f32(scale)
+    x = masked_rows(g, V, dt)
+    store = torch.full((6, V + pad), 7.0, dtype=DT[dt], device="cuda")
+    store[:, :V] = x.cuda()
+    t = g.integers(-1, V, (6, 2)).astype(np.int32)
+    t[0, 0] = int(np.flatnonzero(np.isneginf(x[0].double().numpy()))[0])             # a masked target
+    dl = g.normal(0, 1, (6, 2)).astype(np.float32)
+    de = None if size is None else (size * g.uniform(-1, 1, 6)).astype(np.float32)
+    d_t = torch.from_numpy(t).cuda()
+    r = B.szo_token_logprobs(store[:, :V], d_t, scale=scale)
+    got = B.szo_token_logprobs_bwd(store[:, :V], d_t, r.lse, r.entropy, torch.from_numpy(dl).cuda(), None if de is None else torch.from_numpy(de).cuda(),
+                                   scale=scale).double().cpu().numpy()
+    assert (got[2] == 0).all()                           # nothing left
+    use = np.array([0, 1, 3, 4, 5])
+    xs, de64 = x.double().numpy()[use], None if de is None else de[use].astype(np.float64)
+    want = ref.logprobs_grad(xs, scale, t[use], dl[use].astype(np.float64), de64)
+    tol = grad_bound(want, xs, scale, t[use], dl[use].astype(np.float64), de64, dt)
+    lp, _, ent = ref.logprobs(xs, scale)
+    weight = np.abs(dl[use].astype(np.float64)).sum(1, keepdims=True)
+    if de64 is not None:
+        weight = weight + np.abs(de64)[:, None] * (np.abs(np.where(np.isneginf(lp), 0, lp)) + np.abs(ent)[:, None])
+    tol = tol + scale * 2.0 ** -125 * weight
+    bad = ~(np.abs(got[use] - want) <= tol)
+    assert not bad.any(), (np.argwhere(bad)[:4], got[use][bad][:4], want[bad][:4])
