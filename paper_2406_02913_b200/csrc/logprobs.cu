@@ -541,12 +541,13 @@ token_logprobs_bwd_kernel(const T* logits, int64_t ld, int vocab, float scale, c
   const int n = n_own;
   // With c = scale log2 e, ref = RN(lse log2 e) and y = x c - ref, one fma: p = 2^(y + delta), log p = (y + delta) ln 2 with
   // delta = ref - lse log2 e, so that scale times the formula without its targets is 2^y (A + B y).  Masked logits are raised
-  // to a floor as in the forward pass; where the floor is too near (fp16) or ref too large, the plain form.
+  // to a floor as in the forward pass; where the floor is too near (fp16), ref too large, or A or B so large that a product with the
+  // floor (2^20) may overflow, the plain form.
   const float c = scale * kLog2e, ref = lse * kLog2e, delta = -fmaf(lse, kLog2e, -ref), F = exp2f(delta);
   const float a = -sum_s - gh * ent;                              // p (a - gh log p)
   const float B = -gh * kLn2 * F * scale, A = fmaf(B, delta, a * F * scale);
   const T low = floor_of<T>(c);
-  const bool fast = fabsf(lse) < kBigRef && ref > fmaf(widen<T>(low), c, 200.f);
+  const bool fast = fabsf(lse) < kBigRef && ref > fmaf(widen<T>(low), c, 200.f) && fmaf(fabsf(B), 4e6f, fabsf(A)) < 1e37f;
   const uint64_t c2 = pair(c, c), r2 = pair(-ref, -ref), A2 = pair(A, A), B2 = pair(B, B);
   for (; v < v_hi; v += kUnroll * kThreads) {
     load4(next, v + kUnroll * kThreads);
@@ -566,9 +567,9 @@ token_logprobs_bwd_kernel(const T* logits, int64_t ld, int vocab, float scale, c
           g[i] = unpair(mul2(pair(ex2(f.x), ex2(f.y)), fma2(B2, y, A2)));
         }
       } else {
-        auto plain = [&](float x) {
-          const float lp = fmaxf(__fmul_rn(x, scale) - lse, -120.f);
-          return lse == -INFINITY ? 0.f : isnan(lse) ? lse : scale * ex2(lp * kLog2e) * fmaf(-gh, lp, a);
+        auto plain = [&](float x) {                               // (p times each factor first: nothing overflows that the result does not)
+          const float lp = fmaxf(__fmul_rn(x, scale) - lse, -120.f), p = ex2(lp * kLog2e);
+          return lse == -INFINITY ? 0.f : isnan(lse) ? lse : scale * fmaf(-(p * gh), lp, p * a);
         };
 #pragma unroll
         for (int i = 0; i < kN / 2; ++i) g[i] = make_float2(plain(widen<T>(r[u].x[2 * i])), plain(widen<T>(r[u].x[2 * i + 1])));

@@ -299,7 +299,7 @@ def test_masked_rows_at_every_scale(B, dt, scale, V, pad):
 
 
 GRADIENTS = {"wide": [(1e-30, None), (1e-30, 1.0), (1e-3, None), (0.02, 1.0), (0.021, 1.0), (1.0, 100.0), (1.0, 1e4), (1.0, 1e6),
-                      (50.0, 1.0), (50.0, 100.0), (100.0, 1e6), (1e4, 1.0), (1e30, None)],
+                      (1.0, 1e36), (1.0, 1e37), (1e-3, 1e37), (50.0, 1.0), (50.0, 100.0), (100.0, 1e6), (1e4, 1.0), (1e30, None)],
              "f16": [(1e-30, None), (1e-3, None), (0.02, 1.0), (0.02, 1e4), (1.0, 100.0), (50.0, 1.0), (50.0, None)]}      # (results within fp16)
 
 
