@@ -295,16 +295,15 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
       if (lane == 0) tc::mbar_arrive(bar(kQFull));
       asm volatile("bar.sync %0, %1;" ::"r"(1 + 4 * i + (warp & 3)), "r"(64) : "memory");
     }
-    const float rs = peaks[1][i][0][rr], poison = peaks[1][i][1][rr];
+    const float rs = peaks[1][i][0][rr], poison = rpos < 0 ? 0.f : peaks[1][i][1][rr];      // (padding rows are zeros whatever they hold)
     float m = -INFINITY, l = 0.f;
-    const int limit0 = rpos - p0 - half * (kTile / 2), masked_from = (lo[i] - p0) / kTile;      // (a negative quotient: 0 or below, all masked)
+    const int limit0 = rpos - p0 - half * (kTile / 2);
     // (a wait that gave up changes nothing here: every warp of a row tile meets the others as often, whatever it read)
     for (int j = 0; j < n_kv[i]; ++j) {
       wait_warp(kMeta + (j & 3), j >> 2, 20);
       wait_warp(kSFull + i, j, 20);
       tc::tc_fence_after();
       const Step* st = &meta[j & 3][half * (kTile / kStep / 2)];
-      const int limit = rpos - p0 - j * kTile - half * (kTile / 2);       // columns up to this one are seen
       uint32_t v[32];
       if (p0 + j * kTile + kTile - 1 > lo[i]) {                   // what a row does not see becomes -inf in S itself: one form of the rest
 #pragma unroll 1

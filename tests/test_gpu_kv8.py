@@ -481,3 +481,32 @@ def test_binding_refusals(B):
     with pytest.raises(ValueError):
         B.Kv8Batch(w.d_table.long(), torch.zeros(1, dtype=torch.int32, device="cuda"), 2)
     assert B.device_status() == 0
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("new", [3, 9, 150])
+@pytest.mark.parametrize("cap", [200, 13000])
+def test_padding_rows_of_any_content_are_zeros(B, dt, new, cap):
+    """Rows at negative positions hold whatever was in memory, NaN and infinities among it: zeros come out, and the other rows are
+    those of padding rows of zeros.  With the long page table the positions are cut and joined."""
+    caps, lens = [cap, 200, 200], [2, 0, 64]
+    w = World(B, caps, 1, 16, 64, seed=new)
+    fill(B, w, lens)
+    news = [new, new, min(new, 64) + 1]
+    batch, start, rows = w.batch(lens, news)
+    q = torch.randn(rows, 2, 64, device="cuda").to(DT[dt])
+    dirty = q.clone()
+    pad = torch.zeros(rows, dtype=torch.bool)
+    for b in range(3):
+        pad[start[b]:start[b + 1] - min(lens[b], news[b])] = True
+    at = torch.nonzero(pad)[:, 0].cuda()
+    q[at] = 0
+    dirty[at] = float("inf")
+    dirty[at[::2], :, ::3] = float("nan")
+    dirty[at[1::3], 0] = -float("inf")
+    want, got = torch.full_like(q, 5.0), torch.full_like(q, 5.0)
+    B.szo_attention_kv8(w.cache, batch, q, out=want)
+    B.szo_attention_kv8(w.cache, batch, dirty, out=got)
+    assert (want[at] == 0).all() and not want[start[0]:start[3]].isnan().any()
+    assert torch.equal(got, want)
+    assert B.device_status() == 0
