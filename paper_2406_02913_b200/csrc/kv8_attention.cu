@@ -180,13 +180,13 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   };
   const int32_t* table = V.table + static_cast<int64_t>(b) * V.max_pages;
   const int s_end = min(2 * u_hi, steps);
-  auto load_entry = [&](int s) { return s + lane < s_end ? __ldg(table + ((s + lane) >> (V.page_shift - 4))) : -2; };
-  auto load_meta = [&](int entry, int s) {
+  auto load_entry = [&](int s) { return s + lane < s_end ? __ldg(table + ((s + lane) >> (V.page_shift - 4))) : -1; };
+  auto load_meta = [&](int entry, int s) {                        // (whether an entry is needed goes by its place: any value may stand in the table)
     Meta r{-1, make_float2(0.f, 0.f)};
     if (static_cast<uint32_t>(entry) < static_cast<uint64_t>(V.n_pages)) {
       r.row = ((entry * V.hkv + h) << V.page_shift) + (((s + lane) << 4) & ((1 << V.page_shift) - 1));
       r.sc = __ldg(V.scales + static_cast<int64_t>(entry) * V.hkv + h);
-    } else if (entry != -2) {
+    } else if (s + lane < s_end) {
       report_page(V);
     }
     return r;

@@ -522,16 +522,14 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     // 32: 158 us, in boxes of 16 163)
     const int box = box_tokens(V), boxes = kRawTokens / box;
     const int32_t* table = V.table + static_cast<int64_t>(b) * V.max_pages;
-    auto load_entry = [&](int j) {
-      const int step = (j0 + j) * (kTile / kStep) + lane;
-      return lane < kTile / kStep && step < n_steps ? __ldg(table + (step >> (V.page_shift - 4))) : -2;
-    };
+    auto needed = [&](int j) { return lane < kTile / kStep && (j0 + j) * (kTile / kStep) + lane < n_steps; };
+    auto load_entry = [&](int j) { return needed(j) ? __ldg(table + (((j0 + j) * (kTile / kStep) + lane) >> (V.page_shift - 4))) : -1; };
     int entry = load_entry(0), place = -1, raw = 0;
     uint32_t raw_phase = 1;
     float2 sc = make_float2(0.f, 0.f);
     auto take_entry = [&](int j) {
       const bool there = static_cast<uint32_t>(entry) < static_cast<uint64_t>(V.n_pages);
-      if (entry != -2 && !there) report_page(V);
+      if (!there && needed(j)) report_page(V);                    // (any value may stand in the table)
       place = there ? ((entry * V.hkv + h) << V.page_shift) + ((p0 + j * kTile + lane * kStep) & ((1 << V.page_shift) - 1)) : -1;
       if (there) sc = __ldg(V.scales + static_cast<int64_t>(entry) * V.hkv + h);
     };

@@ -510,3 +510,29 @@ def test_padding_rows_of_any_content_are_zeros(B, dt, new, cap):
     assert (want[at] == 0).all() and not want[start[0]:start[3]].isnan().any()
     assert torch.equal(got, want)
     assert B.device_status() == 0
+
+
+@pytest.mark.parametrize("dt,new", [("bf16", 1), ("f32", 1), ("bf16", 9), ("bf16", 150)])
+@pytest.mark.parametrize("cap", [300, 13000])
+def test_every_page_id_of_no_page_is_reported(B, dt, new, cap):
+    """A needed entry outside [0, n_pages), -2 like any other, is reported by every operator, and its positions are left out."""
+    w = World(B, [cap, 200], 1, 16, 64, seed=6)
+    fill(B, w, [290, 200])
+    out = []
+    for bad in (-1, -2, -3, w.cache.n_pages, -2 ** 31, 2 ** 31 - 1):
+        t = w.d_table.clone()
+        t[0, 2] = bad
+        batch = B.Kv8Batch(t, torch.tensor([290, 200], dtype=torch.int32, device="cuda"), 2 * new)
+        q = torch.from_numpy(np.random.default_rng(1).normal(0, 1, (2 * new, 2, 64))).to(DT[dt]).cuda()
+        assert B.device_status() == 0
+        o = B.szo_attention_kv8(w.cache, batch, q)
+        assert B.device_status() == ERR_ARG, bad
+        B.szo_kv8_read(w.cache, B.Kv8Batch(t, batch.kv_len, 2 * 290))
+        assert B.device_status() == ERR_ARG, bad
+        out.append(o)
+    assert all(torch.equal(o, out[0]) for o in out) and out[0].isfinite().all()
+    # entries that no position needs are not read: -2 behind the last page
+    t = w.d_table.clone()
+    t[0, -(-290 // 16):] = -2
+    B.szo_attention_kv8(w.cache, B.Kv8Batch(t[:1], torch.tensor([290], dtype=torch.int32, device="cuda"), new), q[:new])
+    assert B.device_status() == 0
