@@ -980,11 +980,14 @@ struct szo_model {
   void *kcache = nullptr, *vcache = nullptr;     // [n_layers][max_batch][max_seq][n_kv_heads * head_dim], act dtype
   // 8-bit cache (szo_model_enable_decode_kv8): sequence b owns the pages b * kv8_pages .. of every layer
   uint8_t* kv8_codes = nullptr;                  // [n_layers][keys, values][max_batch * kv8_pages][n_kv_heads][kv8_page][head_dim]
-  float* kv8_scales = nullptr;                   // [n_layers][max_batch * kv8_pages][n_kv_heads][2]
+  float* kv8_scales = nullptr;                   // [n_layers] x kv8_scale_floats: [max_batch * kv8_pages][n_kv_heads][2]
   int32_t *kv8_table = nullptr, *kv8_len = nullptr;    // [max_batch][kv8_pages]; [max_batch], set by every call
   void* kv8_ws = nullptr;
   size_t kv8_ws_bytes = 0;
   int kv8_page = 0, kv8_pages = 0;
+  int64_t kv8_scale_floats() const {             // of a layer; whole 16 bytes, on which every layer's scales have to start
+    return static_cast<int64_t>(round_up(static_cast<size_t>(cfg.max_batch) * kv8_pages * cfg.n_kv_heads * 2, 4));
+  }
   float* h2 = nullptr;                           // [2][d_model]: second copy of the residual stream of a one- or two-row token step
   int sparse_dt = SZO_F32;                       // storage format of the sparse values (szo_model_set_sparse_storage)
   void* S16_out = nullptr;                       // caller-owned mirror of the stored form, or NULL
@@ -1450,7 +1453,7 @@ szo_status run_decode_t(szo_model* m, const int32_t* tokens, int B, int Tn, cons
       }
       const int64_t pages = static_cast<int64_t>(c.max_batch) * m->kv8_pages, bytes = pages * m->kv8_page * dkv;
       uint8_t* codes = m->kv8_codes + l * 2 * bytes;
-      const szo_kv8_cache cache{codes, codes + bytes, m->kv8_scales + l * pages * Hkv * 2, pages, m->kv8_page, Hkv, hd};
+      const szo_kv8_cache cache{codes, codes + bytes, m->kv8_scales + l * m->kv8_scale_floats(), pages, m->kv8_page, Hkv, hd};
       const szo_kv8_batch batch{m->kv8_table, m->kv8_len, nullptr, M, B, m->kv8_pages, Tn};
       SZO_TRY(szo_kv8_write(&cache, &batch, k, v, static_cast<szo_dtype>(act), dkv, dkv, st));
       SZO_TRY(szo_attention_kv8(&cache, &batch, q, d, o, d, static_cast<szo_dtype>(act), H, scale, m->kv8_ws, m->kv8_ws_bytes, st));
@@ -2001,7 +2004,8 @@ szo_status szo_model_enable_decode_kv8(szo_model_t* m, int32_t page_tokens, void
   const int64_t per_seq = ceil_div(c.max_seq, page_tokens), pages = per_seq * c.max_batch;
   SZO_REQUIRE(pages < (int64_t(1) << 31) / page_tokens / c.n_kv_heads, SZO_ERR_SHAPE, "max_batch * max_seq is too large for the 8-bit cache");
   const size_t bytes = static_cast<size_t>(c.n_layers) * 2 * pages * page_tokens * c.n_kv_heads * hd;
-  const size_t scales = static_cast<size_t>(c.n_layers) * pages * c.n_kv_heads * 2 * sizeof(float);
+  m->kv8_pages = static_cast<int>(per_seq);
+  const size_t scales = static_cast<size_t>(c.n_layers) * m->kv8_scale_floats() * sizeof(float);
   // the most that szo_attention_kv8 asks for at these shapes: one partial tile of 256 rows per SM
   const size_t ws = static_cast<size_t>(148) * 256 * (hd + 2) * sizeof(float);
   uint8_t* codes = nullptr;
@@ -2017,7 +2021,6 @@ szo_status szo_model_enable_decode_kv8(szo_model_t* m, int32_t page_tokens, void
   SZO_TRY(enable_decode_common(m, st));
   m->kv8_ws_bytes = ws;
   m->kv8_page = page_tokens;
-  m->kv8_pages = static_cast<int>(per_seq);
   m->kv8_codes = codes;
   return SZO_OK;
 }

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from oracle import model_oracle as mo
+from paper_2406_02913_b200 import workloads as wl
 from tests import kv8_reference as ref
 from tests.fixtures import DecoderFixture
 
@@ -243,3 +244,27 @@ def test_generate_and_score_together(B):
         gw = ref.logprobs_grad(lg, 0.9, tt, np.ones((3, 2)), np.ones(3))
         assert np.abs(grad.double().cpu().numpy() - gw).max() <= 2e-5
     assert B.device_status() == 0
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("nseq,seq", [(1, 40), (3, 33)])
+def test_one_key_value_head_and_an_odd_number_of_pages(B, act, nseq, seq, monkeypatch):
+    """Every layer's scales start where szo_kv8_write takes them, whatever pages x heads is (tolerances: above)."""
+    monkeypatch.setitem(wl.MODEL_SHAPES, "tiny_one_kv_head", dict(wl.MODEL_SHAPES["tiny"], n_kv_heads=1, n_layers=3))
+    fx = DecoderFixture("tiny_one_kv_head", seed=6, mask="random", B=nseq, S=seq)
+    om = fx.oracle_model()
+    toks = fx.batch(0)
+    lin_W = om.lin_W(om.S)
+    a, md, tol = (B.SZO_F32, B.MODE_FP32_VALIDATE, 2e-3) if act == "f32" else (B.SZO_BF16, B.MODE_SPARSE_ADD, 4e-2)
+    as_stored = (lambda x: x.float().double()) if act == "f32" else (lambda x: x.bfloat16().double())
+    m = B.Model(fx.shape, fx.names, fx.gpu_tensors(torch, None), torch.from_numpy(fx.S_init.copy()).cuda(), act_dtype=a, linear_mode=md, max_batch=nseq,
+                max_seq=seq)
+    m.enable_decode(kv8_page_tokens=16)
+    cache, at = kv8_cache(om.cfg.n_layers, 16, as_stored), 0
+    for T in (20, 1, 5, 1, 1, 4):
+        want = mo.decode_step(om.cfg, om.params, lin_W, toks[:, at:at + T], cache).numpy()
+        got = m.decode_step(torch.from_numpy(np.ascontiguousarray(toks[:, at:at + T])).cuda(), at).cpu().numpy()
+        at += T
+        assert np.max(np.abs(got - want)) <= tol * np.max(np.abs(want))
+    assert B.device_status() == 0
+    m.close()
