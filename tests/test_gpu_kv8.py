@@ -536,3 +536,21 @@ def test_every_page_id_of_no_page_is_reported(B, dt, new, cap):
     t[0, -(-290 // 16):] = -2
     B.szo_attention_kv8(w.cache, B.Kv8Batch(t[:1], torch.tensor([290], dtype=torch.int32, device="cuda"), new), q[:new])
     assert B.device_status() == 0
+
+
+def test_same_bits_for_ragged_batches_and_chunks(B):
+    """Single tokens of many ragged sequences, chunks with a cut last round: the same bits again, with other calls in between."""
+    g = np.random.default_rng(3)
+    lens = [int(n) for n in g.integers(300, 2500, 32)]
+    w = World(B, lens, 8, 64, 128, seed=23)
+    batch, _, rows = w.batch(lens, lens)
+    B.szo_kv8_write(w.cache, batch, *torch.randn(2, rows, 8, 128, device="cuda").unbind(0))
+    for dt, news in (("bf16", [1] * 32), ("f16", [1] * 32), ("bf16", [200] * 4 + [0] * 28)):
+        batch, _, rows = w.batch(lens, news)
+        q, other = (torch.randn(rows, 32, 128, device="cuda").to(DT[dt]) for _ in range(2))
+        want, got = torch.zeros_like(q), torch.zeros_like(q)
+        B.szo_attention_kv8(w.cache, batch, q, out=want)
+        for _ in range(10):
+            B.szo_attention_kv8(w.cache, batch, other, out=got)
+            B.szo_attention_kv8(w.cache, batch, q, out=got)
+            assert torch.equal(got, want)
