@@ -357,7 +357,10 @@ szo_status szo_kv8_read(const szo_kv8_cache* cache, const szo_kv8_batch* batch, 
 /* Causal softmax attention of the rows over the cache: the query at position p attends to positions 0 .. p of its
  * sequence (its own among them: write first).  o = softmax(scale * q k^T) v, statistics and sums in fp32; q, o: dtype
  * [rows][n_heads*head_dim], rows q_stride / o_stride elements apart; grouped-query attention when n_kv_heads <
- * n_heads; scale finite (1/sqrt(head_dim) for szo_attention's).  A row that attends to nothing (padding) becomes zeros.
+ * n_heads; scale finite (1/sqrt(head_dim) for szo_attention's).  A row that attends to nothing (padding) becomes zeros,
+ * whatever its query holds; the query of another row that holds a NaN or an infinity makes its row NaN.  The products take 16-bit
+ * queries exactly, but for elements below 2^-14 of their row's largest, and the softmax's weights in fp16's 11 bits; fp32 queries and
+ * their weights in two fp16 parts, 22 bits.
  * A NaN element of the cache reaches the rows that attend to it and no others.  workspace: at least
  * szo_attention_kv8_workspace_bytes(cache, batch, n_heads) bytes (0, up to 20 MB otherwise: it depends on the shapes
  * only, not on the lengths), contents irrelevant on entry; calls that may run at the same time need one each. */
@@ -368,8 +371,8 @@ szo_status szo_attention_kv8(const szo_kv8_cache* cache, const szo_kv8_batch* ba
 
 /* ---- Log probabilities of given tokens (the quantity that the losses of Section 2 and the candidate comparison of
  * the classification experiments are made of), with the distribution's entropy and best alternatives.  Row r of
- * logits (dtype SZO_F32, SZO_BF16 or SZO_F16 [rows][vocab], rows row_stride >= vocab elements apart, any alignment of
- * rows) is x = scale * logits[r] (scale in [1e-30, 1e30]: one over the temperature), p = softmax(x):
+ * logits (dtype SZO_F32, SZO_BF16 or SZO_F16 [rows][vocab], rows row_stride >= vocab elements apart; the buffer starts on
+ * 16 bytes, its other rows anywhere) is x = scale * logits[r] (scale in [1e-30, 1e30]: one over the temperature), p = softmax(x):
  *   logp[r][i]   fp32 [rows][n_targets]  x[t] - lse, t = targets[r][i] (int32); 0 where t < 0 (padding); t >= vocab:
  *                NaN, and the device status word reports SZO_ERR_INVALID_ARG.  n_targets in [0, 64]
  *   entropy[r]   fp32 [rows] or NULL     - sum p log p (terms with p = 0 count nothing)

@@ -412,7 +412,7 @@ class Kv8Batch:
     """Which rows of a call stand at which cached positions (szo_kv8_batch): page_table int32 [batch, max_pages],
     kv_len int32 [batch] (positions of each sequence, the call's rows among them), start int32 [batch + 1] with
     max_new (rows of each sequence, at most max_new), or None: rows // batch rows each.  The tensors are read
-    when the work runs, so their contents may change between calls."""
+    when the work runs, so their contents may change between calls; they start on 16 bytes."""
 
     def __init__(self, page_table: torch.Tensor, kv_len: torch.Tensor, rows: int, start: torch.Tensor | None = None,
                  max_new: int | None = None):
@@ -490,7 +490,8 @@ def szo_kv8_read(cache: Kv8Cache, batch: Kv8Batch, dtype=torch.bfloat16, out=Non
 
 def szo_attention_kv8(cache: Kv8Cache, batch: Kv8Batch, q: torch.Tensor, scale: float | None = None, out=None):
     """Causal attention of the rows q ([rows, n_heads, head_dim] or [rows, n_heads * head_dim]) over the cache,
-    which already holds their own keys and values.  scale: 1 / sqrt(head_dim) where None.  Returns o like q."""
+    which already holds their own keys and values.  scale: 1 / sqrt(head_dim) where None.  Returns o like q; rows of no
+    sequence are left as they were (without `out`: undefined)."""
     st, rows, d = _kv8_stream(cache, batch), batch.rows, cache.head_dim
     heads = (q.numel() // (rows * d)) if rows else cache.n_kv_heads
     qs = _row_buffer(q, cache.device, rows, heads, d, "q")
@@ -534,7 +535,8 @@ def _logit_rows(logits, targets):
 
 def szo_token_logprobs(logits: torch.Tensor, targets: torch.Tensor | None = None, n_top: int = 0, scale: float = 1.0) -> TokenLogprobs:
     """Log probabilities of targets[r] (int32 [rows, n_targets], negative: none) under softmax(scale * logits[r]), with
-    the entropy, log sum exp and the n_top best alternatives of every row."""
+    the entropy, log sum exp and the n_top best alternatives of every row.  Tensors start on 16 bytes, as everywhere in the
+    library (rows of logits after the first may start anywhere); a view that does not is refused: clone it."""
     rows, vocab, ld, nt, device = _logit_rows(logits, targets)
     # one allocation for the results; every part starts on 16 bytes
     r4, t4, a4 = (rows + 3) & ~3, (rows * nt + 3) & ~3, (rows * n_top + 3) & ~3

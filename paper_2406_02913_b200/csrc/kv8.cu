@@ -5,9 +5,10 @@
 // (lengths -> page id -> rows -> amax -> codes) when there are few.  One block owns one (page, head): the
 // amax that sets its scale then needs no second pass and no atomics, and the rows stay in registers
 // between the two uses.  Inside a block a warp owns 16 slots of the keys or of the values, and all its loads are under way
-// before the first is used.  Measured (bf16, 8 heads of 128): 8 x 2048 new positions written in 18.6 us (4.8 TB/s, 0.75 of the
-// measured copy bandwidth; what is left is the chain above, with 2 blocks per SM), contexts of 4 x 8192 read in 33.5 us (5.9
-// TB/s, 0.92); 32 single tokens written in 3.5 us, which is launch and chain.
+// before the first is used.  Measured (8 heads of 128; inputs of several calls in turn, together larger than L2): 8 x 2048 new
+// positions written in 20.8 us from bf16 (4.3 TB/s, 0.67 of the measured copy bandwidth; 18.5 us where the same 90 MB come again and
+// partly stay in L2), 35.7 us from fp32 (4.2 TB/s): what is left is the chain above, with 2 blocks per SM (fp32: 1); contexts of 4 x
+// 8192 read in 34.2 us to bf16 (5.8 TB/s, 0.90), 56.9 us to fp32 (5.8 TB/s); 32 single tokens written in 3.6 us, which is launch and chain.
 #include "kv8.cuh"
 
 namespace szo {

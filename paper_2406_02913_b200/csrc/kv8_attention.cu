@@ -16,8 +16,9 @@
 //     cluster per sequence and head leaves SMs idle (few sequences and heads, long contexts: seven clusters of 16 such
 //     blocks fit this GPU), blocks of 12 warps, one per SM, write their partial results to a workspace and a second,
 //     chained launch joins them.  Both join in a fixed order: the same bits every time.
-// Measured (bf16, 32 heads over 8 of 128): one sequence of 131071 positions 50.1 us (5.4 TB/s, 0.83 of the measured copy
-// bandwidth), 32 of 513 to 8192 57.2 us (5.0 TB/s; the longest sequence's blocks are the last), 64 of 2048 with 40 heads over 40
+// Measured (16-bit, 32 heads over 8 of 128): one sequence of 131071 positions 50.1 to 51.5 us (5.2 to 5.4 TB/s, 0.81 to 0.83 of the
+// measured copy bandwidth), 32 of 513 to 8192, the longest first, 57.2 to 57.9 us (4.9 to 5.0 TB/s; the longest
+// last 59.5, three shuffled orders 61 to 66), 64 of 2048 with 40 heads over 40
 // 195 us (6.9 TB/s: reads alone, faster than the copy), one of 1024 6.9 us (launch, two trips to memory, join).
 //
 // Numbers.  Codes become fp16 exactly (one cvt per two).  A query row is divided by the power of two of its largest

@@ -6,9 +6,9 @@
 // the time that 16-bit logits take to arrive) and the instructions around them (4.5 per logit), so maxima and sums run
 // as packed pairs, the scale and log2 e are one factor of one packed fma, and m moves only when it is exceeded by e^8.
 // lse = m + log s and H = log s - t / s come out of the same pass.  Few rows are cut over the blocks of a cluster and
-// joined through distributed shared memory.  Measured: 4096 x 50272 bf16, one target each, 76 us (5.4 TB/s, 0.84 of the
-// measured copy bandwidth); 2048 x 32000 with 5 best tokens 43 us (without 30); 8 x 32000 with 5 best 7 us, which is the chain
-// of a launch, two trips to memory, the ranking and the join.  Five blocks per SM without best tokens (48 registers; four: 89 us
+// joined through distributed shared memory.  Measured: 4096 x 50272 bf16, two targets each, 76 us (5.4 TB/s, 0.84 of the
+// measured copy bandwidth); 2048 x 32000 bf16 with 5 best tokens 43 us (without 30); 8 x 32000 with 5 best 7 us in bf16 and 7.9 in fp32 (20
+// best: 8.9), which is the chain of a launch, two trips to memory, the ranking and the join.  Five blocks per SM without best tokens (48 registers; four: 89 us
 // for the first), four with (five: 0.9 of the time for 2048 x 32000, 1.1 for 494 x 63388 in fp32).
 //
 // Best alternatives: the n-th largest of 64 groups' largest logits is a lower bound of the row's n-th largest, and only
@@ -482,8 +482,8 @@ token_logprobs_kernel(const T* __restrict__ logits, int64_t ld, int vocab, float
 
 // d_logits[j] = scale * ( sum_i d_logp[i] (1[j = t_i] - p_j) - d_entropy p_j (log p_j + H) ): a stream of one read and one
 // write, which bounds it.  Block = one of `parts` shares of a row's vectors: four vectors per thread are on their way while four
-// are worked on; the row's targets are sorted out once, while the first are.  Measured: 2048 x 32000 bf16 48 us (5.45 TB/s, 0.84
-// of the measured copy bandwidth), 24 x 50271 5.7 us.
+// are worked on; the row's targets are sorted out once, while the first are.  Measured: 2048 x 32000 bf16 48.7 us (5.4 TB/s, 0.84
+// of the measured copy bandwidth), 24 x 50271 fp32 5.4 us.
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 4)
 token_logprobs_bwd_kernel(const T* logits, int64_t ld, int vocab, float scale, const int32_t* __restrict__ targets, int n_targets,
