@@ -369,6 +369,56 @@ szo_status szo_attention_kv8(const szo_kv8_cache* cache, const szo_kv8_batch* ba
                              void* o, int64_t o_stride, szo_dtype dtype, int32_t n_heads, float scale, void* workspace,
                              size_t workspace_bytes, void* stream);
 
+/* ---- The same attention for sequences that continue a shared prompt (candidate answers of a classification prompt,
+ * samples of one question): sequences seqs[g] .. seqs[g+1]-1 are group g, and the whole pages among the first len[g] positions
+ * are the same pages in their tables.  The rows of a group go over those positions together, so that the pages are read once per group and
+ * not once per sequence; the rest of its positions (a last part of a page among them) each sequence reads for itself.
+ *   len   int32 [n_groups]     shared positions, from position 0 on
+ *   seqs  int32 [n_groups+1]   ascending; NULL (n_groups 1): all sequences are one group.  Sequences in no group share nothing
+ *   max_seqs                   the most sequences of a group
+ * All on the device, read when the work runs.  The shared pages are read through the table of the group's first sequence.  A group
+ * whose description does not fit (decreasing or beyond the batch, more than max_seqs sequences, len negative or beyond max_pages *
+ * page_tokens) shares nothing, which leaves results as they are, and the status word reports SZO_ERR_SHAPE.  Results, arguments and errors
+ * otherwise as for szo_attention_kv8, up to the order of sums; rows at positions inside the shared part see what they see there. */
+typedef struct {
+  const int32_t* len;
+  const int32_t* seqs;
+  int32_t n_groups, max_seqs;
+} szo_kv8_prefix;
+size_t szo_attention_kv8_prefix_workspace_bytes(const szo_kv8_cache* cache, const szo_kv8_batch* batch, const szo_kv8_prefix* prefix,
+                                                int32_t n_heads);
+szo_status szo_attention_kv8_prefix(const szo_kv8_cache* cache, const szo_kv8_batch* batch, const szo_kv8_prefix* prefix, const void* q,
+                                    int64_t q_stride, void* o, int64_t o_stride, szo_dtype dtype, int32_t n_heads, float scale,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Next-token cross entropy straight from hidden states (the loss of Section 2 on full sequences), without the logits ever
+ * being stored: with x[r][j] = scale * sum_i h[r][i] W[j][i] (scale in [1e-30, 1e30]: one over the temperature)
+ *   lse[r]  fp32 [rows] or NULL   log sum_j exp x[r][j]
+ *   loss[r] fp32 [rows]           lse[r] - x[r][t], t = targets[r] (int32); 0 where t < 0 (no target); t >= vocab: NaN, and the
+ *                                 device status word reports SZO_ERR_INVALID_ARG
+ * h: dtype (SZO_BF16 or SZO_F16) [rows][d], W: the same dtype [vocab][d], rows h_stride / w_stride elements apart; d and the strides multiples
+ * of 8.  Products are exact, sums fp32.  loss is formed from the other tokens' weights, so it keeps its relative precision
+ * where the target has nearly all the probability.  A row whose logits hold a NaN or +inf has NaN results. */
+size_t szo_head_ce_workspace_bytes(int64_t rows, int64_t vocab, int64_t d);
+szo_status szo_head_ce(const void* h, int64_t h_stride, const void* W, int64_t w_stride, szo_dtype dtype, int64_t rows, int64_t vocab,
+                       int64_t d, float scale, const int32_t* targets, float* loss, float* lse, void* workspace, size_t workspace_bytes,
+                       void* stream);
+/* Its gradient.  With d_loss fp32 [rows] and d_lse fp32 [rows] (NULL: zeros) the gradients of the results and lse as szo_head_ce gave it:
+ *   G[r][j] = scale * ((a + d_lse[r]) p_j - a 1[j = t]),  p_j = exp(x[r][j] - lse[r]),  a = d_loss[r], 0 where t is outside [0, vocab)
+ *   dh = G W      dtype [rows][d],  rows dh_stride apart (NULL: not wanted, as for dW)
+ *   dW = G^T h    dtype [vocab][d], rows dw_stride apart; not added to what is there
+ * G exists only for a piece of the vocabulary at a time, rounded to dtype (for SZO_F16 relative to the power of two of its row's
+ * weights, so that small weights lose nothing); all sums are fp32 and each result is rounded once.  A row that weighs
+ * nothing (no target and d_lse 0, or an lse of -inf) gives dh zeros and adds nothing to dW, whatever its h holds.  In dW of SZO_F16 a row whose
+ * weight is 2^-j of the largest one's enters with h * 2^-j rounded to fp16, so elements of h below 2^(j-14) lose bits.
+ * workspace: szo_head_ce_bwd_workspace_bytes bytes (want_dh, want_dw: whether the pointers are given); contents irrelevant on entry;
+ * calls that may run at the same time need one each, as for szo_head_ce. */
+size_t szo_head_ce_bwd_workspace_bytes(int64_t rows, int64_t vocab, int64_t d, int32_t want_dh, int32_t want_dw);
+szo_status szo_head_ce_bwd(const void* h, int64_t h_stride, const void* W, int64_t w_stride, szo_dtype dtype, int64_t rows, int64_t vocab,
+                           int64_t d, float scale, const int32_t* targets, const float* lse, const float* d_loss, const float* d_lse,
+                           void* dh, int64_t dh_stride, void* dW, int64_t dw_stride, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
 /* ---- Log probabilities of given tokens (the quantity that the losses of Section 2 and the candidate comparison of
  * the classification experiments are made of), with the distribution's entropy and best alternatives.  Row r of
  * logits (dtype SZO_F32, SZO_BF16 or SZO_F16 [rows][vocab], rows row_stride >= vocab elements apart; the buffer starts on

@@ -50,6 +50,10 @@ class Kv8BatchStruct(C.Structure):
                 ("batch", C.c_int32), ("max_pages", C.c_int32), ("max_new", C.c_int32)]
 
 
+class Kv8PrefixStruct(C.Structure):
+    _fields_ = [("len", C.c_void_p), ("seqs", C.c_void_p), ("n_groups", C.c_int32), ("max_seqs", C.c_int32)]
+
+
 class LinearWeights(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("zeros", C.c_void_p),
                 ("idx", C.c_void_p), ("nnz", C.c_int64), ("bias", C.c_void_p)]
@@ -116,6 +120,16 @@ _SIGS = {
     "szo_attention_kv8": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_int32,
                                       C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]),
     "szo_attention_kv8_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_void_p, C.c_int32]),
+    "szo_attention_kv8_prefix": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int,
+                                             C.c_int32, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "szo_attention_kv8_prefix_workspace_bytes": (C.c_size_t, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32]),
+    "szo_head_ce": (C.c_int32, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_float,
+                                C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "szo_head_ce_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
+    "szo_head_ce_bwd": (C.c_int32, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_float,
+                                    C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                    C.c_void_p, C.c_size_t, C.c_void_p]),
+    "szo_head_ce_bwd_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int32]),
     "szo_token_logprobs": (C.c_int32, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_float, C.c_void_p, C.c_int32,
                                        C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "szo_token_logprobs_bwd": (C.c_int32, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_float, C.c_void_p,
@@ -506,6 +520,126 @@ def szo_attention_kv8(cache: Kv8Cache, batch: Kv8Batch, q: torch.Tensor, scale: 
         _check(L.szo_attention_kv8(cache.ref, batch.ref, q.data_ptr(), qs, o.data_ptr(), os_, _DT[q.dtype], heads,
                                    d ** -0.5 if scale is None else scale, None if ws is None else ws.data_ptr(), need, st))
     return o
+
+
+class Kv8Prefix:
+    """Which sequences of a batch share their first positions (szo_kv8_prefix): length int32 [n_groups], the shared
+    positions of each group; seqs int32 [n_groups + 1] with max_seqs (group g is sequences seqs[g] .. seqs[g+1]-1, at most
+    max_seqs), or None: the whole batch is one group.  Read when the work runs, like the batch's tensors."""
+
+    def __init__(self, length: torch.Tensor, seqs: torch.Tensor | None = None, max_seqs: int | None = None):
+        n_groups = length.numel()
+        for name, t in (("length", length), ("seqs", seqs)):
+            if t is not None:
+                _here(t, torch.int32, name)
+                if t.dim() != 1 or not t.is_contiguous():
+                    raise ValueError(f"{name} must be a contiguous vector")
+        if seqs is None:
+            if n_groups != 1:
+                raise ValueError("without seqs there is one group")
+        elif seqs.numel() != n_groups + 1:
+            raise ValueError("seqs must be [n_groups + 1]")
+        elif max_seqs is None:
+            raise ValueError("seqs needs max_seqs, the most sequences of a group")
+        self.length, self.seqs = length, seqs
+        self.struct = Kv8PrefixStruct(length.data_ptr() or None, None if seqs is None else seqs.data_ptr(), n_groups, max_seqs or 0)
+        self.ref = C.addressof(self.struct)
+        self.device = length.get_device()
+
+
+def szo_attention_kv8_prefix(cache: Kv8Cache, batch: Kv8Batch, prefix: Kv8Prefix, q: torch.Tensor, scale: float | None = None, out=None):
+    """szo_attention_kv8 for sequences that continue shared prompts: the pages that the sequences of a group have in common
+    are read once for the group."""
+    st, rows, d = _kv8_stream(cache, batch), batch.rows, cache.head_dim
+    if prefix.device != cache.device:
+        raise ValueError("prefix must be on the cache's device")
+    heads = (q.numel() // (rows * d)) if rows else cache.n_kv_heads
+    qs = _row_buffer(q, cache.device, rows, heads, d, "q")
+    o = torch.empty_like(q) if out is None else out
+    os_ = _row_buffer(o, cache.device, rows, heads, d, "out")
+    if o.dtype != q.dtype:
+        raise ValueError("out must have q's type")
+    if rows:
+        L = lib()
+        need = L.szo_attention_kv8_prefix_workspace_bytes(cache.ref, batch.ref, prefix.ref, heads)
+        ws = torch.empty((need,), dtype=torch.uint8, device=cache.codes.device) if need else None
+        _check(L.szo_attention_kv8_prefix(cache.ref, batch.ref, prefix.ref, q.data_ptr(), qs, o.data_ptr(), os_, _DT[q.dtype], heads,
+                                          d ** -0.5 if scale is None else scale, None if ws is None else ws.data_ptr(), need, st))
+    return o
+
+
+# ------------------------------------------------------------------------------ cross entropy from hidden states
+class HeadCe(NamedTuple):
+    loss: torch.Tensor          # fp32 [rows]
+    lse: torch.Tensor           # fp32 [rows]
+
+
+def _head_rows(h, W, targets):
+    """rows, vocab, d, the row strides and the device of checked arguments."""
+    device = h.get_device()
+    if not h.is_cuda or device != _device():
+        raise ValueError(f"h must be a CUDA tensor of the current device (got {h.device})")
+    if h.dim() != 2 or W.dim() != 2 or W.shape[1] != h.shape[1] or h.dtype != W.dtype or W.get_device() != device:
+        raise ValueError("h must be [rows, d] and W [vocab, d], of the same type and device")
+    if h.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"h and W must be bfloat16 or float16 (got {h.dtype})")
+    (rows, d), vocab = h.shape, W.shape[0]
+    if (d > 1 and (h.stride(1) != 1 or W.stride(1) != 1)):
+        raise ValueError("h and W must have contiguous rows")
+    if targets.dtype != torch.int32 or targets.dim() != 1 or targets.numel() != rows or not targets.is_contiguous() or targets.get_device() != device:
+        raise ValueError("targets must be a contiguous int32 tensor [rows] on h's device")
+    return rows, vocab, d, h.stride(0) if rows > 1 else d, W.stride(0) if vocab > 1 else d, device
+
+
+def szo_head_ce(h: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, scale: float = 1.0) -> HeadCe:
+    """Cross entropy of targets[r] (int32 [rows], negative: none) under softmax(scale * h[r] W^T), and log sum exp of every row;
+    h [rows, d], W [vocab, d], bf16 or fp16.  The logits are never stored."""
+    rows, vocab, d, hs, ws_, device = _head_rows(h, W, targets)
+    r4 = (rows + 3) & ~3
+    f = torch.empty(2 * r4, dtype=torch.float32, device=h.device)     # one allocation, two parts that start on 16 bytes
+    loss, lse = f.as_strided((rows,), (1,), 0), f.as_strided((rows,), (1,), r4)
+    if rows:
+        L = lib()
+        need = L.szo_head_ce_workspace_bytes(rows, vocab, d)
+        ws = torch.empty((need,), dtype=torch.uint8, device=h.device)
+        _check(L.szo_head_ce(h.data_ptr(), hs, W.data_ptr(), ws_, _DT[h.dtype], rows, vocab, d, scale, targets.data_ptr(), loss.data_ptr(),
+                             lse.data_ptr(), ws.data_ptr(), need, _raw_stream(device)))
+    return HeadCe(loss, lse)
+
+
+def szo_head_ce_bwd(h: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, d_loss: torch.Tensor,
+                    d_lse: torch.Tensor | None = None, scale: float = 1.0, need_dh: bool = True, need_dW: bool = True, out_dh=None,
+                    out_dW=None):
+    """Gradient of sum(d_loss * loss) + sum(d_lse * lse) with respect to h and W as (dh, dW), None where not wanted;
+    results go to out_dh and out_dW where given."""
+    rows, vocab, d, hs, ws_, device = _head_rows(h, W, targets)
+
+    def vec(t, name):
+        if t is None:
+            return None
+        if t.dtype != torch.float32 or t.numel() != rows or not t.is_contiguous() or t.get_device() != device:
+            raise ValueError(f"{name} must be a contiguous float32 tensor of {rows} values on h's device")
+        return t.data_ptr() if rows else None
+
+    def out(t, like, name):
+        if t is None:
+            return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+        if t.shape != like.shape or t.dtype != like.dtype or t.get_device() != device or (d > 1 and t.stride(1) != 1):
+            raise ValueError(f"{name} must have the shape, type and device of what it is the gradient of, and contiguous rows")
+        return t
+    p = vec(lse, "lse"), vec(d_loss, "d_loss"), vec(d_lse, "d_lse")
+    dh = out(out_dh, h, "out_dh") if need_dh or out_dh is not None else None
+    dW = out(out_dW, W, "out_dW") if need_dW or out_dW is not None else None
+    if dh is None and dW is None:
+        return None, None
+    L = lib()
+    need = L.szo_head_ce_bwd_workspace_bytes(rows, vocab, d, dh is not None, dW is not None)
+    ws = torch.empty((max(need, 16),), dtype=torch.uint8, device=h.device)
+    _check(L.szo_head_ce_bwd(h.data_ptr(), hs, W.data_ptr(), ws_, _DT[h.dtype], rows, vocab, d, scale, targets.data_ptr(), *p,
+                             None if dh is None else dh.data_ptr(), d if dh is None or rows <= 1 else dh.stride(0),
+                             None if dW is None else dW.data_ptr(), d if dW is None or vocab <= 1 else dW.stride(0), ws.data_ptr(), need,
+                             _raw_stream(device)))
+    return dh, dW
 
 
 # ------------------------------------------------------------------------------ log probabilities

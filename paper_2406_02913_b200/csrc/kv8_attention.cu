@@ -662,6 +662,25 @@ size_t workspace_bytes(const View& V, int H, int hd) {
 
 }  // namespace
 
+szo_status check_rows(const szo_kv8_cache* cache, const void* q, int64_t q_stride, const void* o, int64_t o_stride, szo_dtype dtype,
+                      int32_t n_heads, float scale, const void* workspace) {
+  SZO_REQUIRE(q && o, SZO_ERR_INVALID_ARG, "NULL q or o");
+  SZO_REQUIRE(dtype == SZO_F32 || dtype == SZO_BF16 || dtype == SZO_F16, SZO_ERR_UNSUPPORTED, "dtype must be f32, bf16 or f16");
+  SZO_REQUIRE(n_heads > 0 && n_heads % cache->n_kv_heads == 0, SZO_ERR_SHAPE, "n_heads must be a multiple of n_kv_heads");
+  SZO_REQUIRE(std::isfinite(scale), SZO_ERR_INVALID_ARG, "scale must be finite");
+  const int64_t width = static_cast<int64_t>(n_heads) * cache->head_dim, vec = dtype == SZO_F32 ? 4 : 8;
+  SZO_REQUIRE(q_stride >= width && o_stride >= width, SZO_ERR_SHAPE, "row strides must be at least n_heads * head_dim");
+  SZO_REQUIRE(aligned16(q) && aligned16(o) && aligned16(workspace) && q_stride % vec == 0 && o_stride % vec == 0, SZO_ERR_ALIGNMENT,
+              "buffers and rows must be 16-byte aligned");
+  return SZO_OK;
+}
+szo_status check_sizes(const szo_kv8_cache* cache, const View& V, int32_t n_heads) {
+  SZO_REQUIRE(static_cast<int64_t>(V.max_new) * n_heads <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows and heads");
+  SZO_REQUIRE(cache->n_pages <= 0x7fffffff / cache->n_kv_heads / cache->page_tokens, SZO_ERR_SHAPE,
+              "n_pages * n_kv_heads * page_tokens must be below 2^31");
+  return SZO_OK;
+}
+
 template <typename T, int HD>
 szo_status launch_join(const View& V, const Rows& A, const float* ws, int R, int row_tiles, int nsplit, bool long_first, int64_t item0,
                        int64_t n_items, cudaStream_t st) {
@@ -705,18 +724,9 @@ szo_status szo_attention_kv8(const szo_kv8_cache* cache, const szo_kv8_batch* ba
                              void* stream) {
   kv8::View V;
   SZO_TRY(kv8::make_view(cache, batch, &V));
-  SZO_REQUIRE(q && o, SZO_ERR_INVALID_ARG, "NULL q or o");
-  SZO_REQUIRE(dtype == SZO_F32 || dtype == SZO_BF16 || dtype == SZO_F16, SZO_ERR_UNSUPPORTED, "dtype must be f32, bf16 or f16");
-  SZO_REQUIRE(n_heads > 0 && n_heads % cache->n_kv_heads == 0, SZO_ERR_SHAPE, "n_heads must be a multiple of n_kv_heads");
-  SZO_REQUIRE(std::isfinite(scale), SZO_ERR_INVALID_ARG, "scale must be finite");
-  const int64_t width = static_cast<int64_t>(n_heads) * cache->head_dim, vec = dtype == SZO_F32 ? 4 : 8;
-  SZO_REQUIRE(q_stride >= width && o_stride >= width, SZO_ERR_SHAPE, "row strides must be at least n_heads * head_dim");
-  SZO_REQUIRE(aligned16(q) && aligned16(o) && aligned16(workspace) && q_stride % vec == 0 && o_stride % vec == 0, SZO_ERR_ALIGNMENT,
-              "buffers and rows must be 16-byte aligned");
+  SZO_TRY(kv8::check_rows(cache, q, q_stride, o, o_stride, dtype, n_heads, scale, workspace));
   if (V.batch == 0 || V.max_new == 0 || V.rows == 0) return SZO_OK;
-  SZO_REQUIRE(static_cast<int64_t>(V.max_new) * n_heads <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows and heads");
-  SZO_REQUIRE(cache->n_pages <= 0x7fffffff / cache->n_kv_heads / cache->page_tokens, SZO_ERR_SHAPE,
-              "n_pages * n_kv_heads * page_tokens must be below 2^31");
+  SZO_TRY(kv8::check_sizes(cache, V, n_heads));
   const size_t need = kv8::workspace_bytes(V, n_heads, cache->head_dim);
   SZO_REQUIRE(need == 0 || (workspace && workspace_bytes >= need), SZO_ERR_WORKSPACE, "workspace: %zu bytes needed, %zu given", need,
               workspace ? workspace_bytes : size_t(0));

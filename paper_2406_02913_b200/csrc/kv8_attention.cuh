@@ -18,6 +18,11 @@ struct Rows {
   float scale;
 };
 
+// The checks of a call's row buffers, and of what its kernels count in 32 bits (kv8_attention.cu)
+szo_status check_rows(const szo_kv8_cache* cache, const void* q, int64_t q_stride, const void* o, int64_t o_stride, szo_dtype dtype,
+                      int32_t n_heads, float scale, const void* workspace);
+szo_status check_sizes(const szo_kv8_cache* cache, const View& V, int32_t n_heads);
+
 // Many query rows per key/value head (kv8_attention_tc.cu); 16-bit types only
 template <typename T, int HD> szo_status launch_attention_tc(const View& V, const Rows& A, float* ws, cudaStream_t st);
 size_t workspace_bytes_tc(const View& V, int H, int hd);
