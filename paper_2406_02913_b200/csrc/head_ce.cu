@@ -10,6 +10,7 @@
 #include <cmath>
 
 #include "head_ce.cuh"
+#include "tc_common.cuh"
 
 namespace szo {
 namespace head {
@@ -17,7 +18,6 @@ namespace head {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kSide = 64, kDepthK = 16, kThreads = 256;
 
 template <typename T> __device__ __forceinline__ float widen(T x);
 template <> __device__ __forceinline__ float widen<__half>(__half x) { return __half2float(x); }
@@ -25,63 +25,6 @@ template <> __device__ __forceinline__ float widen<__nv_bfloat16>(__nv_bfloat16 
 template <typename T> __device__ __forceinline__ T narrow(float x);
 template <> __device__ __forceinline__ __half narrow<__half>(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-
-// A product of two 16-bit matrices by strides: sum_k A(m, k) B(n, k), 64 x 64 per block, 4 x 4 per thread.
-template <typename T> struct Operand {
-  const T* p;
-  int64_t s_row, s_k, rows;
-};
-template <typename T>
-__device__ __forceinline__ void tile_product(const Operand<T>& A, const Operand<T>& B, int64_t m0, int64_t n0, int64_t K, float (&acc)[4][4]) {
-  __shared__ float as[kDepthK][kSide + 4], bs[kDepthK][kSide + 4];
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
-  for (int64_t k0 = 0; k0 < K; k0 += kDepthK) {
-    for (int i = threadIdx.x; i < kSide * kDepthK; i += kThreads) {
-      const int r = i / kDepthK, k = i % kDepthK;
-      as[k][r] = m0 + r < A.rows && k0 + k < K ? widen<T>(A.p[(m0 + r) * A.s_row + (k0 + k) * A.s_k]) : 0.f;
-      bs[k][r] = n0 + r < B.rows && k0 + k < K ? widen<T>(B.p[(n0 + r) * B.s_row + (k0 + k) * B.s_k]) : 0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kDepthK; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(as[k][ty * 4 + i], bs[k][tx * 4 + j], acc[i][j]);
-    __syncthreads();
-  }
-}
-
-// Statistics of 64 x 64 logits: grid (row tiles, vocabulary tiles)
-template <typename T>
-__global__ void __launch_bounds__(kThreads) head_stats_kernel(Operand<T> h, Operand<T> W, int64_t d, float c, const int32_t* __restrict__ targets,
-                                                              float2* __restrict__ part, float* __restrict__ xt) {
-  float acc[4][4];
-  const int64_t m0 = static_cast<int64_t>(blockIdx.x) * kSide, n0 = static_cast<int64_t>(blockIdx.y) * kSide;
-  tile_product(h, W, m0, n0, d, acc);
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (int i = 0; i < 4; ++i) {
-    const int64_t r = m0 + ty * 4 + i;
-    const int64_t t = r < h.rows ? targets[r] : -1;
-    float m = -INFINITY, s = 0.f;
-    for (int j = 0; j < 4; ++j) {
-      const int64_t col = n0 + tx * 4 + j;
-      acc[i][j] *= c;
-      if (col == t && t < W.rows) xt[r] = acc[i][j];
-      if (col == t || col >= W.rows) acc[i][j] = -INFINITY;
-      m = fmaxf(m, acc[i][j]);
-    }
-    for (int o = 8; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const float ref = m == -INFINITY ? 0.f : m;
-    for (int j = 0; j < 4; ++j) s += exp2f(acc[i][j] - ref);
-    for (int o = 8; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (tx == 0 && r < h.rows) part[blockIdx.y * h.rows + r] = make_float2(m, s);
-  }
-}
 
 // Joins a row's parts: 32 rows per block, eight warps of parts, joined in warp order
 __global__ void __launch_bounds__(256) head_join_kernel(const float2* __restrict__ part, const float* __restrict__ xt, const int32_t* __restrict__ targets,
@@ -170,72 +113,23 @@ __global__ void head_copy_kernel(const T* __restrict__ h, int64_t h_stride, int6
   *reinterpret_cast<uint4*>(out + r * d + c) = x;
 }
 
+// dh: the sums of a row (of `parts` parts, in their order) times its power of two, rounded
 template <typename T>
-__global__ void __launch_bounds__(kThreads) head_grad_kernel(Operand<T> h, Operand<T> W, int64_t d, int64_t j0, float c, const int32_t* __restrict__ targets,
-                                                             const float4* __restrict__ info, T* __restrict__ G, int64_t g_stride) {
-  float acc[4][4];
-  const int64_t m0 = static_cast<int64_t>(blockIdx.x) * kSide, n0 = static_cast<int64_t>(blockIdx.y) * kSide;
-  tile_product(h, W, m0, n0, d, acc);
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (int i = 0; i < 4; ++i) {
-    const int64_t r = m0 + ty * 4 + i;
-    if (r >= h.rows) continue;
-    const float4 f = info[r];
-    const int64_t t = static_cast<int64_t>(targets[r]) - j0;
-    for (int j = 0; j < 4; ++j) {
-      const int64_t col = n0 + tx * 4 + j;
-      if (col >= W.rows) continue;
-      const float x = fmaf(acc[i][j], c, -f.x), p = exp2f(x);
-      float g = f.y * p;
-      if (col == t) g = fmaf(f.y - f.z, p, f.z * expm1f(x * kLn2));
-      if (f.y == 0.f && f.z == 0.f) g = 0.f;
-      G[r * g_stride + col] = narrow<T>(g);
-    }
-  }
-}
-
-// acc = or += A B^T in fp32
-template <typename T>
-__global__ void __launch_bounds__(kThreads) head_sum_kernel(Operand<T> A, Operand<T> B, int64_t K, float* __restrict__ out, int64_t stride, bool add) {
-  float acc[4][4];
-  const int64_t m0 = static_cast<int64_t>(blockIdx.x) * kSide, n0 = static_cast<int64_t>(blockIdx.y) * kSide;
-  tile_product(A, B, m0, n0, K, acc);
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int64_t r = m0 + ty * 4 + i, col = n0 + tx * 4 + j;
-      if (r >= A.rows || col >= B.rows) continue;
-      float* p = out + r * stride + col;
-      *p = add ? *p + acc[i][j] : acc[i][j];
-    }
-}
-// out = A B^T times the power of two that the rows were brought to, rounded
-template <typename T>
-__global__ void __launch_bounds__(kThreads) head_out_kernel(Operand<T> A, Operand<T> B, int64_t K, T* __restrict__ out, int64_t stride,
-                                                            const int32_t* __restrict__ exponent) {
-  float acc[4][4];
-  const int64_t m0 = static_cast<int64_t>(blockIdx.x) * kSide, n0 = static_cast<int64_t>(blockIdx.y) * kSide;
-  tile_product(A, B, m0, n0, K, acc);
-  const float f = weight_of<T>(exponent);
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int64_t r = m0 + ty * 4 + i, col = n0 + tx * 4 + j;
-      if (r < A.rows && col < B.rows) out[r * stride + col] = narrow<T>(acc[i][j] * f);
-    }
-}
-
-// dh: the sums of a row times its power of two, rounded
-template <typename T>
-__global__ void head_round_kernel(const float* __restrict__ acc, int64_t rows, int64_t d, const float4* __restrict__ info, T* __restrict__ out,
-                                  int64_t stride) {
+__global__ void head_round_kernel(const float* __restrict__ acc, int parts, int64_t rows, int64_t d, const float4* __restrict__ info,
+                                  T* __restrict__ out, int64_t stride) {
   const int64_t per = d / 8, i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
   if (i >= rows * per) return;
   const int64_t r = i / per, c = i % per * 8;
   const float f = info[r].w;
+  float x[8] = {};
+  for (int p = 0; p < parts; ++p) {
+    const float4* from = reinterpret_cast<const float4*>(acc + (p * rows + r) * d + c);
+    const float4 lo = from[0], hi = from[1];
+    x[0] += lo.x, x[1] += lo.y, x[2] += lo.z, x[3] += lo.w, x[4] += hi.x, x[5] += hi.y, x[6] += hi.z, x[7] += hi.w;
+  }
   alignas(16) T y[8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) y[k] = narrow<T>(acc[r * d + c + k] * f);
+  for (int k = 0; k < 8; ++k) y[k] = narrow<T>(x[k] * f);
   *reinterpret_cast<uint4*>(out + r * stride + c) = *reinterpret_cast<const uint4*>(y);
 }
 
@@ -243,48 +137,59 @@ __global__ void head_round_kernel(const float* __restrict__ acc, int64_t rows, i
 struct Shape {
   int64_t rows, vocab, d;
 };
-struct Parts {                                                    // of a workspace, in bytes from its start
-  size_t part, xt, info, exponent, copy, G, acc, total;
+struct Plan {
+  size_t part, xt;                                                // of a workspace, in bytes from its start
+  size_t info, exponent, copy, G[2], acc;
+  size_t total;
   int64_t piece;                                                  // vocabulary rows of a piece
+  int dh_parts;
 };
-Parts forward_parts(const Shape& s) {
-  Parts p = {};
+struct Taker {
   size_t at = 0;
-  auto take = [&](size_t bytes) {
+  size_t operator()(size_t bytes) {
     const size_t from = at;
     at += round_up(bytes, 256);
     return from;
-  };
-  p.part = take(static_cast<size_t>(ceil_div(s.vocab, kSide)) * s.rows * sizeof(float2));
+  }
+};
+int tiles_of(int64_t n) { return static_cast<int>(ceil_div(n, kTile)); }
+Plan forward_plan(const Shape& s) {
+  Plan p = {};
+  Taker take;
+  p.part = take(static_cast<size_t>(2 * tiles_of(s.vocab)) * s.rows * sizeof(float2));
   p.xt = take(static_cast<size_t>(s.rows) * sizeof(float));
-  p.total = at;
+  p.total = take.at;
   return p;
 }
-Parts backward_parts(const Shape& s, bool dh, bool dw) {
-  Parts p = {};
-  size_t at = 0;
-  auto take = [&](size_t bytes) {
-    const size_t from = at;
-    at += round_up(bytes, 256);
-    return from;
-  };
-  p.piece = s.vocab < 8192 ? static_cast<int64_t>(round_up(s.vocab, 64)) : 8192;
+// Pieces: G of one is at most 64 MB (half of L2), and a piece is 8192 to 65536 vocabulary rows.
+Plan backward_plan(const Shape& s, bool dh, bool dw) {
+  Plan p = {};
+  Taker take;
+  int64_t piece = (int64_t(64) << 20) / (2 * s.rows) / kTile * kTile;
+  piece = piece < 8192 ? 8192 : piece > 65536 ? 65536 : piece;
+  p.piece = piece < s.vocab ? piece : static_cast<int64_t>(round_up(s.vocab, kTile));
   p.info = take(static_cast<size_t>(s.rows) * sizeof(float4));
   p.exponent = take(sizeof(int32_t));
   if (dw) p.copy = take(static_cast<size_t>(s.rows) * s.d * 2);
-  p.G = take(static_cast<size_t>(s.rows) * p.piece * 2);
-  if (dh) p.acc = take(static_cast<size_t>(s.rows) * s.d * sizeof(float));
-  p.total = at;
+  for (int i = 0; i < (p.piece < s.vocab ? 2 : 1); ++i) p.G[i] = take(static_cast<size_t>(s.rows) * p.piece * 2);
+  // few tiles of dh: its long sums over the vocabulary are cut so that every pair of SMs has a tile
+  p.dh_parts = 1;
+  const int64_t tiles = static_cast<int64_t>(tiles_of(s.rows)) * tiles_of(s.d), nkb = ceil_div(s.vocab < p.piece ? s.vocab : p.piece, kBlockK);
+  while (p.dh_parts < 16 && tiles * (p.dh_parts + 1) <= 74 && nkb >= 8 * (p.dh_parts + 1)) ++p.dh_parts;
+  if (dh) p.acc = take(static_cast<size_t>(p.dh_parts) * s.rows * s.d * sizeof(float));
+  p.total = take.at;
   return p;
 }
 bool fits(int64_t rows, int64_t vocab, int64_t d) {
-  constexpr int64_t kMost = 0x7fffff00;
-  return rows >= 0 && vocab > 0 && d > 0 && d % 8 == 0 && rows <= kMost && vocab <= kMost && d <= kMost;
+  constexpr int64_t kMost = 0x7fffff00, kTiles = 1 << 25;        // (tiles of a product, and blocks of a launch, are counted in 32 bits)
+  if (rows < 0 || vocab <= 0 || d <= 0 || d % 8 != 0 || rows > kMost || vocab > kMost || d > kMost) return false;
+  const int64_t m = ceil_div(rows, kTile), n = ceil_div(vocab, kTile), k = ceil_div(d, kTile);
+  return m * n <= kTiles && m * k <= kTiles && n * k <= kTiles;
 }
 szo_status check(const void* h, int64_t h_stride, const void* W, int64_t w_stride, szo_dtype dtype, int64_t rows, int64_t vocab, int64_t d,
                  float scale, const int32_t* targets) {
   SZO_REQUIRE(dtype == SZO_BF16 || dtype == SZO_F16, SZO_ERR_UNSUPPORTED, "dtype must be bf16 or f16");
-  SZO_REQUIRE(fits(rows, vocab, d), SZO_ERR_SHAPE, "rows >= 0, vocab > 0 and d a positive multiple of 8, each below 2^31 - 256");
+  SZO_REQUIRE(fits(rows, vocab, d), SZO_ERR_SHAPE, "rows >= 0, vocab > 0 and d a positive multiple of 8, below 2^31 - 256, and each two of them below 2^25 tiles of 256 x 256");
   SZO_REQUIRE(std::isfinite(scale) && scale >= 1e-30f && scale <= 1e30f, SZO_ERR_INVALID_ARG, "scale must be in [1e-30, 1e30]");
   SZO_REQUIRE(W != nullptr && (rows == 0 || (h != nullptr && targets != nullptr)), SZO_ERR_INVALID_ARG, "NULL h, W or targets");
   SZO_REQUIRE(h_stride >= d && w_stride >= d, SZO_ERR_SHAPE, "row strides must be at least d");
@@ -294,61 +199,150 @@ szo_status check(const void* h, int64_t h_stride, const void* W, int64_t w_strid
 }
 unsigned blocks_of(int64_t n, int per) { return static_cast<unsigned>(ceil_div(n, per)); }
 
+template <typename T> constexpr CUtensorMapDataType kMapType =
+    std::is_same<T, __nv_bfloat16>::value ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+// A 16-bit matrix in boxes of 64 elements of `rows_box` rows
 template <typename T>
-szo_status forward(const Shape& s, const T* h, int64_t hs, const T* W, int64_t ws_, float scale, const int32_t* targets, float* loss, float* lse,
-                   unsigned char* ws, int32_t* status, cudaStream_t st) {
-  const Parts p = forward_parts(s);
-  float2* part = reinterpret_cast<float2*>(ws + p.part);
-  float* xt = reinterpret_cast<float*>(ws + p.xt);
-  const int parts = static_cast<int>(ceil_div(s.vocab, kSide));
-  head_stats_kernel<T><<<dim3(blocks_of(s.rows, kSide), parts), kThreads, 0, st>>>(Operand<T>{h, hs, 1, s.rows}, Operand<T>{W, ws_, 1, s.vocab}, s.d,
-                                                                                 scale * kLog2e, targets, part, xt);
-  count_launch();
-  SZO_CHECK_LAUNCH("head_stats_kernel");
-  head_join_kernel<<<blocks_of(s.rows, 32), 256, 0, st>>>(part, xt, targets, s.rows, s.vocab, parts, loss, lse, status);
+szo_status matrix_map(CUtensorMap* map, const T* base, int64_t rows, int64_t cols, int64_t stride, int rows_box) {
+  const uint64_t dims[2] = {static_cast<uint64_t>(cols), static_cast<uint64_t>(rows)}, strides[1] = {static_cast<uint64_t>(stride) * 2};
+  const uint32_t box[2] = {64, static_cast<uint32_t>(rows_box)};
+  return encode_map(map, kMapType<T>, base, 2, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+// An operand: as many rows of a box as there are, up to 128, where its rows are not contracted; 64 where they are
+template <typename T>
+szo_status operand_a(Job* j, const T* base, int64_t rows, int64_t cols, int64_t stride, bool mn) {
+  const int box = mn ? 64 : rows < 128 ? static_cast<int>(round_up(rows, 8)) : 128;
+  j->a_mn = mn;
+  j->a_bytes = mn ? 128 * kBlockK * 2 : box * kBlockK * 2;
+  return matrix_map(&j->a, base, rows, cols, stride, box);
+}
+template <typename T>
+szo_status operand_b(Job* j, const T* base, int64_t rows, int64_t cols, int64_t stride, bool mn, int64_t k0, int64_t n0) {
+  j->b_mn = mn;
+  j->b_k0 = static_cast<int>(k0);
+  j->b_n0 = static_cast<int>(n0);
+  return matrix_map(&j->b, base, rows, cols, stride, mn ? 64 : 128);
+}
+void sizes(Job* j, Kind kind, int64_t m, int64_t n, int64_t k, int parts) {
+  j->kind = kind;
+  j->m_limit = static_cast<int>(m);
+  j->m_tiles = tiles_of(m);
+  j->n_tiles = tiles_of(n);
+  j->nkb = static_cast<int>(ceil_div(k, kBlockK));
+  j->parts = parts;
+  j->units = j->m_tiles * j->n_tiles * parts;
+}
+// Tiles of m in equal bands whose part of A (16-bit) is at most 48 MB: it stays in L2 while B goes by
+int band_of(int64_t m, int64_t k) {
+  const int64_t tiles = tiles_of(m), most = (int64_t(48) << 20) / (kTile * k * 2);
+  if (tiles <= most || most < 1) return 0;
+  return static_cast<int>(ceil_div(tiles, ceil_div(tiles, most)));
+}
+
+template <typename T> struct Inputs {
+  const T* h;
+  int64_t hs;
+  const T* W;
+  int64_t ws;
+  float scale;
+  const int32_t* targets;
+};
+
+template <typename T>
+szo_status forward(const Shape& s, const Inputs<T>& in, float* loss, float* lse, unsigned char* ws, int32_t* status, cudaStream_t st) {
+  const Plan p = forward_plan(s);
+  Jobs P = {};
+  Job& j = P.job[0];
+  SZO_TRY(operand_a(&j, in.h, s.rows, s.d, in.hs, false));
+  SZO_TRY(operand_b(&j, in.W, s.vocab, s.d, in.ws, false, 0, 0));
+  sizes(&j, kStats, s.rows, s.vocab, s.d, 1);
+  j.m_band = band_of(s.rows, s.d);
+  P.n_jobs = 1;
+  P.units = j.units;
+  P.targets = in.targets;
+  P.part = reinterpret_cast<float2*>(ws + p.part);
+  P.xt = reinterpret_cast<float*>(ws + p.xt);
+  P.rows = s.rows;
+  P.n_end = static_cast<int>(s.vocab);
+  P.c = in.scale * kLog2e;
+  P.status = status;
+  SZO_TRY(launch_jobs<T>(P, st));
+  head_join_kernel<<<blocks_of(s.rows, 32), 256, 0, st>>>(P.part, P.xt, in.targets, s.rows, s.vocab, 2 * j.n_tiles, loss, lse, status);
   count_launch();
   SZO_CHECK_LAUNCH("head_join_kernel");
   return SZO_OK;
 }
 
 template <typename T>
-szo_status backward(const Shape& s, const T* h, int64_t hs, const T* W, int64_t ws_, float scale, const int32_t* targets, const float* lse,
-                    const float* d_loss, const float* d_lse, T* dh, int64_t dhs, T* dw, int64_t dws, unsigned char* ws, cudaStream_t st) {
-  const Parts p = backward_parts(s, dh != nullptr, dw != nullptr);
+szo_status backward(const Shape& s, const Inputs<T>& in, const float* lse, const float* d_loss, const float* d_lse, T* dh, int64_t dhs, T* dw, int64_t dws,
+                    unsigned char* ws, int32_t* status, cudaStream_t st) {
+  const Plan p = backward_plan(s, dh != nullptr, dw != nullptr);
   float4* info = reinterpret_cast<float4*>(ws + p.info);
   int32_t* exponent = reinterpret_cast<int32_t*>(ws + p.exponent);
   T* copy = reinterpret_cast<T*>(ws + p.copy);
-  T* G = reinterpret_cast<T*>(ws + p.G);
   float* acc = reinterpret_cast<float*>(ws + p.acc);
   SZO_CHECK_CUDA(cudaMemsetAsync(exponent, 0x80, sizeof(int32_t), st));      // (below every exponent)
-  head_rows_kernel<<<blocks_of(s.rows, 256), 256, 0, st>>>(targets, lse, d_loss, d_lse, s.rows, s.vocab, scale, !std::is_same<T, __nv_bfloat16>::value,
+  head_rows_kernel<<<blocks_of(s.rows, 256), 256, 0, st>>>(in.targets, lse, d_loss, d_lse, s.rows, s.vocab, in.scale, !std::is_same<T, __nv_bfloat16>::value,
                                                          info, exponent);
   count_launch();
   if (dw != nullptr) {
-    head_copy_kernel<T><<<blocks_of(s.rows * (s.d / 8), 256), 256, 0, st>>>(h, hs, s.rows, s.d, info, exponent, copy);
+    head_copy_kernel<T><<<blocks_of(s.rows * (s.d / 8), 256), 256, 0, st>>>(in.h, in.hs, s.rows, s.d, info, exponent, copy);
     count_launch();
   }
-  for (int64_t j0 = 0; j0 < s.vocab; j0 += p.piece) {
-    const int64_t n = s.vocab - j0 < p.piece ? s.vocab - j0 : p.piece;
-    head_grad_kernel<T><<<dim3(blocks_of(s.rows, kSide), blocks_of(n, kSide)), kThreads, 0, st>>>(
-        Operand<T>{h, hs, 1, s.rows}, Operand<T>{W + j0 * ws_, ws_, 1, n}, s.d, j0, scale * kLog2e, targets, info, G, p.piece);
-    count_launch();
-    if (dh != nullptr) {
-      head_sum_kernel<T><<<dim3(blocks_of(s.rows, kSide), blocks_of(s.d, kSide)), kThreads, 0, st>>>(
-          Operand<T>{G, p.piece, 1, s.rows}, Operand<T>{W + j0 * ws_, 1, ws_, s.d}, n, acc, s.d, j0 > 0);
-      count_launch();
+  SZO_CHECK_LAUNCH("head_rows_kernel");
+  // Launch i takes G of piece i and, of piece i - 1, dh and dW: what a launch reads, the launch before it wrote
+  const int pieces = static_cast<int>(ceil_div(s.vocab, p.piece));
+  for (int i = 0; i <= pieces; ++i) {
+    Jobs P = {};
+    P.targets = in.targets;
+    P.info = info;
+    P.exponent = exponent;
+    P.rows = s.rows;
+    P.c = in.scale * kLog2e;
+    P.status = status;
+    if (i > 0) {
+      const int64_t j0 = (i - 1) * p.piece, n = s.vocab - j0 < p.piece ? s.vocab - j0 : p.piece;
+      const T* G = reinterpret_cast<const T*>(ws + p.G[(i - 1) & 1]);
+      if (dh != nullptr) {
+        Job& j = P.job[P.n_jobs++];
+        SZO_TRY(operand_a(&j, G, s.rows, n, p.piece, false));
+        SZO_TRY(operand_b(&j, in.W, s.vocab, s.d, in.ws, true, j0, 0));
+        const uint64_t dims[3] = {static_cast<uint64_t>(s.d), static_cast<uint64_t>(s.rows), static_cast<uint64_t>(p.dh_parts)};
+        const uint64_t strides[2] = {static_cast<uint64_t>(s.d) * 4, static_cast<uint64_t>(s.rows) * s.d * 4};
+        const uint32_t box[3] = {32, 32, 1};
+        SZO_TRY(encode_map(&j.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, acc, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B));
+        const int64_t nkb = ceil_div(n, kBlockK);                 // (a short last piece may have fewer blocks than parts)
+        sizes(&j, kSum, s.rows, s.d, n, nkb < p.dh_parts ? static_cast<int>(nkb) : p.dh_parts);
+        j.add = i > 1;
+      }
+      if (dw != nullptr) {
+        Job& j = P.job[P.n_jobs++];
+        SZO_TRY(operand_a(&j, G, s.rows, n, p.piece, true));
+        SZO_TRY(operand_b(&j, copy, s.rows, s.d, s.d, true, 0, 0));
+        SZO_TRY(matrix_map(&j.out, dw, s.vocab, s.d, dws, 32));
+        sizes(&j, kOut, n, s.d, s.rows, 1);
+        j.out_row0 = static_cast<int>(j0);
+      }
     }
-    if (dw != nullptr) {
-      head_out_kernel<T><<<dim3(blocks_of(n, kSide), blocks_of(s.d, kSide)), kThreads, 0, st>>>(
-          Operand<T>{G, 1, p.piece, n}, Operand<T>{copy, 1, s.d, s.d}, s.rows, dw + j0 * dws, dws, exponent);
-      count_launch();
+    if (i < pieces) {
+      const int64_t j0 = i * p.piece, n = s.vocab - j0 < p.piece ? s.vocab - j0 : p.piece;
+      Job& j = P.job[P.n_jobs++];
+      SZO_TRY(operand_a(&j, in.h, s.rows, s.d, in.hs, false));
+      SZO_TRY(operand_b(&j, in.W, s.vocab, s.d, in.ws, false, 0, j0));
+      SZO_TRY(matrix_map(&j.out, reinterpret_cast<T*>(ws + p.G[i & 1]), s.rows, n, p.piece, 32));
+      sizes(&j, kGrad, s.rows, n, s.d, 1);
+      j.m_band = band_of(s.rows, s.d);
+      P.n_end = static_cast<int>(n);
+      P.target0 = static_cast<int>(j0);
     }
+    for (int k = 0; k < P.n_jobs; ++k) P.units += P.job[k].units;
+    SZO_TRY(launch_jobs<T>(P, st));
   }
   if (dh != nullptr) {
-    head_round_kernel<T><<<blocks_of(s.rows * (s.d / 8), 256), 256, 0, st>>>(acc, s.rows, s.d, info, dh, dhs);
+    head_round_kernel<T><<<blocks_of(s.rows * (s.d / 8), 256), 256, 0, st>>>(acc, p.dh_parts, s.rows, s.d, info, dh, dhs);
     count_launch();
+    SZO_CHECK_LAUNCH("head_round_kernel");
   }
-  SZO_CHECK_LAUNCH("the kernels of szo_head_ce_bwd");
   return SZO_OK;
 }
 
@@ -361,7 +355,7 @@ using namespace szo;
 extern "C" {
 
 size_t szo_head_ce_workspace_bytes(int64_t rows, int64_t vocab, int64_t d) {
-  return head::fits(rows, vocab, d) && rows > 0 ? head::forward_parts({rows, vocab, d}).total : 0;
+  return head::fits(rows, vocab, d) && rows > 0 ? head::forward_plan({rows, vocab, d}).total : 0;
 }
 
 szo_status szo_head_ce(const void* h, int64_t h_stride, const void* W, int64_t w_stride, szo_dtype dtype, int64_t rows, int64_t vocab, int64_t d,
@@ -378,15 +372,16 @@ szo_status szo_head_ce(const void* h, int64_t h_stride, const void* W, int64_t w
   const head::Shape s{rows, vocab, d};
   auto* ws = static_cast<unsigned char*>(workspace);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (dtype == SZO_BF16)
-    return head::forward(s, static_cast<const __nv_bfloat16*>(h), h_stride, static_cast<const __nv_bfloat16*>(W), w_stride, scale, targets, loss, lse, ws,
-                         status, st);
-  return head::forward(s, static_cast<const __half*>(h), h_stride, static_cast<const __half*>(W), w_stride, scale, targets, loss, lse, ws, status, st);
+  auto run = [&](auto zero) {
+    using T = decltype(zero);
+    return head::forward<T>(s, {static_cast<const T*>(h), h_stride, static_cast<const T*>(W), w_stride, scale, targets}, loss, lse, ws, status, st);
+  };
+  return dtype == SZO_BF16 ? run(__nv_bfloat16{}) : run(__half{});
 }
 
 size_t szo_head_ce_bwd_workspace_bytes(int64_t rows, int64_t vocab, int64_t d, int32_t want_dh, int32_t want_dw) {
   if (!head::fits(rows, vocab, d) || rows == 0 || (!want_dh && !want_dw)) return 0;
-  return head::backward_parts({rows, vocab, d}, want_dh != 0, want_dw != 0).total;
+  return head::backward_plan({rows, vocab, d}, want_dh != 0, want_dw != 0).total;
 }
 
 szo_status szo_head_ce_bwd(const void* h, int64_t h_stride, const void* W, int64_t w_stride, szo_dtype dtype, int64_t rows, int64_t vocab, int64_t d,
@@ -409,11 +404,14 @@ szo_status szo_head_ce_bwd(const void* h, int64_t h_stride, const void* W, int64
               workspace ? workspace_bytes : size_t(0));
   const head::Shape s{rows, vocab, d};
   auto* ws = static_cast<unsigned char*>(workspace);
-  if (dtype == SZO_BF16)
-    return head::backward(s, static_cast<const __nv_bfloat16*>(h), h_stride, static_cast<const __nv_bfloat16*>(W), w_stride, scale, targets, lse, d_loss,
-                          d_lse, static_cast<__nv_bfloat16*>(dh), dh_stride, static_cast<__nv_bfloat16*>(dW), dw_stride, ws, st);
-  return head::backward(s, static_cast<const __half*>(h), h_stride, static_cast<const __half*>(W), w_stride, scale, targets, lse, d_loss, d_lse,
-                        static_cast<__half*>(dh), dh_stride, static_cast<__half*>(dW), dw_stride, ws, st);
+  int32_t* status = device_status_word();
+  SZO_REQUIRE(status != nullptr, SZO_ERR_CUDA, "no device status word (no CUDA device?)");
+  auto run = [&](auto zero) {
+    using T = decltype(zero);
+    return head::backward<T>(s, {static_cast<const T*>(h), h_stride, static_cast<const T*>(W), w_stride, scale, targets}, lse, d_loss, d_lse,
+                             static_cast<T*>(dh), dh_stride, static_cast<T*>(dW), dw_stride, ws, status, st);
+  };
+  return dtype == SZO_BF16 ? run(__nv_bfloat16{}) : run(__half{});
 }
 
 }  // extern "C"

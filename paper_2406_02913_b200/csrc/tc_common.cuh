@@ -258,6 +258,9 @@ __device__ __forceinline__ uint4 dequant_word(uint32_t w, float2 p) {
 
 }  // namespace tc
 
+// Tensor map of rank 2 or 3, dims and box innermost first, strides (bytes) of the dimensions after the first; zero fill (gemm_tc.cu).
+szo_status encode_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,
+                      const uint32_t* box, CUtensorMapSwizzle swizzle);
 // Tensor map of a row-major matrix [rows, cols], box [box_rows x box_cols], zero fill (gemm_tc.cu).
 szo_status encode_map_2d(CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t rows, int64_t cols, int elem_bytes,
                          int box_rows, int box_cols, CUtensorMapSwizzle swizzle);
