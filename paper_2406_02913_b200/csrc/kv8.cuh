@@ -42,7 +42,7 @@ struct Seq {
   int n, len;
   int64_t row0;
 };
-__device__ __forceinline__ Seq load_seq(const View& V, int b) {
+__device__ __forceinline__ bool read_seq(const View& V, int b, Seq* out) {      // false: it does not fit
   Seq s{V.max_new, V.kv_len[b], static_cast<int64_t>(b) * V.max_new};
   bool ok = s.len >= 0 && s.len <= static_cast<int64_t>(V.max_pages) << V.page_shift;
   if (V.start != nullptr) {
@@ -51,10 +51,13 @@ __device__ __forceinline__ Seq load_seq(const View& V, int b) {
     s.n = s1 - s0;
     ok = ok && s0 >= 0 && s1 >= s0 && s1 <= V.rows && s.n <= V.max_new;
   }
-  if (!ok) {
-    atomicExch(V.status, static_cast<int32_t>(SZO_ERR_SHAPE));
-    s.n = s.len = 0;
-  }
+  if (!ok) s.n = s.len = 0;
+  *out = s;
+  return ok;
+}
+__device__ __forceinline__ Seq load_seq(const View& V, int b) {
+  Seq s;
+  if (!read_seq(V, b, &s)) atomicExch(V.status, static_cast<int32_t>(SZO_ERR_SHAPE));
   return s;
 }
 __device__ __forceinline__ void report_page(const View& V) { atomicExch(V.status, static_cast<int32_t>(SZO_ERR_INVALID_ARG)); }

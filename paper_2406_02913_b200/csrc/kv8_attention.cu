@@ -119,10 +119,10 @@ __host__ __device__ __forceinline__ int box_tokens(const View& V) { return V.pag
 
 template <int HD> constexpr int kRingBytes = kDepth * kUnit * HD * 2;       // per warp
 
-template <typename T, int HD, int NT, int kWarps>
+template <typename T, int HD, int NT, int kWarps, bool kPart = false>
 __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? (kWarps == 4 ? 3 : 1) : 1)
 kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, View V, const T* __restrict__ q,
-                     int64_t q_stride, T* __restrict__ o, int64_t o_stride, int H, float scale_log2e, int row_tiles, int nsplit, float* __restrict__ ws) {
+                     int64_t q_stride, T* __restrict__ o, int64_t o_stride, int H, float scale_log2e, int row_tiles, int nsplit, float* __restrict__ ws, const Part part_of) {
   constexpr int R = 8 * NT, kK = HD / 16, kRing = kRingBytes<HD>;
   constexpr bool kSplit = sizeof(T) == 4;
   static_assert(R * HD * 4 <= kRing, "a warp's partial result takes the place of its ring");
@@ -143,7 +143,9 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   const int rt = item % row_tiles;
   item /= row_tiles;
   const int h = item % V.hkv, b = item / V.hkv, G = H / V.hkv;
-  const Seq seq = load_seq(V, b);
+  const Work work = kPart ? load_work(V, part_of, b) : Work{load_seq(V, b), 0, b};
+  const Seq seq = work.seq;
+  const bool prefix = kPart && part_of.prefix;
   const int r0 = rt * R, n_rows = static_cast<int>(min(static_cast<int64_t>(seq.n) * G - r0, static_cast<int64_t>(R)));
   if (n_rows <= 0) return;                                        // (the same in every block of a cluster)
   for (int i = threadIdx.x; i < HD; i += kWarps * 32) nan_at[i] = 0x7fffffff;
@@ -155,7 +157,12 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   }
   __syncwarp();
   const int first = seq.len - seq.n;                              // position of the sequence's row 0; negative: padding
-  const int pos_lo = first + r0 / G, pos_hi = first + (r0 + n_rows - 1) / G;
+  auto last_of = [&](int r) {                                     // the last position that row r of the tile sees
+    if (prefix) return min(__ldg(part_of.pos + seq.row0 + (r0 + r) / G), seq.len - 1);
+    return first + (r0 + r) / G;
+  };
+  int pos_lo = first + r0 / G;
+  const int pos_hi = prefix ? seq.len - 1 : first + (r0 + n_rows - 1) / G;
 
   // this warp's units of two steps; a last unit may have one
   const int steps = pos_hi < 0 ? 0 : pos_hi / kStep + 1, units = (steps + 1) / 2;
@@ -179,7 +186,7 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     int row;                                                      // -1: no page, or behind this warp's share
     float2 sc;                                                    // as stored
   };
-  const int32_t* table = V.table + static_cast<int64_t>(b) * V.max_pages;
+  const int32_t* table = V.table + static_cast<int64_t>(work.owner) * V.max_pages + (work.skip >> V.page_shift);
   const int s_end = min(2 * u_hi, steps);
   auto load_entry = [&](int s) { return s + lane < s_end ? __ldg(table + ((s + lane) >> (V.page_shift - 4))) : -1; };
   auto load_meta = [&](int entry, int s) {                        // (whether an entry is needed goes by its place: any value may stand in the table)
@@ -262,10 +269,15 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     for (int u = 0; u < 2; ++u) {                                 // this thread's scores are those of rows 2 t, 2 t + 1
       rs[n][u] = __shfl_sync(0xffffffffu, mine, (2 * t + u) * 4);
       const int rr = 8 * n + 2 * t + u;
-      rpos[n][u] = rr < n_rows ? first + (r0 + rr) / G : pos_hi;
+      rpos[n][u] = rr < n_rows ? last_of(rr) : pos_hi;
     }
   }
-  __syncthreads();
+  if (kPart && prefix) {                                          // every row sees all of it, or each unit is masked
+    const int r = threadIdx.x;
+    pos_lo = __syncthreads_and(r >= n_rows || last_of(r) == pos_hi) ? pos_hi : -1;
+  } else {
+    __syncthreads();
+  }
 
   take_scales();
   int slot = 0;
@@ -446,7 +458,18 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
       bm[i] = fmaf(f, part(x)[at], bm[i]);
       rl[i] = fmaf(f, wl[x * R + r], rl[i]);
     }
-    if (first + (r0 + r) / G >= nan_at[d]) bm[i] = __int_as_float(0x7fffffff);
+    if ((prefix ? (r < n_rows ? last_of(r) : -1) : first + (r0 + r) / G) >= nan_at[d]) bm[i] = __int_as_float(0x7fffffff);
+  }
+  if constexpr (kPart) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int at = threadIdx.x + i * kThreads, r = at / HD;
+      if (at >= n_rows * HD) continue;
+      const int64_t row_head = split * part_of.row_heads + (seq.row0 + (r0 + r) / G) * H + h * G + (r0 + r) % G;
+      part_of.sums[row_head * HD + at % HD] = bm[i];
+      if (at % HD == 0) part_of.stats[row_head] = make_float2(rm[i] - kOffset, rl[i]);
+    }
+    return;
   }
   auto store = [&](int r, int d, float sum, float ll) {
     o[(seq.row0 + (r0 + r) / G) * o_stride + (h * G + (r0 + r) % G) * static_cast<int64_t>(HD) + d] =
@@ -573,17 +596,23 @@ szo_status codes_map(const uint8_t* codes, const View& V, int hd, int rows, CUte
                        hd == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
-template <typename T, int HD, int NT, int kWarps>
-szo_status launch_rows(const View& V, const Rows& A, int nsplit, float* ws, cudaStream_t st) {
+template <typename T, int HD, int NT, int kWarps, bool kPart = false>
+szo_status launch_rows(const View& V, const Rows& A, int nsplit, float* ws, cudaStream_t st, const Part& part = Part{}) {
   constexpr int R = 8 * NT;
   const size_t smem = static_cast<size_t>(kWarps) * kRingBytes<HD> + 1024;
-  const int64_t tiles = ceil_div(static_cast<int64_t>(V.max_new) * (A.H / V.hkv), R);
+  const int64_t tiles = ceil_div(static_cast<int64_t>(kPart ? part.max_rows : V.max_new) * (A.H / V.hkv), R);
   unsigned blocks;
-  SZO_TRY(grid_items(tiles * nsplit, V, &blocks));
+  if (kPart) {
+    const int64_t n = tiles * nsplit * part.items * V.hkv;
+    SZO_REQUIRE(n <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows, heads and sequences for one launch");
+    blocks = static_cast<unsigned>(n);
+  } else {
+    SZO_TRY(grid_items(tiles * nsplit, V, &blocks));
+  }
   CUtensorMap map_k, map_v;
   SZO_TRY(codes_map(V.k, V, HD, box_tokens(V), &map_k));
   SZO_TRY(codes_map(V.v, V, HD, box_tokens(V), &map_v));
-  auto kern = kv8_attention_kernel<T, HD, NT, kWarps>;
+  auto kern = kv8_attention_kernel<T, HD, NT, kWarps, kPart>;
   SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
   SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   cudaLaunchConfig_t cfg = {};
@@ -596,9 +625,9 @@ szo_status launch_rows(const View& V, const Rows& A, int nsplit, float* ws, cuda
   attr[0].val.clusterDim.x = nsplit;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = nsplit > 1 && ws == nullptr ? 1 : 0;
+  cfg.numAttrs = nsplit > 1 && ws == nullptr && !kPart ? 1 : 0;
   SZO_CHECK_CUDA(cudaLaunchKernelEx(&cfg, kern, map_k, map_v, V, static_cast<const T*>(A.q), A.q_stride, static_cast<T*>(A.o), A.o_stride, A.H,
-                                    A.scale * 1.4426950408889634f, static_cast<int>(tiles), nsplit, ws));
+                                    A.scale * 1.4426950408889634f, static_cast<int>(tiles), nsplit, ws, part));
   count_launch();
   if (ws == nullptr) return SZO_OK;
   return launch_join<T, HD>(V, A, ws, R, static_cast<int>(tiles), nsplit, false, 0, tiles * V.batch * V.hkv, st);
@@ -661,6 +690,19 @@ size_t workspace_bytes(const View& V, int H, int hd) {
 }
 
 }  // namespace
+
+template <typename T, int HD> szo_status launch_part(const View& V, const Rows& A, const Part& part, int nsplit, cudaStream_t st) {
+  const int64_t rows = static_cast<int64_t>(part.max_rows) * (A.H / V.hkv);
+  return rows <= 8 ? launch_rows<T, HD, 1, 4, true>(V, A, nsplit, nullptr, st, part) : launch_rows<T, HD, 2, 4, true>(V, A, nsplit, nullptr, st, part);
+}
+#define SZO_KV8_PART(T, HD) template szo_status launch_part<T, HD>(const View&, const Rows&, const Part&, int, cudaStream_t)
+SZO_KV8_PART(float, 64);
+SZO_KV8_PART(float, 128);
+SZO_KV8_PART(__nv_bfloat16, 64);
+SZO_KV8_PART(__nv_bfloat16, 128);
+SZO_KV8_PART(__half, 64);
+SZO_KV8_PART(__half, 128);
+#undef SZO_KV8_PART
 
 szo_status check_rows(const szo_kv8_cache* cache, const void* q, int64_t q_stride, const void* o, int64_t o_stride, szo_dtype dtype,
                       int32_t n_heads, float scale, const void* workspace) {

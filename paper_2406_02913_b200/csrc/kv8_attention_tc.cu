@@ -168,9 +168,9 @@ struct TcSplit {
   int nsplit;
 };
 
-template <typename T, int HD>
+template <typename T, int HD, bool kPart = false>
 __global__ void __launch_bounds__(kTcThreads, 1)
-kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, View V, const T* __restrict__ q, int64_t q_stride, T* __restrict__ o, int64_t o_stride, int H, float scale, int row_tiles, TcSplit part, float* __restrict__ ws) {
+kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, View V, const T* __restrict__ q, int64_t q_stride, T* __restrict__ o, int64_t o_stride, int H, float scale, int row_tiles, TcSplit part, float* __restrict__ ws, const Part part_of) {
   constexpr int kBytes = kTile * HD * 2;                          // of an operand tile
   constexpr int kLanes = HD / 16, kRowsPass = kConv * 32 / kLanes;
   extern __shared__ __align__(1024) unsigned char smem_tc[];
@@ -186,13 +186,15 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   __shared__ int abort_flag;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int64_t others = static_cast<int64_t>(V.batch) * V.hkv;
+  const int64_t others = static_cast<int64_t>(kPart ? part_of.items : V.batch) * V.hkv;
   const bool cut = blockIdx.x >= part.whole;
   const unsigned item = cut ? part.whole + (blockIdx.x - part.whole) / part.nsplit : blockIdx.x;
   const int split = cut ? (blockIdx.x - part.whole) % part.nsplit : 0, nsplit = cut ? part.nsplit : 1;
   const int rt = row_tiles - 1 - static_cast<int>(item / others);                // the longest rows first
   const int h = static_cast<int>(item % others) % V.hkv, b = static_cast<int>(item % others) / V.hkv, G = H / V.hkv;
-  const Seq seq = load_seq(V, b);
+  const Work work = kPart ? load_work(V, part_of, b) : Work{load_seq(V, b), 0, b};
+  const Seq seq = work.seq;
+  const bool prefix = kPart && part_of.prefix;
   const unsigned r0 = static_cast<unsigned>(rt) * 2 * kTile;                     // (rows and heads of a call stay below 2^31)
   const int64_t left = static_cast<int64_t>(seq.n) * G - r0;
   if (left <= 0) return;
@@ -204,16 +206,22 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   for (int i = 0; i < 2; ++i) {
     const int rows = n_rows - kTile * i < kTile ? n_rows - kTile * i : kTile;
     lo[i] = pos_of(kTile * i);
-    const int hi = rows > 0 ? pos_of(kTile * i + rows - 1) : -1;
+    const int hi = rows <= 0 ? -1 : prefix ? seq.len - 1 : pos_of(kTile * i + rows - 1);
     n_kv[i] = hi < 0 ? 0 : hi / kTile + 1;
   }
+  // the last position that row r sees (rows that are not there: anything, they are not stored)
+  auto last_of = [&](int r) {
+    const int rr = r < n_rows ? r : n_rows - 1;
+    if (prefix) return min(__ldg(part_of.pos + seq.row0 + (r0 + rr) / static_cast<unsigned>(G)), seq.len - 1);
+    return pos_of(rr);
+  };
   // this block's steps [j0, j0 + n), counted from j0 from here on
   const int n_all = n_kv[1] > n_kv[0] ? n_kv[1] : n_kv[0];
   const int j0 = static_cast<int>(static_cast<int64_t>(n_all) * split / nsplit), n = static_cast<int>(static_cast<int64_t>(n_all) * (split + 1) / nsplit) - j0;
   const int p0 = j0 * kTile;                                      // position of the first column of step 0
 #pragma unroll
   for (int i = 0; i < 2; ++i) n_kv[i] = min(max(n_kv[i] - j0, 0), n);
-  const int n_steps = (pos_of(n_rows - 1) < 0 ? -1 : pos_of(n_rows - 1) / kStep) + 1;      // of 16 positions
+  const int pos_hi = prefix ? seq.len - 1 : pos_of(n_rows - 1), n_steps = (pos_hi < 0 ? -1 : pos_hi / kStep) + 1;      // of 16 positions
 
   const uint32_t base = (tc::smem_u32(smem_tc) + 1023u) & ~1023u;
   auto v_tile = [&](int s) { return base + s * kBytes; };
@@ -245,7 +253,8 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   for (int i = tid; i < HD; i += kTcThreads) nan_at[i] = 0x7fffffff;
   if (warp == kMmaWarp) tmem_alloc(tc::smem_u32(&tmem_ptr), kTmemCols);
   tc::tc_fence_before();
-  __syncthreads();
+  if (kPart && prefix) lo[0] = lo[1] = __syncthreads_and(tid >= n_rows || last_of(tid) == pos_hi) ? pos_hi : -1;      // (all rows see all of it, or each step is masked)
+  else __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = tmem_ptr;
   auto wait = [&](int i, int phase, unsigned backoff) { return tc::mbar_wait(bar(i), phase & 1, &abort_flag, V.status, backoff); };
@@ -256,7 +265,7 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     const int i = warp >> 3, half = (warp >> 2) & 1, rr = (warp & 3) * 32 + lane, r = i * kTile + rr;      // row tile, columns, row of it, of the block
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_addr = tmem + lanes + i * kTile + half * (kTile / 2), o_addr = tmem + lanes + 2 * kTile + i * kTile + half * (HD / 2);
-    const int rpos = pos_of(r < n_rows ? r : n_rows - 1);         // (rows that are not there: anything, they are not stored)
+    const int rpos = last_of(r);
     // The queries: a warp brings 16 rows, a row's dims over kQLanes lanes, all loads before the first use
     {
       constexpr int kQLanes = HD / 8, kQRows = 32 / kQLanes, kPasses = 16 / kQRows;
@@ -394,10 +403,13 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     l = peaks[0][i][0][rr] + peaks[0][i][1][rr];
     tc::tc_fence_after();
     const int d0 = half * (HD / 2);                               // this thread's share of the row's dims
-    float* wp = ws + static_cast<int64_t>(blockIdx.x - part.whole) * (2 * kTile * (HD + 2));       // (a share's: sums, maxima, sums of weights)
-    const float inv = cut ? 1.f : l == 0.f ? 0.f : 1.0f / l;
+    float* wp = kPart ? part_of.sums : ws + static_cast<int64_t>(blockIdx.x - part.whole) * (2 * kTile * (HD + 2));       // (a share's: sums, maxima, sums of weights)
+    const bool open = kPart || cut;                               // sums go out as they are, to be joined
+    const float inv = open ? 1.f : l == 0.f ? 0.f : 1.0f / l;
     const unsigned at = r0 + r;
-    const int64_t mine = cut ? static_cast<int64_t>(r) * HD + d0
+    const int64_t row_head = split * part_of.row_heads + (seq.row0 + at / static_cast<unsigned>(G)) * H + h * G + at % static_cast<unsigned>(G);
+    const int64_t mine = kPart ? row_head * HD + d0
+                         : cut ? static_cast<int64_t>(r) * HD + d0
                              : (seq.row0 + at / static_cast<unsigned>(G)) * o_stride + (h * G + at % static_cast<unsigned>(G)) * static_cast<int64_t>(HD) + d0;
     // Rows go out through shared memory (all of its tiles are done with), 32 rows of at most 128 bytes per warp: whole
     // lines per store, where a thread that stored its own row would touch 32 lines with each
@@ -431,7 +443,7 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         v[u] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(v[u]) * inv);      // nothing attended to: zeros
         if (rpos >= nan_at[d0 + 32 * c + u]) v[u] = 0x7fffffffu;
       }
-      if (cut) {
+      if (open) {
 #pragma unroll
         for (int u = 0; u < 8; ++u) put(u, v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
         flush(std::integral_constant<int, 8>{}, wp + 32 * c);
@@ -446,8 +458,9 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
         }
       }
     }
-    if (!cut) flush(std::integral_constant<int, HD / 16>{}, o);
-    if (cut && r < n_rows && half == 0) {
+    if (!open) flush(std::integral_constant<int, HD / 16>{}, o);
+    if (kPart && r < n_rows && half == 0) part_of.stats[row_head] = make_float2(m - kTcOffset, l);
+    if (!kPart && cut && r < n_rows && half == 0) {
       wp[2 * kTile * HD + r] = m;
       wp[2 * kTile * (HD + 1) + r] = l;
     }
@@ -521,7 +534,7 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     // A box of the maps is a page's tokens or 64 of them (32 sequences of 12 tokens at 4096 positions, pages of
     // 32: 158 us, in boxes of 16 163)
     const int box = box_tokens(V), boxes = kRawTokens / box;
-    const int32_t* table = V.table + static_cast<int64_t>(b) * V.max_pages;
+    const int32_t* table = V.table + static_cast<int64_t>(work.owner) * V.max_pages + (work.skip >> V.page_shift);
     auto needed = [&](int j) { return lane < kTile / kStep && (j0 + j) * (kTile / kStep) + lane < n_steps; };
     auto load_entry = [&](int j) { return needed(j) ? __ldg(table + (((j0 + j) * (kTile / kStep) + lane) >> (V.page_shift - 4))) : -1; };
     int entry = load_entry(0), place = -1, raw = 0;
@@ -654,25 +667,40 @@ size_t workspace_bytes_tc(const View& V, int H, int hd) {
   return static_cast<size_t>(p.items - p.whole) * p.nsplit * 2 * kTile * (hd + 2) * sizeof(float);
 }
 
-template <typename T, int HD>
-szo_status launch_attention_tc(const View& V, const Rows& A, float* ws, cudaStream_t st) {
-  const TcCut p = tc_plan(V, A.H);
-  SZO_REQUIRE(p.items <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows, heads and sequences for one launch");
+template <typename T, int HD, bool kPart>
+szo_status launch_tc(const View& V, const Rows& A, int64_t tiles, unsigned blocks, TcSplit cut, float* ws, const Part& part, cudaStream_t st) {
   const int smem = 6 * kTile * HD * 2 + kRawSlots * kRawTokens * HD + 1024;
   CUtensorMap map_k, map_v;
   const int64_t rows = (V.n_pages * V.hkv) << V.page_shift;
   SZO_TRY(encode_map_2d(&map_k, CU_TENSOR_MAP_DATA_TYPE_UINT8, V.k, rows, HD, 1, box_tokens(V), HD, CU_TENSOR_MAP_SWIZZLE_NONE));
   SZO_TRY(encode_map_2d(&map_v, CU_TENSOR_MAP_DATA_TYPE_UINT8, V.v, rows, HD, 1, box_tokens(V), HD, CU_TENSOR_MAP_SWIZZLE_NONE));
-  auto kern = kv8_attention_tc_kernel<T, HD>;
+  auto kern = kv8_attention_tc_kernel<T, HD, kPart>;
   SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  const unsigned blocks = static_cast<unsigned>(p.whole + (p.items - p.whole) * p.nsplit);
   kern<<<blocks, kTcThreads, smem, st>>>(map_k, map_v, V, static_cast<const T*>(A.q), A.q_stride, static_cast<T*>(A.o), A.o_stride, A.H, A.scale,
-                                         static_cast<int>(p.tiles), TcSplit{static_cast<unsigned>(p.whole), p.nsplit}, ws);
+                                         static_cast<int>(tiles), cut, ws, part);
   count_launch();
   SZO_CHECK_LAUNCH("kv8_attention_tc_kernel");
+  return SZO_OK;
+}
+
+template <typename T, int HD>
+szo_status launch_attention_tc(const View& V, const Rows& A, float* ws, cudaStream_t st) {
+  const TcCut p = tc_plan(V, A.H);
+  SZO_REQUIRE(p.items <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows, heads and sequences for one launch");
+  const unsigned blocks = static_cast<unsigned>(p.whole + (p.items - p.whole) * p.nsplit);
+  SZO_TRY((launch_tc<T, HD, false>(V, A, p.tiles, blocks, TcSplit{static_cast<unsigned>(p.whole), p.nsplit}, ws, Part{}, st)));
   if (p.whole == p.items) return SZO_OK;
   return launch_join<T, HD>(V, A, ws, 2 * kTile, static_cast<int>(p.tiles), p.nsplit, true, p.whole, p.items - p.whole, st);
 }
+template <typename T, int HD> szo_status launch_part_tc(const View& V, const Rows& A, const Part& part, int nsplit, cudaStream_t st) {
+  const int64_t tiles = ceil_div(static_cast<int64_t>(part.max_rows) * (A.H / V.hkv), 2 * kTile), items = tiles * part.items * V.hkv;
+  SZO_REQUIRE(items * nsplit <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows, heads and sequences for one launch");
+  return launch_tc<T, HD, true>(V, A, tiles, static_cast<unsigned>(items * nsplit), TcSplit{0, nsplit}, nullptr, part, st);
+}
+template szo_status launch_part_tc<__nv_bfloat16, 64>(const View&, const Rows&, const Part&, int, cudaStream_t);
+template szo_status launch_part_tc<__nv_bfloat16, 128>(const View&, const Rows&, const Part&, int, cudaStream_t);
+template szo_status launch_part_tc<__half, 64>(const View&, const Rows&, const Part&, int, cudaStream_t);
+template szo_status launch_part_tc<__half, 128>(const View&, const Rows&, const Part&, int, cudaStream_t);
 template szo_status launch_attention_tc<__nv_bfloat16, 64>(const View&, const Rows&, float*, cudaStream_t);
 template szo_status launch_attention_tc<__nv_bfloat16, 128>(const View&, const Rows&, float*, cudaStream_t);
 template szo_status launch_attention_tc<__half, 64>(const View&, const Rows&, float*, cudaStream_t);

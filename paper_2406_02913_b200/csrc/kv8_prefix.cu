@@ -1,7 +1,10 @@
 // Attention over the 8-bit paged cache for sequences that continue shared prompts.
 //
-// A row's softmax over its positions is joined from two parts with their own maxima and sums: the whole pages that its group
-// shares, and the rest of its sequence's positions.
+// A row's softmax over its positions is joined from parts with their own maxima and sums: the whole pages that its group
+// shares, where the rows of all the group's sequences are taken together (so a shared code is read once for 8 to 256 rows of several
+// sequences, and prompts of a few rows each fill tensor-core tiles), and the rest of its sequence's positions.  Both are passes
+// of the attention kernels of kv8_attention.cu and kv8_attention_tc.cu that leave sums, maxima and sums of weights unfinished,
+// each cut into shares of the positions that fill the SMs; a last kernel joins a row's shares in their order.
 #include <cmath>
 
 #include "kv8_prefix.cuh"
@@ -11,63 +14,139 @@ namespace kv8 {
 
 namespace {
 
-// One warp per (row, head): lanes split the head dimension
-template <typename T, int HD>
-__global__ void __launch_bounds__(128) kv8_prefix_row_kernel(View V, Prefix P, const T* __restrict__ q, int64_t q_stride, T* __restrict__ o,
-                                                             int64_t o_stride, int H, float scale_log2e) {
-  constexpr int kPer = HD / 32;
-  const int lane = threadIdx.x & 31;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-  const int head = static_cast<int>(item % H);
-  const int64_t bi = item / H;
-  const int b = static_cast<int>(bi / V.max_new), i = static_cast<int>(bi % V.max_new);
-  if (b >= V.batch) return;
-  if (item == 0)
-    for (int g = lane; g < P.n_groups; g += 32) load_shared(V, P, g, true);
-  const Seq s = load_seq(V, b);
-  if (i >= s.n) return;
-  const Shared sh = load_shared(V, P, group_of(P, b), false);
-  const int h = head / (H / V.hkv), pos = s.len - s.n + i;
-  const int64_t row = s.row0 + i;
-  float x[kPer], m = -INFINITY, l = 0.f, acc[kPer];
-  bool fine = true;
-  for (int k = 0; k < kPer; ++k) {
-    x[k] = widen<T>(q[row * q_stride + static_cast<int64_t>(head) * HD + lane * kPer + k]);
-    fine = fine && isfinite(x[k]);
-    acc[k] = 0.f;
-  }
-  fine = __all_sync(0xffffffffu, fine);
-  for (int p = 0; p <= pos; ++p) {
-    const int page = load_page(V, p < sh.len ? sh.first : b, p >> V.page_shift);
-    if (page < 0) continue;
-    const int64_t at = page_offset(V, page, h, HD) + static_cast<int64_t>(p & ((1 << V.page_shift) - 1)) * HD + lane * kPer;
-    const float2 sc = V.scales[static_cast<int64_t>(page) * V.hkv + h];
-    float dot = 0.f, v[kPer];
-    for (int k = 0; k < kPer; ++k) {
-      dot = fmaf(x[k], decode2f(V.k[at + k]).x, dot);
-      v[k] = decode2f(V.v[at + k]).x * exp2_int(scale_exponent(sc.y));
+// What the passes read of the groups (block g) and of the sequences that share nothing (the last block).  A group with a
+// sequence whose description does not fit shares nothing: its rows could not be told apart.
+__global__ void __launch_bounds__(256) kv8_groups_kernel(View V, Prefix P, int4* __restrict__ groups, int32_t* __restrict__ shared, int32_t* __restrict__ pos) {
+  const int g = blockIdx.x;
+  if (g == P.n_groups) {
+    for (int b = threadIdx.x; b < V.batch; b += blockDim.x) {
+      const int mine = group_of(P, b);
+      if (mine < 0 || load_shared(V, P, mine, false).len == 0) shared[b] = 0;
     }
-    for (int off = 16; off; off >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, off);
-    const float t = dot * exp2_int(scale_exponent(sc.x)) * scale_log2e, mn = fmaxf(m, t), ref = mn == -INFINITY ? 0.f : mn;
-    const float c = exp2f(m - ref), w = exp2f(t - ref);
-    m = mn;
-    l = fmaf(l, c, w);
-    for (int k = 0; k < kPer; ++k) acc[k] = fmaf(acc[k], c, w * v[k]);
+    return;
   }
-  for (int k = 0; k < kPer; ++k) {
-    float y = l == 0.f ? 0.f : acc[k] / l;
-    if (!fine && pos >= 0) y = __int_as_float(0x7fffffff);
-    o[row * o_stride + static_cast<int64_t>(head) * HD + lane * kPer + k] = narrow<T>(y);
+  const Shared s = load_shared(V, P, g, threadIdx.x == 0);
+  bool ok = true;
+  for (int b = s.first + threadIdx.x; b < s.last; b += blockDim.x) {
+    Seq q;
+    ok = read_seq(V, b, &q) && group_of(P, b) == g && ok;
+  }
+  const int len = __syncthreads_and(ok) ? s.len : 0;
+  if (threadIdx.x == 0) {
+    const int row0 = len == 0 ? 0 : V.start != nullptr ? V.start[s.first] : s.first * V.max_new;
+    const int rows = len == 0 ? 0 : V.start != nullptr ? V.start[s.last] - row0 : (s.last - s.first) * V.max_new;
+    groups[g] = make_int4(row0, rows, len, s.first);
+  }
+  if (s.len == 0) return;
+  for (int b = s.first + threadIdx.x / 32; b < s.last; b += blockDim.x / 32) {
+    if (group_of(P, b) != g) continue;
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) shared[b] = len;
+    if (len == 0) continue;
+    Seq q;
+    read_seq(V, b, &q);
+    for (int i = lane; i < q.n; i += 32) pos[q.row0 + i] = q.len - q.n + i;
   }
 }
 
-template <typename T, int HD> szo_status launch_prefix(const View& V, const Prefix& P, const Rows& A, float* ws, cudaStream_t st) {
-  const int64_t items = static_cast<int64_t>(V.batch) * V.max_new * A.H;
-  SZO_REQUIRE(items <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows and heads for one launch");
-  kv8_prefix_row_kernel<T, HD><<<static_cast<unsigned>(ceil_div(items, 4)), 128, 0, st>>>(V, P, static_cast<const T*>(A.q), A.q_stride, static_cast<T*>(A.o),
-                                                                                          A.o_stride, A.H, A.scale * 1.4426950408889634f);
+// Joins the shares of the rows of all sequences, HD / 4 threads per row and head: grid (token of a sequence, heads)
+constexpr int kJoinThreads = 256;
+template <typename T, int HD>
+__global__ void __launch_bounds__(kJoinThreads) kv8_shares_kernel(View V, Part part, int n_prefix, int n_own, T* __restrict__ o, int64_t o_stride, int H) {
+  constexpr int kLanes = HD / 4;
+  const int b = blockIdx.x / V.max_new, i = blockIdx.x % V.max_new;
+  const Seq s = load_seq(V, b);
+  const int head = blockIdx.y * (kJoinThreads / kLanes) + threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  if (i >= s.n || head >= H) return;
+  const int from = part.shared[b] > 0 ? 0 : n_prefix, to = n_prefix + n_own;
+  const int64_t at = (s.row0 + i) * H + head;
+  float m = -INFINITY, l = 0.f;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int k = from; k < to; ++k) m = fmaxf(m, part.stats[k * part.row_heads + at].x);
+#pragma unroll 4
+  for (int k = from; k < to; ++k) {
+    const float2 st = part.stats[k * part.row_heads + at];
+    const float4 x = *reinterpret_cast<const float4*>(part.sums + (k * part.row_heads + at) * HD + 4 * lane);
+    const float f = m == -INFINITY ? 1.f : ex2(st.x - m);
+    sum = make_float4(fmaf(f, x.x, sum.x), fmaf(f, x.y, sum.y), fmaf(f, x.z, sum.z), fmaf(f, x.w, sum.w));
+    l = fmaf(f, st.y, l);
+  }
+  const float inv = l == 0.f ? 1.f : 1.f / l;                     // nothing attended to: sums of 0
+  struct alignas(4 * sizeof(T)) Four { T x[4]; };
+  *reinterpret_cast<Four*>(o + (s.row0 + i) * o_stride + static_cast<int64_t>(head) * HD + 4 * lane) =
+      Four{{narrow<T>(sum.x * inv), narrow<T>(sum.y * inv), narrow<T>(sum.z * inv), narrow<T>(sum.w * inv)}};
+}
+
+struct Pass {
+  bool many;                   // the tensor-core kernel for many rows
+  int max_rows, shares;
+};
+struct SharePlan {
+  bool direct;                 // a sequence's own rows fill tiles: nothing to gain, the attention kernels as they are
+  Pass prefix, own;
+  size_t groups, shared, pos, sums, stats, total;
+  int64_t row_heads;
+};
+// How a pass's positions are cut.  The lengths are on the device, so the rule goes by the number of items (owner, head, row
+// tile): as many shares as fill the SMs once (many rows: one block per SM) or twice (few rows), of 2 steps of 128 (units of 32 per warp) of
+// what the page table could hold.
+Pass make_pass(const View& V, int64_t max_rows, int64_t owners, int H, bool wide_type) {
+  const int64_t rows = max_rows * (H / V.hkv), places = static_cast<int64_t>(V.max_pages) << V.page_shift;
+  Pass p{!wide_type && rows > 32, static_cast<int>(max_rows), 1};
+  const int64_t tile = p.many ? 256 : rows <= 8 ? 8 : 16, items = owners * V.hkv * ceil_div(rows, tile);
+  const int64_t room = p.many ? 148 : 296, least = p.many ? 256 : 128;
+  while (p.shares < 32 && items * (p.shares + 1) <= room && places >= least * (p.shares + 1)) ++p.shares;
+  return p;
+}
+SharePlan share_plan(const View& V, const Prefix& P, int H, int hd, bool wide_type) {
+  SharePlan p = {};
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t from = at;
+    at += round_up(bytes, 256);
+    return from;
+  };
+  p.groups = take(static_cast<size_t>(P.n_groups) * sizeof(int4));
+  p.shared = take(static_cast<size_t>(V.batch) * sizeof(int32_t));
+  p.pos = take(static_cast<size_t>(V.rows) * sizeof(int32_t));
+  p.direct = P.n_groups == 0 || static_cast<int64_t>(V.max_new) * (H / V.hkv) >= 256;
+  if (!p.direct) {
+    const int64_t most = static_cast<int64_t>(P.max_seqs) * V.max_new;
+    p.prefix = make_pass(V, most < V.rows ? most : V.rows, P.n_groups, H, wide_type);
+    p.own = make_pass(V, V.max_new, V.batch, H, wide_type);
+    p.row_heads = V.rows * H;
+    const size_t n = static_cast<size_t>(p.prefix.shares + p.own.shares) * p.row_heads;
+    p.sums = take(n * hd * sizeof(float));
+    p.stats = take(n * sizeof(float2));
+  }
+  p.total = at;
+  return p;
+}
+
+template <typename T, int HD>
+szo_status run_pass(const View& V, const Rows& A, const Part& part, const Pass& pass, cudaStream_t st) {
+  if constexpr (sizeof(T) == 2)
+    if (pass.many) return launch_part_tc<T, HD>(V, A, part, pass.shares, st);
+  return launch_part<T, HD>(V, A, part, pass.shares, st);
+}
+template <typename T, int HD>
+szo_status launch_shares(const View& V, const Prefix& P, const Rows& A, const SharePlan& p, const Part& base, cudaStream_t st) {
+  Part part = base;
+  part.prefix = 1;
+  part.items = P.n_groups;
+  part.max_rows = p.prefix.max_rows;
+  if (part.max_rows > 0) SZO_TRY((run_pass<T, HD>(V, A, part, p.prefix, st)));
+  Part own = base;
+  own.sums += p.prefix.shares * base.row_heads * HD;
+  own.stats += p.prefix.shares * base.row_heads;
+  own.items = V.batch;
+  own.max_rows = V.max_new;
+  SZO_TRY((run_pass<T, HD>(V, A, own, p.own, st)));
+  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(V.batch) * V.max_new), static_cast<unsigned>(ceil_div(A.H, kJoinThreads / (HD / 4))));
+  kv8_shares_kernel<T, HD><<<grid, kJoinThreads, 0, st>>>(V, base, p.prefix.shares, p.own.shares, static_cast<T*>(A.o), A.o_stride, A.H);
   count_launch();
-  SZO_CHECK_LAUNCH("kv8_prefix_row_kernel");
+  SZO_CHECK_LAUNCH("kv8_shares_kernel");
   return SZO_OK;
 }
 
@@ -81,8 +160,6 @@ szo_status make_prefix(const szo_kv8_prefix* p, const View& V, Prefix* out) {
   return SZO_OK;
 }
 
-size_t workspace_bytes(const View&, const Prefix&, int, int) { return 0; }
-
 }  // namespace
 }  // namespace kv8
 }  // namespace szo
@@ -95,7 +172,11 @@ size_t szo_attention_kv8_prefix_workspace_bytes(const szo_kv8_cache* cache, cons
   kv8::View V;
   kv8::Prefix P;
   if (kv8::make_view(cache, batch, &V) != SZO_OK || kv8::make_prefix(prefix, V, &P) != SZO_OK || n_heads <= 0 || n_heads % cache->n_kv_heads != 0) return 0;
-  return kv8::workspace_bytes(V, P, n_heads, cache->head_dim);
+  if (V.batch == 0 || V.max_new == 0 || V.rows == 0) return 0;
+  // (for either kind of type: fp32 takes the kernel for few rows throughout, with other shares)
+  const kv8::SharePlan a = kv8::share_plan(V, P, n_heads, cache->head_dim, false), b = kv8::share_plan(V, P, n_heads, cache->head_dim, true);
+  const size_t most = a.total > b.total ? a.total : b.total;
+  return most + (a.direct ? szo_attention_kv8_workspace_bytes(cache, batch, n_heads) : 0);
 }
 
 szo_status szo_attention_kv8_prefix(const szo_kv8_cache* cache, const szo_kv8_batch* batch, const szo_kv8_prefix* prefix, const void* q, int64_t q_stride,
@@ -108,17 +189,33 @@ szo_status szo_attention_kv8_prefix(const szo_kv8_cache* cache, const szo_kv8_ba
   SZO_TRY(kv8::check_rows(cache, q, q_stride, o, o_stride, dtype, n_heads, scale, workspace));
   if (V.batch == 0 || V.max_new == 0 || V.rows == 0) return SZO_OK;
   SZO_TRY(kv8::check_sizes(cache, V, n_heads));
-  const size_t need = kv8::workspace_bytes(V, P, n_heads, cache->head_dim);
+  SZO_REQUIRE(V.rows * n_heads <= 0x7fffffff && static_cast<int64_t>(V.batch) * V.max_new <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows and heads");
+  const size_t need = szo_attention_kv8_prefix_workspace_bytes(cache, batch, prefix, n_heads);
   SZO_REQUIRE(need == 0 || (workspace && workspace_bytes >= need), SZO_ERR_WORKSPACE, "workspace: %zu bytes needed, %zu given", need,
               workspace ? workspace_bytes : size_t(0));
   SZO_TRY(kv8::set_status_word(&V));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  auto* ws = static_cast<unsigned char*>(workspace);
+  const kv8::SharePlan p = kv8::share_plan(V, P, n_heads, cache->head_dim, dtype == SZO_F32);
+  kv8::Part part = {};
+  part.groups = reinterpret_cast<const int4*>(ws + p.groups);
+  part.shared = reinterpret_cast<const int32_t*>(ws + p.shared);
+  part.pos = reinterpret_cast<const int32_t*>(ws + p.pos);
+  part.sums = reinterpret_cast<float*>(ws + p.sums);
+  part.stats = reinterpret_cast<float2*>(ws + p.stats);
+  part.row_heads = p.row_heads;
+  kv8::kv8_groups_kernel<<<static_cast<unsigned>(P.n_groups + 1), 256, 0, st>>>(V, P, reinterpret_cast<int4*>(ws + p.groups),
+                                                                             reinterpret_cast<int32_t*>(ws + p.shared), reinterpret_cast<int32_t*>(ws + p.pos));
+  count_launch();
+  SZO_CHECK_LAUNCH("kv8_groups_kernel");
+  if (p.direct)                                                   // (the groups' descriptions are still looked at)
+    return szo_attention_kv8(cache, batch, q, q_stride, o, o_stride, dtype, n_heads, scale, ws + p.total, workspace_bytes - p.total, stream);
   const kv8::Rows A{q, o, q_stride, o_stride, n_heads, scale};
-  float* ws = static_cast<float*>(workspace);
   const bool wide = cache->head_dim == 128;
-  if (dtype == SZO_F32) return wide ? kv8::launch_prefix<float, 128>(V, P, A, ws, st) : kv8::launch_prefix<float, 64>(V, P, A, ws, st);
-  if (dtype == SZO_BF16) return wide ? kv8::launch_prefix<__nv_bfloat16, 128>(V, P, A, ws, st) : kv8::launch_prefix<__nv_bfloat16, 64>(V, P, A, ws, st);
-  return wide ? kv8::launch_prefix<__half, 128>(V, P, A, ws, st) : kv8::launch_prefix<__half, 64>(V, P, A, ws, st);
+  if (dtype == SZO_F32) return wide ? kv8::launch_shares<float, 128>(V, P, A, p, part, st) : kv8::launch_shares<float, 64>(V, P, A, p, part, st);
+  if (dtype == SZO_BF16)
+    return wide ? kv8::launch_shares<__nv_bfloat16, 128>(V, P, A, p, part, st) : kv8::launch_shares<__nv_bfloat16, 64>(V, P, A, p, part, st);
+  return wide ? kv8::launch_shares<__half, 128>(V, P, A, p, part, st) : kv8::launch_shares<__half, 64>(V, P, A, p, part, st);
 }
 
 }  // extern "C"

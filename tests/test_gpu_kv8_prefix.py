@@ -57,7 +57,7 @@ class SharedWorld(World):
         return self.B.Kv8Prefix(torch.tensor(self.prefixes, dtype=torch.int32, device="cuda"), torch.from_numpy(ends).cuda(), max(self.sizes))
 
 
-def check(B, w, lens, news, H, dt, scale=None, spread=1.0, gap=1, prefix=None, q=None):
+def check(B, w, lens, news, H, dt, scale=None, spread=1.0, gap=1, prefix=None, q=None, skipped=()):
     batch, start, rows = w.batch(lens, news, gap)
     if q is None:
         q = torch.from_numpy(w.g.normal(0, spread, (rows, H, w.d))).to(DT[dt])
@@ -67,7 +67,9 @@ def check(B, w, lens, news, H, dt, scale=None, spread=1.0, gap=1, prefix=None, q
     assert (got[:gap] == 3).all() and (got[rows - gap:] == 3).all()
     sc = scale if scale is not None else 1 / math.sqrt(w.d)
     for b, (n, m) in enumerate(zip(lens, news)):
-        if m == 0:
+        if b in skipped:
+            assert (got[start[b]:start[b + 1]] == 3).all()
+        if m == 0 or b in skipped:
             continue
         k, v = (w.ref.values(w.pages[b], n, which) for which in (0, 1))
         size = 2.0 ** w.ref.e[w.pages[b][np.arange(n) // w.ref.page], :, 1]
@@ -203,17 +205,8 @@ def test_descriptions_that_do_not_fit_share_nothing(B):
     for new in (1, 40):
         bad = list(lens)
         bad[2] = cap + 1
-        batch, start, rows = w.batch(bad, [new] * count)
-        q = torch.randn(rows, 2, 64, dtype=torch.bfloat16, device="cuda")
-        o = torch.full_like(q, 3.0)
-        B.szo_attention_kv8_prefix(w.cache, batch, w.prefix(), q, out=o)
+        check(B, w, bad, [new] * count, 2, "bf16", skipped=(2,))
         assert B.device_status() == ERR_SHAPE
-        good, _, _ = w.batch(lens, [new] * count)
-        want = B.szo_attention_kv8_prefix(w.cache, good, w.prefix(), q)
-        assert (o[start[2]:start[3]] == 3).all()
-        for b in (0, 1, 3, 4, 5):
-            assert torch.equal(o[start[b]:start[b + 1]], want[start[b]:start[b + 1]])
-        assert B.device_status() == 0
     # page ids of no page, in the shared part and behind it
     for at in (1, 9):
         t = w.d_table.clone()
