@@ -17,6 +17,7 @@ namespace head {
 
 namespace {
 
+constexpr int kNoExponent = static_cast<int>(0x80808080u);       // (below every exponent; what a memset of 0x80 leaves)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 template <typename T> __device__ __forceinline__ float widen(T x);
@@ -26,29 +27,43 @@ template <typename T> __device__ __forceinline__ T narrow(float x);
 template <> __device__ __forceinline__ __half narrow<__half>(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-// Joins a row's parts: 32 rows per block, eight warps of parts, joined in warp order
+// Joins a row's parts: kRows rows per block, 256 / kRows threads over the parts of each, joined in their order.  (Few rows: a
+// block each, or a thread's chain of loads is what it waits for: 8 rows of 1000 parts 16 us with 32 rows per block.)
+template <int kRows>
 __global__ void __launch_bounds__(256) head_join_kernel(const float2* __restrict__ part, const float* __restrict__ xt, const int32_t* __restrict__ targets,
                                                         int64_t rows, int64_t vocab, int parts, float* __restrict__ loss, float* __restrict__ lse,
                                                         int32_t* status) {
-  __shared__ float ms[8][32], ss[8][32];
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int64_t r = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+  constexpr int kLanes = 256 / kRows;                             // threads of a row
+  __shared__ float ms[8][kRows], ss[8][kRows];
+  chain_release();
+  chain_wait();
+  const int lane = threadIdx.x % kRows, w = threadIdx.x / kRows, warp = threadIdx.x / 32;
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * kRows + lane;
+  const bool there = r < rows;
+  const float2* p = part + (there ? r : rows - 1);
   float m = -INFINITY, s = 0.f;
-  if (r < rows)
-    for (int i = w; i < parts; i += 8) {
-      const float2 p = part[i * rows + r];
-      const float mn = fmaxf(m, p.x), ref = mn == -INFINITY ? 0.f : mn;
-      s = s * exp2f(m - ref) + p.y * exp2f(p.x - ref);
-      m = mn;
-    }
-  ms[w][lane] = m;
-  ss[w][lane] = s;
+#pragma unroll 8
+  for (int i = w; i < parts; i += kLanes) m = fmaxf(m, p[i * rows].x);
+#pragma unroll
+  for (int o = kRows; o < 32; o *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (threadIdx.x % 32 < kRows) ms[warp][lane] = m;
   __syncthreads();
-  if (w != 0 || r >= rows) return;
+#pragma unroll
   for (int i = 0; i < 8; ++i) m = fmaxf(m, ms[i][lane]);
   const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll 8
+  for (int i = w; i < parts; i += kLanes) {
+    const float2 x = p[i * rows];
+    s += x.y * exp2f(x.x - ref);
+  }
+#pragma unroll
+  for (int o = kRows; o < 32; o *= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (threadIdx.x % 32 < kRows) ss[warp][lane] = s;
+  __syncthreads();
+  if (threadIdx.x >= kRows || !there) return;
   s = 0.f;
-  for (int i = 0; i < 8; ++i) s += ss[i][lane] * exp2f(ms[i][lane] - ref);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s += ss[i][lane];
   const int32_t t = targets[r];
   float out = 0.f, total;
   if (t < 0 || t >= vocab) {
@@ -71,31 +86,48 @@ __global__ void __launch_bounds__(256) head_join_kernel(const float2* __restrict
 
 // What the gradient needs of a row: x = lse in base 2, y = weight of p, z = weight of the target (both times scale and, for fp16, a
 // power of two that brings the larger to [2^13, 2^14)), w = that power's inverse.  Rows that weigh nothing have y = z = 0.
-__global__ void head_rows_kernel(const int32_t* __restrict__ targets, const float* __restrict__ lse, const float* __restrict__ d_loss,
-                                 const float* __restrict__ d_lse, int64_t rows, int64_t vocab, float scale, bool half, float4* __restrict__ info,
-                                 int32_t* __restrict__ exponent) {
-  const int64_t r = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-  if (r >= rows) return;
-  const int32_t t = targets[r];
-  const float a = t >= 0 && t < vocab ? d_loss[r] : 0.f, b = d_lse != nullptr ? d_lse[r] : 0.f, l = lse[r];
-  float y = scale * (a + b), z = scale * a, inv = 1.f;
-  if (l == -INFINITY) y = z = 0.f;
-  if (half && (y != 0.f || z != 0.f)) {
-    const float top = fmaxf(fmaxf(fabsf(y), fabsf(z)), fabsf(scale * b));
-    const int e = min(max(((__float_as_int(top) >> 23) & 255) - 127, -100), 100);      // (rows beyond: as near as it goes)
-    const float f = __int_as_float((13 - e + 127) << 23);
-    y *= f;
-    z *= f;
-    inv = __int_as_float((e - 13 + 127) << 23);
-    atomicMax(exponent, e);
+// One block looks at all rows, so that it knows the largest; more than that many rows go over several, which meet in `exponent`.
+constexpr int kRowThreads = 1024;
+__global__ void __launch_bounds__(kRowThreads) head_rows_kernel(const int32_t* __restrict__ targets, const float* __restrict__ lse,
+                                                                const float* __restrict__ d_loss, const float* __restrict__ d_lse, int64_t rows,
+                                                                int64_t vocab, float scale, bool half, float4* __restrict__ info,
+                                                                int32_t* __restrict__ exponent) {
+  __shared__ int tops[kRowThreads / 32];
+  chain_release();
+  int most = kNoExponent;
+#pragma unroll 2
+  for (int64_t r = static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x; r < rows; r += static_cast<int64_t>(gridDim.x) * kRowThreads) {
+    const int32_t t = targets[r];
+    const float d = d_loss[r], b = d_lse != nullptr ? d_lse[r] : 0.f, l = lse[r], a = t >= 0 && t < vocab ? d : 0.f;
+    float y = scale * (a + b), z = scale * a, inv = 1.f;
+    if (l == -INFINITY) y = z = 0.f;
+    if (half && (y != 0.f || z != 0.f)) {
+      const float top = fmaxf(fmaxf(fabsf(y), fabsf(z)), fabsf(scale * b));
+      const int e = min(max(((__float_as_int(top) >> 23) & 255) - 127, -100), 100);      // (rows beyond: as near as it goes)
+      const float f = __int_as_float((13 - e + 127) << 23);
+      y *= f;
+      z *= f;
+      inv = __int_as_float((e - 13 + 127) << 23);
+      most = max(most, e);
+    }
+    info[r] = make_float4(l * kLog2e, y, z, inv);
   }
-  info[r] = make_float4(l * kLog2e, y, z, inv);
+  most = __reduce_max_sync(0xffffffffu, most);
+  if (threadIdx.x % 32 == 0) tops[threadIdx.x / 32] = most;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  most = __reduce_max_sync(0xffffffffu, tops[threadIdx.x]);
+  if (threadIdx.x != 0) return;
+  if (gridDim.x == 1) *exponent = most;
+  else atomicMax(exponent, most);
 }
 
 // h for dW: rows that weigh nothing become zeros; fp16 rows are brought to the largest weight (exactly but for what falls below fp16's range)
 template <typename T>
 __global__ void head_copy_kernel(const T* __restrict__ h, int64_t h_stride, int64_t rows, int64_t d, const float4* __restrict__ info,
                                  const int32_t* __restrict__ exponent, T* __restrict__ out) {
+  chain_release();
+  chain_wait();
   const int64_t per = d / 8, i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
   if (i >= rows * per) return;
   const int64_t r = i / per, c = i % per * 8;
@@ -117,6 +149,8 @@ __global__ void head_copy_kernel(const T* __restrict__ h, int64_t h_stride, int6
 template <typename T>
 __global__ void head_round_kernel(const float* __restrict__ acc, int parts, int64_t rows, int64_t d, const float4* __restrict__ info,
                                   T* __restrict__ out, int64_t stride) {
+  chain_release();
+  chain_wait();
   const int64_t per = d / 8, i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
   if (i >= rows * per) return;
   const int64_t r = i / per, c = i % per * 8;
@@ -142,7 +176,7 @@ struct Plan {
   size_t info, exponent, copy, G[2], acc;
   size_t total;
   int64_t piece;                                                  // vocabulary rows of a piece
-  int dh_parts;
+  int parts, dh_parts;
 };
 struct Taker {
   size_t at = 0;
@@ -153,10 +187,21 @@ struct Taker {
   }
 };
 int tiles_of(int64_t n) { return static_cast<int>(ceil_div(n, kTile)); }
+constexpr int kPairs = 74;                                        // (of a B200; the rules below only lose balance on another number)
+// Up to this many rows of hidden states are the columns of a product, and not its rows: at 128 both ways take as long
+constexpr int64_t kFewRows = 128;
+bool few(int64_t rows) { return rows <= kFewRows; }
+// Height of tiles over n vocabulary entries that gives every pair of SMs the same share
+int step_of(int64_t n) {
+  const int64_t rounds = ceil_div(tiles_of(n), kPairs);
+  return static_cast<int>(round_up(static_cast<size_t>(ceil_div(n, rounds * kPairs)), 16));
+}
 Plan forward_plan(const Shape& s) {
   Plan p = {};
   Taker take;
-  p.part = take(static_cast<size_t>(2 * tiles_of(s.vocab)) * s.rows * sizeof(float2));
+  const int step = step_of(s.vocab);
+  p.parts = few(s.rows) ? static_cast<int>(ceil_div(s.vocab, step) * 2 * ceil_div(step / 2, 32)) : 2 * tiles_of(s.vocab);
+  p.part = take(static_cast<size_t>(p.parts) * s.rows * sizeof(float2));
   p.xt = take(static_cast<size_t>(s.rows) * sizeof(float));
   p.total = take.at;
   return p;
@@ -172,10 +217,18 @@ Plan backward_plan(const Shape& s, bool dh, bool dw) {
   p.exponent = take(sizeof(int32_t));
   if (dw) p.copy = take(static_cast<size_t>(s.rows) * s.d * 2);
   for (int i = 0; i < (p.piece < s.vocab ? 2 : 1); ++i) p.G[i] = take(static_cast<size_t>(s.rows) * p.piece * 2);
-  // few tiles of dh: its long sums over the vocabulary are cut so that every pair of SMs has a tile
+  // few tiles of dh: its long sums over the vocabulary are cut so that the rounds of tiles over the pairs of SMs are as full
+  // as they get, in parts of 8 blocks of 64 at least
   p.dh_parts = 1;
-  const int64_t tiles = static_cast<int64_t>(tiles_of(s.rows)) * tiles_of(s.d), nkb = ceil_div(s.vocab < p.piece ? s.vocab : p.piece, kBlockK);
-  while (p.dh_parts < 16 && tiles * (p.dh_parts + 1) <= 74 && nkb >= 8 * (p.dh_parts + 1)) ++p.dh_parts;
+  const int64_t tiles = static_cast<int64_t>(few(s.rows) ? 1 : tiles_of(s.rows)) * tiles_of(s.d), nkb = ceil_div(s.vocab < p.piece ? s.vocab : p.piece, kBlockK);
+  double best = 1e30;
+  for (int n = 1; n <= 16 && nkb >= 8 * n && (n == 1 || tiles * n <= 2 * kPairs); ++n) {
+    const double cost = static_cast<double>(ceil_div(tiles * n, kPairs)) * (static_cast<double>(nkb) / n + 8);      // (a unit's fixed part: about 8 blocks)
+    if (cost < best * 0.98) {
+      best = cost;
+      p.dh_parts = n;
+    }
+  }
   if (dh) p.acc = take(static_cast<size_t>(p.dh_parts) * s.rows * s.d * sizeof(float));
   p.total = take.at;
   return p;
@@ -208,26 +261,30 @@ szo_status matrix_map(CUtensorMap* map, const T* base, int64_t rows, int64_t col
   const uint32_t box[2] = {64, static_cast<uint32_t>(rows_box)};
   return encode_map(map, kMapType<T>, base, 2, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
-// An operand: as many rows of a box as there are, up to 128, where its rows are not contracted; 64 where they are
+// Operands.  `rows_box`: rows that a CTA brings per stage where they are not contracted (64 of them, twice 64 elements, where they are)
 template <typename T>
-szo_status operand_a(Job* j, const T* base, int64_t rows, int64_t cols, int64_t stride, bool mn) {
-  const int box = mn ? 64 : rows < 128 ? static_cast<int>(round_up(rows, 8)) : 128;
+szo_status operand_a(Job* j, const T* base, int64_t rows, int64_t cols, int64_t stride, bool mn, int64_t m0, int64_t k0, int rows_box) {
   j->a_mn = mn;
-  j->a_bytes = mn ? 128 * kBlockK * 2 : box * kBlockK * 2;
-  return matrix_map(&j->a, base, rows, cols, stride, box);
+  j->a_m0 = static_cast<int>(m0);
+  j->a_k0 = static_cast<int>(k0);
+  j->bytes += (mn ? 128 : rows_box) * kBlockK * 2;
+  return matrix_map(&j->a, base, rows, cols, stride, mn ? 64 : rows_box);
 }
 template <typename T>
-szo_status operand_b(Job* j, const T* base, int64_t rows, int64_t cols, int64_t stride, bool mn, int64_t k0, int64_t n0) {
+szo_status operand_b(Job* j, const T* base, int64_t rows, int64_t cols, int64_t stride, bool mn, int64_t n0, int64_t k0, int rows_box) {
   j->b_mn = mn;
-  j->b_k0 = static_cast<int>(k0);
   j->b_n0 = static_cast<int>(n0);
-  return matrix_map(&j->b, base, rows, cols, stride, mn ? 64 : 128);
+  j->b_k0 = static_cast<int>(k0);
+  j->bytes += (mn ? 128 : rows_box) * kBlockK * 2;
+  return matrix_map(&j->b, base, rows, cols, stride, mn ? 64 : rows_box);
 }
-void sizes(Job* j, Kind kind, int64_t m, int64_t n, int64_t k, int parts) {
+void sizes(Job* j, Kind kind, int64_t m, int64_t n, int64_t k, int parts, int m_step = kTile, int n_step = kTile) {
   j->kind = kind;
   j->m_limit = static_cast<int>(m);
-  j->m_tiles = tiles_of(m);
-  j->n_tiles = tiles_of(n);
+  j->m_step = m_step;
+  j->n_step = n_step;
+  j->m_tiles = static_cast<int>(ceil_div(m, m_step));
+  j->n_tiles = static_cast<int>(ceil_div(n, n_step));
   j->nkb = static_cast<int>(ceil_div(k, kBlockK));
   j->parts = parts;
   j->units = j->m_tiles * j->n_tiles * parts;
@@ -248,17 +305,29 @@ template <typename T> struct Inputs {
   const int32_t* targets;
 };
 
+// The logits' product over n vocabulary entries from j0 on
+template <typename T> szo_status logits_job(Job* j, const Shape& s, const Inputs<T>& in, int64_t j0, int64_t n, Kind kind, Kind kind_few) {
+  if (few(s.rows)) {
+    const int step = step_of(n), cols = static_cast<int>(round_up(s.rows, 32));
+    SZO_TRY(operand_a(j, in.W, s.vocab, s.d, in.ws, false, j0, 0, step / 2));
+    SZO_TRY(operand_b(j, in.h, s.rows, s.d, in.hs, false, 0, 0, cols / 2));
+    sizes(j, kind_few, n, s.rows, s.d, 1, step, cols);
+    return SZO_OK;
+  }
+  SZO_TRY(operand_a(j, in.h, s.rows, s.d, in.hs, false, 0, 0, 128));
+  SZO_TRY(operand_b(j, in.W, s.vocab, s.d, in.ws, false, j0, 0, 128));
+  sizes(j, kind, s.rows, n, s.d, 1);
+  j->m_band = band_of(s.rows, s.d);
+  return SZO_OK;
+}
+
 template <typename T>
 szo_status forward(const Shape& s, const Inputs<T>& in, float* loss, float* lse, unsigned char* ws, int32_t* status, cudaStream_t st) {
   const Plan p = forward_plan(s);
   Jobs P = {};
-  Job& j = P.job[0];
-  SZO_TRY(operand_a(&j, in.h, s.rows, s.d, in.hs, false));
-  SZO_TRY(operand_b(&j, in.W, s.vocab, s.d, in.ws, false, 0, 0));
-  sizes(&j, kStats, s.rows, s.vocab, s.d, 1);
-  j.m_band = band_of(s.rows, s.d);
+  SZO_TRY(logits_job(&P.job[0], s, in, 0, s.vocab, kStats, kStatsT));
   P.n_jobs = 1;
-  P.units = j.units;
+  P.units = P.job[0].units;
   P.targets = in.targets;
   P.part = reinterpret_cast<float2*>(ws + p.part);
   P.xt = reinterpret_cast<float*>(ws + p.xt);
@@ -266,10 +335,13 @@ szo_status forward(const Shape& s, const Inputs<T>& in, float* loss, float* lse,
   P.n_end = static_cast<int>(s.vocab);
   P.c = in.scale * kLog2e;
   P.status = status;
-  SZO_TRY(launch_jobs<T>(P, st));
-  head_join_kernel<<<blocks_of(s.rows, 32), 256, 0, st>>>(P.part, P.xt, in.targets, s.rows, s.vocab, 2 * j.n_tiles, loss, lse, status);
+  SZO_TRY(launch_jobs<T>(P, false, st));
+  auto join = [&](auto kern, int rows) {
+    return launch_maybe_chained(kern, dim3(blocks_of(s.rows, rows)), dim3(256), 0, st, true, P.part, P.xt, in.targets, s.rows, s.vocab, p.parts, loss, lse,
+                                status);
+  };
+  SZO_CHECK_CUDA(s.rows <= 512 ? join(head_join_kernel<1>, 1) : join(head_join_kernel<8>, 8));
   count_launch();
-  SZO_CHECK_LAUNCH("head_join_kernel");
   return SZO_OK;
 }
 
@@ -281,15 +353,17 @@ szo_status backward(const Shape& s, const Inputs<T>& in, const float* lse, const
   int32_t* exponent = reinterpret_cast<int32_t*>(ws + p.exponent);
   T* copy = reinterpret_cast<T*>(ws + p.copy);
   float* acc = reinterpret_cast<float*>(ws + p.acc);
-  SZO_CHECK_CUDA(cudaMemsetAsync(exponent, 0x80, sizeof(int32_t), st));      // (below every exponent)
-  head_rows_kernel<<<blocks_of(s.rows, 256), 256, 0, st>>>(in.targets, lse, d_loss, d_lse, s.rows, s.vocab, in.scale, !std::is_same<T, __nv_bfloat16>::value,
-                                                         info, exponent);
+  const unsigned row_blocks = s.rows <= 8 * kRowThreads ? 1 : blocks_of(s.rows, kRowThreads);
+  if (row_blocks > 1) SZO_CHECK_CUDA(cudaMemsetAsync(exponent, 0x80, sizeof(int32_t), st));
+  head_rows_kernel<<<row_blocks, kRowThreads, 0, st>>>(in.targets, lse, d_loss, d_lse, s.rows, s.vocab, in.scale, !std::is_same<T, __nv_bfloat16>::value,
+                                                     info, exponent);
   count_launch();
+  SZO_CHECK_LAUNCH("head_rows_kernel");
+  const unsigned vec_blocks = blocks_of(s.rows * (s.d / 8), 256);
   if (dw != nullptr) {
-    head_copy_kernel<T><<<blocks_of(s.rows * (s.d / 8), 256), 256, 0, st>>>(in.h, in.hs, s.rows, s.d, info, exponent, copy);
+    SZO_CHECK_CUDA(launch_maybe_chained(head_copy_kernel<T>, dim3(vec_blocks), dim3(256), 0, st, true, in.h, in.hs, s.rows, s.d, info, exponent, copy));
     count_launch();
   }
-  SZO_CHECK_LAUNCH("head_rows_kernel");
   // Launch i takes G of piece i and, of piece i - 1, dh and dW: what a launch reads, the launch before it wrote
   const int pieces = static_cast<int>(ceil_div(s.vocab, p.piece));
   for (int i = 0; i <= pieces; ++i) {
@@ -299,26 +373,37 @@ szo_status backward(const Shape& s, const Inputs<T>& in, const float* lse, const
     P.exponent = exponent;
     P.rows = s.rows;
     P.c = in.scale * kLog2e;
+    P.g_stride = p.piece;
+    P.sums = acc;
+    P.d = static_cast<int>(s.d);
     P.status = status;
     if (i > 0) {
       const int64_t j0 = (i - 1) * p.piece, n = s.vocab - j0 < p.piece ? s.vocab - j0 : p.piece;
       const T* G = reinterpret_cast<const T*>(ws + p.G[(i - 1) & 1]);
       if (dh != nullptr) {
         Job& j = P.job[P.n_jobs++];
-        SZO_TRY(operand_a(&j, G, s.rows, n, p.piece, false));
-        SZO_TRY(operand_b(&j, in.W, s.vocab, s.d, in.ws, true, j0, 0));
-        const uint64_t dims[3] = {static_cast<uint64_t>(s.d), static_cast<uint64_t>(s.rows), static_cast<uint64_t>(p.dh_parts)};
-        const uint64_t strides[2] = {static_cast<uint64_t>(s.d) * 4, static_cast<uint64_t>(s.rows) * s.d * 4};
-        const uint32_t box[3] = {32, 32, 1};
-        SZO_TRY(encode_map(&j.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, acc, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B));
         const int64_t nkb = ceil_div(n, kBlockK);                 // (a short last piece may have fewer blocks than parts)
-        sizes(&j, kSum, s.rows, s.d, n, nkb < p.dh_parts ? static_cast<int>(nkb) : p.dh_parts);
+        const int parts = nkb < p.dh_parts ? static_cast<int>(nkb) : p.dh_parts;
+        if (few(s.rows)) {
+          const int cols = static_cast<int>(round_up(s.rows, 32));
+          SZO_TRY(operand_a(&j, in.W, s.vocab, s.d, in.ws, true, 0, j0, 0));
+          SZO_TRY(operand_b(&j, G, s.rows, n, p.piece, false, 0, 0, cols / 2));
+          sizes(&j, kSumT, s.d, s.rows, n, parts, kTile, cols);
+        } else {
+          SZO_TRY(operand_a(&j, G, s.rows, n, p.piece, false, 0, 0, 128));
+          SZO_TRY(operand_b(&j, in.W, s.vocab, s.d, in.ws, true, 0, j0, 0));
+          const uint64_t dims[3] = {static_cast<uint64_t>(s.d), static_cast<uint64_t>(s.rows), static_cast<uint64_t>(p.dh_parts)};
+          const uint64_t strides[2] = {static_cast<uint64_t>(s.d) * 4, static_cast<uint64_t>(s.rows) * s.d * 4};
+          const uint32_t box[3] = {32, 32, 1};
+          SZO_TRY(encode_map(&j.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, acc, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B));
+          sizes(&j, kSum, s.rows, s.d, n, parts);
+        }
         j.add = i > 1;
       }
       if (dw != nullptr) {
         Job& j = P.job[P.n_jobs++];
-        SZO_TRY(operand_a(&j, G, s.rows, n, p.piece, true));
-        SZO_TRY(operand_b(&j, copy, s.rows, s.d, s.d, true, 0, 0));
+        SZO_TRY(operand_a(&j, G, s.rows, n, p.piece, true, 0, 0, 0));
+        SZO_TRY(operand_b(&j, copy, s.rows, s.d, s.d, true, 0, 0, 0));
         SZO_TRY(matrix_map(&j.out, dw, s.vocab, s.d, dws, 32));
         sizes(&j, kOut, n, s.d, s.rows, 1);
         j.out_row0 = static_cast<int>(j0);
@@ -327,21 +412,18 @@ szo_status backward(const Shape& s, const Inputs<T>& in, const float* lse, const
     if (i < pieces) {
       const int64_t j0 = i * p.piece, n = s.vocab - j0 < p.piece ? s.vocab - j0 : p.piece;
       Job& j = P.job[P.n_jobs++];
-      SZO_TRY(operand_a(&j, in.h, s.rows, s.d, in.hs, false));
-      SZO_TRY(operand_b(&j, in.W, s.vocab, s.d, in.ws, false, 0, j0));
-      SZO_TRY(matrix_map(&j.out, reinterpret_cast<T*>(ws + p.G[i & 1]), s.rows, n, p.piece, 32));
-      sizes(&j, kGrad, s.rows, n, s.d, 1);
-      j.m_band = band_of(s.rows, s.d);
+      SZO_TRY(logits_job(&j, s, in, j0, n, kGrad, kGradT));
+      P.G = ws + p.G[i & 1];
+      if (!few(s.rows)) SZO_TRY(matrix_map(&j.out, static_cast<T*>(P.G), s.rows, n, p.piece, 32));
       P.n_end = static_cast<int>(n);
       P.target0 = static_cast<int>(j0);
     }
     for (int k = 0; k < P.n_jobs; ++k) P.units += P.job[k].units;
-    SZO_TRY(launch_jobs<T>(P, st));
+    SZO_TRY(launch_jobs<T>(P, true, st));
   }
   if (dh != nullptr) {
-    head_round_kernel<T><<<blocks_of(s.rows * (s.d / 8), 256), 256, 0, st>>>(acc, p.dh_parts, s.rows, s.d, info, dh, dhs);
+    SZO_CHECK_CUDA(launch_maybe_chained(head_round_kernel<T>, dim3(vec_blocks), dim3(256), 0, st, true, acc, p.dh_parts, s.rows, s.d, info, dh, dhs));
     count_launch();
-    SZO_CHECK_LAUNCH("head_round_kernel");
   }
   return SZO_OK;
 }

@@ -10,22 +10,27 @@
 namespace szo {
 namespace head {
 
-constexpr int kTile = 256;                     // rows and columns of a tile
+constexpr int kTile = 256;                     // rows and columns of a tile, at most
 constexpr int kBlockK = 64;                    // contracted elements of a stage
 
-// A product D[m][n] = sum_k A(m, k) B(n, k) in tiles of 256 x 256, and what becomes of a tile
+// A product D[m][n] = sum_k A(m, k) B(n, k) in tiles of up to 256 x 256, and what becomes of a tile
 enum Kind : int {
   kStats,      // (m, s) of every row and 128 columns, the target's logit
   kGrad,       // G in the 16-bit type
   kSum,        // fp32 sums, stored or (add) added to what is there
-  kOut         // times a power of two, rounded to the 16-bit type
+  kOut,        // times a power of two, rounded to the 16-bit type
+  // few rows of hidden states: they are the columns of D
+  kStatsT,     // (m, s) of every column and 32 rows, the target's logit
+  kGradT,
+  kSumT
 };
 struct Job {
   CUtensorMap a, b, out;                       // operands by boxes of 64 elements; out: boxes of 32 rows
   int kind;
   int a_mn, b_mn;                              // the operand's rows are the contracted dimension
-  int a_bytes;                                 // of A per stage and CTA (fewer where there are fewer than 128 rows)
-  int b_k0, b_n0;                              // where B's piece starts, in its contracted / other dimension
+  int bytes;                                   // of both operands per stage and CTA
+  int a_m0, a_k0, b_n0, b_k0;                  // where the operands' pieces start
+  int m_step, n_step;                          // a tile's rows and columns; each CTA brings half of either
   int m_tiles, n_tiles, m_band;                // tiles of m are taken in bands of m_band (0: all)
   int nkb, parts, units;                       // blocks of 64 contracted elements, cut into `parts`; units = tiles * parts
   int out_row0;                                // the tile's first row in `out`
@@ -39,15 +44,20 @@ struct Jobs {
   const int32_t* targets;
   const float4* info;
   const int32_t* exponent;                     // of the largest weight (fp16)
-  float2* part;                                // [2 * n_tiles][rows]
+  float2* part;                                // [parts of the vocabulary][rows]
   float* xt;
   int64_t rows;
-  int n_end;                                   // columns that there are (of this piece)
-  int target0;                                 // the vocabulary index of column 0
+  int n_end;                                   // vocabulary entries that there are (of this piece)
+  int target0;                                 // index of the first
   float c;                                     // scale * log2 e
+  // kGradT, kSumT
+  void* G;
+  int64_t g_stride;
+  float* sums;                                 // [parts][rows][d]
+  int d;
   int32_t* status;
 };
-template <typename T> szo_status launch_jobs(const Jobs& P, cudaStream_t st);
+template <typename T> szo_status launch_jobs(const Jobs& P, bool chained, cudaStream_t st);
 
 #ifdef __CUDACC__
 // For dW of fp16 the rows of G stand at 2^13 times their weight's power of two and those of h at that power over the largest

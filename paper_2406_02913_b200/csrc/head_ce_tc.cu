@@ -7,6 +7,8 @@
 //   logits   h [rows][d],  W [vocab][d]             both along their rows
 //   dh       G [rows][vocab],  W [vocab][d]         W's rows are contracted
 //   dW       G [rows][vocab],  h [rows][d]          both operands' rows are contracted
+// With at most 128 rows of hidden states these are the columns of D (N = 32 to 128) and the vocabulary (for dh: d) its rows, so that
+// the products take a fraction of the time in which W arrives; tiles are then as high as makes the clusters' shares equal.
 // Roles of a CTA's 12 warps: 0 brings the operands (both CTAs' copies arrive on the leader's barriers), 1 issues the products
 // (leader only), 2 has the TMEM, 4-11 the epilogue: two warps per 32 rows, 128 columns each, a thread per row.
 // Tiles are written through 4 KB of shared memory per warp by TMA, which leaves out what lies outside.
@@ -25,6 +27,7 @@ using namespace tc;
 constexpr int kHalf = 128, kStages = 6, kOperandBytes = kHalf * kBlockK * 2, kStageBytes = 2 * kOperandBytes;
 constexpr int kEpiWarp0 = 4, kEpiWarps = 8, kWarps = kEpiWarp0 + kEpiWarps, kOutBytes = 4096;
 constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kOutBytes + 1024;
+constexpr int kMaxDevices = 64;
 constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ uint32_t cluster_ctarank() {
@@ -110,6 +113,39 @@ template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi)
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+template <typename T> __device__ __forceinline__ T round_to(float x);
+template <> __device__ __forceinline__ __nv_bfloat16 round_to<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half round_to<__half>(float x) { return __float2half_rn(x); }
+__device__ __forceinline__ void load16(uint32_t taddr, float (&f)[16]) {
+  uint32_t v[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]),
+        "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr)
+      : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]),
+                 "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])::"memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(v[i]);
+}
+// Reduces 16 columns held by 32 lanes (one row each): lane l gets column lane_column(l), in 16 exchanges
+__device__ __forceinline__ int lane_column(int lane) { return lane >> 1; }
+__device__ __forceinline__ int column_lane(int column) { return column << 1; }
+template <typename F> __device__ __forceinline__ float columns_reduce(float (&x)[16], int lane, F f) {
+#pragma unroll
+  for (int n = 8, o = 16; n >= 1; n >>= 1, o >>= 1) {             // columns [0, n) stay where bit o of the lane is 0, [n, 2 n) where it is 1
+    const bool up = (lane & o) != 0;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float keep = up ? x[n + i] : x[i], give = up ? x[i] : x[n + i];
+      x[i] = f(keep, __shfl_xor_sync(0xffffffffu, give, o));
+    }
+  }
+  return f(x[0], __shfl_xor_sync(0xffffffffu, x[0], 1));
+}
+
 // Operand tiles (128-byte swizzle).  Contracted along its rows: 128 rows of 64 elements.  Rows contracted: two blocks of 64 rows (k) of 64
 // elements, 8192 bytes apart.
 __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, int mn) {
@@ -168,11 +204,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  chain_release();
   if (warp == 2) alloc_tmem(smem_u32(&tmem_slot));
   tc_fence_before();
   __syncthreads();
   cluster_sync_all();          // the peer's barriers exist before anyone arrives on them
   tc_fence_after();
+  chain_wait();
   const uint32_t tmem = tmem_slot;
   const int pair = static_cast<int>(blockIdx.x >> 1), n_pairs = static_cast<int>(gridDim.x >> 1);
 
@@ -185,9 +223,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
         const Unit t = unit_of(P, u);
         const Job& J = P.job[t.j];
         const CUtensorMap *ma = &J.a, *mb = &J.b;
-        const int a0 = t.m * kTile + rank * kHalf, b0 = J.b_n0 + t.n * kTile + rank * kHalf;
-        const uint32_t bytes = 2u * (J.a_bytes + kOperandBytes);
-        const int a_mn = J.a_mn, b_mn = J.b_mn, b_k0 = J.b_k0;
+        const int a0 = J.a_m0 + t.m * J.m_step + rank * (J.m_step / 2), b0 = J.b_n0 + t.n * J.n_step + rank * (J.n_step / 2);
+        const uint32_t bytes = 2u * J.bytes;
+        const int a_mn = J.a_mn, b_mn = J.b_mn, a_k0 = J.a_k0, b_k0 = J.b_k0;
         for (int kb = t.kb0; kb < t.kb1; ++kb) {
           if (!mbar_wait(empty(x.idx), x.phase ^ 1u, abort_flag, P.status)) {
             ok = false;
@@ -197,8 +235,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
           const uint32_t bar = of_leader(full(x.idx)), sa = base + x.idx * kStageBytes, sb = sa + kOperandBytes;
           const int k = kb * kBlockK;
           if (a_mn) {
-            load_box(sa, ma, a0, k, bar);
-            load_box(sa + 8192, ma, a0 + 64, k, bar);
+            load_box(sa, ma, a0, a_k0 + k, bar);
+            load_box(sa + 8192, ma, a0 + 64, a_k0 + k, bar);
           } else {
             load_box(sa, ma, k, a0, bar);
           }
@@ -219,13 +257,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
       RingPos x{0, 0};
       bool ok = true;
       int lt = 0;
-      // kind::f16: fp32 sums, both operands of type T, M = N = 256; bits 15 / 16: rows of A / B are contracted
+      // kind::f16: fp32 sums, both operands of type T, M = 256; bits 15 / 16: rows of A / B are contracted
       constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
-      constexpr uint32_t kIdesc = (1u << 4) | (kType << 7) | (kType << 10) | (static_cast<uint32_t>(kTile >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
+      constexpr uint32_t kIdesc = (1u << 4) | (kType << 7) | (kType << 10) | (static_cast<uint32_t>(kTile >> 4) << 24);
       for (int u = pair; u < P.units && ok; u += n_pairs, ++lt) {
         const Unit t = unit_of(P, u);
         const int a_mn = P.job[t.j].a_mn, b_mn = P.job[t.j].b_mn;
-        const uint32_t idesc = kIdesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
+        const uint32_t idesc = kIdesc | (static_cast<uint32_t>(P.job[t.j].n_step >> 3) << 17) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
         const int step_a = a_mn ? 2048 >> 4 : 32 >> 4, step_b = b_mn ? 2048 >> 4 : 32 >> 4, as = lt & 1;
         if (!mbar_wait(acc_empty(as), static_cast<uint32_t>((lt >> 1) & 1) ^ 1u, abort_flag, P.status)) break;
         tc_fence_after();
@@ -264,8 +302,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
     for (int u = pair; u < P.units; u += n_pairs, ++lt) {
       const Unit t = unit_of(P, u);
       const Job& J = P.job[t.j];
-      const int as = lt & 1, row0 = t.m * kTile + rank * kHalf + quarter * 32, row = row0 + lane, col0 = t.n * kTile + half * kHalf;
-      const bool there = row < J.m_limit;
+      const int as = lt & 1, mine = quarter * 32 + lane;           // (its place in this CTA's half of the tile)
+      const int row0 = t.m * J.m_step + rank * (J.m_step / 2) + quarter * 32, row = row0 + lane, col0 = t.n * J.n_step + half * (J.n_step / 2);
+      const bool there = row < J.m_limit && mine < J.m_step / 2;
       int target = -1;
       float4 info = make_float4(0.f, 0.f, 0.f, 0.f);
       float factor = 1.f;
@@ -276,8 +315,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
       if (target >= P.n_end - col0) target = -1;
       if (!mbar_wait(acc_full(as), static_cast<uint32_t>((lt >> 1) & 1), abort_flag, P.status, 128)) break;
       tc_fence_after();
-      const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + as * kTile + half * kHalf;
-      const bool live = row0 < J.m_limit;                         // some row of this warp is there
+      const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + as * kTile + half * (J.n_step / 2);
+      // some row of this warp is there (kStatsT: might be, its part is written all the same)
+      const bool live = (row0 < J.m_limit || J.kind == kStatsT) && quarter * 32 < J.m_step / 2;
       if (!live) {
       } else if (J.kind == kStats) {
         float m = -INFINITY, s = 0.f;
@@ -357,6 +397,57 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
             store_commit();
           }
         }
+      } else if (J.kind >= kStatsT) {
+        // a thread is a vocabulary entry (kSumT: an element of d), the columns are rows of hidden states, 16 at a time
+        const int last = static_cast<int>(P.rows), n_half = J.n_step / 2;
+#pragma unroll 1
+        for (int c = 0; c < n_half; c += 16) {
+          const int r0 = col0 + c;
+          if (r0 >= last) break;
+          float v[16];
+          load16(acc + c, v);
+          if (J.kind == kSumT) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (there && r0 + i < last) {
+                float* to = P.sums + (t.part * P.rows + r0 + i) * P.d + row;
+                *to = J.add ? *to + v[i] : v[i];
+              }
+          } else if (J.kind == kGradT) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              if (r0 + i >= last) break;
+              const float4 f = __ldg(P.info + r0 + i);
+              const float x = min_nan(fmaf(v[i], P.c, -f.x), 0.f), p = ex2(x);
+              float g = f.y * p;
+              if (__ldg(P.targets + r0 + i) == P.target0 + row) g = fmaf(f.y - f.z, p, f.z * expm1f(x * kLn2));
+              if (f.y == 0.f && f.z == 0.f) g = 0.f;
+              if (there) static_cast<T*>(P.G)[(r0 + i) * P.g_stride + row] = round_to<T>(g);
+            }
+          } else {
+            float top[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              if (!there) v[i] = -INFINITY;
+              if (r0 + i < last && there && __ldg(P.targets + r0 + i) == row) {
+                P.xt[r0 + i] = v[i] * P.c;
+                v[i] = -INFINITY;
+              }
+              top[i] = v[i];
+            }
+            const float mx = columns_reduce(top, lane, [](float a, float b) { return fmaxf(a, b); });
+            float sum[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float m = __shfl_sync(0xffffffffu, mx, column_lane(i)), ref = m == -INFINITY ? 0.f : m;
+              sum[i] = ex2((v[i] - ref) * P.c);
+            }
+            const float s = columns_reduce(sum, lane, [](float a, float b) { return a + b; });
+            const int col = lane_column(lane);
+            if ((lane & 1) == 0 && r0 + col < last)
+              P.part[static_cast<int64_t>((t.m * 2 + rank) * ((J.m_step / 2 + 31) / 32) + quarter) * P.rows + r0 + col] = make_float2(mx * P.c, s);
+          }
+        }
       } else {
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
@@ -399,20 +490,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
 
 }  // namespace
 
-template <typename T> szo_status launch_jobs(const Jobs& P, cudaStream_t st) {
+template <typename T> szo_status launch_jobs(const Jobs& P, bool chained, cudaStream_t st) {
   auto kern = head_jobs_kernel<T>;
-  int dev = 0, sms = 0;
+  // per device: the function's attribute and the number of SM pairs, looked up once
+  static std::mutex mu;
+  static int pairs_of[kMaxDevices] = {};
+  int dev = 0;
   SZO_CHECK_CUDA(cudaGetDevice(&dev));
-  SZO_CHECK_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-  SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
-  const int pairs = P.units < sms / 2 ? P.units : sms / 2;
-  kern<<<static_cast<unsigned>(2 * pairs), kWarps * 32, kSmem, st>>>(P);
+  SZO_REQUIRE(dev >= 0 && dev < kMaxDevices, SZO_ERR_UNSUPPORTED, "device ordinal %d out of range", dev);
+  int pairs;
+  {
+    std::lock_guard<std::mutex> lock(mu);
+    if (pairs_of[dev] == 0) {
+      int sms = 0;
+      SZO_CHECK_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+      SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+      pairs_of[dev] = sms / 2;
+    }
+    pairs = pairs_of[dev];
+  }
+  if (P.units < pairs) pairs = P.units;
+  SZO_CHECK_CUDA(launch_maybe_chained(kern, dim3(static_cast<unsigned>(2 * pairs)), dim3(kWarps * 32), kSmem, st, chained, P));
   count_launch();
-  SZO_CHECK_LAUNCH("head_jobs_kernel");
   return SZO_OK;
 }
-template szo_status launch_jobs<__nv_bfloat16>(const Jobs&, cudaStream_t);
-template szo_status launch_jobs<__half>(const Jobs&, cudaStream_t);
+template szo_status launch_jobs<__nv_bfloat16>(const Jobs&, bool, cudaStream_t);
+template szo_status launch_jobs<__half>(const Jobs&, bool, cudaStream_t);
 
 }  // namespace head
 }  // namespace szo
