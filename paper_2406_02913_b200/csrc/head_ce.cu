@@ -267,7 +267,7 @@ szo_status operand_a(Job* j, const T* base, int64_t rows, int64_t cols, int64_t 
   j->a_mn = mn;
   j->a_m0 = static_cast<int>(m0);
   j->a_k0 = static_cast<int>(k0);
-  j->bytes += (mn ? 128 : rows_box) * kBlockK * 2;
+  j->a_bytes = (mn ? 128 : rows_box) * kBlockK * 2;
   return matrix_map(&j->a, base, rows, cols, stride, mn ? 64 : rows_box);
 }
 template <typename T>
@@ -275,7 +275,7 @@ szo_status operand_b(Job* j, const T* base, int64_t rows, int64_t cols, int64_t 
   j->b_mn = mn;
   j->b_n0 = static_cast<int>(n0);
   j->b_k0 = static_cast<int>(k0);
-  j->bytes += (mn ? 128 : rows_box) * kBlockK * 2;
+  j->b_bytes = (mn ? 128 : rows_box) * kBlockK * 2;
   return matrix_map(&j->b, base, rows, cols, stride, mn ? 64 : rows_box);
 }
 void sizes(Job* j, Kind kind, int64_t m, int64_t n, int64_t k, int parts, int m_step = kTile, int n_step = kTile) {

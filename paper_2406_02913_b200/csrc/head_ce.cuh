@@ -28,7 +28,7 @@ struct Job {
   CUtensorMap a, b, out;                       // operands by boxes of 64 elements; out: boxes of 32 rows
   int kind;
   int a_mn, b_mn;                              // the operand's rows are the contracted dimension
-  int bytes;                                   // of both operands per stage and CTA
+  int a_bytes, b_bytes;                        // of the operands per stage and CTA
   int a_m0, a_k0, b_n0, b_k0;                  // where the operands' pieces start
   int m_step, n_step;                          // a tile's rows and columns; each CTA brings half of either
   int m_tiles, n_tiles, m_band;                // tiles of m are taken in bands of m_band (0: all)
@@ -40,6 +40,7 @@ struct Job {
 struct Jobs {
   Job job[3];
   int n_jobs, units;
+  int b_at, stage_bytes, stages;               // the ring: B's place in a stage (set by launch_jobs)
   // kStats, kGrad
   const int32_t* targets;
   const float4* info;
@@ -57,7 +58,7 @@ struct Jobs {
   int d;
   int32_t* status;
 };
-template <typename T> szo_status launch_jobs(const Jobs& P, bool chained, cudaStream_t st);
+template <typename T> szo_status launch_jobs(Jobs& P, bool chained, cudaStream_t st);
 
 #ifdef __CUDACC__
 // For dW of fp16 the rows of G stand at 2^13 times their weight's power of two and those of h at that power over the largest

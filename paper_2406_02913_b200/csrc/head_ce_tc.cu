@@ -12,6 +12,7 @@
 // Roles of a CTA's 12 warps: 0 brings the operands (both CTAs' copies arrive on the leader's barriers), 1 issues the products
 // (leader only), 2 has the TMEM, 4-11 the epilogue: two warps per 32 rows, 128 columns each, a thread per row.
 // Tiles are written through 4 KB of shared memory per warp by TMA, which leaves out what lies outside.
+#include <algorithm>
 #include <mutex>
 
 #include "head_ce.cuh"
@@ -24,9 +25,9 @@ namespace {
 
 using namespace tc;
 
-constexpr int kHalf = 128, kStages = 6, kOperandBytes = kHalf * kBlockK * 2, kStageBytes = 2 * kOperandBytes;
+constexpr int kHalf = 128, kMostStages = 12, kRingBytes = 6 * 2 * kHalf * kBlockK * 2;
 constexpr int kEpiWarp0 = 4, kEpiWarps = 8, kWarps = kEpiWarp0 + kEpiWarps, kOutBytes = 4096;
-constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kOutBytes + 1024;
+constexpr int kSmem = kRingBytes + kEpiWarps * kOutBytes + 1024;
 constexpr int kMaxDevices = 64;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -181,7 +182,7 @@ __device__ __forceinline__ Unit unit_of(const Jobs& P, int u) {
 template <typename T>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head_jobs_kernel(const __grid_constant__ Jobs P) {
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) unsigned long long bars[2 * kStages + 4];
+  __shared__ __align__(8) unsigned long long bars[2 * kMostStages + 4];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag_s;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -189,12 +190,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
   const int rank = static_cast<int>(cluster_ctarank());
   volatile int* abort_flag = &abort_flag_s;
   auto full = [&](int s) { return smem_u32(&bars[s]); };                          // leader: both CTAs' operands landed
-  auto empty = [&](int s) { return smem_u32(&bars[kStages + s]); };               // the products that read the stage are done
-  auto acc_full = [&](int a) { return smem_u32(&bars[2 * kStages + a]); };
-  auto acc_empty = [&](int a) { return smem_u32(&bars[2 * kStages + 2 + a]); };   // leader: both CTAs' epilogues have read the sums
+  auto empty = [&](int s) { return smem_u32(&bars[kMostStages + s]); };               // the products that read the stage are done
+  auto acc_full = [&](int a) { return smem_u32(&bars[2 * kMostStages + a]); };
+  auto acc_empty = [&](int a) { return smem_u32(&bars[2 * kMostStages + 2 + a]); };   // leader: both CTAs' epilogues have read the sums
   if (threadIdx.x == 0) {
     abort_flag_s = 0;
-    for (int s = 0; s < kStages; ++s) {
+    for (int s = 0; s < kMostStages; ++s) {
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
     }
@@ -224,7 +225,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
         const Job& J = P.job[t.j];
         const CUtensorMap *ma = &J.a, *mb = &J.b;
         const int a0 = J.a_m0 + t.m * J.m_step + rank * (J.m_step / 2), b0 = J.b_n0 + t.n * J.n_step + rank * (J.n_step / 2);
-        const uint32_t bytes = 2u * J.bytes;
+        const uint32_t bytes = 2u * (J.a_bytes + J.b_bytes);
         const int a_mn = J.a_mn, b_mn = J.b_mn, a_k0 = J.a_k0, b_k0 = J.b_k0;
         for (int kb = t.kb0; kb < t.kb1; ++kb) {
           if (!mbar_wait(empty(x.idx), x.phase ^ 1u, abort_flag, P.status)) {
@@ -232,7 +233,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
             break;
           }
           if (rank == 0) mbar_expect_tx(full(x.idx), bytes);
-          const uint32_t bar = of_leader(full(x.idx)), sa = base + x.idx * kStageBytes, sb = sa + kOperandBytes;
+          const uint32_t bar = of_leader(full(x.idx)), sa = base + x.idx * P.stage_bytes, sb = sa + P.b_at;
           const int k = kb * kBlockK;
           if (a_mn) {
             load_box(sa, ma, a0, a_k0 + k, bar);
@@ -246,7 +247,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
           } else {
             load_box(sb, mb, k, b0, bar);
           }
-          x.advance(kStages);
+          x.advance(P.stages);
         }
       }
     }
@@ -274,12 +275,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
             break;
           }
           tc_fence_after();
-          const uint32_t sa = base + x.idx * kStageBytes;
-          const uint64_t da = operand_desc(sa, a_mn), db = operand_desc(sa + kOperandBytes, b_mn);
+          const uint32_t sa = base + x.idx * P.stage_bytes;
+          const uint64_t da = operand_desc(sa, a_mn), db = operand_desc(sa + P.b_at, b_mn);
 #pragma unroll
           for (int k = 0; k < kBlockK / 16; ++k) mma_pair(d, da + k * step_a, db + k * step_b, idesc, kb > t.kb0 || k > 0);
           commit_both(empty(x.idx));
-          x.advance(kStages);
+          x.advance(P.stages);
         }
         commit_both(acc_full(as));
       }
@@ -288,7 +289,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
   } else if (warp >= kEpiWarp0) {
     // ---------------------------------------------------------------- epilogue: 32 rows, 128 columns
     const int w = warp - kEpiWarp0, quarter = warp & 3, half = w >> 2;
-    const uint32_t stage = base + kStages * kStageBytes + w * kOutBytes;
+    const uint32_t stage = base + kRingBytes + w * kOutBytes;
     auto place = [&](int chunk) { return stage + lane * 128 + ((chunk ^ (lane & 7)) << 4); };
     auto reuse = [&]() {                                          // the warp's 4 KB may be written again
       if (lane == 0) store_wait_read();
@@ -414,22 +415,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
                 *to = J.add ? *to + v[i] : v[i];
               }
           } else if (J.kind == kGradT) {
+            float4 f[16];
+            int hit[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              if (r0 + i >= last) break;
-              const float4 f = __ldg(P.info + r0 + i);
-              const float x = min_nan(fmaf(v[i], P.c, -f.x), 0.f), p = ex2(x);
-              float g = f.y * p;
-              if (__ldg(P.targets + r0 + i) == P.target0 + row) g = fmaf(f.y - f.z, p, f.z * expm1f(x * kLn2));
-              if (f.y == 0.f && f.z == 0.f) g = 0.f;
-              if (there) static_cast<T*>(P.G)[(r0 + i) * P.g_stride + row] = round_to<T>(g);
+              const int r = min(r0 + i, last - 1);
+              f[i] = __ldg(P.info + r);
+              hit[i] = __ldg(P.targets + r);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float x = min_nan(fmaf(v[i], P.c, -f[i].x), 0.f), p = ex2(x);
+              float g = f[i].y * p;
+              if (hit[i] == P.target0 + row) g = fmaf(f[i].y - f[i].z, p, f[i].z * expm1f(x * kLn2));
+              if (f[i].y == 0.f && f[i].z == 0.f) g = 0.f;
+              if (there && r0 + i < last) static_cast<T*>(P.G)[(r0 + i) * P.g_stride + row] = round_to<T>(g);
             }
           } else {
             float top[16];
+            int hit[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) hit[i] = __ldg(P.targets + min(r0 + i, last - 1));
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               if (!there) v[i] = -INFINITY;
-              if (r0 + i < last && there && __ldg(P.targets + r0 + i) == row) {
+              if (r0 + i < last && there && hit[i] == row) {
                 P.xt[r0 + i] = v[i] * P.c;
                 v[i] = -INFINITY;
               }
@@ -490,7 +500,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
 
 }  // namespace
 
-template <typename T> szo_status launch_jobs(const Jobs& P, bool chained, cudaStream_t st) {
+template <typename T> szo_status launch_jobs(Jobs& P, bool chained, cudaStream_t st) {
   auto kern = head_jobs_kernel<T>;
   // per device: the function's attribute and the number of SM pairs, looked up once
   static std::mutex mu;
@@ -510,12 +520,18 @@ template <typename T> szo_status launch_jobs(const Jobs& P, bool chained, cudaSt
     pairs = pairs_of[dev];
   }
   if (P.units < pairs) pairs = P.units;
+  // the ring: as many stages as fit of what the jobs' operands need, so that a few rows (a small B) keep as many bytes of W on their
+  // way (8 rows: 53 us with 6 stages)
+  P.b_at = P.stage_bytes = 0;
+  for (int i = 0; i < P.n_jobs; ++i) P.b_at = std::max(P.b_at, static_cast<int>(round_up(P.job[i].a_bytes, 1024)));
+  for (int i = 0; i < P.n_jobs; ++i) P.stage_bytes = std::max(P.stage_bytes, P.b_at + static_cast<int>(round_up(P.job[i].b_bytes, 1024)));
+  P.stages = std::min(kMostStages, kRingBytes / P.stage_bytes);
   SZO_CHECK_CUDA(launch_maybe_chained(kern, dim3(static_cast<unsigned>(2 * pairs)), dim3(kWarps * 32), kSmem, st, chained, P));
   count_launch();
   return SZO_OK;
 }
-template szo_status launch_jobs<__nv_bfloat16>(const Jobs&, bool, cudaStream_t);
-template szo_status launch_jobs<__half>(const Jobs&, bool, cudaStream_t);
+template szo_status launch_jobs<__nv_bfloat16>(Jobs&, bool, cudaStream_t);
+template szo_status launch_jobs<__half>(Jobs&, bool, cudaStream_t);
 
 }  // namespace head
 }  // namespace szo

@@ -134,8 +134,15 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   unsigned char* ring0 = smem_kv8 + ((1024u - (tc::smem_u32(smem_kv8) & 1023u)) & 1023u);
   auto part = [&](int warp) { return reinterpret_cast<float*>(ring0 + warp * kRing); };     // [R][HD]; the block's sum ends up in part(0)
 
-  chain_release();
-  chain_wait();
+  if constexpr (kPart) {
+    // a pass over shared positions waits for the groups' description before it lets the sequences' pass begin, which so has it too; that
+    // one runs beside it and waits before it takes its shares
+    if (part_of.prefix) chain_wait();
+    chain_release();
+  } else {
+    chain_release();
+    chain_wait();
+  }
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   unsigned item = blockIdx.x;
   const int split = item % nsplit;
@@ -147,7 +154,10 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   const Seq seq = work.seq;
   const bool prefix = kPart && part_of.prefix;
   const int r0 = rt * R, n_rows = static_cast<int>(min(static_cast<int64_t>(seq.n) * G - r0, static_cast<int64_t>(R)));
-  if (n_rows <= 0) return;                                        // (the same in every block of a cluster)
+  if (n_rows <= 0) {                                              // (the same in every block of a cluster)
+    if (kPart && !part_of.prefix) chain_wait();                   // (the launch after this one relies on the one before it)
+    return;
+  }
   for (int i = threadIdx.x; i < HD; i += kWarps * 32) nan_at[i] = 0x7fffffff;
   if (threadIdx.x == 0) abort_flag = 0;
   const uint32_t ring = tc::smem_u32(ring0) + w * kRing, bars = tc::smem_u32(&full[w][0]);
@@ -460,7 +470,7 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     }
     if ((prefix ? (r < n_rows ? last_of(r) : -1) : first + (r0 + r) / G) >= nan_at[d]) bm[i] = __int_as_float(0x7fffffff);
   }
-  if constexpr (kPart) {
+  if (prefix) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int at = threadIdx.x + i * kThreads, r = at / HD;
@@ -475,7 +485,7 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     o[(seq.row0 + (r0 + r) / G) * o_stride + (h * G + (r0 + r) % G) * static_cast<int64_t>(HD) + d] =
         narrow<T>(ll == 0.f ? sum : sum / ll);                    // nothing attended to: sum = 0
   };
-  if (nsplit == 1) {
+  if (nsplit == 1 && !kPart) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int at = threadIdx.x + i * kThreads;
@@ -483,7 +493,7 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     }
     return;
   }
-  if (ws != nullptr) {                                            // [item][split]: R * HD sums, R maxima, R sums of weights
+  if (!kPart && ws != nullptr) {                                  // [item][split]: R * HD sums, R maxima, R sums of weights
     float* mine = ws + static_cast<int64_t>(blockIdx.x) * (R * (HD + 2));
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -510,6 +520,53 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     }
   }
   cg::cluster_group cluster = cg::this_cluster();
+  if constexpr (kPart) {
+    // this block's share of the rows, four dims per thread: the cluster's blocks in their order, then the shares of the shared positions in
+    // theirs, all of their loads under way at once
+    if (nsplit > 1) cluster.sync();
+    else __syncthreads();
+    chain_wait();
+    const int quads = n_rows * (HD / 4), lo = quads * split / nsplit, hi = quads * (split + 1) / nsplit;
+    for (int i = lo + static_cast<int>(threadIdx.x); i < hi; i += kThreads) {
+      const int r = i / (HD / 4), d = i % (HD / 4) * 4;
+      const int64_t row_head = (seq.row0 + (r0 + r) / G) * H + h * G + (r0 + r) % G;
+      float mm = -INFINITY, ll = 0.f;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      auto add = [&](float m2, float l2, const float4& x) {
+        const float top = fmaxf(mm, m2), ref = top == -INFINITY ? 0.f : top, f0 = ex2(mm - ref), f1 = ex2(m2 - ref);
+        sum = make_float4(fmaf(f1, x.x, f0 * sum.x), fmaf(f1, x.y, f0 * sum.y), fmaf(f1, x.z, f0 * sum.z), fmaf(f1, x.w, f0 * sum.w));
+        ll = fmaf(f1, l2, f0 * ll);
+        mm = top;
+      };
+      for (int x = 0; x < nsplit; ++x) {
+        const float* from = nsplit > 1 ? cluster.map_shared_rank(part(0), x) : part(0);
+        add((nsplit > 1 ? cluster.map_shared_rank(wm, x) : wm)[r] - kOffset, (nsplit > 1 ? cluster.map_shared_rank(wl, x) : wl)[r],
+            *reinterpret_cast<const float4*>(from + r * HD + d));
+      }
+      if (work.skip > 0) {
+        constexpr int kAhead = 8;
+        for (int k0 = 0; k0 < part_of.shares; k0 += kAhead) {
+          float2 st[kAhead];
+          float4 x[kAhead];
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k) {
+            const int64_t at = (k0 + k < part_of.shares ? k0 + k : k0) * part_of.row_heads + row_head;
+            st[k] = __ldcg(part_of.stats + at);
+            x[k] = __ldcg(reinterpret_cast<const float4*>(part_of.sums + at * HD + d));
+          }
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k)
+            if (k0 + k < part_of.shares) add(st[k].x, st[k].y, x[k]);
+        }
+      }
+      const float inv = ll == 0.f ? 1.f : 1.f / ll;               // nothing attended to: sums of 0
+      struct alignas(4 * sizeof(T)) Four { T x[4]; };
+      *reinterpret_cast<Four*>(o + (seq.row0 + (r0 + r) / G) * o_stride + (h * G + (r0 + r) % G) * static_cast<int64_t>(HD) + d) =
+          Four{{narrow<T>(sum.x * inv), narrow<T>(sum.y * inv), narrow<T>(sum.z * inv), narrow<T>(sum.w * inv)}};
+    }
+    if (nsplit > 1) cluster.sync();
+    return;
+  }
   cluster.sync();
   const int from = R * HD * split / nsplit, share = R * HD * (split + 1) / nsplit - from;
   for (int i = threadIdx.x; i < share; i += kWarps * 32) {
@@ -620,12 +677,21 @@ szo_status launch_rows(const View& V, const Rows& A, int nsplit, float* ws, cuda
   cfg.blockDim = dim3(kWarps * 32);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = nsplit;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute attr[2];
+  int attrs = 0;
+  if (nsplit > 1 && ws == nullptr && !(kPart && part.prefix)) {
+    attr[attrs].id = cudaLaunchAttributeClusterDimension;
+    attr[attrs].val.clusterDim.x = nsplit;
+    attr[attrs].val.clusterDim.y = attr[attrs].val.clusterDim.z = 1;
+    ++attrs;
+  }
+  if (kPart) {
+    attr[attrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[attrs].val.programmaticStreamSerializationAllowed = 1;
+    ++attrs;
+  }
   cfg.attrs = attr;
-  cfg.numAttrs = nsplit > 1 && ws == nullptr && !kPart ? 1 : 0;
+  cfg.numAttrs = attrs;
   SZO_CHECK_CUDA(cudaLaunchKernelEx(&cfg, kern, map_k, map_v, V, static_cast<const T*>(A.q), A.q_stride, static_cast<T*>(A.o), A.o_stride, A.H,
                                     A.scale * 1.4426950408889634f, static_cast<int>(tiles), nsplit, ws, part));
   count_launch();
@@ -693,6 +759,9 @@ size_t workspace_bytes(const View& V, int H, int hd) {
 
 template <typename T, int HD> szo_status launch_part(const View& V, const Rows& A, const Part& part, int nsplit, cudaStream_t st) {
   const int64_t rows = static_cast<int64_t>(part.max_rows) * (A.H / V.hkv);
+  // (sequences of more items than blocks of 4 warps fit on the SMs at once: blocks of 2.  64 sequences of up to 512 positions of their own,
+  // 8 heads: 46 us, with blocks of 4 warps 48)
+  if (!part.prefix && rows <= 8 && static_cast<int64_t>(part.items) * V.hkv > 148 * 3) return launch_rows<T, HD, 1, 2, true>(V, A, nsplit, nullptr, st, part);
   return rows <= 8 ? launch_rows<T, HD, 1, 4, true>(V, A, nsplit, nullptr, st, part) : launch_rows<T, HD, 2, 4, true>(V, A, nsplit, nullptr, st, part);
 }
 #define SZO_KV8_PART(T, HD) template szo_status launch_part<T, HD>(const View&, const Rows&, const Part&, int, cudaStream_t)

@@ -29,10 +29,12 @@ struct Part {
   float2* stats;
   int64_t row_heads;           // of a share
   int prefix;                  // 1: the rows of a group over the shared positions; 0: a sequence's rows over the rest
+  int shares;                  // of the shared positions; a sequence's pass of the kernel for few rows finishes its rows with them
   int items;                   // groups or sequences
   int max_rows;                // the most rows of one
 };
-template <typename T, int HD> szo_status launch_part(const View& V, const Rows& A, const Part& part, int nsplit, cudaStream_t st);      // few rows
+// (few rows: a sequence's pass takes its own number of shares, joined in clusters; chained launches, see kv8_prefix.cu)
+template <typename T, int HD> szo_status launch_part(const View& V, const Rows& A, const Part& part, int nsplit, cudaStream_t st);
 template <typename T, int HD> szo_status launch_part_tc(const View& V, const Rows& A, const Part& part, int nsplit, cudaStream_t st);
 
 // The checks of a call's row buffers, and of what its kernels count in 32 bits (kv8_attention.cu)
@@ -58,10 +60,10 @@ struct Work {
 };
 __device__ __forceinline__ Work load_work(const View& V, const Part& part, int b) {
   if (part.prefix) {
-    const int4 g = part.groups[b];
+    const int4 g = __ldcg(part.groups + b);
     return Work{Seq{g.z > 0 ? g.y : 0, g.z, g.x}, 0, g.w};
   }
-  Work w{load_seq(V, b), part.shared[b], b};
+  Work w{load_seq(V, b), __ldcg(part.shared + b), b};
   w.seq.len -= w.skip;
   return w;
 }

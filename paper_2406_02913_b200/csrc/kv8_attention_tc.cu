@@ -185,6 +185,10 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   __shared__ uint32_t tmem_ptr;
   __shared__ int abort_flag;
 
+  if constexpr (kPart) {                                          // (as in the kernel for few rows)
+    if (part_of.prefix) chain_wait();
+    chain_release();
+  }
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int64_t others = static_cast<int64_t>(kPart ? part_of.items : V.batch) * V.hkv;
   const bool cut = blockIdx.x >= part.whole;
@@ -197,7 +201,10 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   const bool prefix = kPart && part_of.prefix;
   const unsigned r0 = static_cast<unsigned>(rt) * 2 * kTile;                     // (rows and heads of a call stay below 2^31)
   const int64_t left = static_cast<int64_t>(seq.n) * G - r0;
-  if (left <= 0) return;
+  if (left <= 0) {
+    if (kPart && !prefix) chain_wait();
+    return;
+  }
   const int n_rows = static_cast<int>(left < 2 * kTile ? left : 2 * kTile);
   const int first = seq.len - seq.n;                              // position of the sequence's row 0; negative: padding
   auto pos_of = [&](int r) { return first + static_cast<int>((r0 + r) / static_cast<unsigned>(G)); };
@@ -639,6 +646,7 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     tc::tc_fence_after();
     tmem_dealloc(tmem, kTmemCols);
   }
+  if (kPart && !prefix) chain_wait();                             // (the join behind this launch relies on the one before it too)
 }
 
 }  // namespace
@@ -676,8 +684,8 @@ szo_status launch_tc(const View& V, const Rows& A, int64_t tiles, unsigned block
   SZO_TRY(encode_map_2d(&map_v, CU_TENSOR_MAP_DATA_TYPE_UINT8, V.v, rows, HD, 1, box_tokens(V), HD, CU_TENSOR_MAP_SWIZZLE_NONE));
   auto kern = kv8_attention_tc_kernel<T, HD, kPart>;
   SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  kern<<<blocks, kTcThreads, smem, st>>>(map_k, map_v, V, static_cast<const T*>(A.q), A.q_stride, static_cast<T*>(A.o), A.o_stride, A.H, A.scale,
-                                         static_cast<int>(tiles), cut, ws, part);
+  SZO_CHECK_CUDA(launch_maybe_chained(kern, dim3(blocks), dim3(kTcThreads), smem, st, kPart, map_k, map_v, V, static_cast<const T*>(A.q), A.q_stride,
+                                      static_cast<T*>(A.o), A.o_stride, A.H, A.scale, static_cast<int>(tiles), cut, ws, part));
   count_launch();
   SZO_CHECK_LAUNCH("kv8_attention_tc_kernel");
   return SZO_OK;

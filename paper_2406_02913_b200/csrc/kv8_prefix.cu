@@ -4,7 +4,8 @@
 // shares, where the rows of all the group's sequences are taken together (so a shared code is read once for 8 to 256 rows of several
 // sequences, and prompts of a few rows each fill tensor-core tiles), and the rest of its sequence's positions.  Both are passes
 // of the attention kernels of kv8_attention.cu and kv8_attention_tc.cu that leave sums, maxima and sums of weights unfinished,
-// each cut into shares of the positions that fill the SMs; a last kernel joins a row's shares in their order.
+// each cut into shares of the positions that fill the SMs.  Where a sequence has few rows its pass runs beside the groups' one, waits for
+// its end and finishes the rows, shares in their order; where it has many, a last kernel does.
 #include <cmath>
 
 #include "kv8_prefix.cuh"
@@ -14,33 +15,49 @@ namespace kv8 {
 
 namespace {
 
-// What the passes read of the groups (block g) and of the sequences that share nothing (the last block).  A group with a
-// sequence whose description does not fit shares nothing: its rows could not be told apart.
+// What the passes read of the groups (block g) and of the sequences outside of every group (the last block).  A group with a
+// sequence whose description does not fit shares nothing: its rows could not be told apart; none does where seqs does not ascend.
 __global__ void __launch_bounds__(256) kv8_groups_kernel(View V, Prefix P, int4* __restrict__ groups, int32_t* __restrict__ shared, int32_t* __restrict__ pos) {
-  const int g = blockIdx.x;
-  if (g == P.n_groups) {
-    for (int b = threadIdx.x; b < V.batch; b += blockDim.x) {
-      const int mine = group_of(P, b);
-      if (mine < 0 || load_shared(V, P, mine, false).len == 0) shared[b] = 0;
-    }
+  chain_release();
+  const int g = blockIdx.x, n = P.n_groups;
+  const bool last = g == n;
+  int first = 0, end = V.batch, len = 0, lo = 0, hi = n > 0 ? V.batch : 0;        // this group's sequences and positions; those of all groups
+  bool ok = true;
+  if (P.seqs != nullptr) {
+    lo = P.seqs[0];
+    hi = P.seqs[n];
+    first = P.seqs[last ? 0 : g];
+    end = P.seqs[last ? 0 : g + 1];
+    for (int i = threadIdx.x; i < n; i += blockDim.x) ok = ok && P.seqs[i] <= P.seqs[i + 1];
+  }
+  if (!last) len = P.len[g];
+  const bool ascending = __syncthreads_and(ok);
+  if (last) {
+    for (int b = threadIdx.x; b < V.batch; b += blockDim.x)
+      if (!ascending || b < lo || b >= hi) shared[b] = 0;
+    if (!ascending && threadIdx.x == 0) atomicExch(V.status, static_cast<int32_t>(SZO_ERR_SHAPE));
     return;
   }
-  const Shared s = load_shared(V, P, g, threadIdx.x == 0);
-  bool ok = true;
-  for (int b = s.first + threadIdx.x; b < s.last; b += blockDim.x) {
+  const bool fits = first >= 0 && end >= first && end <= V.batch && end - first <= P.max_seqs && len >= 0 &&
+                    len <= static_cast<int64_t>(V.max_pages) << V.page_shift;
+  if (!fits && threadIdx.x == 0) atomicExch(V.status, static_cast<int32_t>(SZO_ERR_SHAPE));
+  len = ascending && fits ? len >> V.page_shift << V.page_shift : 0;
+  first = max(first, 0);
+  end = min(end, V.batch);
+  ok = true;
+  for (int b = first + threadIdx.x; b < end; b += blockDim.x) {
     Seq q;
-    ok = read_seq(V, b, &q) && group_of(P, b) == g && ok;
+    ok = read_seq(V, b, &q) && ok;
   }
-  const int len = __syncthreads_and(ok) ? s.len : 0;
+  if (!__syncthreads_and(ok) || first >= end) len = 0;
   if (threadIdx.x == 0) {
-    const int row0 = len == 0 ? 0 : V.start != nullptr ? V.start[s.first] : s.first * V.max_new;
-    const int rows = len == 0 ? 0 : V.start != nullptr ? V.start[s.last] - row0 : (s.last - s.first) * V.max_new;
-    groups[g] = make_int4(row0, rows, len, s.first);
+    const int row0 = len == 0 ? 0 : V.start != nullptr ? V.start[first] : first * V.max_new;
+    const int rows = len == 0 ? 0 : V.start != nullptr ? V.start[end] - row0 : (end - first) * V.max_new;
+    groups[g] = make_int4(row0, rows, len, first);
   }
-  if (s.len == 0) return;
-  for (int b = s.first + threadIdx.x / 32; b < s.last; b += blockDim.x / 32) {
-    if (group_of(P, b) != g) continue;
-    const int lane = threadIdx.x & 31;
+  if (!ascending) return;
+  const int lane = threadIdx.x & 31;
+  for (int b = first + threadIdx.x / 32; b < end; b += blockDim.x / 32) {
     if (lane == 0) shared[b] = len;
     if (len == 0) continue;
     Seq q;
@@ -54,6 +71,7 @@ constexpr int kJoinThreads = 256;
 template <typename T, int HD>
 __global__ void __launch_bounds__(kJoinThreads) kv8_shares_kernel(View V, Part part, int n_prefix, int n_own, T* __restrict__ o, int64_t o_stride, int H) {
   constexpr int kLanes = HD / 4;
+  chain_wait();
   const int b = blockIdx.x / V.max_new, i = blockIdx.x % V.max_new;
   const Seq s = load_seq(V, b);
   const int head = blockIdx.y * (kJoinThreads / kLanes) + threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
@@ -90,15 +108,22 @@ struct SharePlan {
 };
 // How a pass's positions are cut.  The lengths are on the device, so the rule goes by the number of items (owner, head, row
 // tile): as many shares as fill the SMs once (many rows: one block per SM) or twice (few rows), of 2 steps of 128 (units of 32 per warp) of
-// what the page table could hold.
-Pass make_pass(const View& V, int64_t max_rows, int64_t owners, int H, bool wide_type) {
+// what the page table could hold.  A sequence's pass for few rows joins its shares in a cluster: a power of two up to 8.
+Pass make_pass(const View& V, int64_t max_rows, int64_t owners, int H, bool wide_type, bool prefix) {
   const int64_t rows = max_rows * (H / V.hkv), places = static_cast<int64_t>(V.max_pages) << V.page_shift;
   Pass p{!wide_type && rows > 32, static_cast<int>(max_rows), 1};
   const int64_t tile = p.many ? 256 : rows <= 8 ? 8 : 16, items = owners * V.hkv * ceil_div(rows, tile);
   const int64_t room = p.many ? 148 : 296, least = p.many ? 256 : 128;
-  while (p.shares < 32 && items * (p.shares + 1) <= room && places >= least * (p.shares + 1)) ++p.shares;
+  if (prefix || p.many) {
+    while (p.shares < 32 && items * (p.shares + 1) <= room && places >= least * (p.shares + 1)) ++p.shares;
+  } else {
+    while (p.shares < 8 && items * p.shares * 2 <= room && places >= least * 2 * p.shares) p.shares *= 2;
+  }
   return p;
 }
+// Up to this much to read, if every sequence reads all that its table could hold, the sequences' own attention is as fast: it is one
+// launch, and shared pages come from L2
+constexpr int64_t kDirectBytes = int64_t(96) << 20;
 SharePlan share_plan(const View& V, const Prefix& P, int H, int hd, bool wide_type) {
   SharePlan p = {};
   size_t at = 0;
@@ -110,13 +135,14 @@ SharePlan share_plan(const View& V, const Prefix& P, int H, int hd, bool wide_ty
   p.groups = take(static_cast<size_t>(P.n_groups) * sizeof(int4));
   p.shared = take(static_cast<size_t>(V.batch) * sizeof(int32_t));
   p.pos = take(static_cast<size_t>(V.rows) * sizeof(int32_t));
-  p.direct = P.n_groups == 0 || static_cast<int64_t>(V.max_new) * (H / V.hkv) >= 256;
+  p.direct = P.n_groups == 0 || P.max_seqs == 0 || static_cast<int64_t>(V.max_new) * (H / V.hkv) >= 256 ||
+             (static_cast<int64_t>(V.batch) * V.max_pages << V.page_shift) * V.hkv * hd * 2 <= kDirectBytes;
   if (!p.direct) {
     const int64_t most = static_cast<int64_t>(P.max_seqs) * V.max_new;
-    p.prefix = make_pass(V, most < V.rows ? most : V.rows, P.n_groups, H, wide_type);
-    p.own = make_pass(V, V.max_new, V.batch, H, wide_type);
+    p.prefix = make_pass(V, most < V.rows ? most : V.rows, P.n_groups, H, wide_type, true);
+    p.own = make_pass(V, V.max_new, V.batch, H, wide_type, false);
     p.row_heads = V.rows * H;
-    const size_t n = static_cast<size_t>(p.prefix.shares + p.own.shares) * p.row_heads;
+    const size_t n = static_cast<size_t>(p.prefix.shares + (p.own.many ? p.own.shares : 0)) * p.row_heads;
     p.sums = take(n * hd * sizeof(float));
     p.stats = take(n * sizeof(float2));
   }
@@ -136,17 +162,19 @@ szo_status launch_shares(const View& V, const Prefix& P, const Rows& A, const Sh
   part.prefix = 1;
   part.items = P.n_groups;
   part.max_rows = p.prefix.max_rows;
-  if (part.max_rows > 0) SZO_TRY((run_pass<T, HD>(V, A, part, p.prefix, st)));
+  SZO_TRY((run_pass<T, HD>(V, A, part, p.prefix, st)));
   Part own = base;
-  own.sums += p.prefix.shares * base.row_heads * HD;
-  own.stats += p.prefix.shares * base.row_heads;
   own.items = V.batch;
   own.max_rows = V.max_new;
+  own.shares = p.prefix.shares;
+  if (!p.own.many) return run_pass<T, HD>(V, A, own, p.own, st);
+  own.sums += p.prefix.shares * base.row_heads * HD;
+  own.stats += p.prefix.shares * base.row_heads;
   SZO_TRY((run_pass<T, HD>(V, A, own, p.own, st)));
   const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(V.batch) * V.max_new), static_cast<unsigned>(ceil_div(A.H, kJoinThreads / (HD / 4))));
-  kv8_shares_kernel<T, HD><<<grid, kJoinThreads, 0, st>>>(V, base, p.prefix.shares, p.own.shares, static_cast<T*>(A.o), A.o_stride, A.H);
+  SZO_CHECK_CUDA(launch_maybe_chained(kv8_shares_kernel<T, HD>, grid, dim3(kJoinThreads), 0, st, true, V, base, p.prefix.shares, p.own.shares,
+                                      static_cast<T*>(A.o), A.o_stride, A.H));
   count_launch();
-  SZO_CHECK_LAUNCH("kv8_shares_kernel");
   return SZO_OK;
 }
 

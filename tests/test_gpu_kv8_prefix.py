@@ -34,6 +34,13 @@ class SharedWorld(World):
                 self.table[b, :len(self.pages[b])] = self.pages[b]
             at += n
         self.d_table.copy_(torch.from_numpy(self.table))
+        # the same table with room for so many pages that reading them for every sequence would be a lot: shared pages are then
+        # taken apart; with the narrow one a small batch goes to the attention that shares nothing
+        self.narrow = self.d_table
+        room = -(-(100 << 20) // (len(caps) * page * hkv * d * 2)) + 1
+        self.wide = torch.full((len(caps), room), -7, dtype=torch.int32, device="cuda")
+        self.wide[:, :self.narrow.shape[1]] = self.narrow
+        self.d_table = self.wide
 
     def fill(self, lens, dt="bf16", loud=1.0, nan=()):
         """Everything that the sequences' first lens positions need; nan: (sequence, position, head, dim, which)."""
@@ -58,12 +65,22 @@ class SharedWorld(World):
 
 
 def check(B, w, lens, news, H, dt, scale=None, spread=1.0, gap=1, prefix=None, q=None, skipped=()):
+    w.d_table = w.narrow
     batch, start, rows = w.batch(lens, news, gap)
     if q is None:
         q = torch.from_numpy(w.g.normal(0, spread, (rows, H, w.d))).to(DT[dt])
-    out = torch.full_like(q, 3.0).cuda()
-    B.szo_attention_kv8_prefix(w.cache, batch, prefix or w.prefix(), q.cuda(), scale=scale, out=out)
-    got = out.double().cpu().numpy()
+    got = []
+    for table in (w.narrow, w.wide):
+        w.d_table = table
+        batch, start, rows = w.batch(lens, news, gap)
+        out = torch.full_like(q, 3.0).cuda()
+        B.szo_attention_kv8_prefix(w.cache, batch, prefix or w.prefix(), q.cuda(), scale=scale, out=out)
+        got.append(out.double().cpu().numpy())
+    for one in got:
+        compare(w, one, q, start, rows, lens, news, H, dt, scale, gap, skipped)
+
+
+def compare(w, got, q, start, rows, lens, news, H, dt, scale, gap, skipped):
     assert (got[:gap] == 3).all() and (got[rows - gap:] == 3).all()
     sc = scale if scale is not None else 1 / math.sqrt(w.d)
     for b, (n, m) in enumerate(zip(lens, news)):
@@ -78,7 +95,6 @@ def check(B, w, lens, news, H, dt, scale=None, spread=1.0, gap=1, prefix=None, q
         assert np.array_equal(np.isnan(mine), np.isnan(o)), (b, n, m, np.argwhere(np.isnan(mine) != np.isnan(o))[:4])
         bad = np.abs(np.nan_to_num(mine - o)) > np.nan_to_num(attention_bound(o, wide, big, n, w.d, dt, top[..., None]), nan=1.0)
         assert not bad.any(), (b, n, m, np.argwhere(bad)[:4], np.abs(mine - o).max())
-    return batch, q, out
 
 
 SHAPES = [(64, 1, 1, 16), (128, 2, 1, 16), (128, 1, 4, 64), (64, 2, 5, 32), (128, 1, 8, 128), (64, 1, 9, 16), (128, 2, 3, 32)]
@@ -194,7 +210,7 @@ def test_descriptions_that_do_not_fit_share_nothing(B):
     w = SharedWorld(B, [count], [128], lens, 1, 16, 64, seed=26)
     w.fill(lens)
     ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
-    cap = w.table.shape[1] * 16
+    cap = w.wide.shape[1] * 16
     for prefix in (B.Kv8Prefix(ints(-1)), B.Kv8Prefix(ints(cap + 1)), B.Kv8Prefix(ints(128), ints(0, count + 1), max_seqs=count + 1),
                    B.Kv8Prefix(ints(128), ints(4, 2), max_seqs=count), B.Kv8Prefix(ints(128), ints(-1, 4), max_seqs=count),
                    B.Kv8Prefix(ints(128), ints(0, count), max_seqs=count - 1)):
@@ -235,6 +251,9 @@ def test_agrees_with_attention_that_shares_nothing(B, dt, H, hkv, d, page, new, 
     codes[(codes & 127) == 127] = 3
     scales = torch.exp2(torch.randint(-9, -6, (n_pages, hkv, 2), device="cuda", generator=g).float())
     cache = B.Kv8Cache(codes, scales)
+    room = -(-(100 << 20) // (count * page * hkv * d * 2)) + 1             # (see SharedWorld)
+    if room > per:
+        table = torch.cat([table, torch.full((count, room - per), -7, dtype=torch.int32, device="cuda")], 1)
     batch = B.Kv8Batch(table, torch.tensor(lens, dtype=torch.int32, device="cuda"), count * new)
     shared = B.Kv8Prefix(torch.tensor([prefix], dtype=torch.int32, device="cuda"))
     q = torch.randn(count * new, H, d, device="cuda", generator=g).to(DT[dt])
