@@ -6,7 +6,7 @@
 //   lse = M + log2(S + 2^(x_t - M)),   loss = log(1 + S 2^(M - x_t)):
 // loss does not come from the difference of two numbers of the size of lse, so a confident row's keeps its relative precision.
 // Backward: G = scale ((a + b) p - a 1[t]) (a = d_loss, b = d_lse), p = 2^(x - lse), for a piece of the vocabulary at a time, in the
-// 16-bit type of the products that follow; p - 1 of the target is formed before the rounding (expm1).
+// 16-bit type of the products that follow; p - 1 of the target is formed before the rounding.
 #include <cmath>
 
 #include "head_ce.cuh"
@@ -86,63 +86,91 @@ __global__ void __launch_bounds__(256) head_join_kernel(const float2* __restrict
 
 // What the gradient needs of a row: x = lse in base 2, y = weight of p, z = weight of the target (both times scale and, for fp16, a
 // power of two that brings the larger to [2^13, 2^14)), w = that power's inverse.  Rows that weigh nothing have y = z = 0.
-// One block looks at all rows, so that it knows the largest; more than that many rows go over several, which meet in `exponent`.
-constexpr int kRowThreads = 1024;
-__global__ void __launch_bounds__(kRowThreads) head_rows_kernel(const int32_t* __restrict__ targets, const float* __restrict__ lse,
-                                                                const float* __restrict__ d_loss, const float* __restrict__ d_lse, int64_t rows,
-                                                                int64_t vocab, float scale, bool half, float4* __restrict__ info,
-                                                                int32_t* __restrict__ exponent) {
-  __shared__ int tops[kRowThreads / 32];
-  chain_release();
+struct RowArgs {
+  const int32_t* targets;
+  const float *lse, *d_loss, *d_lse;
+  int64_t rows, vocab;
+  float scale;
+};
+template <typename T> constexpr bool kIsHalf = std::is_same<T, __half>::value;
+template <typename T> __device__ __forceinline__ float4 row_info(const RowArgs& A, int64_t r, int* exponent) {
+  const int32_t t = A.targets[r];
+  const float d = A.d_loss[r], b = A.d_lse != nullptr ? A.d_lse[r] : 0.f, l = A.lse[r], a = t >= 0 && t < A.vocab ? d : 0.f;
+  float y = A.scale * (a + b), z = A.scale * a, inv = 1.f;
+  *exponent = kNoExponent;
+  if (l == -INFINITY) y = z = 0.f;
+  if (kIsHalf<T> && (y != 0.f || z != 0.f)) {
+    const float top = fmaxf(fmaxf(fabsf(y), fabsf(z)), fabsf(A.scale * b));
+    const int e = min(max(((__float_as_int(top) >> 23) & 255) - 127, -100), 100);      // (rows beyond: as near as it goes)
+    const float f = __int_as_float((13 - e + 127) << 23);
+    y *= f;
+    z *= f;
+    inv = __int_as_float((e - 13 + 127) << 23);
+    *exponent = e;
+  }
+  return make_float4(l * kLog2e, y, z, inv);
+}
+// The largest exponent of all rows, in every thread of the block
+template <typename T> __device__ __forceinline__ int largest_exponent(const RowArgs& A) {
+  __shared__ int tops[32];
   int most = kNoExponent;
-#pragma unroll 2
-  for (int64_t r = static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x; r < rows; r += static_cast<int64_t>(gridDim.x) * kRowThreads) {
-    const int32_t t = targets[r];
-    const float d = d_loss[r], b = d_lse != nullptr ? d_lse[r] : 0.f, l = lse[r], a = t >= 0 && t < vocab ? d : 0.f;
-    float y = scale * (a + b), z = scale * a, inv = 1.f;
-    if (l == -INFINITY) y = z = 0.f;
-    if (half && (y != 0.f || z != 0.f)) {
-      const float top = fmaxf(fmaxf(fabsf(y), fabsf(z)), fabsf(scale * b));
-      const int e = min(max(((__float_as_int(top) >> 23) & 255) - 127, -100), 100);      // (rows beyond: as near as it goes)
-      const float f = __int_as_float((13 - e + 127) << 23);
-      y *= f;
-      z *= f;
-      inv = __int_as_float((e - 13 + 127) << 23);
-      most = max(most, e);
-    }
-    info[r] = make_float4(l * kLog2e, y, z, inv);
+#pragma unroll 4
+  for (int64_t r = threadIdx.x; r < A.rows; r += blockDim.x) {
+    int e;
+    row_info<T>(A, r, &e);
+    most = max(most, e);
   }
   most = __reduce_max_sync(0xffffffffu, most);
   if (threadIdx.x % 32 == 0) tops[threadIdx.x / 32] = most;
   __syncthreads();
-  if (threadIdx.x >= 32) return;
-  most = __reduce_max_sync(0xffffffffu, tops[threadIdx.x]);
-  if (threadIdx.x != 0) return;
-  if (gridDim.x == 1) *exponent = most;
-  else atomicMax(exponent, most);
+  most = tops[0];
+  for (int i = 1; i < static_cast<int>(blockDim.x) / 32; ++i) most = max(most, tops[i]);
+  return most;
 }
-
-// h for dW: rows that weigh nothing become zeros; fp16 rows are brought to the largest weight (exactly but for what falls below fp16's range)
+// Up to this many rows every block of the next kernel looks for the largest itself; more are looked at once, before it
+constexpr int64_t kScanRows = 2048;
+template <typename T> __global__ void __launch_bounds__(1024) head_exponent_kernel(RowArgs A, int32_t* __restrict__ exponent) {
+  chain_release();
+  const int most = largest_exponent<T>(A);
+  if (threadIdx.x == 0) *exponent = most;
+}
+// Rows' infos, zeroed counters and, for dW (`copy`), h with rows that weigh nothing as zeros and fp16 rows brought to the largest weight
+// (exactly but for what falls below fp16's range): eight elements per thread
 template <typename T>
-__global__ void head_copy_kernel(const T* __restrict__ h, int64_t h_stride, int64_t rows, int64_t d, const float4* __restrict__ info,
-                                 const int32_t* __restrict__ exponent, T* __restrict__ out) {
+__global__ void __launch_bounds__(256) head_prepare_kernel(RowArgs A, const T* __restrict__ h, int64_t h_stride, int64_t d, float4* __restrict__ info,
+                                                           int32_t* __restrict__ exponent, T* __restrict__ copy, int32_t* __restrict__ counters,
+                                                           int64_t n_counters) {
   chain_release();
   chain_wait();
-  const int64_t per = d / 8, i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-  if (i >= rows * per) return;
+  if (blockIdx.x == 0)
+    for (int64_t i = threadIdx.x; i < n_counters; i += blockDim.x) counters[i] = 0;
+  int most = kNoExponent;
+  if (kIsHalf<T> && copy != nullptr) {
+    if (A.rows <= kScanRows) {
+      most = largest_exponent<T>(A);
+      if (blockIdx.x == 0 && threadIdx.x == 0) *exponent = most;
+    } else {
+      most = *exponent;
+    }
+  }
+  const int64_t per = copy != nullptr ? d / 8 : 1, i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+  if (i >= A.rows * per) return;
   const int64_t r = i / per, c = i % per * 8;
-  const float4 f = info[r];
+  int e;
+  const float4 f = row_info<T>(A, r, &e);
+  if (c == 0) info[r] = f;
+  if (copy == nullptr) return;
   uint4 x = make_uint4(0u, 0u, 0u, 0u);
   if (f.y != 0.f || f.z != 0.f) {
     x = *reinterpret_cast<const uint4*>(h + r * h_stride + c);
-    if constexpr (sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value) {
-      const float to = f.w * __int_as_float((13 - *exponent + 127) << 23);
-      T* e = reinterpret_cast<T*>(&x);
+    if constexpr (kIsHalf<T>) {
+      const float to = f.w * __int_as_float((13 - most + 127) << 23);
+      T* el = reinterpret_cast<T*>(&x);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) e[k] = narrow<T>(widen<T>(e[k]) * to);
+      for (int k = 0; k < 8; ++k) el[k] = narrow<T>(widen<T>(el[k]) * to);
     }
   }
-  *reinterpret_cast<uint4*>(out + r * d + c) = x;
+  *reinterpret_cast<uint4*>(copy + r * d + c) = x;
 }
 
 // dh: the sums of a row (of `parts` parts, in their order) times its power of two, rounded
@@ -173,10 +201,12 @@ struct Shape {
 };
 struct Plan {
   size_t part, xt;                                                // of a workspace, in bytes from its start
-  size_t info, exponent, copy, G[2], acc;
+  size_t info, exponent, counters, copy, G, acc;
   size_t total;
-  int64_t piece;                                                  // vocabulary rows of a piece
-  int parts, dh_parts;
+  int parts;                                                      // forward: of the vocabulary
+  int64_t piece;                                                  // vocabulary entries of a piece of G
+  int pieces, lag, buffers;
+  int dh_parts, sums;                                             // shares of dh's sum over a piece; sums kept apart in all
 };
 struct Taker {
   size_t at = 0;
@@ -206,21 +236,32 @@ Plan forward_plan(const Shape& s) {
   p.total = take.at;
   return p;
 }
-// Pieces: G of one is at most 64 MB (half of L2), and a piece is 8192 to 65536 vocabulary rows.
+// Gradient.  G of a piece is about 64 MB (half of L2), and a piece 8192 to 65536 entries.  Many rows: one launch for all pieces, dh and dW
+// following G `lag` pieces behind, far enough that hardly a unit waits for one that runs beside it, and no SM for the end of a piece (4096 rows
+// of 32000 x 4096 in a launch per piece 1614 us, in one 1476); the sums of dh are kept in one place, piece after piece.  Few rows: a launch per
+// piece, since units that wait for others cost more than the end of a launch there (16 rows of 32000 x 4096 95 us, in one launch
+// 107, with dh so close behind G that it finds W in L2); the sums of the pieces are kept apart.
 Plan backward_plan(const Shape& s, bool dh, bool dw) {
   Plan p = {};
   Taker take;
-  int64_t piece = (int64_t(64) << 20) / (2 * s.rows) / kTile * kTile;
+  const bool is_few = few(s.rows);
+  int64_t piece = (int64_t(64) << 20) / (2 * s.rows);
   piece = piece < 8192 ? 8192 : piece > 65536 ? 65536 : piece;
-  p.piece = piece < s.vocab ? piece : static_cast<int64_t>(round_up(s.vocab, kTile));
+  if (piece > s.vocab) piece = s.vocab;
+  p.piece = static_cast<int64_t>(round_up(static_cast<size_t>(piece), kTile));
+  p.pieces = static_cast<int>(ceil_div(s.vocab, p.piece));
+  p.lag = is_few ? 1 : static_cast<int>(ceil_div(kPairs + kPairs / 4, tiles_of(s.rows) * ceil_div(p.piece, kTile)));
+  if (p.lag > p.pieces) p.lag = p.pieces;
+  p.buffers = p.lag + 2 < p.pieces ? p.lag + 2 : p.pieces;
   p.info = take(static_cast<size_t>(s.rows) * sizeof(float4));
   p.exponent = take(sizeof(int32_t));
+  p.counters = take(static_cast<size_t>(counters_of(p.pieces)) * sizeof(int32_t));
   if (dw) p.copy = take(static_cast<size_t>(s.rows) * s.d * 2);
-  for (int i = 0; i < (p.piece < s.vocab ? 2 : 1); ++i) p.G[i] = take(static_cast<size_t>(s.rows) * p.piece * 2);
-  // few tiles of dh: its long sums over the vocabulary are cut so that the rounds of tiles over the pairs of SMs are as full
-  // as they get, in parts of 8 blocks of 64 at least
+  p.G = take(static_cast<size_t>(s.rows) * p.piece * p.buffers * 2);
+  // few tiles of dh: its sums over a piece are cut so that the rounds of tiles over the pairs of SMs are as full as they get, in shares of
+  // 8 blocks of 64 at least
   p.dh_parts = 1;
-  const int64_t tiles = static_cast<int64_t>(few(s.rows) ? 1 : tiles_of(s.rows)) * tiles_of(s.d), nkb = ceil_div(s.vocab < p.piece ? s.vocab : p.piece, kBlockK);
+  const int64_t tiles = static_cast<int64_t>(is_few ? p.pieces : tiles_of(s.rows)) * tiles_of(s.d), nkb = p.piece / kBlockK;
   double best = 1e30;
   for (int n = 1; n <= 16 && nkb >= 8 * n && (n == 1 || tiles * n <= 2 * kPairs); ++n) {
     const double cost = static_cast<double>(ceil_div(tiles * n, kPairs)) * (static_cast<double>(nkb) / n + 8);      // (a unit's fixed part: about 8 blocks)
@@ -229,7 +270,10 @@ Plan backward_plan(const Shape& s, bool dh, bool dw) {
       p.dh_parts = n;
     }
   }
-  if (dh) p.acc = take(static_cast<size_t>(p.dh_parts) * s.rows * s.d * sizeof(float));
+  const int64_t last = ceil_div(s.vocab - (p.pieces - 1) * p.piece, kBlockK);
+  p.sums = is_few ? (p.pieces - 1) * p.dh_parts + static_cast<int>(last < p.dh_parts ? last : p.dh_parts)
+                  : static_cast<int>(p.pieces > 1 || last >= p.dh_parts ? p.dh_parts : last);
+  if (dh) p.acc = take(static_cast<size_t>(p.sums) * s.rows * s.d * sizeof(float));
   p.total = take.at;
   return p;
 }
@@ -263,31 +307,38 @@ szo_status matrix_map(CUtensorMap* map, const T* base, int64_t rows, int64_t col
 }
 // Operands.  `rows_box`: rows that a CTA brings per stage where they are not contracted (64 of them, twice 64 elements, where they are)
 template <typename T>
-szo_status operand_a(Job* j, const T* base, int64_t rows, int64_t cols, int64_t stride, bool mn, int64_t m0, int64_t k0, int rows_box) {
+szo_status operand_a(Job* j, const T* base, int64_t rows, int64_t cols, int64_t stride, bool mn, Offset from, int rows_box) {
   j->a_mn = mn;
-  j->a_m0 = static_cast<int>(m0);
-  j->a_k0 = static_cast<int>(k0);
+  j->a_from = from;
   j->a_bytes = (mn ? 128 : rows_box) * kBlockK * 2;
   return matrix_map(&j->a, base, rows, cols, stride, mn ? 64 : rows_box);
 }
 template <typename T>
-szo_status operand_b(Job* j, const T* base, int64_t rows, int64_t cols, int64_t stride, bool mn, int64_t n0, int64_t k0, int rows_box) {
+szo_status operand_b(Job* j, const T* base, int64_t rows, int64_t cols, int64_t stride, bool mn, Offset from, int rows_box) {
   j->b_mn = mn;
-  j->b_n0 = static_cast<int>(n0);
-  j->b_k0 = static_cast<int>(k0);
+  j->b_from = from;
   j->b_bytes = (mn ? 128 : rows_box) * kBlockK * 2;
   return matrix_map(&j->b, base, rows, cols, stride, mn ? 64 : rows_box);
 }
-void sizes(Job* j, Kind kind, int64_t m, int64_t n, int64_t k, int parts, int m_step = kTile, int n_step = kTile) {
+// The product's extent: m, n or k (vocab_dim 0, 1, 2) is the piece of the vocabulary, `piece` entries, `last` in the last one
+void sizes(Job* j, Kind kind, int vocab_dim, int64_t m, int64_t n, int64_t k, int64_t piece, int64_t last, int parts = 1, int m_step = kTile,
+           int n_step = kTile) {
   j->kind = kind;
+  j->vocab_dim = vocab_dim;
   j->m_limit = static_cast<int>(m);
   j->m_step = m_step;
   j->n_step = n_step;
-  j->m_tiles = static_cast<int>(ceil_div(m, m_step));
-  j->n_tiles = static_cast<int>(ceil_div(n, n_step));
-  j->nkb = static_cast<int>(ceil_div(k, kBlockK));
-  j->parts = parts;
-  j->units = j->m_tiles * j->n_tiles * parts;
+  auto extent = [&](int64_t v) {
+    Extent e;
+    e.m_tiles = static_cast<int>(ceil_div(vocab_dim == 0 ? v : m, m_step));
+    e.n_tiles = static_cast<int>(ceil_div(vocab_dim == 1 ? v : n, n_step));
+    e.nkb = static_cast<int>(ceil_div(vocab_dim == 2 ? v : k, kBlockK));
+    e.parts = parts < e.nkb ? parts : e.nkb;
+    e.units = e.m_tiles * e.n_tiles * e.parts;
+    return e;
+  };
+  j->full = extent(piece);
+  j->last = extent(last);
 }
 // Tiles of m in equal bands whose part of A (16-bit) is at most 48 MB: it stays in L2 while B goes by
 int band_of(int64_t m, int64_t k) {
@@ -305,37 +356,42 @@ template <typename T> struct Inputs {
   const int32_t* targets;
 };
 
-// The logits' product over n vocabulary entries from j0 on
-template <typename T> szo_status logits_job(Job* j, const Shape& s, const Inputs<T>& in, int64_t j0, int64_t n, Kind kind, Kind kind_few) {
+// The logits' product over a piece of the vocabulary; few rows: in tiles of `step` vocabulary entries
+template <typename T> szo_status logits_job(Job* j, const Shape& s, const Inputs<T>& in, int64_t piece, int64_t last, int step, Kind kind, Kind kind_few) {
   if (few(s.rows)) {
-    const int step = step_of(n), cols = static_cast<int>(round_up(s.rows, 32));
-    SZO_TRY(operand_a(j, in.W, s.vocab, s.d, in.ws, false, j0, 0, step / 2));
-    SZO_TRY(operand_b(j, in.h, s.rows, s.d, in.hs, false, 0, 0, cols / 2));
-    sizes(j, kind_few, n, s.rows, s.d, 1, step, cols);
+    const int cols = static_cast<int>(round_up(s.rows, 32));
+    SZO_TRY(operand_a(j, in.W, s.vocab, s.d, in.ws, false, kVocab, step / 2));
+    SZO_TRY(operand_b(j, in.h, s.rows, s.d, in.hs, false, kNone, cols / 2));
+    sizes(j, kind_few, 0, 0, s.rows, s.d, piece, last, 1, step, cols);
     return SZO_OK;
   }
-  SZO_TRY(operand_a(j, in.h, s.rows, s.d, in.hs, false, 0, 0, 128));
-  SZO_TRY(operand_b(j, in.W, s.vocab, s.d, in.ws, false, j0, 0, 128));
-  sizes(j, kind, s.rows, n, s.d, 1);
+  SZO_TRY(operand_a(j, in.h, s.rows, s.d, in.hs, false, kNone, 128));
+  SZO_TRY(operand_b(j, in.W, s.vocab, s.d, in.ws, false, kVocab, 128));
+  sizes(j, kind, 1, s.rows, 0, s.d, piece, last);
   j->m_band = band_of(s.rows, s.d);
   return SZO_OK;
+}
+Jobs no_jobs() {
+  Jobs P = {};
+  for (Job& j : P.job) j.kind = -1;
+  P.pieces = P.buffers = 1;
+  return P;
 }
 
 template <typename T>
 szo_status forward(const Shape& s, const Inputs<T>& in, float* loss, float* lse, unsigned char* ws, int32_t* status, cudaStream_t st) {
   const Plan p = forward_plan(s);
-  Jobs P = {};
-  SZO_TRY(logits_job(&P.job[0], s, in, 0, s.vocab, kStats, kStatsT));
-  P.n_jobs = 1;
-  P.units = P.job[0].units;
+  Jobs P = no_jobs();
+  SZO_TRY(logits_job(&P.job[0], s, in, s.vocab, s.vocab, step_of(s.vocab), kStats, kStatsT));
+  P.vocab = P.piece = static_cast<int>(s.vocab);
+  P.units = P.job[0].last.units;
   P.targets = in.targets;
   P.part = reinterpret_cast<float2*>(ws + p.part);
   P.xt = reinterpret_cast<float*>(ws + p.xt);
   P.rows = s.rows;
-  P.n_end = static_cast<int>(s.vocab);
   P.c = in.scale * kLog2e;
   P.status = status;
-  SZO_TRY(launch_jobs<T>(P, false, st));
+  SZO_TRY(launch_jobs<T>(P, few(s.rows), false, st));
   auto join = [&](auto kern, int rows) {
     return launch_maybe_chained(kern, dim3(blocks_of(s.rows, rows)), dim3(256), 0, st, true, P.part, P.xt, in.targets, s.rows, s.vocab, p.parts, loss, lse,
                                 status);
@@ -350,79 +406,89 @@ szo_status backward(const Shape& s, const Inputs<T>& in, const float* lse, const
                     unsigned char* ws, int32_t* status, cudaStream_t st) {
   const Plan p = backward_plan(s, dh != nullptr, dw != nullptr);
   float4* info = reinterpret_cast<float4*>(ws + p.info);
-  int32_t* exponent = reinterpret_cast<int32_t*>(ws + p.exponent);
-  T* copy = reinterpret_cast<T*>(ws + p.copy);
+  int32_t *exponent = reinterpret_cast<int32_t*>(ws + p.exponent), *counters = reinterpret_cast<int32_t*>(ws + p.counters);
+  T *copy = dw != nullptr ? reinterpret_cast<T*>(ws + p.copy) : nullptr, *G = reinterpret_cast<T*>(ws + p.G);
   float* acc = reinterpret_cast<float*>(ws + p.acc);
-  const unsigned row_blocks = s.rows <= 8 * kRowThreads ? 1 : blocks_of(s.rows, kRowThreads);
-  if (row_blocks > 1) SZO_CHECK_CUDA(cudaMemsetAsync(exponent, 0x80, sizeof(int32_t), st));
-  head_rows_kernel<<<row_blocks, kRowThreads, 0, st>>>(in.targets, lse, d_loss, d_lse, s.rows, s.vocab, in.scale, !std::is_same<T, __nv_bfloat16>::value,
-                                                     info, exponent);
-  count_launch();
-  SZO_CHECK_LAUNCH("head_rows_kernel");
-  const unsigned vec_blocks = blocks_of(s.rows * (s.d / 8), 256);
-  if (dw != nullptr) {
-    SZO_CHECK_CUDA(launch_maybe_chained(head_copy_kernel<T>, dim3(vec_blocks), dim3(256), 0, st, true, in.h, in.hs, s.rows, s.d, info, exponent, copy));
+  const RowArgs rows{in.targets, lse, d_loss, d_lse, s.rows, s.vocab, in.scale};
+  const bool scan = kIsHalf<T> && dw != nullptr && s.rows > kScanRows;
+  if (scan) {
+    head_exponent_kernel<T><<<1, 1024, 0, st>>>(rows, exponent);
     count_launch();
+    SZO_CHECK_LAUNCH("head_exponent_kernel");
   }
-  // Launch i takes G of piece i and, of piece i - 1, dh and dW: what a launch reads, the launch before it wrote
-  const int pieces = static_cast<int>(ceil_div(s.vocab, p.piece));
-  for (int i = 0; i <= pieces; ++i) {
-    Jobs P = {};
-    P.targets = in.targets;
-    P.info = info;
-    P.exponent = exponent;
-    P.rows = s.rows;
-    P.c = in.scale * kLog2e;
-    P.g_stride = p.piece;
-    P.sums = acc;
-    P.d = static_cast<int>(s.d);
-    P.status = status;
-    if (i > 0) {
-      const int64_t j0 = (i - 1) * p.piece, n = s.vocab - j0 < p.piece ? s.vocab - j0 : p.piece;
-      const T* G = reinterpret_cast<const T*>(ws + p.G[(i - 1) & 1]);
-      if (dh != nullptr) {
-        Job& j = P.job[P.n_jobs++];
-        const int64_t nkb = ceil_div(n, kBlockK);                 // (a short last piece may have fewer blocks than parts)
-        const int parts = nkb < p.dh_parts ? static_cast<int>(nkb) : p.dh_parts;
-        if (few(s.rows)) {
-          const int cols = static_cast<int>(round_up(s.rows, 32));
-          SZO_TRY(operand_a(&j, in.W, s.vocab, s.d, in.ws, true, 0, j0, 0));
-          SZO_TRY(operand_b(&j, G, s.rows, n, p.piece, false, 0, 0, cols / 2));
-          sizes(&j, kSumT, s.d, s.rows, n, parts, kTile, cols);
-        } else {
-          SZO_TRY(operand_a(&j, G, s.rows, n, p.piece, false, 0, 0, 128));
-          SZO_TRY(operand_b(&j, in.W, s.vocab, s.d, in.ws, true, 0, j0, 0));
-          const uint64_t dims[3] = {static_cast<uint64_t>(s.d), static_cast<uint64_t>(s.rows), static_cast<uint64_t>(p.dh_parts)};
-          const uint64_t strides[2] = {static_cast<uint64_t>(s.d) * 4, static_cast<uint64_t>(s.rows) * s.d * 4};
-          const uint32_t box[3] = {32, 32, 1};
-          SZO_TRY(encode_map(&j.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, acc, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B));
-          sizes(&j, kSum, s.rows, s.d, n, parts);
-        }
-        j.add = i > 1;
-      }
-      if (dw != nullptr) {
-        Job& j = P.job[P.n_jobs++];
-        SZO_TRY(operand_a(&j, G, s.rows, n, p.piece, true, 0, 0, 0));
-        SZO_TRY(operand_b(&j, copy, s.rows, s.d, s.d, true, 0, 0, 0));
-        SZO_TRY(matrix_map(&j.out, dw, s.vocab, s.d, dws, 32));
-        sizes(&j, kOut, n, s.d, s.rows, 1);
-        j.out_row0 = static_cast<int>(j0);
-      }
+  const unsigned vec_blocks = blocks_of(s.rows * (s.d / 8), 256);
+  SZO_CHECK_CUDA(launch_maybe_chained(head_prepare_kernel<T>, dim3(dw != nullptr ? vec_blocks : blocks_of(s.rows, 256)), dim3(256), 0, st, scan, rows, in.h,
+                                      in.hs, s.d, info, exponent, copy, counters, counters_of(p.pieces)));
+  count_launch();
+
+  Jobs P = no_jobs();
+  P.vocab = static_cast<int>(s.vocab);
+  P.piece = static_cast<int>(p.piece);
+  P.pieces = p.pieces;
+  P.lag = p.lag;
+  P.buffers = p.buffers;
+  P.targets = in.targets;
+  P.info = info;
+  P.exponent = exponent;
+  P.rows = s.rows;
+  P.c = in.scale * kLog2e;
+  P.G = G;
+  P.g_stride = p.piece * p.buffers;
+  P.sums = acc;
+  P.d = static_cast<int>(s.d);
+  P.status = status;
+  const int64_t last = s.vocab - (p.pieces - 1) * p.piece;
+  // (G is contracted in blocks of 64: it ends on one)
+  SZO_TRY(logits_job(&P.job[0], s, in, p.piece, static_cast<int64_t>(round_up(static_cast<size_t>(last), kBlockK)), step_of(p.piece), kGrad, kGradT));
+  if (!few(s.rows)) SZO_TRY(matrix_map(&P.job[0].out, G, s.rows, P.g_stride, P.g_stride, 32));
+  if (dh != nullptr) {
+    Job& j = P.job[1];
+    if (few(s.rows)) {
+      const int cols = static_cast<int>(round_up(s.rows, 32));
+      SZO_TRY(operand_a(&j, in.W, s.vocab, s.d, in.ws, true, kVocab, 0));
+      SZO_TRY(operand_b(&j, G, s.rows, P.g_stride, P.g_stride, false, kBuffer, cols / 2));
+      sizes(&j, kSumT, 2, s.d, s.rows, 0, p.piece, last, p.dh_parts, kTile, cols);
+    } else {
+      SZO_TRY(operand_a(&j, G, s.rows, P.g_stride, P.g_stride, false, kBuffer, 128));
+      SZO_TRY(operand_b(&j, in.W, s.vocab, s.d, in.ws, true, kVocab, 0));
+      const uint64_t dims[3] = {static_cast<uint64_t>(s.d), static_cast<uint64_t>(s.rows), static_cast<uint64_t>(p.sums)};
+      const uint64_t strides[2] = {static_cast<uint64_t>(s.d) * 4, static_cast<uint64_t>(s.rows) * s.d * 4};
+      const uint32_t box[3] = {32, 32, 1};
+      SZO_TRY(encode_map(&j.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, acc, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B));
+      sizes(&j, kSum, 2, s.rows, s.d, 0, p.piece, last, p.dh_parts);
     }
-    if (i < pieces) {
-      const int64_t j0 = i * p.piece, n = s.vocab - j0 < p.piece ? s.vocab - j0 : p.piece;
-      Job& j = P.job[P.n_jobs++];
-      SZO_TRY(logits_job(&j, s, in, j0, n, kGrad, kGradT));
-      P.G = ws + p.G[i & 1];
-      if (!few(s.rows)) SZO_TRY(matrix_map(&j.out, static_cast<T*>(P.G), s.rows, n, p.piece, 32));
-      P.n_end = static_cast<int>(n);
-      P.target0 = static_cast<int>(j0);
+  }
+  if (dw != nullptr) {
+    Job& j = P.job[2];
+    SZO_TRY(operand_a(&j, G, s.rows, P.g_stride, P.g_stride, true, kBuffer, 0));
+    SZO_TRY(operand_b(&j, copy, s.rows, s.d, s.d, true, kNone, 0));
+    SZO_TRY(matrix_map(&j.out, dw, s.vocab, s.d, dws, 32));
+    sizes(&j, kOut, 0, 0, s.d, s.rows, p.piece, last);
+  }
+  auto units = [&](int job, int i) -> int64_t {
+    const Job& j = P.job[job];
+    return j.kind < 0 || i < 0 || i >= p.pieces ? 0 : i == p.pieces - 1 ? j.last.units : j.full.units;
+  };
+  const int steps = p.pieces + p.lag;
+  int64_t all = 0;                                                // (below 2^31: see fits)
+  for (int i = 0; i < steps; ++i) {
+    const int64_t n = units(0, i) + units(1, i - p.lag) + units(2, i - p.lag);
+    if (few(s.rows)) {
+      P.step = i;
+      P.units = static_cast<int>(n);
+      P.idle = 0;
+      for (int k = 0; k < 3; ++k) P.idle |= units(k, k == 0 ? i : i - p.lag) == 0 ? 1 << k : 0;
+      SZO_TRY(launch_jobs<T>(P, true, true, st));
     }
-    for (int k = 0; k < P.n_jobs; ++k) P.units += P.job[k].units;
-    SZO_TRY(launch_jobs<T>(P, true, st));
+    all += n;
+  }
+  if (!few(s.rows)) {
+    P.counters = counters;
+    P.units = static_cast<int>(all);
+    SZO_TRY(launch_jobs<T>(P, false, true, st));
   }
   if (dh != nullptr) {
-    SZO_CHECK_CUDA(launch_maybe_chained(head_round_kernel<T>, dim3(vec_blocks), dim3(256), 0, st, true, acc, p.dh_parts, s.rows, s.d, info, dh, dhs));
+    SZO_CHECK_CUDA(launch_maybe_chained(head_round_kernel<T>, dim3(vec_blocks), dim3(256), 0, st, true, acc, p.sums, s.rows, s.d, info, dh, dhs));
     count_launch();
   }
   return SZO_OK;

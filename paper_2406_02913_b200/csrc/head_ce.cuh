@@ -24,32 +24,39 @@ enum Kind : int {
   kGradT,
   kSumT
 };
+enum Offset : int { kNone, kVocab, kBuffer };  // of an operand's vocabulary dimension: the piece's first entry, or its buffer of G
+struct Extent {                                // of a product over a piece: tiles, blocks of 64 contracted elements, and the shares that these are cut into
+  int m_tiles, n_tiles, nkb, parts, units;     // units = m_tiles * n_tiles * parts
+};
 struct Job {
   CUtensorMap a, b, out;                       // operands by boxes of 64 elements; out: boxes of 32 rows
-  int kind;
+  int kind;                                    // -1: no such job
+  int vocab_dim;                               // which dimension is the piece of the vocabulary: 0 m, 1 n, 2 k
   int a_mn, b_mn;                              // the operand's rows are the contracted dimension
+  int a_from, b_from;                          // Offset
   int a_bytes, b_bytes;                        // of the operands per stage and CTA
-  int a_m0, a_k0, b_n0, b_k0;                  // where the operands' pieces start
   int m_step, n_step;                          // a tile's rows and columns; each CTA brings half of either
-  int m_tiles, n_tiles, m_band;                // tiles of m are taken in bands of m_band (0: all)
-  int nkb, parts, units;                       // blocks of 64 contracted elements, cut into `parts`; units = tiles * parts
-  int out_row0;                                // the tile's first row in `out`
-  int m_limit;                                 // rows of D that there are
-  int add;
+  int m_limit;                                 // rows of D that there are (where they are not the vocabulary)
+  int m_band;                                  // tiles of m are taken in bands of m_band (0: all)
+  Extent full, last;                           // over a piece, over the last one
 };
+// The units of work, in their order: for s = 0, 1, ..  job 0 of piece s, then jobs 1 and 2 of piece s - lag.  Jobs 1 and 2 read what job 0
+// has written of their piece, in a ring of buffers.  A launch takes all steps s, its units handed out as they are asked for and waiting for
+// what they read (`counters`), or one step, its units dealt out in turn.
 struct Jobs {
   Job job[3];
-  int n_jobs, units;
-  int b_at, stage_bytes, stages;               // the ring: B's place in a stage (set by launch_jobs)
-  // kStats, kGrad
+  int vocab, piece, pieces, lag, buffers;
+  int step, units;                             // the first step of the launch, and its units
+  int idle;                                    // bit j: the launch has no units of job j (the ring need not hold its operands)
+  int b_at, stage_bytes, stages;               // the ring of operands: B's place in a stage (set by launch_jobs)
+  int32_t* counters;                           // NULL, or zeroed: the next unit, and per piece the epilogues' arrivals for job 0 and for
+                                               // jobs 1 and 2
   const int32_t* targets;
   const float4* info;
   const int32_t* exponent;                     // of the largest weight (fp16)
   float2* part;                                // [parts of the vocabulary][rows]
   float* xt;
   int64_t rows;
-  int n_end;                                   // vocabulary entries that there are (of this piece)
-  int target0;                                 // index of the first
   float c;                                     // scale * log2 e
   // kGradT, kSumT
   void* G;
@@ -58,7 +65,9 @@ struct Jobs {
   int d;
   int32_t* status;
 };
-template <typename T> szo_status launch_jobs(Jobs& P, bool chained, cudaStream_t st);
+inline int64_t counters_of(int64_t pieces) { return 1 + 2 * pieces; }
+// few: the jobs are those of few rows of hidden states (kStatsT, kGradT, kSumT)
+template <typename T> szo_status launch_jobs(Jobs& P, bool few, bool chained, cudaStream_t st);
 
 #ifdef __CUDACC__
 // For dW of fp16 the rows of G stand at 2^13 times their weight's power of two and those of h at that power over the largest

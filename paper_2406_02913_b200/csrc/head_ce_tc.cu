@@ -25,9 +25,11 @@ namespace {
 
 using namespace tc;
 
-constexpr int kHalf = 128, kMostStages = 12, kRingBytes = 6 * 2 * kHalf * kBlockK * 2;
+constexpr int kHalf = 128, kMostStages = 12;
+// (with few rows their columns' data take 4 KB of shared memory)
+template <bool kFew> constexpr int kRingBytes = 6 * 2 * kHalf * kBlockK * 2 - (kFew ? 4096 : 0);
 constexpr int kEpiWarp0 = 4, kEpiWarps = 8, kWarps = kEpiWarp0 + kEpiWarps, kOutBytes = 4096;
-constexpr int kSmem = kRingBytes + kEpiWarps * kOutBytes + 1024;
+template <bool kFew> constexpr int kSmem = kRingBytes<kFew> + kEpiWarps * kOutBytes + 1024;
 constexpr int kMaxDevices = 64;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -107,6 +109,20 @@ __device__ __forceinline__ float min_nan(float a, float b) {
   asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
+// p - 1 for p = e^t, t <= 0, to fp32's precision: the exponential's series where they cancel (nine terms: 2^-26 at t = -1/2).  (A few instructions:
+// the function of the library, unrolled over a tile's columns, made a launch of a few rows wait for instructions.)
+__device__ __forceinline__ float below_one(float t, float p) {
+  float s = 1.f / 362880.f;
+  s = fmaf(s, t, 1.f / 40320.f);
+  s = fmaf(s, t, 1.f / 5040.f);
+  s = fmaf(s, t, 1.f / 720.f);
+  s = fmaf(s, t, 1.f / 120.f);
+  s = fmaf(s, t, 1.f / 24.f);
+  s = fmaf(s, t, 1.f / 6.f);
+  s = fmaf(s, t, 0.5f);
+  s = fmaf(s, t, 1.f);
+  return t > -0.5f ? s * t : p - 1.f;
+}
 template <typename T> __device__ __forceinline__ uint32_t pack(float lo, float hi);
 template <> __device__ __forceinline__ uint32_t pack<__nv_bfloat16>(float lo, float hi) { return pack_bf16x2(lo, hi); }
 template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi) {
@@ -154,36 +170,125 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, int mn) {
          (1ull << 46) | (2ull << 61);
 }
 
+// ---- The order of the units
+__device__ __forceinline__ int piece_len(const Jobs& P, int i) { return min(P.piece, P.vocab - i * P.piece); }
+__device__ __forceinline__ const Extent& extent_of(const Jobs& P, int j, int i) { return i == P.pieces - 1 ? P.job[j].last : P.job[j].full; }
+__device__ __forceinline__ int units_of(const Jobs& P, int j, int i) { return P.job[j].kind < 0 || i < 0 || i >= P.pieces ? 0 : extent_of(P, j, i).units; }
 struct Unit {
-  int j, m, n, part, kb0, kb1;
+  int j, i, m, n, part, kb0, kb1;
 };
-__device__ __forceinline__ Unit unit_of(const Jobs& P, int u) {
-  Unit r;
-  r.j = 0;
-  while (r.j + 1 < P.n_jobs && u >= P.job[r.j].units) u -= P.job[r.j++].units;
-  const Job& J = P.job[r.j];
-  const int tiles = J.m_tiles * J.n_tiles;
-  r.part = u / tiles;
-  int t = u - r.part * tiles;
-  int m0 = 0, width = J.m_tiles;
-  if (J.m_band > 0) {
-    const int band = t / (J.n_tiles * J.m_band);
-    t -= band * J.n_tiles * J.m_band;
-    m0 = band * J.m_band;
-    width = min(J.m_band, J.m_tiles - m0);
+// Walks along the units: a role asks for rising ones only
+struct Walk {
+  int s, j = 0, first = 0;
+  __device__ __forceinline__ Unit seek(const Jobs& P, int u) {
+    Unit r;
+    while (true) {
+      r.i = j == 0 ? s : s - P.lag;
+      const int n = units_of(P, j, r.i);
+      if (u < first + n) break;
+      first += n;
+      if (++j == 3) {
+        j = 0;
+        ++s;
+      }
+    }
+    const Extent& e = extent_of(P, j, r.i);
+    r.j = j;
+    const int tiles = e.m_tiles * e.n_tiles;
+    u -= first;
+    r.part = e.parts > 1 ? u / tiles : 0;
+    int t = u - r.part * tiles, m0 = 0, width = e.m_tiles;
+    const int in_band = P.job[j].m_band;
+    if (in_band > 0) {
+      const int band = t / (e.n_tiles * in_band);
+      t -= band * e.n_tiles * in_band;
+      m0 = band * in_band;
+      width = min(in_band, e.m_tiles - m0);
+    }
+    r.n = t / width;
+    r.m = m0 + t - r.n * width;
+    r.kb0 = 0;
+    r.kb1 = e.nkb;
+    if (e.parts > 1) {                                            // (parts are few: no overflow below 2^31 / 16 blocks)
+      r.kb0 = e.nkb * r.part / e.parts;
+      r.kb1 = e.nkb * (r.part + 1) / e.parts;
+    }
+    return r;
   }
-  r.n = t / width;
-  r.m = m0 + t - r.n * width;
-  r.kb0 = static_cast<int>(static_cast<int64_t>(J.nkb) * r.part / J.parts);
-  r.kb1 = static_cast<int>(static_cast<int64_t>(J.nkb) * (r.part + 1) / J.parts);
+};
+// Arrivals that mean that job 0 (done 0) or jobs 1 and 2 (done 1) of piece i are finished: every epilogue warp of both CTAs, once per unit
+__device__ __forceinline__ int arrivals_of(const Jobs& P, int i, int done) {
+  return 2 * kEpiWarps * (done == 0 ? units_of(P, 0, i) : units_of(P, 1, i) + units_of(P, 2, i));
+}
+__device__ __forceinline__ int32_t* counter_of(const Jobs& P, int i, int done) { return P.counters + 1 + 2 * i + done; }
+// Waits, with a limit, until they are; what the counted epilogues wrote may then be read, by TMA too.  Units are handed out in their order
+// and wait for earlier ones only, so what is waited for runs already, on whatever SMs this launch has.
+__device__ __forceinline__ bool await_piece(const Jobs& P, int i, int done, volatile int* abort_flag) {
+  const int32_t* at = counter_of(P, i, done);
+  const int want = arrivals_of(P, i, done);
+  const long long t0 = clock64();
+  for (int polls = 0;; ++polls) {
+    int32_t v;
+    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(at) : "memory");
+    if (v >= want) break;
+    __nanosleep(64);
+    if ((polls & 255) == 255) {
+      if (*abort_flag) return false;
+      if (clock64() - t0 > kWaitLimitCycles) {
+        *abort_flag = 1;
+        atomicExch(P.status, static_cast<int32_t>(SZO_ERR_TIMEOUT));
+        return false;
+      }
+    }
+  }
+  asm volatile("fence.proxy.async;" ::: "memory");
+  return true;
+}
+__device__ __forceinline__ void arrive_piece(const Jobs& P, int i, int done) {
+  asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(counter_of(P, i, done)), "r"(1) : "memory");
+}
+
+// ---- Units on their way through a cluster: the leader's warp 3 takes the next one from the counter and gives it to every role of both CTAs
+constexpr int kFeedSlots = 2, kFeedReaders = 2 * kEpiWarps + 3;   // epilogues, both operand warps, the products' thread
+__device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+  const long long t0 = clock64();
+  for (int polls = 0;; ++polls) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    __nanosleep(32);
+    if ((polls & 1023) == 1023) {
+      if (*abort_flag) return false;
+      if (clock64() - t0 > kWaitLimitCycles) {
+        *abort_flag = 1;
+        atomicExch(status, static_cast<int32_t>(SZO_ERR_TIMEOUT));
+        return false;
+      }
+    }
+  }
+}
+__device__ __forceinline__ uint32_t of_peer(uint32_t local) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local), "r"(1));
   return r;
 }
 
-template <typename T>
+// kFew: few rows of hidden states, launches of one step (a kernel of its own: a launch of a few microseconds waits for instructions)
+template <typename T, bool kFew>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head_jobs_kernel(const __grid_constant__ Jobs P) {
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) unsigned long long bars[2 * kMostStages + 4];
+  __shared__ __align__(8) unsigned long long bars[2 * kMostStages + 4 + 2 * kFeedSlots];
   __shared__ uint32_t tmem_slot;
+  __shared__ volatile int feed[kFeedSlots];
+  constexpr int kMostColumns = 128;
+  __shared__ float4 columns_info[kFew ? kMostColumns : 1];
+  __shared__ int columns_target[kFew ? kMostColumns : 1];
   __shared__ int abort_flag_s;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -193,8 +298,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
   auto empty = [&](int s) { return smem_u32(&bars[kMostStages + s]); };               // the products that read the stage are done
   auto acc_full = [&](int a) { return smem_u32(&bars[2 * kMostStages + a]); };
   auto acc_empty = [&](int a) { return smem_u32(&bars[2 * kMostStages + 2 + a]); };   // leader: both CTAs' epilogues have read the sums
+  auto feed_full = [&](int s) { return smem_u32(&bars[2 * kMostStages + 4 + s]); };
+  auto feed_empty = [&](int s) { return smem_u32(&bars[2 * kMostStages + 4 + kFeedSlots + s]); };      // leader
   if (threadIdx.x == 0) {
     abort_flag_s = 0;
+    for (int s = 0; s < kFeedSlots; ++s) {
+      mbar_init(feed_full(s), 1);
+      mbar_init(feed_empty(s), kFeedReaders);
+    }
     for (int s = 0; s < kMostStages; ++s) {
       mbar_init(full(s), 1);
       mbar_init(empty(s), 1);
@@ -214,19 +325,46 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
   chain_wait();
   const uint32_t tmem = tmem_slot;
   const int pair = static_cast<int>(blockIdx.x >> 1), n_pairs = static_cast<int>(gridDim.x >> 1);
+  // The next unit for a role, or -1.  `one`: the role is a single thread, else a warp
+  int next_static = pair;
+  RingPos fed{0, 0};
+  auto next_unit = [&](bool one) {
+    if (kFew || P.counters == nullptr) {
+      const int u = next_static;
+      next_static += n_pairs;
+      return u < P.units ? u : -1;
+    }
+    if (!wait_cluster(feed_full(fed.idx), fed.phase, abort_flag, P.status)) return -1;
+    const int u = feed[fed.idx];
+    if (u >= P.units) return -1;
+    if (!one) __syncwarp();
+    if (u >= 0 && (one || lane == 0)) arrive_at(of_leader(feed_empty(fed.idx)));      // (u has been read: the arrival depends on it)
+    fed.advance(kFeedSlots);
+    return u;
+  };
 
   if (warp == 0) {
     // ---------------------------------------------------------------- operands
     if (elect()) {
       RingPos x{0, 0};
+      Walk walk{P.step};
       bool ok = true;
-      for (int u = pair; u < P.units && ok; u += n_pairs) {
-        const Unit t = unit_of(P, u);
+      int written = -1;                                           // G of this piece is complete
+      for (int u; ok && (u = next_unit(true)) >= 0;) {
+        const Unit t = walk.seek(P, u);
         const Job& J = P.job[t.j];
+        if (!kFew && t.j > 0 && t.i != written && P.counters != nullptr) {
+          if (!await_piece(P, t.i, 0, abort_flag)) break;
+          written = t.i;
+        }
         const CUtensorMap *ma = &J.a, *mb = &J.b;
-        const int a0 = J.a_m0 + t.m * J.m_step + rank * (J.m_step / 2), b0 = J.b_n0 + t.n * J.n_step + rank * (J.n_step / 2);
+        const int in_vocab = t.i * P.piece, in_buffers = P.buffers > 1 ? t.i % P.buffers * P.piece : 0;
+        const int ao = J.a_from == kVocab ? in_vocab : J.a_from == kBuffer ? in_buffers : 0;
+        const int bo = J.b_from == kVocab ? in_vocab : J.b_from == kBuffer ? in_buffers : 0;
+        const bool along_k = J.vocab_dim == 2;
+        const int a0 = (along_k ? 0 : ao) + t.m * J.m_step + rank * (J.m_step / 2), b0 = (along_k ? 0 : bo) + t.n * J.n_step + rank * (J.n_step / 2);
         const uint32_t bytes = 2u * (J.a_bytes + J.b_bytes);
-        const int a_mn = J.a_mn, b_mn = J.b_mn, a_k0 = J.a_k0, b_k0 = J.b_k0;
+        const int a_mn = J.a_mn, b_mn = J.b_mn, a_k0 = along_k ? ao : 0, b_k0 = along_k ? bo : 0;
         for (int kb = t.kb0; kb < t.kb1; ++kb) {
           if (!mbar_wait(empty(x.idx), x.phase ^ 1u, abort_flag, P.status)) {
             ok = false;
@@ -239,13 +377,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
             load_box(sa, ma, a0, a_k0 + k, bar);
             load_box(sa + 8192, ma, a0 + 64, a_k0 + k, bar);
           } else {
-            load_box(sa, ma, k, a0, bar);
+            load_box(sa, ma, a_k0 + k, a0, bar);
           }
           if (b_mn) {
             load_box(sb, mb, b0, b_k0 + k, bar);
             load_box(sb + 8192, mb, b0 + 64, b_k0 + k, bar);
           } else {
-            load_box(sb, mb, k, b0, bar);
+            load_box(sb, mb, b_k0 + k, b0, bar);
           }
           x.advance(P.stages);
         }
@@ -261,8 +399,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
       // kind::f16: fp32 sums, both operands of type T, M = 256; bits 15 / 16: rows of A / B are contracted
       constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
       constexpr uint32_t kIdesc = (1u << 4) | (kType << 7) | (kType << 10) | (static_cast<uint32_t>(kTile >> 4) << 24);
-      for (int u = pair; u < P.units && ok; u += n_pairs, ++lt) {
-        const Unit t = unit_of(P, u);
+      Walk walk{P.step};
+      for (int u; ok && (u = next_unit(true)) >= 0; ++lt) {
+        const Unit t = walk.seek(P, u);
         const int a_mn = P.job[t.j].a_mn, b_mn = P.job[t.j].b_mn;
         const uint32_t idesc = kIdesc | (static_cast<uint32_t>(P.job[t.j].n_step >> 3) << 17) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
         const int step_a = a_mn ? 2048 >> 4 : 32 >> 4, step_b = b_mn ? 2048 >> 4 : 32 >> 4, as = lt & 1;
@@ -286,10 +425,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
       }
     }
     __syncwarp();
+  } else if (warp == 3) {
+    // ---------------------------------------------------------------- units (leader only)
+    if (!kFew && rank == 0 && P.counters != nullptr && elect()) {
+      RingPos f{0, 0};
+      for (int u = 0; u < P.units;) {
+        if (!wait_cluster(feed_empty(f.idx), f.phase ^ 1u, abort_flag, P.status)) break;
+        u = atomicAdd(P.counters, 1);
+        feed[f.idx] = u;
+        const uint32_t there = of_peer(smem_u32(const_cast<int*>(&feed[f.idx])));
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there), "r"(u) : "memory");
+        mbar_arrive(feed_full(f.idx));
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(of_peer(feed_full(f.idx))) : "memory");
+        f.advance(kFeedSlots);
+      }
+    }
+    __syncwarp();
   } else if (warp >= kEpiWarp0) {
     // ---------------------------------------------------------------- epilogue: 32 rows, 128 columns
     const int w = warp - kEpiWarp0, quarter = warp & 3, half = w >> 2;
-    const uint32_t stage = base + kRingBytes + w * kOutBytes;
+    const uint32_t stage = base + kRingBytes<kFew> + w * kOutBytes;
     auto place = [&](int chunk) { return stage + lane * 128 + ((chunk ^ (lane & 7)) << 4); };
     auto reuse = [&]() {                                          // the warp's 4 KB may be written again
       if (lane == 0) store_wait_read();
@@ -299,34 +454,58 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
       fence_async_smem();
       __syncwarp();
     };
-    int lt = 0;
-    for (int u = pair; u < P.units; u += n_pairs, ++lt) {
-      const Unit t = unit_of(P, u);
+    if constexpr (kFew) {
+      // what the columns need: their targets and, for the gradient, infos (at most 128)
+      const int i = threadIdx.x - kEpiWarp0 * 32;
+      if (i < kMostColumns && P.job[0].kind >= 0) {
+        const int64_t r = i < P.rows ? i : P.rows - 1;
+        columns_target[i] = P.targets[r];
+        if (P.job[0].kind == kGradT) columns_info[i] = P.info[r];
+      }
+      asm volatile("bar.sync 1, %0;" ::"r"(kEpiWarps * 32) : "memory");
+    }
+    int lt = 0, free_before = P.buffers, added = -1;             // pieces below free_before have a buffer of G to write to; sums of piece `added` are there
+    Walk walk{P.step};
+    bool ok = true;
+    for (int u; ok && (u = next_unit(false)) >= 0; ++lt) {
+      const Unit t = walk.seek(P, u);
       const Job& J = P.job[t.j];
       const int as = lt & 1, mine = quarter * 32 + lane;           // (its place in this CTA's half of the tile)
       const int row0 = t.m * J.m_step + rank * (J.m_step / 2) + quarter * 32, row = row0 + lane, col0 = t.n * J.n_step + half * (J.n_step / 2);
-      const bool there = row < J.m_limit && mine < J.m_step / 2;
+      const int n_end = piece_len(P, t.i), m_limit = J.vocab_dim == 0 ? n_end : J.m_limit, target0 = t.i * P.piece, buffer0 = P.buffers > 1 ? t.i % P.buffers * P.piece : 0;
+      const bool there = row < m_limit && mine < J.m_step / 2;
       int target = -1;
       float4 info = make_float4(0.f, 0.f, 0.f, 0.f);
       float factor = 1.f;
-      if (J.kind <= kGrad && there) target = P.targets[row];
-      if (J.kind == kGrad && there) info = P.info[row];
+      if (!kFew && J.kind <= kGrad && there) target = P.targets[row];
+      if (!kFew && J.kind == kGrad && there) info = P.info[row];
       if (J.kind == kOut) factor = weight_of<T>(P.exponent);
-      target = target >= 0 ? target - P.target0 - col0 : -1;      // (its place in these columns, or outside of [0, 128))
-      if (target >= P.n_end - col0) target = -1;
+      target = target >= 0 ? target - target0 - col0 : -1;        // (its place in these columns, or outside of [0, 128))
+      if (target >= n_end - col0) target = -1;
       if (!mbar_wait(acc_full(as), static_cast<uint32_t>((lt >> 1) & 1), abort_flag, P.status, 128)) break;
       tc_fence_after();
       const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + as * kTile + half * (J.n_step / 2);
-      // some row of this warp is there (kStatsT: might be, its part is written all the same)
-      const bool live = (row0 < J.m_limit || J.kind == kStatsT) && quarter * 32 < J.m_step / 2;
-      if (!live) {
-      } else if (J.kind == kStats) {
+      // some row of this warp is there (the vocabulary along m: might be, its part is written all the same)
+      const bool live = (row0 < m_limit || J.kind == kStatsT || J.kind == kGradT) && quarter * 32 < J.m_step / 2;
+      if (kFew) {
+      } else if (J.kind == kGrad) {
+        // the buffer of G was that of an earlier piece: its readers have to be through
+        if (t.i >= free_before && P.counters != nullptr) {
+          ok = __all_sync(0xffffffffu, await_piece(P, t.i - P.buffers, 1, abort_flag));
+          free_before = t.i + 1;
+        }
+      } else if (J.kind == kSum && t.i > 0 && t.i - 1 != added && P.counters != nullptr) {
+        ok = __all_sync(0xffffffffu, await_piece(P, t.i - 1, 1, abort_flag));      // (what this piece's sums are added to)
+        added = t.i - 1;
+      }
+      if (!live || !ok) {
+      } else if (!kFew && J.kind == kStats) {
         float m = -INFINITY, s = 0.f;
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t v[32];
           tmem_ld32(acc + 32 * c, v);
-          const int left = P.n_end - (col0 + 32 * c), hit = target - 32 * c;
+          const int left = n_end - (col0 + 32 * c), hit = target - 32 * c;
           if (left < 32) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -352,21 +531,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
           m = mn;
         }
         if (there) P.part[static_cast<int64_t>(2 * t.n + half) * P.rows + row] = make_float2(m * P.c, s);
-      } else if (J.kind == kGrad) {
+      } else if (!kFew && J.kind == kGrad) {
         const bool weighs = info.y != 0.f || info.z != 0.f;
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t v[32];
           tmem_ld32(acc + 32 * c, v);
           if ((c & 1) == 0) reuse();
-          const int hit = target - 32 * c;
+          const int hit = target - 32 * c, left = n_end - (col0 + 32 * c);
           const bool any = __any_sync(0xffffffffu, hit >= 0 && hit < 32);
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             const float x = min_nan(fmaf(__uint_as_float(v[i]), P.c, -info.x), 0.f), p = ex2(x);      // (rounding may put x above lse)
             float g = info.y * p;
-            if (any && i == hit) g = fmaf(info.y - info.z, p, info.z * expm1f(x * kLn2));
-            v[i] = weighs ? __float_as_uint(g) : 0u;
+            if (any && i == hit) g = fmaf(info.y - info.z, p, info.z * below_one(x * kLn2, p));
+            v[i] = weighs && i < left ? __float_as_uint(g) : 0u;  // (columns behind the vocabulary are contracted with zeros: they must be finite)
           }
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
@@ -378,12 +557,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
           if (c & 1) {
             written();
             if (lane == 0) {
-              store_box(&J.out, stage, col0 + 32 * (c - 1), J.out_row0 + row0);
+              store_box(&J.out, stage, buffer0 + col0 + 32 * (c - 1), row0);
               store_commit();
             }
           }
         }
-      } else if (J.kind == kSum) {
+      } else if (!kFew && J.kind == kSum) {
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t v[32];
@@ -393,14 +572,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
           for (int q = 0; q < 8; ++q) put16(place(q), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
           written();
           if (lane == 0) {
-            if (J.add) add_box3(&J.out, stage, col0 + 32 * c, row0, t.part);
+            if (t.i > 0) add_box3(&J.out, stage, col0 + 32 * c, row0, t.part);
             else store_box3(&J.out, stage, col0 + 32 * c, row0, t.part);
             store_commit();
           }
         }
-      } else if (J.kind >= kStatsT) {
+      } else if (kFew && J.kind >= kStatsT) {
         // a thread is a vocabulary entry (kSumT: an element of d), the columns are rows of hidden states, 16 at a time
-        const int last = static_cast<int>(P.rows), n_half = J.n_step / 2;
+        const int last = static_cast<int>(P.rows), n_half = J.n_step / 2, padded = (n_end + kBlockK - 1) / kBlockK * kBlockK;
 #pragma unroll 1
         for (int c = 0; c < n_half; c += 16) {
           const int r0 = col0 + c;
@@ -411,35 +590,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
 #pragma unroll
             for (int i = 0; i < 16; ++i)
               if (there && r0 + i < last) {
-                float* to = P.sums + (t.part * P.rows + r0 + i) * P.d + row;
-                *to = J.add ? *to + v[i] : v[i];
+                P.sums[((static_cast<int64_t>(t.i) * J.full.parts + t.part) * P.rows + r0 + i) * P.d + row] = v[i];
               }
           } else if (J.kind == kGradT) {
-            float4 f[16];
-            int hit[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const int r = min(r0 + i, last - 1);
-              f[i] = __ldg(P.info + r);
-              hit[i] = __ldg(P.targets + r);
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float x = min_nan(fmaf(v[i], P.c, -f[i].x), 0.f), p = ex2(x);
-              float g = f[i].y * p;
-              if (hit[i] == P.target0 + row) g = fmaf(f[i].y - f[i].z, p, f[i].z * expm1f(x * kLn2));
-              if (f[i].y == 0.f && f[i].z == 0.f) g = 0.f;
-              if (there && r0 + i < last) static_cast<T*>(P.G)[(r0 + i) * P.g_stride + row] = round_to<T>(g);
+              const float4 f = columns_info[r0 + i];
+              const float x = min_nan(fmaf(v[i], P.c, -f.x), 0.f), p = ex2(x);
+              float g = f.y * p;
+              if (columns_target[r0 + i] == target0 + row) g = fmaf(f.y - f.z, p, f.z * below_one(x * kLn2, p));
+              if (!there || (f.y == 0.f && f.z == 0.f)) g = 0.f;
+              if (mine < J.m_step / 2 && row < padded && r0 + i < last) static_cast<T*>(P.G)[(r0 + i) * P.g_stride + buffer0 + row] = round_to<T>(g);
             }
           } else {
             float top[16];
-            int hit[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) hit[i] = __ldg(P.targets + min(r0 + i, last - 1));
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               if (!there) v[i] = -INFINITY;
-              if (r0 + i < last && there && hit[i] == row) {
+              if (r0 + i < last && there && columns_target[r0 + i] == row) {
                 P.xt[r0 + i] = v[i] * P.c;
                 v[i] = -INFINITY;
               }
@@ -474,7 +642,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
           if (c & 1) {
             written();
             if (lane == 0) {
-              store_box(&J.out, stage, col0 + 32 * (c - 1), J.out_row0 + row0);
+              store_box(&J.out, stage, col0 + 32 * (c - 1), target0 + row0);
               store_commit();
             }
           }
@@ -483,6 +651,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
       tc_fence_before();
       __syncwarp();
       if (lane == 0) arrive_at(of_leader(acc_empty(as)));
+      if (!kFew && P.counters != nullptr && lane == 0) {
+        store_wait();                                             // this warp's part of the unit is written
+        if (ok) arrive_piece(P, t.i, t.j > 0);
+      }
     }
     if (lane == 0) store_wait();
     __syncwarp();
@@ -500,8 +672,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
 
 }  // namespace
 
-template <typename T> szo_status launch_jobs(Jobs& P, bool chained, cudaStream_t st) {
-  auto kern = head_jobs_kernel<T>;
+template <typename T, bool kFew> szo_status launch(Jobs& P, bool chained, cudaStream_t st) {
+  auto kern = head_jobs_kernel<T, kFew>;
   // per device: the function's attribute and the number of SM pairs, looked up once
   static std::mutex mu;
   static int pairs_of[kMaxDevices] = {};
@@ -514,24 +686,30 @@ template <typename T> szo_status launch_jobs(Jobs& P, bool chained, cudaStream_t
     if (pairs_of[dev] == 0) {
       int sms = 0;
       SZO_CHECK_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-      SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+      SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<kFew>));
       pairs_of[dev] = sms / 2;
     }
     pairs = pairs_of[dev];
   }
   if (P.units < pairs) pairs = P.units;
   // the ring: as many stages as fit of what the jobs' operands need, so that a few rows (a small B) keep as many bytes of W on their
-  // way (8 rows: 53 us with 6 stages)
+  // way (8 rows: 53 us with 6 stages, 51 with 12)
   P.b_at = P.stage_bytes = 0;
-  for (int i = 0; i < P.n_jobs; ++i) P.b_at = std::max(P.b_at, static_cast<int>(round_up(P.job[i].a_bytes, 1024)));
-  for (int i = 0; i < P.n_jobs; ++i) P.stage_bytes = std::max(P.stage_bytes, P.b_at + static_cast<int>(round_up(P.job[i].b_bytes, 1024)));
-  P.stages = std::min(kMostStages, kRingBytes / P.stage_bytes);
-  SZO_CHECK_CUDA(launch_maybe_chained(kern, dim3(static_cast<unsigned>(2 * pairs)), dim3(kWarps * 32), kSmem, st, chained, P));
+  auto used = [&](int j) { return P.job[j].kind >= 0 && !(P.idle >> j & 1); };
+  for (int j = 0; j < 3; ++j)
+    if (used(j)) P.b_at = std::max(P.b_at, static_cast<int>(round_up(P.job[j].a_bytes, 1024)));
+  for (int j = 0; j < 3; ++j)
+    if (used(j)) P.stage_bytes = std::max(P.stage_bytes, P.b_at + static_cast<int>(round_up(P.job[j].b_bytes, 1024)));
+  P.stages = std::min(kMostStages, kRingBytes<kFew> / P.stage_bytes);
+  SZO_CHECK_CUDA(launch_maybe_chained(kern, dim3(static_cast<unsigned>(2 * pairs)), dim3(kWarps * 32), kSmem<kFew>, st, chained, P));
   count_launch();
   return SZO_OK;
 }
-template szo_status launch_jobs<__nv_bfloat16>(Jobs&, bool, cudaStream_t);
-template szo_status launch_jobs<__half>(Jobs&, bool, cudaStream_t);
+template <typename T> szo_status launch_jobs(Jobs& P, bool few, bool chained, cudaStream_t st) {
+  return few ? launch<T, true>(P, chained, st) : launch<T, false>(P, chained, st);
+}
+template szo_status launch_jobs<__nv_bfloat16>(Jobs&, bool, bool, cudaStream_t);
+template szo_status launch_jobs<__half>(Jobs&, bool, bool, cudaStream_t);
 
 }  // namespace head
 }  // namespace szo
