@@ -35,6 +35,7 @@ struct Job {
   int a_mn, b_mn;                              // the operand's rows are the contracted dimension
   int a_from, b_from;                          // Offset
   int a_bytes, b_bytes;                        // of the operands per stage and CTA
+  int keep_from;                               // few rows: entry of W from which on L2 is to keep what is read (-1: no matter)
   int m_step, n_step;                          // a tile's rows and columns; each CTA brings half of either
   int m_limit;                                 // rows of D that there are (where they are not the vocabulary)
   int m_band;                                  // tiles of m are taken in bands of m_band (0: all)

@@ -60,6 +60,12 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(leader_bar)
       : "memory");
 }
+__device__ __forceinline__ void load_box_hint(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t leader_bar, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(leader_bar), "l"(policy)
+      : "memory");
+}
 __device__ __forceinline__ void store_box(const CUtensorMap* map, uint32_t src, int x, int y) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y),
                "r"(src)
@@ -176,9 +182,10 @@ __device__ __forceinline__ const Extent& extent_of(const Jobs& P, int j, int i) 
 __device__ __forceinline__ int units_of(const Jobs& P, int j, int i) { return P.job[j].kind < 0 || i < 0 || i >= P.pieces ? 0 : extent_of(P, j, i).units; }
 struct Unit {
   int j, i, m, n, part, kb0, kb1;
+  int from_end, stride;                        // kSumT: the kb-th of its blocks is from_end - kb * stride
 };
 // Walks along the units: a role asks for rising ones only
-struct Walk {
+template <bool kFew> struct Walk {
   int s, j = 0, first = 0;
   __device__ __forceinline__ Unit seek(const Jobs& P, int u) {
     Unit r;
@@ -209,7 +216,12 @@ struct Walk {
     r.m = m0 + t - r.n * width;
     r.kb0 = 0;
     r.kb1 = e.nkb;
-    if (e.parts > 1) {                                            // (parts are few: no overflow below 2^31 / 16 blocks)
+    if (kFew && P.job[j].vocab_dim == 2) {
+      // dh of few rows: all shares walk together from the vocabulary's end, which the logits' launch has left in L2, to its start
+      r.from_end = e.nkb - 1 - r.part;
+      r.stride = e.parts;
+      r.kb1 = r.from_end / e.parts + 1;
+    } else if (e.parts > 1) {                                     // (parts are few: no overflow below 2^31 / 16 blocks)
       r.kb0 = e.nkb * r.part / e.parts;
       r.kb1 = e.nkb * (r.part + 1) / e.parts;
     }
@@ -347,9 +359,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
     // ---------------------------------------------------------------- operands
     if (elect()) {
       RingPos x{0, 0};
-      Walk walk{P.step};
+      Walk<kFew> walk{P.step};
       bool ok = true;
       int written = -1;                                           // G of this piece is complete
+      const uint64_t keep = l2_policy_evict_last(), drop = l2_policy_evict_first();
       for (int u; ok && (u = next_unit(true)) >= 0;) {
         const Unit t = walk.seek(P, u);
         const Job& J = P.job[t.j];
@@ -372,8 +385,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
           }
           if (rank == 0) mbar_expect_tx(full(x.idx), bytes);
           const uint32_t bar = of_leader(full(x.idx)), sa = base + x.idx * P.stage_bytes, sb = sa + P.b_at;
-          const int k = kb * kBlockK;
-          if (a_mn) {
+          const int k = (kFew && along_k ? t.from_end - kb * t.stride : kb) * kBlockK;
+          if (kFew && J.keep_from >= 0) {
+            // W of few rows' gradient: what the logits read last stays for dh, which reads it first and for the last time
+            const uint64_t policy = !a_mn && a0 >= J.keep_from ? keep : drop;
+            if (a_mn) {
+              load_box_hint(sa, ma, a0, a_k0 + k, bar, policy);
+              load_box_hint(sa + 8192, ma, a0 + 64, a_k0 + k, bar, policy);
+            } else {
+              load_box_hint(sa, ma, a_k0 + k, a0, bar, policy);
+            }
+          } else if (a_mn) {
             load_box(sa, ma, a0, a_k0 + k, bar);
             load_box(sa + 8192, ma, a0 + 64, a_k0 + k, bar);
           } else {
@@ -399,7 +421,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
       // kind::f16: fp32 sums, both operands of type T, M = 256; bits 15 / 16: rows of A / B are contracted
       constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
       constexpr uint32_t kIdesc = (1u << 4) | (kType << 7) | (kType << 10) | (static_cast<uint32_t>(kTile >> 4) << 24);
-      Walk walk{P.step};
+      Walk<kFew> walk{P.step};
       for (int u; ok && (u = next_unit(true)) >= 0; ++lt) {
         const Unit t = walk.seek(P, u);
         const int a_mn = P.job[t.j].a_mn, b_mn = P.job[t.j].b_mn;
@@ -465,7 +487,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWarps * 32, 1) head
       asm volatile("bar.sync 1, %0;" ::"r"(kEpiWarps * 32) : "memory");
     }
     int lt = 0, free_before = P.buffers, added = -1;             // pieces below free_before have a buffer of G to write to; sums of piece `added` are there
-    Walk walk{P.step};
+    Walk<kFew> walk{P.step};
     bool ok = true;
     for (int u; ok && (u = next_unit(false)) >= 0; ++lt) {
       const Unit t = walk.seek(P, u);
