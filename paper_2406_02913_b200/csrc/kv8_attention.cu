@@ -526,43 +526,62 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     if (nsplit > 1) cluster.sync();
     else __syncthreads();
     chain_wait();
-    const int quads = n_rows * (HD / 4), lo = quads * split / nsplit, hi = quads * (split + 1) / nsplit;
-    for (int i = lo + static_cast<int>(threadIdx.x); i < hi; i += kThreads) {
-      const int r = i / (HD / 4), d = i % (HD / 4) * 4;
-      const int64_t row_head = (seq.row0 + (r0 + r) / G) * H + h * G + (r0 + r) % G;
-      float mm = -INFINITY, ll = 0.f;
-      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-      auto add = [&](float m2, float l2, const float4& x) {
-        const float top = fmaxf(mm, m2), ref = top == -INFINITY ? 0.f : top, f0 = ex2(mm - ref), f1 = ex2(m2 - ref);
-        sum = make_float4(fmaf(f1, x.x, f0 * sum.x), fmaf(f1, x.y, f0 * sum.y), fmaf(f1, x.z, f0 * sum.z), fmaf(f1, x.w, f0 * sum.w));
-        ll = fmaf(f1, l2, f0 * ll);
-        mm = top;
-      };
-      for (int x = 0; x < nsplit; ++x) {
-        const float* from = nsplit > 1 ? cluster.map_shared_rank(part(0), x) : part(0);
-        add((nsplit > 1 ? cluster.map_shared_rank(wm, x) : wm)[r] - kOffset, (nsplit > 1 ? cluster.map_shared_rank(wl, x) : wl)[r],
-            *reinterpret_cast<const float4*>(from + r * HD + d));
+    const int quads = n_rows * (HD / 4), lo = quads * split / nsplit, n_mine = quads * (split + 1) / nsplit - lo;
+    struct Sum {
+      float m = -INFINITY, l = 0.f;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      __device__ __forceinline__ void add(float m2, float l2, const float4& y) {
+        const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top, f0 = ex2(m - ref), f1 = ex2(m2 - ref);
+        x = make_float4(fmaf(f1, y.x, f0 * x.x), fmaf(f1, y.y, f0 * x.y), fmaf(f1, y.z, f0 * x.z), fmaf(f1, y.w, f0 * x.w));
+        l = fmaf(f1, l2, f0 * l);
+        m = top;
       }
-      if (work.skip > 0) {
+    };
+    // where the block has more threads than such pieces, `teams` threads share one, taking every teams-th share
+    const int teams = n_mine > 0 ? min(max(kThreads / n_mine, 1), kWarps) : 1, team = teams > 1 ? static_cast<int>(threadIdx.x) / n_mine : 0;
+    Sum* others = reinterpret_cast<Sum*>(ring0 + R * HD * 4);     // (behind the block's sum, which the cluster reads)
+    static_assert((kWarps - 1) * kThreads * sizeof(Sum) + R * HD * 4 <= kWarps * kRingBytes<HD>, "");
+    for (int i0 = teams > 1 ? static_cast<int>(threadIdx.x) - team * n_mine : static_cast<int>(threadIdx.x); teams > 1 ? i0 >= 0 : i0 < n_mine;
+         i0 = teams > 1 ? -1 : i0 + kThreads) {
+      const int i = lo + i0, r = i / (HD / 4), d = i % (HD / 4) * 4;
+      const int64_t row_head = (seq.row0 + (r0 + r) / G) * H + h * G + (r0 + r) % G;
+      Sum s;
+      if (team == 0)
+        for (int x = 0; x < nsplit; ++x) {
+          const float* from = nsplit > 1 ? cluster.map_shared_rank(part(0), x) : part(0);
+          s.add((nsplit > 1 ? cluster.map_shared_rank(wm, x) : wm)[r] - kOffset, (nsplit > 1 ? cluster.map_shared_rank(wl, x) : wl)[r],
+                *reinterpret_cast<const float4*>(from + r * HD + d));
+        }
+      if (work.skip > 0 && team < teams) {
         constexpr int kAhead = 8;
-        for (int k0 = 0; k0 < part_of.shares; k0 += kAhead) {
+        for (int k0 = team; k0 < part_of.shares; k0 += kAhead * teams) {
           float2 st[kAhead];
           float4 x[kAhead];
 #pragma unroll
           for (int k = 0; k < kAhead; ++k) {
-            const int64_t at = (k0 + k < part_of.shares ? k0 + k : k0) * part_of.row_heads + row_head;
+            const int kk = k0 + k * teams;
+            const int64_t at = (kk < part_of.shares ? kk : k0) * part_of.row_heads + row_head;
             st[k] = __ldcg(part_of.stats + at);
             x[k] = __ldcg(reinterpret_cast<const float4*>(part_of.sums + at * HD + d));
           }
 #pragma unroll
           for (int k = 0; k < kAhead; ++k)
-            if (k0 + k < part_of.shares) add(st[k].x, st[k].y, x[k]);
+            if (k0 + k * teams < part_of.shares) s.add(st[k].x, st[k].y, x[k]);
         }
       }
-      const float inv = ll == 0.f ? 1.f : 1.f / ll;               // nothing attended to: sums of 0
+      if (teams > 1) {
+        if (team > 0 && team < teams) others[(team - 1) * kThreads + i0] = s;
+        __syncthreads();                                          // (every thread makes one trip)
+        if (team > 0) break;
+        for (int k = 1; k < teams; ++k) {
+          const Sum& y = others[(k - 1) * kThreads + i0];
+          s.add(y.m, y.l, y.x);
+        }
+      }
+      const float inv = s.l == 0.f ? 1.f : 1.f / s.l;             // nothing attended to: sums of 0
       struct alignas(4 * sizeof(T)) Four { T x[4]; };
       *reinterpret_cast<Four*>(o + (seq.row0 + (r0 + r) / G) * o_stride + (h * G + (r0 + r) % G) * static_cast<int64_t>(HD) + d) =
-          Four{{narrow<T>(sum.x * inv), narrow<T>(sum.y * inv), narrow<T>(sum.z * inv), narrow<T>(sum.w * inv)}};
+          Four{{narrow<T>(s.x.x * inv), narrow<T>(s.x.y * inv), narrow<T>(s.x.z * inv), narrow<T>(s.x.w * inv)}};
     }
     if (nsplit > 1) cluster.sync();
     return;
@@ -582,6 +601,282 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     store(r, at % HD, sum, ll);
   }
   cluster.sync();                                                 // nobody leaves while its sums are being read
+}
+
+// The same for up to 32 rows of a group over its shared positions, 16-bit types: every code is turned into fp16 once for all of them
+// (two tiles of 16 rows do so twice: 8 sequences of 4 rows on 65536 shared positions, 8 heads of 128, 69 us, here 65).  What
+// bounds it is the latency of the chain in each of its 8 warps per SM (issue 35 %): 254 registers leave no room for more.  The queries' fragments do not fit the registers beside 32 rows of sums: they stay in shared
+// memory, and 16 positions are taken at a time.
+template <typename T, int HD>
+__global__ void __launch_bounds__(128, 2)
+kv8_prefix_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, View V, const T* __restrict__ q,
+                       int64_t q_stride, int H, float scale_log2e, int nsplit, const Part part_of) {
+  constexpr int NT = 4, R = 8 * NT, kWarps = 4, kThreads = kWarps * 32, kK = HD / 16, kRing = kRingBytes<HD>;
+  static_assert(R * HD * 4 <= kRing, "a warp's partial result takes the place of its ring");
+  extern __shared__ __align__(1024) unsigned char smem_kv8[];
+  __shared__ uint2 q_frag[NT][kK][32];
+  __shared__ float row_scale[R], wm[kWarps * R], wl[kWarps * R];
+  __shared__ int row_last[R], nan_at[HD];
+  __shared__ __align__(8) uint64_t full[kWarps][kDepth];
+  __shared__ int abort_flag;
+  unsigned char* ring0 = smem_kv8 + ((1024u - (tc::smem_u32(smem_kv8) & 1023u)) & 1023u);
+  chain_wait();
+  chain_release();
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  unsigned item = blockIdx.x;
+  const int split = item % nsplit;
+  item /= nsplit;
+  const int h = item % V.hkv, b = item / V.hkv, G = H / V.hkv;
+  const Work work = load_work(V, part_of, b);
+  const Seq seq = work.seq;
+  const int n_rows = static_cast<int>(min(static_cast<int64_t>(seq.n) * G, static_cast<int64_t>(R)));
+  if (n_rows <= 0) return;
+  for (int i = threadIdx.x; i < HD; i += kThreads) nan_at[i] = 0x7fffffff;
+  if (threadIdx.x == 0) abort_flag = 0;
+  const uint32_t ring = tc::smem_u32(ring0) + w * kRing, bars = tc::smem_u32(&full[w][0]);
+  if (lane == 0) {
+    for (int i = 0; i < kDepth; ++i) tc::mbar_init(bars + 8 * i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  // this warp's units of two steps; a last unit may have one
+  const int pos_hi = seq.len - 1, steps = pos_hi / kStep + 1, units = (steps + 1) / 2;
+  int u_lo = static_cast<int>(static_cast<int64_t>(units) * split / nsplit), u_hi = static_cast<int>(static_cast<int64_t>(units) * (split + 1) / nsplit);
+  {
+    const int span = u_hi - u_lo, base = u_lo;
+    u_lo = base + span * w / kWarps;
+    u_hi = base + span * (w + 1) / kWarps;
+  }
+  struct Meta {
+    int row;                                                      // -1: no page, or behind this warp's share
+    float2 sc;
+  };
+  const int32_t* table = V.table + static_cast<int64_t>(work.owner) * V.max_pages;
+  const int s_end = min(2 * u_hi, steps);
+  auto load_entry = [&](int s) { return s + lane < s_end ? __ldg(table + ((s + lane) >> (V.page_shift - 4))) : -1; };
+  auto load_meta = [&](int entry, int s) {
+    Meta r{-1, make_float2(0.f, 0.f)};
+    if (static_cast<uint32_t>(entry) < static_cast<uint64_t>(V.n_pages)) {
+      r.row = ((entry * V.hkv + h) << V.page_shift) + (((s + lane) << 4) & ((1 << V.page_shift) - 1));
+      r.sc = __ldg(V.scales + static_cast<int64_t>(entry) * V.hkv + h);
+    } else if (s + lane < s_end) {
+      report_page(V);
+    }
+    return r;
+  };
+  const int box = box_tokens(V), nb = kUnit / box;
+  auto issue = [&](int slot, int row) {
+    const uint32_t bar = bars + 8 * slot;
+    const unsigned live = __ballot_sync(0xffffffffu, lane < 2 * nb && row >= 0);
+    if (lane == 0) tc::mbar_expect_tx(bar, __popc(live) * box * HD);
+    __syncwarp();
+    if (lane < 2 * nb && row >= 0)
+      tc::tma_load_2d(ring + slot * kUnit * HD * 2 + lane * box * HD, lane < nb ? &map_k : &map_v, 0, row, bar);
+  };
+  int entry = load_entry(2 * u_lo), entry_n = load_entry(2 * u_lo + 32);
+  Meta mc = load_meta(entry, 2 * u_lo);
+#pragma unroll
+  for (int i = 0; i < kDepth; ++i) {
+    const int row = __shfl_sync(0xffffffffu, mc.row, 2 * i + (lane & (nb - 1)));
+    if (u_lo + i < u_hi) issue(i, row);
+  }
+  Meta mn = load_meta(entry_n, 2 * u_lo + 32);
+  entry_n = load_entry(2 * u_lo + 64);
+  float ks_c, fe_c;
+  auto take_scales = [&]() {
+    ks_c = exp2_int(scale_exponent(mc.sc.x));
+    fe_c = mc.row >= 0 ? static_cast<float>(scale_exponent(mc.sc.y)) : -INFINITY;
+  };
+  {
+    // queries: warp w prepares the fragments of rows 8 w .. 8 w + 7 (see the kernel above)
+    const int r = 8 * w + g;
+    float x[kK][4], amax = 0.f;
+    bool fine = true;
+    const T* qp = q + (seq.row0 + r / G) * q_stride + (h * G + r % G) * static_cast<int64_t>(HD) + HD / 4 * t;
+#pragma unroll
+    for (int i = 0; i < HD / 4; i += Vec<T>::kN) {
+      Vec<T> v = {};
+      if (r < n_rows) v = *reinterpret_cast<const Vec<T>*>(qp + i);
+#pragma unroll
+      for (int u = 0; u < Vec<T>::kN; ++u) {
+        const float y = widen<T>(v.x[u]);
+        x[(i + u) / 4][(i + u) % 4] = y;
+        amax = fmaxf(amax, fabsf(y));
+        fine = fine && isfinite(y);
+      }
+    }
+#pragma unroll
+    for (int off = 1; off <= 2; off <<= 1) {
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, off));
+      fine = __shfl_xor_sync(0xffffffffu, static_cast<int>(fine), off) && fine;
+    }
+    const int e = min(max((__float_as_int(amax) >> 23) - 127, -126), 126);
+    const float inv = exp2_int(-e);
+#pragma unroll
+    for (int i = 0; i < kK; ++i) q_frag[w][i][lane] = make_uint2(pack_f16(x[i][0] * inv, x[i][1] * inv), pack_f16(x[i][2] * inv, x[i][3] * inv));
+    if (t == 0) {
+      row_scale[r] = fine ? exp2_int(e) * scale_log2e : __int_as_float(0x7fffffff);
+      row_last[r] = r < n_rows ? min(__ldg(part_of.pos + seq.row0 + r / G), pos_hi) : pos_hi;
+    }
+  }
+  __syncthreads();
+  const bool all = __syncthreads_and(row_last[lane] == pos_hi);   // every row sees all of it, or each step is masked
+  float acc[NT][HD / 16][4], m[NT][2], l[NT][2], rs[NT][2];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      m[n][u] = -INFINITY;
+      l[n][u] = 0.f;
+      rs[n][u] = row_scale[8 * n + 2 * t + u];                    // this thread's scores are those of rows 2 t, 2 t + 1
+    }
+#pragma unroll
+    for (int i = 0; i < HD / 16; ++i) acc[n][i][0] = acc[n][i][1] = acc[n][i][2] = acc[n][i][3] = 0.f;
+  }
+  take_scales();
+  int slot = 0;
+  uint32_t phase = 0;
+  for (int u = u_lo; u < u_hi; ++u) {
+    const int i = 2 * (u - u_lo) & 31;
+    if (!__all_sync(0xffffffffu, tc::mbar_wait(bars + 8 * slot, phase, &abort_flag, V.status, 0))) break;
+    const uint32_t at = ring + slot * kUnit * HD * 2;
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      const float ks = __shfl_sync(0xffffffffu, ks_c, i + a), fe = __shfl_sync(0xffffffffu, fe_c, i + a);
+      const bool have = fe != -INFINITY, masked = !all || !have;
+      const float el = have ? exp2_int(-static_cast<int>(fe)) : 0.f;
+      float c[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.f;
+      {
+        uint32_t kk[2][kK];
+        load_keys<HD>(kk, at + a * kStep * HD, g, t);
+#pragma unroll
+        for (int k = 0; k < kK; ++k) {
+          const uint32_t a0 = decode2(kk[0][k]), a1 = decode2(kk[1][k]), a2 = decode2(kk[0][k] >> 16), a3 = decode2(kk[1][k] >> 16);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const uint2 f = q_frag[n][k][lane];
+            mma_f16(c[n], a0, a1, a2, a3, f.x, f.y);
+          }
+        }
+      }
+      uint32_t vv[4][HD / 32];
+      load_values<HD>(vv, at + (2 + a) * kStep * HD, g, t);
+      uint32_t pa[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[j] = fmaf(c[n][j], rs[n][j & 1] * ks, fe);
+          if (masked && (!have || u * kUnit + a * kStep + g + 8 * (j >> 1) > row_last[8 * n + 2 * t + (j & 1)])) x[j] = -INFINITY;
+        }
+        float mx[2] = {fmaxf(x[0], x[2]), fmaxf(x[1], x[3])};
+        if (__any_sync(0xffffffffu, mx[0] > m[n][0] + kSlack || mx[1] > m[n][1] + kSlack)) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int off = 4; off <= 16; off <<= 1) mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], off));
+            const float top = fmaxf(m[n][j], mx[j]), corr = top == -INFINITY ? 1.f : ex2(m[n][j] - top);
+            m[n][j] = top;
+            l[n][j] *= corr;
+#pragma unroll
+            for (int k = 0; k < HD / 16; ++k) {
+              acc[n][k][j] *= corr;
+              acc[n][k][j + 2] *= corr;
+            }
+          }
+        }
+        float y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = ex2(x[j] - (m[n][j & 1] == -INFINITY ? 0.f : m[n][j & 1] - kOffset));
+        l[n][0] = fmaf(el, y[0] + y[2], l[n][0]);
+        l[n][1] = fmaf(el, y[1] + y[3], l[n][1]);
+        pa[n][0] = transpose8x8(pack_f16(y[0], y[1]));
+        pa[n][1] = transpose8x8(pack_f16(y[2], y[3]));
+      }
+      if (masked) {                                               // (0 * NaN: see the kernel above)
+#pragma unroll
+        for (int i2 = 0; i2 < 4; ++i2) {
+#pragma unroll
+          for (int j = 0; j < HD / 32; ++j) {
+            if (!have) vv[i2][j] = 0;
+            uint32_t bad = ((vv[i2][j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+            vv[i2][j] &= ~((bad >> 7) * 0xffu);
+            while (bad) {
+              const int byte = (__ffs(bad) - 1) >> 3;
+              bad &= bad - 1;
+              atomicMin(nan_at + HD / 8 * g + 4 * j + byte, u * kUnit + a * kStep + 2 * t + (i2 & 1) + 8 * (i2 >> 1));
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < HD / 32; ++j) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const uint32_t x0 = tc::prmt(vv[0][j], vv[1][j], x ? 0x7362 : 0x5140), x1 = tc::prmt(vv[2][j], vv[3][j], x ? 0x7362 : 0x5140);
+          const uint32_t a0 = decode2(x0), a1 = decode2(x0 >> 16), a2 = decode2(x1), a3 = decode2(x1 >> 16);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_f16(acc[n][2 * j + x], a0, a1, a2, a3, pa[n][0], pa[n][1]);
+        }
+      }
+    }
+    const int i3 = i + 2 * kDepth, src = (i3 & 31) + (lane & (nb - 1));
+    const int rc = __shfl_sync(0xffffffffu, mc.row, src), rn = __shfl_sync(0xffffffffu, mn.row, src);
+    if (u + kDepth < u_hi) issue(slot, i3 < 32 ? rc : rn);
+    if (i == 30) {
+      mc = mn;
+      take_scales();
+      mn = load_meta(entry_n, 2 * u + 34);
+      entry_n = load_entry(2 * u + 66);
+    }
+    if (++slot == kDepth) {
+      slot = 0;
+      phase ^= 1;
+    }
+  }
+  // the block's warps joined in warp order, four dims per thread
+  float* mine = reinterpret_cast<float*>(ring0 + w * kRing);
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int off = 4; off <= 16; off <<= 1) l[n][u] += __shfl_xor_sync(0xffffffffu, l[n][u], off);
+      const int r = 8 * n + 2 * t + u;
+      if (g == 0) {
+        wm[w * R + r] = m[n][u];
+        wl[w * R + r] = l[n][u];
+      }
+#pragma unroll
+      for (int j = 0; j < HD / 16; ++j) *reinterpret_cast<float2*>(mine + r * HD + HD / 8 * g + 2 * j) = make_float2(acc[n][j][u], acc[n][j][u + 2]);
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n_rows * (HD / 4); i += kThreads) {
+    const int r = i / (HD / 4), d = i % (HD / 4) * 4;
+    float top = -INFINITY, ll = 0.f;
+#pragma unroll
+    for (int x = 0; x < kWarps; ++x) top = fmaxf(top, wm[x * R + r]);
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int x = 0; x < kWarps; ++x) {
+      const float f = top == -INFINITY ? 1.f : ex2(wm[x * R + r] - top);
+      const float4 y = *reinterpret_cast<const float4*>(ring0 + x * kRing + (r * HD + d) * 4);
+      sum = make_float4(fmaf(f, y.x, sum.x), fmaf(f, y.y, sum.y), fmaf(f, y.z, sum.z), fmaf(f, y.w, sum.w));
+      ll = fmaf(f, wl[x * R + r], ll);
+    }
+    const float nan = __int_as_float(0x7fffffff);
+    if (row_last[r] >= nan_at[d]) sum.x = nan;
+    if (row_last[r] >= nan_at[d + 1]) sum.y = nan;
+    if (row_last[r] >= nan_at[d + 2]) sum.z = nan;
+    if (row_last[r] >= nan_at[d + 3]) sum.w = nan;
+    const int64_t row_head = split * part_of.row_heads + (seq.row0 + r / G) * H + h * G + r % G;
+    *reinterpret_cast<float4*>(part_of.sums + row_head * HD + d) = sum;
+    if (d == 0) part_of.stats[row_head] = make_float2(top - kOffset, ll);
+  }
 }
 
 // Joins the shares' partial results in the workspace: HD / 4 threads per row, four dims each.  With many shares (kGroups =
@@ -757,8 +1052,24 @@ size_t workspace_bytes(const View& V, int H, int hd) {
 
 }  // namespace
 
+template <typename T, int HD> szo_status launch_prefix_rows(const View& V, const Rows& A, int nsplit, cudaStream_t st, const Part& part) {
+  const size_t smem = static_cast<size_t>(4) * kRingBytes<HD> + 1024;
+  const int64_t blocks = static_cast<int64_t>(nsplit) * part.items * V.hkv;
+  SZO_REQUIRE(blocks <= 0x7fffffff, SZO_ERR_SHAPE, "too many rows, heads and sequences for one launch");
+  CUtensorMap map_k, map_v;
+  SZO_TRY(codes_map(V.k, V, HD, box_tokens(V), &map_k));
+  SZO_TRY(codes_map(V.v, V, HD, box_tokens(V), &map_v));
+  auto kern = kv8_prefix_rows_kernel<T, HD>;
+  SZO_CHECK_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+  SZO_CHECK_CUDA(launch_maybe_chained(kern, dim3(static_cast<unsigned>(blocks)), dim3(128), smem, st, true, map_k, map_v, V, static_cast<const T*>(A.q),
+                                      A.q_stride, A.H, A.scale * 1.4426950408889634f, nsplit, part));
+  count_launch();
+  return SZO_OK;
+}
 template <typename T, int HD> szo_status launch_part(const View& V, const Rows& A, const Part& part, int nsplit, cudaStream_t st) {
   const int64_t rows = static_cast<int64_t>(part.max_rows) * (A.H / V.hkv);
+  if constexpr (sizeof(T) == 2)
+    if (part.prefix && rows > 16 && rows <= kPrefixRows) return launch_prefix_rows<T, HD>(V, A, nsplit, st, part);
   // (sequences of more items than blocks of 4 warps fit on the SMs at once: blocks of 2.  64 sequences of up to 512 positions of their own,
   // 8 heads: 46 us, with blocks of 4 warps 48)
   if (!part.prefix && rows <= 8 && static_cast<int64_t>(part.items) * V.hkv > 148 * 3) return launch_rows<T, HD, 1, 2, true>(V, A, nsplit, nullptr, st, part);

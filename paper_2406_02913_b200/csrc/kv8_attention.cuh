@@ -7,6 +7,7 @@
 namespace szo {
 namespace kv8 {
 
+constexpr int kPrefixRows = 32;                // rows of a group, 16-bit types, that one block takes
 constexpr int kStep = 16;                      // positions that certainly share a page
 
 // The row buffers and heads of a call

@@ -107,15 +107,17 @@ struct SharePlan {
   int64_t row_heads;
 };
 // How a pass's positions are cut.  The lengths are on the device, so the rule goes by the number of items (owner, head, row
-// tile): as many shares as fill the SMs once (many rows: one block per SM) or twice (few rows), of 2 steps of 128 (units of 32 per warp) of
-// what the page table could hold.  A sequence's pass for few rows joins its shares in a cluster: a power of two up to 8.
+// tile): few rows: as many shares as fill the SMs twice (8 sequences of 4 rows on 65536 shared positions, 8 heads: 37 shares 65 us, 30 72, 48
+// 88), many: three quarters of them once, since the sequences' pass runs beside (64 sequences on 8192: 14 shares 43.5 us, 10 46.5,
+// 18 46); of 2 steps of 128 (units of 32 per warp) at least of what the page table could hold.  A sequence's pass for few rows
+// joins its shares in a cluster: a power of two up to 8.
 Pass make_pass(const View& V, int64_t max_rows, int64_t owners, int H, bool wide_type, bool prefix) {
   const int64_t rows = max_rows * (H / V.hkv), places = static_cast<int64_t>(V.max_pages) << V.page_shift;
   Pass p{!wide_type && rows > 32, static_cast<int>(max_rows), 1};
-  const int64_t tile = p.many ? 256 : rows <= 8 ? 8 : 16, items = owners * V.hkv * ceil_div(rows, tile);
-  const int64_t room = p.many ? 148 : 296, least = p.many ? 256 : 128;
+  const int64_t tile = p.many ? 256 : rows <= 8 ? 8 : prefix && !wide_type && rows > 16 ? kPrefixRows : 16, items = owners * V.hkv * ceil_div(rows, tile);
+  const int64_t room = p.many ? (prefix ? 112 : 148) : 296, least = p.many ? 256 : 128;
   if (prefix || p.many) {
-    while (p.shares < 32 && items * (p.shares + 1) <= room && places >= least * (p.shares + 1)) ++p.shares;
+    while (p.shares < 64 && items * (p.shares + 1) <= room && places >= least * (p.shares + 1)) ++p.shares;
   } else {
     while (p.shares < 8 && items * p.shares * 2 <= room && places >= least * 2 * p.shares) p.shares *= 2;
   }
