@@ -533,6 +533,17 @@ szo_status szo_model_decode_step(szo_model_t* m, const int32_t* tokens, int32_t 
  * (16, 32, 64 or 128).  szo_model_decode_step then works as described above; its results carry the cache's rounding
  * (a key or value is off by at most 2^-4 of its size).  Once, and not together with szo_model_enable_decode. */
 szo_status szo_model_enable_decode_kv8(szo_model_t* m, int32_t page_tokens, void* stream);
+/* Several sequences continue one prompt (samples, candidate answers): sequences 0 .. B-1 take the first n positions of sequence 0's 8-bit
+ * cache as their own.  Whole pages are shared and not copied, the rest of a last page is; the calls of szo_model_decode_step that follow
+ * read the shared ones once for all (szo_attention_kv8_prefix).  They may not write positions below the shared pages' end
+ * (SZO_ERR_INVALID_ARG).  B = 1 or n = 0 ends the sharing: other sequences than 0 then have their own pages again, with what they held
+ * before.  Needs szo_model_enable_decode_kv8; may allocate. */
+szo_status szo_model_decode_share(szo_model_t* m, int32_t B, int32_t n, void* stream);
+/* Next-token loss of every position of B sequences of S tokens, without logits being stored (szo_head_ce on the last hidden
+ * states): loss fp32 [B*S] for targets int32 [B*S] (negative: none, loss 0; targets[b*S+s] is the token after position s), and lse
+ * fp32 [B*S] or NULL.  One forward as for szo_model_loss; models of either loss_kind, bf16 activations (SZO_ERR_UNSUPPORTED else). */
+szo_status szo_model_token_losses(szo_model_t* m, const int32_t* tokens, int32_t B, int32_t S, const int32_t* targets, const float* S_vals,
+                                  float* loss, float* lse, void* stream);
 /* Log probabilities of given tokens at every position of B sequences of S tokens (the terms that the next-token loss
  * sums, and those of any other candidates): one forward as for szo_model_loss, then szo_token_logprobs on the fp32
  * logits of all B*S positions.  targets int32 [B*S][n_targets]; outputs as for szo_token_logprobs with rows = B*S (row

@@ -159,6 +159,9 @@ _SIGS = {
     "szo_model_enable_decode_kv8": (C.c_int32, [C.c_void_p, C.c_int32, C.c_void_p]),
     "szo_model_token_logprobs": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p,
                                              C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "szo_model_decode_share": (C.c_int32, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]),
+    "szo_model_token_losses": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                           C.c_void_p]),
     "szo_model_decode_step": (C.c_int32, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                                           C.c_void_p, C.c_void_p]),
     "szo_model_last_launches": (C.c_int64, [C.c_void_p]),
@@ -846,6 +849,26 @@ class Model:
         _check(lib().szo_model_token_logprobs(self.h, _ptr(tokens), B, S, p(targets), nt, n_top, _ptr(S_vals), p(r.logp), _ptr(r.entropy),
                                               _ptr(r.lse), p(r.top_ids), p(r.top_logp), _stream()))
         return r
+
+    def token_losses(self, tokens, targets=None, S_vals=None) -> HeadCe:
+        """Next-token loss and log sum exp of every position (fp32 [B * S]) without stored logits: tokens int32 [B, S]; targets
+        int32 [B * S] (negative: none) or None: the tokens that follow (none after the last of a sequence)."""
+        if tokens.dtype != torch.int32 or tokens.dim() != 2:
+            raise ValueError("tokens must be int32 [B, S]")
+        B, S = tokens.shape
+        if targets is None:
+            targets = torch.full_like(tokens, -1)
+            targets[:, :-1] = tokens[:, 1:]
+            targets = targets.view(-1)
+        if targets.dtype != torch.int32 or targets.shape != (B * S,):
+            raise ValueError("targets must be int32 [B * S]")
+        r = HeadCe(*(torch.empty(B * S, dtype=torch.float32, device=tokens.device) for _ in (0, 1)))
+        _check(lib().szo_model_token_losses(self.h, _ptr(tokens), B, S, _ptr(targets), _ptr(S_vals), _ptr(r.loss), _ptr(r.lse), _stream()))
+        return r
+
+    def decode_share(self, B: int, n: int):
+        """Sequences 0 .. B-1 continue the first n cached positions of sequence 0 (8-bit cache); B = 1 or n = 0 ends that."""
+        _check(lib().szo_model_decode_share(self.h, B, n, _stream()))
 
     def decode_step(self, tokens, pos0: int, logits=None, S_vals=None) -> torch.Tensor:
         """tokens int32 [B, T] following pos0 cached positions; returns fp32 logits [B, vocab] of the last one."""

@@ -985,6 +985,10 @@ struct szo_model {
   void* kv8_ws = nullptr;
   size_t kv8_ws_bytes = 0;
   int kv8_page = 0, kv8_pages = 0;
+  // sequences 0 .. kv8_sharers - 1 share their first kv8_shared positions (szo_model_decode_share); on the device: that number, and the
+  // one group of sequences, 0 and its end in the current call
+  int kv8_sharers = 0, kv8_shared = 0;
+  int32_t* kv8_group = nullptr;                  // [12]: the length at 0, the sequences at 4 (16-byte boundaries)
   int64_t kv8_scale_floats() const {             // of a layer; whole 16 bytes, on which every layer's scales have to start
     return static_cast<int64_t>(round_up(static_cast<size_t>(cfg.max_batch) * kv8_pages * cfg.n_kv_heads * 2, 4));
   }
@@ -996,7 +1000,7 @@ struct szo_model {
   int32_t* dec_tokens = nullptr;                 // the call's tokens, at an address that a captured graph can keep
   float* dec_logits = nullptr;                   // [max_batch][vocab]
   struct DecodeGraph {
-    int B, T;
+    int B, T, sharers;
     const float* Sv;
     cudaGraphExec_t exec;
   };
@@ -1044,6 +1048,7 @@ struct ScoreArgs {
   float *logp, *entropy, *lse;
   int32_t* top_ids;
   float* top_logp;
+  float* loss;                                   // not NULL: cross entropy straight from the hidden states, and lse
 };
 template <typename T>
 szo_status run_loss_t(szo_model* m, const int32_t* tokens, const int32_t* labels, const int32_t* cand, int B,
@@ -1189,6 +1194,12 @@ szo_status run_loss_t(szo_model* m, const int32_t* tokens, const int32_t* labels
     pending = y;                  // added by the next norm (next layer's, or the final one)
   }
   double* const loss_out[2] = {loss_dev, loss_dev2};
+  if (score != nullptr && score->loss != nullptr) {
+    add_norm<<<static_cast<unsigned>(Mr), 256, 0, st>>>(m->h, pending, m->top.final_norm_g, m->top.final_norm_b, d, c.norm_eps, opt, 1, 0, a);
+    count_launch();
+    SZO_CHECK_LAUNCH("model kernels");
+    return szo_head_ce(a, d, m->top.lm_head, d, SZO_BF16, M, c.vocab, d, 1.0f, score->targets, score->loss, score->lse, m->ws, m->ws_bytes, st);
+  }
   if (c.loss_kind == 0) {
     add_norm<<<static_cast<unsigned>(Mr), 256, 0, st>>>(m->h, pending, m->top.final_norm_g,
                                                                  m->top.final_norm_b, d, c.norm_eps, opt, 1, 0, a);
@@ -1456,7 +1467,12 @@ szo_status run_decode_t(szo_model* m, const int32_t* tokens, int B, int Tn, cons
       const szo_kv8_cache cache{codes, codes + bytes, m->kv8_scales + l * m->kv8_scale_floats(), pages, m->kv8_page, Hkv, hd};
       const szo_kv8_batch batch{m->kv8_table, m->kv8_len, nullptr, M, B, m->kv8_pages, Tn};
       SZO_TRY(szo_kv8_write(&cache, &batch, k, v, static_cast<szo_dtype>(act), dkv, dkv, st));
-      SZO_TRY(szo_attention_kv8(&cache, &batch, q, d, o, d, static_cast<szo_dtype>(act), H, scale, m->kv8_ws, m->kv8_ws_bytes, st));
+      if (m->kv8_sharers > 1) {
+        const szo_kv8_prefix prefix{m->kv8_group, m->kv8_group + 4, 1, m->kv8_sharers};
+        SZO_TRY(szo_attention_kv8_prefix(&cache, &batch, &prefix, q, d, o, d, static_cast<szo_dtype>(act), H, scale, m->kv8_ws, m->kv8_ws_bytes, st));
+      } else {
+        SZO_TRY(szo_attention_kv8(&cache, &batch, q, d, o, d, static_cast<szo_dtype>(act), H, scale, m->kv8_ws, m->kv8_ws_bytes, st));
+      }
     } else if (Tn <= 16) {
       // rotation, cache append and attention in one launch
       const float2* tab = opt ? nullptr : m->rope_tab;
@@ -1670,6 +1686,13 @@ szo_status szo_model_create(szo_model_t** out, const szo_model_config* cfg, cons
                                 nullptr, 0, nullptr, st));
     const size_t need = szo_linear_workspace_bytes(m->lm_head_plan, 2 * m->Mmax + 256, lmode);
     if (need > ws_need) ws_need = need;
+  }
+  if (c.act_dtype == SZO_BF16) {                 // szo_model_token_losses
+    // (up to 128 rows take finer parts of the vocabulary than more do)
+    for (const int64_t rows : {m->Mmax, m->Mmax < 128 ? m->Mmax : int64_t(128)}) {
+      const size_t need = szo_head_ce_workspace_bytes(rows, c.vocab, c.d_model);
+      if (need > ws_need) ws_need = need;
+    }
   }
   // buffers
   const size_t e = c.act_dtype == SZO_F32 ? 4 : 2;
@@ -2013,6 +2036,7 @@ szo_status szo_model_enable_decode_kv8(szo_model_t* m, int32_t page_tokens, void
   SZO_TRY(dev_alloc(m, &m->kv8_scales, scales));
   SZO_TRY(dev_alloc(m, &m->kv8_table, static_cast<size_t>(pages) * sizeof(int32_t)));
   SZO_TRY(dev_alloc(m, &m->kv8_len, static_cast<size_t>(c.max_batch) * sizeof(int32_t)));
+  SZO_TRY(dev_alloc(m, &m->kv8_group, 12 * sizeof(int32_t)));
   SZO_TRY(dev_alloc(m, reinterpret_cast<char**>(&m->kv8_ws), ws));
   SZO_CHECK_CUDA(cudaMemsetAsync(codes, 0, bytes, st));
   SZO_CHECK_CUDA(cudaMemsetAsync(m->kv8_scales, 0, scales, st));
@@ -2025,6 +2049,84 @@ szo_status szo_model_enable_decode_kv8(szo_model_t* m, int32_t page_tokens, void
   return SZO_OK;
 }
 
+// page_table[b][j] of every sequence: sequence 0's pages for the first `pages` places of sequences below `sharers`, else its own
+__global__ void shared_table_kernel(int32_t* __restrict__ table, int64_t n, int per_seq, int sharers, int pages) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+  if (i >= n) return;
+  const int b = static_cast<int>(i / per_seq), j = static_cast<int>(i % per_seq);
+  table[i] = b < sharers && j < pages ? j : static_cast<int32_t>(i);
+}
+// Sequence 0's page `page` of every layer, codes and scales, to the same page of sequences 1 .. gridDim.y: grid (vectors, sequences, layers * 2)
+__global__ void copy_page_kernel(uint8_t* __restrict__ codes, int64_t kind_bytes, float* __restrict__ scales, int64_t scale_floats, int per_seq,
+                                 int page, int64_t page_bytes, int hkv) {
+  const int to = (static_cast<int>(blockIdx.y) + 1) * per_seq + page, kind = blockIdx.z & 1, layer = blockIdx.z >> 1;
+  uint8_t* base = codes + blockIdx.z * kind_bytes;
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) * 16;
+  if (i < page_bytes)
+    *reinterpret_cast<uint4*>(base + to * page_bytes + i) = *reinterpret_cast<const uint4*>(base + static_cast<int64_t>(page) * page_bytes + i);
+  float* sc = scales + layer * scale_floats;
+  if (blockIdx.x == 0 && kind == 0)
+    for (int h = threadIdx.x; h < 2 * hkv; h += blockDim.x) sc[static_cast<int64_t>(to) * 2 * hkv + h] = sc[static_cast<int64_t>(page) * 2 * hkv + h];
+}
+
+szo_status szo_model_decode_share(szo_model_t* m, int32_t B, int32_t n, void* stream) {
+  SZO_REQUIRE(m != nullptr, SZO_ERR_INVALID_ARG, "model is NULL");
+  SZO_REQUIRE(m->kv8_codes != nullptr, SZO_ERR_INVALID_ARG, "call szo_model_enable_decode_kv8 first");
+  SZO_REQUIRE(B >= 1 && B <= m->cfg.max_batch && n >= 0 && n <= m->cfg.max_seq, SZO_ERR_SHAPE, "need 1 <= B <= %d and 0 <= n <= %d (got B=%d, n=%d)",
+              m->cfg.max_batch, m->cfg.max_seq, B, n);
+  const szo_model_config& c = m->cfg;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int hd = c.d_model / c.n_heads, G = c.n_heads / c.n_kv_heads, whole = n / m->kv8_page;
+  if (B > 1 && whole > 0) {
+    // the most that szo_attention_kv8_prefix asks for: any number of sequences, and of new tokens up to those that share nothing
+    size_t need = m->kv8_ws_bytes;
+    szo_kv8_cache cache{m->kv8_codes, m->kv8_codes, m->kv8_scales, static_cast<int64_t>(c.max_batch) * m->kv8_pages, m->kv8_page, c.n_kv_heads, hd};
+    const szo_kv8_prefix prefix{m->kv8_group, m->kv8_group + 4, 1, B};
+    for (int b = 1; b <= c.max_batch; ++b)
+      for (int T = 1; T <= 256 / G + 1 && T <= c.max_seq && static_cast<int64_t>(b) * T <= m->Mmax; ++T) {
+        const szo_kv8_batch batch{m->kv8_table, m->kv8_len, nullptr, static_cast<int64_t>(b) * T, b, m->kv8_pages, T};
+        const size_t w = szo_attention_kv8_prefix_workspace_bytes(&cache, &batch, &prefix, c.n_heads);
+        if (w > need) need = w;
+      }
+    if (need > m->kv8_ws_bytes) {                // (captured steps keep the earlier one, which stays owned)
+      SZO_TRY(dev_alloc(m, reinterpret_cast<char**>(&m->kv8_ws), need));
+      m->kv8_ws_bytes = need;
+    }
+  }
+  const int64_t pages = static_cast<int64_t>(c.max_batch) * m->kv8_pages;
+  shared_table_kernel<<<blocks_for(pages, 256), 256, 0, st>>>(m->kv8_table, pages, m->kv8_pages, B, whole);
+  count_launch();
+  if (B > 1 && n % m->kv8_page != 0) {
+    const int64_t bytes = static_cast<int64_t>(m->kv8_page) * c.n_kv_heads * hd;
+    copy_page_kernel<<<dim3(blocks_for(bytes / 16, 256), B - 1, 2 * c.n_layers), 256, 0, st>>>(m->kv8_codes, pages * bytes, m->kv8_scales,
+                                                                                           m->kv8_scale_floats(), m->kv8_pages, whole, bytes, c.n_kv_heads);
+    count_launch();
+  }
+  set_i32_kernel<<<1, 1, 0, st>>>(m->kv8_group, whole * m->kv8_page);
+  set_i32_kernel<<<1, 1, 0, st>>>(m->kv8_group + 4, 0);
+  count_launch(2);
+  SZO_CHECK_LAUNCH("the kernels of szo_model_decode_share");
+  m->kv8_sharers = whole > 0 ? B : 0;
+  m->kv8_shared = B > 1 ? whole * m->kv8_page : 0;
+  return SZO_OK;
+}
+
+szo_status szo_model_token_losses(szo_model_t* m, const int32_t* tokens, int32_t B, int32_t S, const int32_t* targets, const float* S_vals, float* loss,
+                                  float* lse, void* stream) {
+  SZO_REQUIRE(m != nullptr, SZO_ERR_INVALID_ARG, "model is NULL");
+  SZO_REQUIRE(m->cfg.act_dtype == SZO_BF16, SZO_ERR_UNSUPPORTED, "needs bf16 activations (use szo_model_token_logprobs)");
+  SZO_REQUIRE(tokens != nullptr && targets != nullptr && loss != nullptr, SZO_ERR_INVALID_ARG, "NULL tokens, targets or loss");
+  SZO_REQUIRE(B >= 1 && S >= 1 && B <= m->cfg.max_batch && S <= m->cfg.max_seq && static_cast<int64_t>(B) * S <= m->Mmax, SZO_ERR_SHAPE,
+              "need 1 <= B <= %d and 1 <= S <= %d (got B=%d, S=%d)", m->cfg.max_batch, m->cfg.max_seq, B, S);
+  SZO_REQUIRE(m->cfg.arch == 0 || S <= m->cfg.max_pos, SZO_ERR_SHAPE, "position beyond the position table");
+  SZO_REQUIRE(aligned16(tokens) && aligned16(targets) && aligned16(loss) && aligned16(lse) && aligned16(S_vals), SZO_ERR_ALIGNMENT,
+              "buffers must be 16-byte aligned");
+  SZO_REQUIRE(device_status_word() != nullptr, SZO_ERR_CUDA, "no device status word");
+  const ScoreArgs score{targets, 1, 0, nullptr, nullptr, lse, nullptr, nullptr, loss};
+  return run_loss_t<__nv_bfloat16>(m, tokens, nullptr, nullptr, B, S, S_vals ? S_vals : m->S_all, nullptr, static_cast<cudaStream_t>(stream), nullptr,
+                                   nullptr, &score);
+}
+
 szo_status szo_model_token_logprobs(szo_model_t* m, const int32_t* tokens, int32_t B, int32_t S, const int32_t* targets, int32_t n_targets,
                                     int32_t n_top, const float* S_vals, float* logp, float* entropy, float* lse, int32_t* top_ids,
                                     float* top_logp, void* stream) {
@@ -2033,7 +2135,7 @@ szo_status szo_model_token_logprobs(szo_model_t* m, const int32_t* tokens, int32
   SZO_TRY(check_batch(m, tokens, nullptr, nullptr, B, S));
   SZO_TRY(check_token_logprobs(m->logits, SZO_F32, static_cast<int64_t>(B) * S, m->cfg.vocab, m->cfg.vocab, 1.0f, targets, n_targets, n_top,
                                logp, entropy, lse, top_ids, top_logp));
-  const ScoreArgs score{targets, n_targets, n_top, logp, entropy, lse, top_ids, top_logp};
+  const ScoreArgs score{targets, n_targets, n_top, logp, entropy, lse, top_ids, top_logp, nullptr};
   const float* Sv = S_vals ? S_vals : m->S_all;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (m->cfg.act_dtype == SZO_F32) return run_loss_t<float>(m, tokens, nullptr, nullptr, B, S, Sv, nullptr, st, nullptr, nullptr, &score);
@@ -2049,6 +2151,8 @@ szo_status szo_model_decode_step(szo_model_t* m, const int32_t* tokens, int32_t 
               T, pos0);
   SZO_REQUIRE(static_cast<int64_t>(B) * T <= m->Mmax, SZO_ERR_SHAPE, "B * T exceeds max_batch * max_seq");
   SZO_REQUIRE(m->cfg.arch == 0 || pos0 + T <= m->cfg.max_pos, SZO_ERR_SHAPE, "position beyond the position table");
+  SZO_REQUIRE(pos0 >= m->kv8_shared, SZO_ERR_INVALID_ARG,
+              "positions below %d are shared by %d sequences and may not be written (szo_model_decode_share(m, 1, 0) ends that)", m->kv8_shared, m->kv8_sharers);
   const float* Sv = S_vals ? S_vals : m->S_all;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   auto run = [&](const int32_t* toks, float* out) -> szo_status {
@@ -2060,6 +2164,10 @@ szo_status szo_model_decode_step(szo_model_t* m, const int32_t* tokens, int32_t 
   if (m->kv8_codes != nullptr) {
     fill_i32_kernel<<<blocks_for(B, 256), 256, 0, st>>>(m->kv8_len, B, pos0 + T);
     count_launch();
+    if (m->kv8_sharers > 1) {
+      set_i32_kernel<<<1, 1, 0, st>>>(m->kv8_group + 5, B < m->kv8_sharers ? B : m->kv8_sharers);
+      count_launch();
+    }
   }
   // A token step is several hundred short launches: on a stream that can be captured it is recorded once
   // per (B, T, sparse values) as a CUDA graph and replayed (the position comes from device memory, the
@@ -2071,7 +2179,7 @@ szo_status szo_model_decode_step(szo_model_t* m, const int32_t* tokens, int32_t 
   SZO_CHECK_CUDA(cudaMemcpyAsync(m->dec_tokens, tokens, static_cast<size_t>(B) * T * sizeof(int32_t), cudaMemcpyDeviceToDevice, st));
   cudaGraphExec_t exec = nullptr;
   for (const auto& g : m->dec_graphs)
-    if (g.B == B && g.T == T && g.Sv == Sv) exec = g.exec;
+    if (g.B == B && g.T == T && g.sharers == m->kv8_sharers && g.Sv == Sv) exec = g.exec;
   if (exec == nullptr) {
     SZO_CHECK_CUDA(cudaStreamBeginCapture(st, cudaStreamCaptureModeThreadLocal));
     const szo_status rc = run(m->dec_tokens, m->dec_logits);
@@ -2089,7 +2197,7 @@ szo_status szo_model_decode_step(szo_model_t* m, const int32_t* tokens, int32_t 
       cudaGraphExecDestroy(m->dec_graphs.front().exec);
       m->dec_graphs.erase(m->dec_graphs.begin());
     }
-    m->dec_graphs.push_back({B, T, Sv, exec});
+    m->dec_graphs.push_back({B, T, m->kv8_sharers, Sv, exec});
   }
   SZO_CHECK_CUDA(cudaGraphLaunch(exec, st));
   SZO_CHECK_CUDA(cudaMemcpyAsync(logits_dev, m->dec_logits, static_cast<size_t>(B) * m->cfg.vocab * sizeof(float),
