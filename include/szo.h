@@ -376,10 +376,15 @@ szo_status szo_attention_kv8(const szo_kv8_cache* cache, const szo_kv8_batch* ba
  *   len   int32 [n_groups]     shared positions, from position 0 on
  *   seqs  int32 [n_groups+1]   ascending; NULL (n_groups 1): all sequences are one group.  Sequences in no group share nothing
  *   max_seqs                   the most sequences of a group
- * All on the device, read when the work runs.  The shared pages are read through the table of the group's first sequence.  A group
+ * All on the device, read when the work runs.  The shared pages are read through the table of the group's longest sequence.  A group
  * whose description does not fit (decreasing or beyond the batch, more than max_seqs sequences, len negative or beyond max_pages *
- * page_tokens) shares nothing, which leaves results as they are, and the status word reports SZO_ERR_SHAPE.  Results, arguments and errors
- * otherwise as for szo_attention_kv8, up to the order of sums; rows at positions inside the shared part see what they see there. */
+ * page_tokens) shares nothing, which leaves results as they are, and the status word reports SZO_ERR_SHAPE; so does, without a report of its
+ * own, a group with a skipped sequence, and every group where seqs does not ascend.  Results, arguments and errors otherwise as for
+ * szo_attention_kv8, up to the order of sums (rows * n_heads below 2^31); rows at positions inside the shared part see what they see there.
+ * Where a sequence's own rows fill the tensor cores' tiles (256 rows per key/value head), or all that the batch's tables could hold is
+ * little (96 MB), sharing gains nothing and szo_attention_kv8 does the work.  workspace: szo_attention_kv8_prefix_workspace_bytes bytes (it
+ * depends on the shapes only; a few times the output in fp32), contents irrelevant on entry; calls that may run at the same time need one
+ * each. */
 typedef struct {
   const int32_t* len;
   const int32_t* seqs;

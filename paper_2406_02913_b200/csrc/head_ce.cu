@@ -182,8 +182,10 @@ __global__ void head_round_kernel(const float* __restrict__ acc, int parts, int6
   const int64_t per = d / 8, i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
   if (i >= rows * per) return;
   const int64_t r = i / per, c = i % per * 8;
-  const float f = info[r].w;
+  const float4 of = info[r];
+  const float f = of.w;
   float x[8] = {};
+  if (of.y == 0.f && of.z == 0.f) parts = 0;                      // a row that weighs nothing: zeros, whatever W holds
   for (int p = 0; p < parts; ++p) {
     const float4* from = reinterpret_cast<const float4*>(acc + (p * rows + r) * d + c);
     const float4 lo = from[0], hi = from[1];

@@ -44,16 +44,24 @@ __global__ void __launch_bounds__(256) kv8_groups_kernel(View V, Prefix P, int4*
   len = ascending && fits ? len >> V.page_shift << V.page_shift : 0;
   first = max(first, 0);
   end = min(end, V.batch);
+  // the pages are read through the table of the longest sequence, the first of several, and as far as it goes: entries that no position
+  // needs are not read
+  __shared__ unsigned long long longest;
+  if (threadIdx.x == 0) longest = 0;
+  __syncthreads();
   ok = true;
   for (int b = first + threadIdx.x; b < end; b += blockDim.x) {
     Seq q;
     ok = read_seq(V, b, &q) && ok;
+    atomicMax(&longest, static_cast<unsigned long long>(static_cast<unsigned>(q.len)) << 32 | (0x7fffffffu - static_cast<unsigned>(b)));
   }
   if (!__syncthreads_and(ok) || first >= end) len = 0;
+  len = min(len, (static_cast<int>(longest >> 32) + (1 << V.page_shift) - 1) >> V.page_shift << V.page_shift);
+  const int owner = 0x7fffffff - static_cast<int>(longest & 0x7fffffffu);
   if (threadIdx.x == 0) {
     const int row0 = len == 0 ? 0 : V.start != nullptr ? V.start[first] : first * V.max_new;
     const int rows = len == 0 ? 0 : V.start != nullptr ? V.start[end] - row0 : (end - first) * V.max_new;
-    groups[g] = make_int4(row0, rows, len, first);
+    groups[g] = make_int4(row0, rows, len, owner);
   }
   if (!ascending) return;
   const int lane = threadIdx.x & 31;

@@ -116,6 +116,43 @@ def test_backward(B, dt, rows, vocab, d):
     assert B.device_status() == 0
 
 
+@pytest.mark.parametrize("dt,rows,vocab,d", [("bf16", 16, 140001, 64), ("f16", 100, 131073, 72), ("bf16", 140, 140001, 64), ("f16", 4100, 50001, 64),
+                                             ("bf16", 2300, 60000, 136)])
+def test_vocabularies_of_many_pieces(B, dt, rows, vocab, d):
+    """G in several pieces of the vocabulary, its buffers used again; last pieces of a few entries."""
+    h, W, t, g = problem(rows, vocab, d, dt, seed=rows)
+    lse = B.szo_head_ce(h, W, t).lse
+    a, b = torch.randn(rows, device="cuda", generator=g), 0.2 * torch.randn(rows, device="cuda", generator=g)
+    check_forward(B.szo_head_ce(h, W, t), h, W, t, 1.0)
+    dh, dW = B.szo_head_ce_bwd(h, W, t, lse, a, b)
+    wh, eh, wW, eW = backward_bounds(h, W, t, lse, a, b, 1.0, dt)
+    within(dh, wh, eh)
+    within(dW, wW, eW)
+    assert torch.equal(B.szo_head_ce_bwd(h, W, t, lse, a, b, need_dW=False)[0], dh)
+    assert torch.equal(B.szo_head_ce_bwd(h, W, t, lse, a, b, need_dh=False)[1], dW)
+    assert B.device_status() == 0
+
+
+def test_two_calls_at_once(B):
+    """Two gradients on two streams share the SMs; each hands out its own units."""
+    p = [problem(600 + 40 * i, 30000, 256, "bf16", 30 + i) for i in (0, 1)]
+    lse = [B.szo_head_ce(h, W, t).lse for h, W, t, _ in p]
+    a = [torch.randn(x[0].shape[0], device="cuda") for x in p]
+    want = [B.szo_head_ce_bwd(*p[i][:3], lse[i], a[i]) for i in (0, 1)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in (0, 1)]
+    for _ in range(3):
+        got = [None, None]
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                got[i] = [B.szo_head_ce_bwd(*p[i][:3], lse[i], a[i]) for _ in range(3)]
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            for dh, dW in got[i]:
+                assert torch.equal(dh, want[i][0]) and torch.equal(dW, want[i][1])
+    assert B.device_status() == 0
+
+
 def test_confident_rows_keep_their_relative_precision(B):
     d, vocab = 128, 2000
     h, W, t, _ = problem(64, vocab, d, "bf16", 3, known=0.0, none=0.0)
@@ -168,6 +205,10 @@ def test_rows_that_weigh_nothing(B, dt):
     # no row weighs anything
     dh, dW = B.szo_head_ce_bwd(h, W, torch.full_like(t, -1), got.lse, a)
     assert (dh == 0).all() and (dW == 0).all()
+    # nor does what W holds
+    Wn = W.clone()
+    Wn[3, 1] = float("inf")
+    assert (B.szo_head_ce_bwd(h, Wn, t, got.lse, a, need_dW=False)[0][dead] == 0).all()
     # a row of which lse says that it has no probability anywhere
     l2 = got.lse.clone()
     l2[live] = -float("inf")

@@ -146,6 +146,33 @@ def test_rows_inside_the_shared_part(B, dt, new):
     assert B.device_status() == 0
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("new", [1, 30])
+def test_groups_whose_first_sequences_are_short(B, dt, new):
+    """Entries of a table that no position of its sequence needs may hold anything: the first sequences end inside the shared part, in one
+    group all do."""
+    sizes, prefixes = [4, 3], [192, 192]
+    lens = [40, 100, 300, 200, 60, 90, 33]
+    w = SharedWorld(B, sizes, prefixes, [300] * 7, 2, 32, 64, seed=31)
+    w.fill([300] * 7)
+    for b, n in enumerate(lens):
+        w.wide[b, -(-n // 32):] = 1 << 28
+        w.narrow[b, -(-n // 32):] = -5
+    check(B, w, lens, [min(new, n) for n in lens], 4, dt)
+    assert B.device_status() == 0
+
+
+@pytest.mark.parametrize("dt,group,count", [("bf16", 4, 300), ("f16", 1, 700), ("f32", 2, 300)])
+def test_many_sequences(B, dt, group, count):
+    """Groups of more rows than one tile has, and more sequences than a block has threads."""
+    sizes, prefixes = [count - 7, 7], [96, 64]
+    lens = [97 + (5 * i) % 40 for i in range(count)]
+    w = SharedWorld(B, sizes, prefixes, lens, 1, 16, 64, seed=32)
+    w.fill(lens)
+    check(B, w, lens, [1 + (i % 3 == 0) for i in range(count)], group, dt)
+    assert B.device_status() == 0
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("new,count", [(1, 3), (1, 40), (7, 20), (40, 9)])
 def test_sequences_of_no_group_and_batches_without_one(B, dt, new, count):
@@ -226,7 +253,7 @@ def test_descriptions_that_do_not_fit_share_nothing(B):
     # page ids of no page, in the shared part and behind it
     for at in (1, 9):
         t = w.d_table.clone()
-        t[0 if at == 1 else 3, at] = w.cache.n_pages
+        t[slice(None) if at == 1 else 3, at] = w.cache.n_pages     # (a shared page stands in every table)
         for new in (1, 40):
             rows = count * new
             batch = B.Kv8Batch(t, ints(*lens), rows)
