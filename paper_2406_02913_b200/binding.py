@@ -578,36 +578,51 @@ class HeadCe(NamedTuple):
 
 
 def _head_rows(h, W, targets):
-    """rows, vocab, d, the row strides and the device of checked arguments."""
-    device = h.get_device()
-    if not h.is_cuda or device != _device():
+    """rows, vocab, d, the type, the row strides and the device of checked arguments."""
+    device, shape, wshape, dtype = h.get_device(), h.shape, W.shape, h.dtype
+    if device < 0 or device != _device():
         raise ValueError(f"h must be a CUDA tensor of the current device (got {h.device})")
-    if h.dim() != 2 or W.dim() != 2 or W.shape[1] != h.shape[1] or h.dtype != W.dtype or W.get_device() != device:
+    if len(shape) != 2 or len(wshape) != 2 or wshape[1] != shape[1] or dtype != W.dtype or W.get_device() != device:
         raise ValueError("h must be [rows, d] and W [vocab, d], of the same type and device")
-    if h.dtype not in (torch.bfloat16, torch.float16):
-        raise ValueError(f"h and W must be bfloat16 or float16 (got {h.dtype})")
-    (rows, d), vocab = h.shape, W.shape[0]
-    if (d > 1 and (h.stride(1) != 1 or W.stride(1) != 1)):
+    if dtype is not torch.bfloat16 and dtype is not torch.float16:
+        raise ValueError(f"h and W must be bfloat16 or float16 (got {dtype})")
+    (rows, d), vocab, hs, ws = shape, wshape[0], h.stride(), W.stride()
+    if d > 1 and (hs[1] != 1 or ws[1] != 1):
         raise ValueError("h and W must have contiguous rows")
-    if targets.dtype != torch.int32 or targets.dim() != 1 or targets.numel() != rows or not targets.is_contiguous() or targets.get_device() != device:
+    if targets.dtype is not torch.int32 or targets.shape != shape[:1] or targets.get_device() != device or (rows > 1 and targets.stride(0) != 1):
         raise ValueError("targets must be a contiguous int32 tensor [rows] on h's device")
-    return rows, vocab, d, h.stride(0) if rows > 1 else d, W.stride(0) if vocab > 1 else d, device
+    return rows, vocab, d, _DT[dtype], hs[0] if rows > 1 else d, ws[0] if vocab > 1 else d, device
 
 
 def szo_head_ce(h: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, scale: float = 1.0) -> HeadCe:
     """Cross entropy of targets[r] (int32 [rows], negative: none) under softmax(scale * h[r] W^T), and log sum exp of every row;
     h [rows, d], W [vocab, d], bf16 or fp16.  The logits are never stored."""
-    rows, vocab, d, hs, ws_, device = _head_rows(h, W, targets)
+    rows, vocab, d, dt, hs, ws_, device = _head_rows(h, W, targets)
     r4 = (rows + 3) & ~3
-    f = torch.empty(2 * r4, dtype=torch.float32, device=h.device)     # one allocation, two parts that start on 16 bytes
+    f = h.new_empty(2 * r4, dtype=torch.float32)                      # one allocation, two parts that start on 16 bytes
     loss, lse = f.as_strided((rows,), (1,), 0), f.as_strided((rows,), (1,), r4)
     if rows:
         L = lib()
         need = L.szo_head_ce_workspace_bytes(rows, vocab, d)
-        ws = torch.empty((need,), dtype=torch.uint8, device=h.device)
-        _check(L.szo_head_ce(h.data_ptr(), hs, W.data_ptr(), ws_, _DT[h.dtype], rows, vocab, d, scale, targets.data_ptr(), loss.data_ptr(),
-                             lse.data_ptr(), ws.data_ptr(), need, _raw_stream(device)))
+        ws = h.new_empty(need, dtype=torch.uint8)
+        _check(L.szo_head_ce(h.data_ptr(), hs, W.data_ptr(), ws_, dt, rows, vocab, d, scale, targets.data_ptr(), f.data_ptr(), lse.data_ptr(),
+                             ws.data_ptr(), need, _raw_stream(device)))
     return HeadCe(loss, lse)
+
+
+def _head_vector(t, rows, device, name):
+    if t.dtype is not torch.float32 or t.shape != (rows,) or t.get_device() != device or (rows > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous float32 tensor of {rows} values on h's device")
+    return t.data_ptr() if rows else None
+
+
+def _head_gradient(t, like, device, name):
+    """The tensor that a gradient goes to, its address and row stride."""
+    if t is None:
+        t = torch.empty_like(like, memory_format=torch.contiguous_format)
+    elif t.shape != like.shape or t.dtype is not like.dtype or t.get_device() != device or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must have the shape, type and device of what it is the gradient of, and contiguous rows")
+    return t, t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def szo_head_ce_bwd(h: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, d_loss: torch.Tensor,
@@ -615,33 +630,21 @@ def szo_head_ce_bwd(h: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, lse
                     out_dW=None):
     """Gradient of sum(d_loss * loss) + sum(d_lse * lse) with respect to h and W as (dh, dW), None where not wanted;
     results go to out_dh and out_dW where given."""
-    rows, vocab, d, hs, ws_, device = _head_rows(h, W, targets)
-
-    def vec(t, name):
-        if t is None:
-            return None
-        if t.dtype != torch.float32 or t.numel() != rows or not t.is_contiguous() or t.get_device() != device:
-            raise ValueError(f"{name} must be a contiguous float32 tensor of {rows} values on h's device")
-        return t.data_ptr() if rows else None
-
-    def out(t, like, name):
-        if t is None:
-            return torch.empty(like.shape, dtype=like.dtype, device=like.device)
-        if t.shape != like.shape or t.dtype != like.dtype or t.get_device() != device or (d > 1 and t.stride(1) != 1):
-            raise ValueError(f"{name} must have the shape, type and device of what it is the gradient of, and contiguous rows")
-        return t
-    p = vec(lse, "lse"), vec(d_loss, "d_loss"), vec(d_lse, "d_lse")
-    dh = out(out_dh, h, "out_dh") if need_dh or out_dh is not None else None
-    dW = out(out_dW, W, "out_dW") if need_dW or out_dW is not None else None
-    if dh is None and dW is None:
-        return None, None
+    rows, vocab, d, dt, hs, ws_, device = _head_rows(h, W, targets)
+    p_lse, p_loss = _head_vector(lse, rows, device, "lse"), _head_vector(d_loss, rows, device, "d_loss")
+    p_dlse = None if d_lse is None else _head_vector(d_lse, rows, device, "d_lse")
+    dh = dW = p_dh = p_dW = None
+    dhs = dws = d
+    if need_dh or out_dh is not None:
+        dh, p_dh, dhs = _head_gradient(out_dh, h, device, "out_dh")
+    if need_dW or out_dW is not None:
+        dW, p_dW, dws = _head_gradient(out_dW, W, device, "out_dW")
     L = lib()
-    need = L.szo_head_ce_bwd_workspace_bytes(rows, vocab, d, dh is not None, dW is not None)
-    ws = torch.empty((max(need, 16),), dtype=torch.uint8, device=h.device)
-    _check(L.szo_head_ce_bwd(h.data_ptr(), hs, W.data_ptr(), ws_, _DT[h.dtype], rows, vocab, d, scale, targets.data_ptr(), *p,
-                             None if dh is None else dh.data_ptr(), d if dh is None or rows <= 1 else dh.stride(0),
-                             None if dW is None else dW.data_ptr(), d if dW is None or vocab <= 1 else dW.stride(0), ws.data_ptr(), need,
-                             _raw_stream(device)))
+    need = L.szo_head_ce_bwd_workspace_bytes(rows, vocab, d, p_dh is not None, p_dW is not None)
+    ws = h.new_empty(need, dtype=torch.uint8) if need else None
+    if dh is not None or dW is not None:
+        _check(L.szo_head_ce_bwd(h.data_ptr(), hs, W.data_ptr(), ws_, dt, rows, vocab, d, scale, targets.data_ptr(), p_lse, p_loss, p_dlse,
+                                 p_dh or None, dhs, p_dW, dws, None if ws is None else ws.data_ptr(), need, _raw_stream(device)))
     return dh, dW
 
 

@@ -131,6 +131,7 @@ template <typename T> __device__ __forceinline__ int largest_exponent(const RowA
 constexpr int64_t kScanRows = 2048;
 template <typename T> __global__ void __launch_bounds__(1024) head_exponent_kernel(RowArgs A, int32_t* __restrict__ exponent) {
   chain_release();
+  chain_wait();
   const int most = largest_exponent<T>(A);
   if (threadIdx.x == 0) *exponent = most;
 }
@@ -394,7 +395,7 @@ szo_status forward(const Shape& s, const Inputs<T>& in, float* loss, float* lse,
   P.rows = s.rows;
   P.c = in.scale * kLog2e;
   P.status = status;
-  SZO_TRY(launch_jobs<T>(P, few(s.rows), false, st));
+  SZO_TRY(launch_jobs<T>(P, few(s.rows), true, st));
   auto join = [&](auto kern, int rows) {
     return launch_maybe_chained(kern, dim3(blocks_of(s.rows, rows)), dim3(256), 0, st, true, P.part, P.xt, in.targets, s.rows, s.vocab, p.parts, loss, lse,
                                 status);
@@ -415,12 +416,11 @@ szo_status backward(const Shape& s, const Inputs<T>& in, const float* lse, const
   const RowArgs rows{in.targets, lse, d_loss, d_lse, s.rows, s.vocab, in.scale};
   const bool scan = kIsHalf<T> && dw != nullptr && s.rows > kScanRows;
   if (scan) {
-    head_exponent_kernel<T><<<1, 1024, 0, st>>>(rows, exponent);
+    SZO_CHECK_CUDA(launch_maybe_chained(head_exponent_kernel<T>, dim3(1), dim3(1024), 0, st, true, rows, exponent));
     count_launch();
-    SZO_CHECK_LAUNCH("head_exponent_kernel");
   }
   const unsigned vec_blocks = blocks_of(s.rows * (s.d / 8), 256);
-  SZO_CHECK_CUDA(launch_maybe_chained(head_prepare_kernel<T>, dim3(dw != nullptr ? vec_blocks : blocks_of(s.rows, 256)), dim3(256), 0, st, scan, rows, in.h,
+  SZO_CHECK_CUDA(launch_maybe_chained(head_prepare_kernel<T>, dim3(dw != nullptr ? vec_blocks : blocks_of(s.rows, 256)), dim3(256), 0, st, true, rows, in.h,
                                       in.hs, s.d, info, exponent, copy, counters, counters_of(p.pieces)));
   count_launch();
 
