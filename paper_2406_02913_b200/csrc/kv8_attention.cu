@@ -119,6 +119,31 @@ __host__ __device__ __forceinline__ int box_tokens(const View& V) { return V.pag
 
 template <int HD> constexpr int kRingBytes = kDepth * kUnit * HD * 2;       // per warp
 
+// Four dims of a row of a pass's share: the block's warps joined in warp order, NaN where the row sees one, stored
+template <int HD, int R, int kWarps, int kRing>
+__device__ __forceinline__ void store_share(int i, const unsigned char* ring0, const float* wm, const float* wl, const int* nan_at, int last,
+                                            int64_t row_head, const Part& part) {
+  const int r = i / (HD / 4), d = i % (HD / 4) * 4;
+  float top = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int x = 0; x < kWarps; ++x) top = fmaxf(top, wm[x * R + r]);
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int x = 0; x < kWarps; ++x) {
+    const float f = top == -INFINITY ? 1.f : ex2(wm[x * R + r] - top);
+    const float4 y = *reinterpret_cast<const float4*>(ring0 + x * kRing + (r * HD + d) * 4);
+    sum = make_float4(fmaf(f, y.x, sum.x), fmaf(f, y.y, sum.y), fmaf(f, y.z, sum.z), fmaf(f, y.w, sum.w));
+    l = fmaf(f, wl[x * R + r], l);
+  }
+  const float nan = __int_as_float(0x7fffffff);
+  if (last >= nan_at[d]) sum.x = nan;
+  if (last >= nan_at[d + 1]) sum.y = nan;
+  if (last >= nan_at[d + 2]) sum.z = nan;
+  if (last >= nan_at[d + 3]) sum.w = nan;
+  *reinterpret_cast<float4*>(part.sums + row_head * HD + d) = sum;
+  if (d == 0) part.stats[row_head] = make_float2(top - kOffset, l);
+}
+
 template <typename T, int HD, int NT, int kWarps, bool kPart = false>
 __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? (kWarps == 4 ? 3 : 1) : 1)
 kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, View V, const T* __restrict__ q,
@@ -135,8 +160,9 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   auto part = [&](int warp) { return reinterpret_cast<float*>(ring0 + warp * kRing); };     // [R][HD]; the block's sum ends up in part(0)
 
   if constexpr (kPart) {
-    // a pass over shared positions waits for the groups' description before it lets the sequences' pass begin, which so has it too; that
-    // one runs beside it and waits before it takes its shares
+    // a pass over shared positions waits for the groups' description before it lets the sequences' pass begin, which so has it too and runs
+    // beside it; its first block alone waits for the other pass to end (waiting blocks would keep the rest of their launch from the SMs), so
+    // that what is launched behind it finds both done
     if (part_of.prefix) chain_wait();
     chain_release();
   } else {
@@ -155,7 +181,7 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   const bool prefix = kPart && part_of.prefix;
   const int r0 = rt * R, n_rows = static_cast<int>(min(static_cast<int64_t>(seq.n) * G - r0, static_cast<int64_t>(R)));
   if (n_rows <= 0) {                                              // (the same in every block of a cluster)
-    if (kPart && !part_of.prefix) chain_wait();                   // (the launch after this one relies on the one before it)
+    if (kPart && !part_of.prefix && blockIdx.x == 0) chain_wait();
     return;
   }
   for (int i = threadIdx.x; i < HD; i += kWarps * 32) nan_at[i] = 0x7fffffff;
@@ -453,6 +479,15 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
   }
   __syncthreads();
   constexpr int kThreads = kWarps * 32, kPer = (R * HD + kThreads - 1) / kThreads;      // results of this thread: threadIdx.x + i * kThreads
+  if constexpr (kPart) {
+    // (a short loop: as straight code, an element at a time, this took 4 us of a block that has little else to do)
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n_rows * (HD / 4); i += kThreads) store_share<HD, R, kWarps, kRing>(i, ring0, wm, wl, nan_at, last_of(i / (HD / 4)),
+                                                                                                 split * part_of.row_heads + (seq.row0 + (r0 + i / (HD / 4)) / G) * H +
+                                                                                                     h * G + (r0 + i / (HD / 4)) % G, part_of);
+    if (!prefix && blockIdx.x == 0) chain_wait();
+    return;
+  }
   float bm[kPer], rm[kPer], rl[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
@@ -468,24 +503,13 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
       bm[i] = fmaf(f, part(x)[at], bm[i]);
       rl[i] = fmaf(f, wl[x * R + r], rl[i]);
     }
-    if ((prefix ? (r < n_rows ? last_of(r) : -1) : first + (r0 + r) / G) >= nan_at[d]) bm[i] = __int_as_float(0x7fffffff);
-  }
-  if (prefix) {
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int at = threadIdx.x + i * kThreads, r = at / HD;
-      if (at >= n_rows * HD) continue;
-      const int64_t row_head = split * part_of.row_heads + (seq.row0 + (r0 + r) / G) * H + h * G + (r0 + r) % G;
-      part_of.sums[row_head * HD + at % HD] = bm[i];
-      if (at % HD == 0) part_of.stats[row_head] = make_float2(rm[i] - kOffset, rl[i]);
-    }
-    return;
+    if (first + (r0 + r) / G >= nan_at[d]) bm[i] = __int_as_float(0x7fffffff);
   }
   auto store = [&](int r, int d, float sum, float ll) {
     o[(seq.row0 + (r0 + r) / G) * o_stride + (h * G + (r0 + r) % G) * static_cast<int64_t>(HD) + d] =
         narrow<T>(ll == 0.f ? sum : sum / ll);                    // nothing attended to: sum = 0
   };
-  if (nsplit == 1 && !kPart) {
+  if (nsplit == 1) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int at = threadIdx.x + i * kThreads;
@@ -493,7 +517,7 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     }
     return;
   }
-  if (!kPart && ws != nullptr) {                                  // [item][split]: R * HD sums, R maxima, R sums of weights
+  if (ws != nullptr) {                                            // [item][split]: R * HD sums, R maxima, R sums of weights
     float* mine = ws + static_cast<int64_t>(blockIdx.x) * (R * (HD + 2));
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -520,72 +544,6 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
     }
   }
   cg::cluster_group cluster = cg::this_cluster();
-  if constexpr (kPart) {
-    // this block's share of the rows, four dims per thread: the cluster's blocks in their order, then the shares of the shared positions in
-    // theirs, all of their loads under way at once
-    if (nsplit > 1) cluster.sync();
-    else __syncthreads();
-    chain_wait();
-    const int quads = n_rows * (HD / 4), lo = quads * split / nsplit, n_mine = quads * (split + 1) / nsplit - lo;
-    struct Sum {
-      float m = -INFINITY, l = 0.f;
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-      __device__ __forceinline__ void add(float m2, float l2, const float4& y) {
-        const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top, f0 = ex2(m - ref), f1 = ex2(m2 - ref);
-        x = make_float4(fmaf(f1, y.x, f0 * x.x), fmaf(f1, y.y, f0 * x.y), fmaf(f1, y.z, f0 * x.z), fmaf(f1, y.w, f0 * x.w));
-        l = fmaf(f1, l2, f0 * l);
-        m = top;
-      }
-    };
-    // where the block has more threads than such pieces, `teams` threads share one, taking every teams-th share
-    const int teams = n_mine > 0 ? min(max(kThreads / n_mine, 1), kWarps) : 1, team = teams > 1 ? static_cast<int>(threadIdx.x) / n_mine : 0;
-    Sum* others = reinterpret_cast<Sum*>(ring0 + R * HD * 4);     // (behind the block's sum, which the cluster reads)
-    static_assert((kWarps - 1) * kThreads * sizeof(Sum) + R * HD * 4 <= kWarps * kRingBytes<HD>, "");
-    for (int i0 = teams > 1 ? static_cast<int>(threadIdx.x) - team * n_mine : static_cast<int>(threadIdx.x); teams > 1 ? i0 >= 0 : i0 < n_mine;
-         i0 = teams > 1 ? -1 : i0 + kThreads) {
-      const int i = lo + i0, r = i / (HD / 4), d = i % (HD / 4) * 4;
-      const int64_t row_head = (seq.row0 + (r0 + r) / G) * H + h * G + (r0 + r) % G;
-      Sum s;
-      if (team == 0)
-        for (int x = 0; x < nsplit; ++x) {
-          const float* from = nsplit > 1 ? cluster.map_shared_rank(part(0), x) : part(0);
-          s.add((nsplit > 1 ? cluster.map_shared_rank(wm, x) : wm)[r] - kOffset, (nsplit > 1 ? cluster.map_shared_rank(wl, x) : wl)[r],
-                *reinterpret_cast<const float4*>(from + r * HD + d));
-        }
-      if (work.skip > 0 && team < teams) {
-        constexpr int kAhead = 8;
-        for (int k0 = team; k0 < part_of.shares; k0 += kAhead * teams) {
-          float2 st[kAhead];
-          float4 x[kAhead];
-#pragma unroll
-          for (int k = 0; k < kAhead; ++k) {
-            const int kk = k0 + k * teams;
-            const int64_t at = (kk < part_of.shares ? kk : k0) * part_of.row_heads + row_head;
-            st[k] = __ldcg(part_of.stats + at);
-            x[k] = __ldcg(reinterpret_cast<const float4*>(part_of.sums + at * HD + d));
-          }
-#pragma unroll
-          for (int k = 0; k < kAhead; ++k)
-            if (k0 + k * teams < part_of.shares) s.add(st[k].x, st[k].y, x[k]);
-        }
-      }
-      if (teams > 1) {
-        if (team > 0 && team < teams) others[(team - 1) * kThreads + i0] = s;
-        __syncthreads();                                          // (every thread makes one trip)
-        if (team > 0) break;
-        for (int k = 1; k < teams; ++k) {
-          const Sum& y = others[(k - 1) * kThreads + i0];
-          s.add(y.m, y.l, y.x);
-        }
-      }
-      const float inv = s.l == 0.f ? 1.f : 1.f / s.l;             // nothing attended to: sums of 0
-      struct alignas(4 * sizeof(T)) Four { T x[4]; };
-      *reinterpret_cast<Four*>(o + (seq.row0 + (r0 + r) / G) * o_stride + (h * G + (r0 + r) % G) * static_cast<int64_t>(HD) + d) =
-          Four{{narrow<T>(s.x.x * inv), narrow<T>(s.x.y * inv), narrow<T>(s.x.z * inv), narrow<T>(s.x.w * inv)}};
-    }
-    if (nsplit > 1) cluster.sync();
-    return;
-  }
   cluster.sync();
   const int from = R * HD * split / nsplit, share = R * HD * (split + 1) / nsplit - from;
   for (int i = threadIdx.x; i < share; i += kWarps * 32) {
@@ -764,21 +722,25 @@ kv8_prefix_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
       uint32_t vv[4][HD / 32];
       load_values<HD>(vv, at + (2 + a) * kStep * HD, g, t);
       uint32_t pa[NT][2];
+      bool grows = false;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float x[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          x[j] = fmaf(c[n][j], rs[n][j & 1] * ks, fe);
-          if (masked && (!have || u * kUnit + a * kStep + g + 8 * (j >> 1) > row_last[8 * n + 2 * t + (j & 1)])) x[j] = -INFINITY;
+          c[n][j] = fmaf(c[n][j], rs[n][j & 1] * ks, fe);
+          if (masked && (!have || u * kUnit + a * kStep + g + 8 * (j >> 1) > row_last[8 * n + 2 * t + (j & 1)])) c[n][j] = -INFINITY;
         }
-        float mx[2] = {fmaxf(x[0], x[2]), fmaxf(x[1], x[3])};
-        if (__any_sync(0xffffffffu, mx[0] > m[n][0] + kSlack || mx[1] > m[n][1] + kSlack)) {
+        grows = grows || fmaxf(c[n][0], c[n][2]) > m[n][0] + kSlack || fmaxf(c[n][1], c[n][3]) > m[n][1] + kSlack;
+      }
+      if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
+            float mx = fmaxf(c[n][j], c[n][j + 2]);
 #pragma unroll
-            for (int off = 4; off <= 16; off <<= 1) mx[j] = fmaxf(mx[j], __shfl_xor_sync(0xffffffffu, mx[j], off));
-            const float top = fmaxf(m[n][j], mx[j]), corr = top == -INFINITY ? 1.f : ex2(m[n][j] - top);
+            for (int off = 4; off <= 16; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+            const float top = fmaxf(m[n][j], mx), corr = top == -INFINITY ? 1.f : ex2(m[n][j] - top);
             m[n][j] = top;
             l[n][j] *= corr;
 #pragma unroll
@@ -788,13 +750,15 @@ kv8_prefix_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
             }
           }
         }
-        float y[4];
+      }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = ex2(x[j] - (m[n][j & 1] == -INFINITY ? 0.f : m[n][j & 1] - kOffset));
-        l[n][0] = fmaf(el, y[0] + y[2], l[n][0]);
-        l[n][1] = fmaf(el, y[1] + y[3], l[n][1]);
-        pa[n][0] = transpose8x8(pack_f16(y[0], y[1]));
-        pa[n][1] = transpose8x8(pack_f16(y[2], y[3]));
+      for (int n = 0; n < NT; ++n) {
+        const float r0 = m[n][0] == -INFINITY ? 0.f : m[n][0] - kOffset, r1 = m[n][1] == -INFINITY ? 0.f : m[n][1] - kOffset;
+        const float y0 = ex2(c[n][0] - r0), y1 = ex2(c[n][1] - r1), y2 = ex2(c[n][2] - r0), y3 = ex2(c[n][3] - r1);
+        l[n][0] = fmaf(el, y0 + y2, l[n][0]);
+        l[n][1] = fmaf(el, y1 + y3, l[n][1]);
+        pa[n][0] = transpose8x8(pack_f16(y0, y1));
+        pa[n][1] = transpose8x8(pack_f16(y2, y3));
       }
       if (masked) {                                               // (0 * NaN: see the kernel above)
 #pragma unroll
@@ -855,27 +819,10 @@ kv8_prefix_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_c
     }
   }
   __syncthreads();
+#pragma unroll 1
   for (int i = threadIdx.x; i < n_rows * (HD / 4); i += kThreads) {
-    const int r = i / (HD / 4), d = i % (HD / 4) * 4;
-    float top = -INFINITY, ll = 0.f;
-#pragma unroll
-    for (int x = 0; x < kWarps; ++x) top = fmaxf(top, wm[x * R + r]);
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int x = 0; x < kWarps; ++x) {
-      const float f = top == -INFINITY ? 1.f : ex2(wm[x * R + r] - top);
-      const float4 y = *reinterpret_cast<const float4*>(ring0 + x * kRing + (r * HD + d) * 4);
-      sum = make_float4(fmaf(f, y.x, sum.x), fmaf(f, y.y, sum.y), fmaf(f, y.z, sum.z), fmaf(f, y.w, sum.w));
-      ll = fmaf(f, wl[x * R + r], ll);
-    }
-    const float nan = __int_as_float(0x7fffffff);
-    if (row_last[r] >= nan_at[d]) sum.x = nan;
-    if (row_last[r] >= nan_at[d + 1]) sum.y = nan;
-    if (row_last[r] >= nan_at[d + 2]) sum.z = nan;
-    if (row_last[r] >= nan_at[d + 3]) sum.w = nan;
-    const int64_t row_head = split * part_of.row_heads + (seq.row0 + r / G) * H + h * G + r % G;
-    *reinterpret_cast<float4*>(part_of.sums + row_head * HD + d) = sum;
-    if (d == 0) part_of.stats[row_head] = make_float2(top - kOffset, ll);
+    const int r = i / (HD / 4);
+    store_share<HD, R, kWarps, kRing>(i, ring0, wm, wl, nan_at, row_last[r], split * part_of.row_heads + (seq.row0 + r / G) * H + h * G + r % G, part_of);
   }
 }
 
@@ -974,7 +921,7 @@ szo_status launch_rows(const View& V, const Rows& A, int nsplit, float* ws, cuda
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   int attrs = 0;
-  if (nsplit > 1 && ws == nullptr && !(kPart && part.prefix)) {
+  if (nsplit > 1 && ws == nullptr && !kPart) {
     attr[attrs].id = cudaLaunchAttributeClusterDimension;
     attr[attrs].val.clusterDim.x = nsplit;
     attr[attrs].val.clusterDim.y = attr[attrs].val.clusterDim.z = 1;

@@ -30,11 +30,10 @@ struct Part {
   float2* stats;
   int64_t row_heads;           // of a share
   int prefix;                  // 1: the rows of a group over the shared positions; 0: a sequence's rows over the rest
-  int shares;                  // of the shared positions; a sequence's pass of the kernel for few rows finishes its rows with them
   int items;                   // groups or sequences
   int max_rows;                // the most rows of one
 };
-// (few rows: a sequence's pass takes its own number of shares, joined in clusters; chained launches, see kv8_prefix.cu)
+// (chained launches, see kv8_prefix.cu)
 template <typename T, int HD> szo_status launch_part(const View& V, const Rows& A, const Part& part, int nsplit, cudaStream_t st);
 template <typename T, int HD> szo_status launch_part_tc(const View& V, const Rows& A, const Part& part, int nsplit, cudaStream_t st);
 

@@ -202,7 +202,7 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
   const unsigned r0 = static_cast<unsigned>(rt) * 2 * kTile;                     // (rows and heads of a call stay below 2^31)
   const int64_t left = static_cast<int64_t>(seq.n) * G - r0;
   if (left <= 0) {
-    if (kPart && !prefix) chain_wait();
+    if (kPart && !prefix && blockIdx.x == 0) chain_wait();
     return;
   }
   const int n_rows = static_cast<int>(left < 2 * kTile ? left : 2 * kTile);
@@ -273,34 +273,49 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_addr = tmem + lanes + i * kTile + half * (kTile / 2), o_addr = tmem + lanes + 2 * kTile + i * kTile + half * (HD / 2);
     const int rpos = last_of(r);
-    // The queries: a warp brings 16 rows, a row's dims over kQLanes lanes, all loads before the first use
+    // The queries: a warp brings 16 rows, a row's dims over kQLanes lanes
     {
       constexpr int kQLanes = HD / 8, kQRows = 32 / kQLanes, kPasses = 16 / kQRows;
       const int row0 = (warp & 3) * 32 + half * 16 + lane / kQLanes, c = lane % kQLanes;
-      Vec<T> x[kPasses];
-#pragma unroll
-      for (int k = 0; k < kPasses; ++k) {
-        const int qr = i * kTile + row0 + k * kQRows;
-        const unsigned at = r0 + qr;
-        x[k] = {};
-        if (qr < n_rows)
-          x[k] = *reinterpret_cast<const Vec<T>*>(q + (seq.row0 + at / static_cast<unsigned>(G)) * q_stride +
-                                                  (h * G + at % static_cast<unsigned>(G)) * static_cast<int64_t>(HD) + 8 * c);
+      // (as they are into their places, all on their way at once, and changed there: straight code for all passes in registers waits
+      // for instructions 3 us, loads a pass ahead as long for the loads)
+      {
+        const unsigned g = static_cast<unsigned>(G), at = r0 + i * kTile + row0;
+        unsigned tok = at / g, of = at % g;                       // the row's token and head; kQRows rows further in each pass
+#pragma unroll 2
+        for (int k = 0; k < kPasses; ++k) {
+          const bool there = i * kTile + row0 + k * kQRows < n_rows;
+          const T* from = q + (seq.row0 + (there ? tok : r0 / g)) * q_stride + (h * G + (there ? of : 0)) * static_cast<int64_t>(HD) + 8 * c;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tile_chunk(q_tile(i), row0 + k * kQRows, c)),
+                       "l"(__cvta_generic_to_global(from)), "r"(there ? 16 : 0)
+                       : "memory");
+          for (of += kQRows; of >= g; of -= g) ++tok;
+        }
       }
-#pragma unroll
+      asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 1
       for (int k = 0; k < kPasses; ++k) {
-        int top = 0;                                              // the largest magnitude's bits: NaN above infinity above the rest
+        const int row = row0 + k * kQRows;
+        const uint32_t place = tile_chunk(q_tile(i), row, c);
+        Vec<T> x;
+        {
+          uint32_t w[4];
+          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(place) : "memory");
+          *reinterpret_cast<uint4*>(&x) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        // the largest magnitude's bits, of either type in their order as whole numbers: NaN above infinity above the rest
+        const uint32_t* pairs = reinterpret_cast<const uint32_t*>(&x);
+        uint32_t both = __vmaxu2(__vmaxu2(pairs[0] & 0x7fff7fffu, pairs[1] & 0x7fff7fffu), __vmaxu2(pairs[2] & 0x7fff7fffu, pairs[3] & 0x7fff7fffu));
 #pragma unroll
-        for (int u = 0; u < 8; ++u) top = max(top, __float_as_int(widen<T>(x[k].x[u])) & 0x7fffffff);
-#pragma unroll
-        for (int s = 1; s < kQLanes; s *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+        for (int s = 1; s < kQLanes; s *= 2) both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, s));
+        const uint16_t bits = static_cast<uint16_t>(max(both & 0xffffu, both >> 16));
+        const int top = __float_as_int(widen<T>(*reinterpret_cast<const T*>(&bits)));
         const int e = min(max((top >> 23) - 127, -126), 126);
         const float inv = scale < 0.f ? -exp2_int(-e) : exp2_int(-e);
         uint32_t p[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) p[u] = pack_f16(widen<T>(x[k].x[2 * u]) * inv, widen<T>(x[k].x[2 * u + 1]) * inv);
-        const int row = row0 + k * kQRows;
-        sts16(tile_chunk(q_tile(i), row, c), p[0], p[1], p[2], p[3]);
+        for (int u = 0; u < 4; ++u) p[u] = pack_f16(widen<T>(x.x[2 * u]) * inv, widen<T>(x.x[2 * u + 1]) * inv);
+        sts16(place, p[0], p[1], p[2], p[3]);
         if (c == 0) {
           peaks[1][i][0][row] = exp2_int(e) * (fabsf(scale) * 1.4426950408889634f);
           peaks[1][i][1][row] = top < 0x7f800000 ? 0.f : __int_as_float(0x7fffffff);      // a row that holds NaN or an infinity is NaN
@@ -646,7 +661,7 @@ kv8_attention_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_
     tc::tc_fence_after();
     tmem_dealloc(tmem, kTmemCols);
   }
-  if (kPart && !prefix) chain_wait();                             // (the join behind this launch relies on the one before it too)
+  if (kPart && !prefix && blockIdx.x == 0) chain_wait();
 }
 
 }  // namespace

@@ -74,34 +74,57 @@ __global__ void __launch_bounds__(256) kv8_groups_kernel(View V, Prefix P, int4*
   }
 }
 
-// Joins the shares of the rows of all sequences, HD / 4 threads per row and head: grid (token of a sequence, heads)
-constexpr int kJoinThreads = 256;
+// Joins the shares of the rows of all sequences: HD / 4 threads per row and head, four teams of them, every team taking every fourth share;
+// teams joined in order.  Grid (token of a sequence, heads)
+constexpr int kJoinThreads = 256, kTeams = 4;
 template <typename T, int HD>
 __global__ void __launch_bounds__(kJoinThreads) kv8_shares_kernel(View V, Part part, int n_prefix, int n_own, T* __restrict__ o, int64_t o_stride, int H) {
-  constexpr int kLanes = HD / 4;
-  chain_wait();
+  constexpr int kLanes = HD / 4, kHeads = kJoinThreads / kLanes / kTeams, kAhead = 4;
+  struct Sum {
+    float4 x;
+    float m, l;
+  };
+  __shared__ Sum teams[kTeams][kHeads][kLanes];
   const int b = blockIdx.x / V.max_new, i = blockIdx.x % V.max_new;
-  const Seq s = load_seq(V, b);
-  const int head = blockIdx.y * (kJoinThreads / kLanes) + threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
-  if (i >= s.n || head >= H) return;
-  const int from = part.shared[b] > 0 ? 0 : n_prefix, to = n_prefix + n_own;
+  const Seq s = load_seq(V, b);                                   // (before the wait: see the passes)
+  const int lane = threadIdx.x % kLanes, hd = threadIdx.x / kLanes % kHeads, team = threadIdx.x / kLanes / kHeads;
+  const int head = blockIdx.y * kHeads + hd;
+  const bool there = i < s.n && head < H;
+  const int from = there && __ldcg(part.shared + b) > 0 ? 0 : n_prefix, to = there ? n_prefix + n_own : 0;
+  chain_wait();
   const int64_t at = (s.row0 + i) * H + head;
-  float m = -INFINITY, l = 0.f;
-  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-  for (int k = from; k < to; ++k) m = fmaxf(m, part.stats[k * part.row_heads + at].x);
-#pragma unroll 4
-  for (int k = from; k < to; ++k) {
-    const float2 st = part.stats[k * part.row_heads + at];
-    const float4 x = *reinterpret_cast<const float4*>(part.sums + (k * part.row_heads + at) * HD + 4 * lane);
-    const float f = m == -INFINITY ? 1.f : ex2(st.x - m);
-    sum = make_float4(fmaf(f, x.x, sum.x), fmaf(f, x.y, sum.y), fmaf(f, x.z, sum.z), fmaf(f, x.w, sum.w));
-    l = fmaf(f, st.y, l);
+  Sum a{make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f};
+  auto add = [&](float m, float l, const float4& x) {
+    const float top = fmaxf(a.m, m), ref = top == -INFINITY ? 0.f : top, f0 = ex2(a.m - ref), f1 = ex2(m - ref);
+    a.x = make_float4(fmaf(f1, x.x, f0 * a.x.x), fmaf(f1, x.y, f0 * a.x.y), fmaf(f1, x.z, f0 * a.x.z), fmaf(f1, x.w, f0 * a.x.w));
+    a.l = fmaf(f1, l, f0 * a.l);
+    a.m = top;
+  };
+  for (int k0 = from + team; k0 < to; k0 += kAhead * kTeams) {
+    float2 st[kAhead];
+    float4 x[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int64_t p = (k0 + k * kTeams < to ? k0 + k * kTeams : k0) * part.row_heads + at;
+      st[k] = __ldcg(part.stats + p);
+      x[k] = __ldcg(reinterpret_cast<const float4*>(part.sums + p * HD + 4 * lane));
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (k0 + k * kTeams < to) add(st[k].x, st[k].y, x[k]);
   }
-  const float inv = l == 0.f ? 1.f : 1.f / l;                     // nothing attended to: sums of 0
+  teams[team][hd][lane] = a;
+  __syncthreads();
+  if (team != 0 || !there) return;
+#pragma unroll
+  for (int k = 1; k < kTeams; ++k) {
+    const Sum& y = teams[k][hd][lane];
+    add(y.m, y.l, y.x);
+  }
+  const float inv = a.l == 0.f ? 1.f : 1.f / a.l;                 // nothing attended to: sums of 0
   struct alignas(4 * sizeof(T)) Four { T x[4]; };
   *reinterpret_cast<Four*>(o + (s.row0 + i) * o_stride + static_cast<int64_t>(head) * HD + 4 * lane) =
-      Four{{narrow<T>(sum.x * inv), narrow<T>(sum.y * inv), narrow<T>(sum.z * inv), narrow<T>(sum.w * inv)}};
+      Four{{narrow<T>(a.x.x * inv), narrow<T>(a.x.y * inv), narrow<T>(a.x.z * inv), narrow<T>(a.x.w * inv)}};
 }
 
 struct Pass {
@@ -115,20 +138,15 @@ struct SharePlan {
   int64_t row_heads;
 };
 // How a pass's positions are cut.  The lengths are on the device, so the rule goes by the number of items (owner, head, row
-// tile): few rows: as many shares as fill the SMs twice (8 sequences of 4 rows on 65536 shared positions, 8 heads: 37 shares 65 us, 30 72, 48
-// 88), many: three quarters of them once, since the sequences' pass runs beside (64 sequences on 8192: 14 shares 43.5 us, 10 46.5,
-// 18 46); of 2 steps of 128 (units of 32 per warp) at least of what the page table could hold.  A sequence's pass for few rows
-// joins its shares in a cluster: a power of two up to 8.
+// tile).  Shared positions, few rows: as many shares as fill the SMs twice (8 sequences of 4 rows on 65536 positions, 8 heads: 37 shares
+// 62 us, 30 68), many: two thirds of the SMs once, since the sequences' pass runs beside (64 sequences on 8192: 11 or 12 shares 36 us, 9
+// 40, 14 39, 18 43).  A sequence's own: the SMs once.  Of 2 steps of 128 (units of 32 per warp) at least of what the page table could hold.
 Pass make_pass(const View& V, int64_t max_rows, int64_t owners, int H, bool wide_type, bool prefix) {
   const int64_t rows = max_rows * (H / V.hkv), places = static_cast<int64_t>(V.max_pages) << V.page_shift;
   Pass p{!wide_type && rows > 32, static_cast<int>(max_rows), 1};
   const int64_t tile = p.many ? 256 : rows <= 8 ? 8 : prefix && !wide_type && rows > 16 ? kPrefixRows : 16, items = owners * V.hkv * ceil_div(rows, tile);
-  const int64_t room = p.many ? (prefix ? 112 : 148) : 296, least = p.many ? 256 : 128;
-  if (prefix || p.many) {
-    while (p.shares < 64 && items * (p.shares + 1) <= room && places >= least * (p.shares + 1)) ++p.shares;
-  } else {
-    while (p.shares < 8 && items * p.shares * 2 <= room && places >= least * 2 * p.shares) p.shares *= 2;
-  }
+  const int64_t room = prefix ? (p.many ? 96 : 296) : 148, least = p.many ? 256 : 128;
+  while (p.shares < 64 && items * (p.shares + 1) <= room && places >= least * (p.shares + 1)) ++p.shares;
   return p;
 }
 // Up to this much to read, if every sequence reads all that its table could hold, the sequences' own attention is as fast: it is one
@@ -152,7 +170,7 @@ SharePlan share_plan(const View& V, const Prefix& P, int H, int hd, bool wide_ty
     p.prefix = make_pass(V, most < V.rows ? most : V.rows, P.n_groups, H, wide_type, true);
     p.own = make_pass(V, V.max_new, V.batch, H, wide_type, false);
     p.row_heads = V.rows * H;
-    const size_t n = static_cast<size_t>(p.prefix.shares + (p.own.many ? p.own.shares : 0)) * p.row_heads;
+    const size_t n = static_cast<size_t>(p.prefix.shares + p.own.shares) * p.row_heads;
     p.sums = take(n * hd * sizeof(float));
     p.stats = take(n * sizeof(float2));
   }
@@ -176,12 +194,10 @@ szo_status launch_shares(const View& V, const Prefix& P, const Rows& A, const Sh
   Part own = base;
   own.items = V.batch;
   own.max_rows = V.max_new;
-  own.shares = p.prefix.shares;
-  if (!p.own.many) return run_pass<T, HD>(V, A, own, p.own, st);
   own.sums += p.prefix.shares * base.row_heads * HD;
   own.stats += p.prefix.shares * base.row_heads;
   SZO_TRY((run_pass<T, HD>(V, A, own, p.own, st)));
-  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(V.batch) * V.max_new), static_cast<unsigned>(ceil_div(A.H, kJoinThreads / (HD / 4))));
+  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(V.batch) * V.max_new), static_cast<unsigned>(ceil_div(A.H, kJoinThreads / (HD / 4) / kTeams)));
   SZO_CHECK_CUDA(launch_maybe_chained(kv8_shares_kernel<T, HD>, grid, dim3(kJoinThreads), 0, st, true, V, base, p.prefix.shares, p.own.shares,
                                       static_cast<T*>(A.o), A.o_stride, A.H));
   count_launch();
