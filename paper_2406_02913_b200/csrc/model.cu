@@ -984,6 +984,7 @@ struct szo_model {
   int32_t *kv8_table = nullptr, *kv8_len = nullptr;    // [max_batch][kv8_pages]; [max_batch], set by every call
   void* kv8_ws = nullptr;
   size_t kv8_ws_bytes = 0;
+  std::vector<bool> kv8_ws_fits;                 // by the number of sequences that share: kv8_ws is large enough
   int kv8_page = 0, kv8_pages = 0;
   // sequences 0 .. kv8_sharers - 1 share their first kv8_shared positions (szo_model_decode_share); on the device: that number, and the
   // one group of sequences, 0 and its end in the current call
@@ -2013,6 +2014,9 @@ szo_status szo_model_enable_decode(szo_model_t* m, void* stream) {
   return enable_decode_common(m, static_cast<cudaStream_t>(stream));
 }
 
+// The most that szo_attention_kv8 asks for: one partial tile of 256 rows per SM
+static size_t kv8_attention_ws(int head_dim) { return static_cast<size_t>(148) * 256 * (head_dim + 2) * sizeof(float); }
+
 szo_status szo_model_enable_decode_kv8(szo_model_t* m, int32_t page_tokens, void* stream) {
   SZO_REQUIRE(m != nullptr, SZO_ERR_INVALID_ARG, "model is NULL");
   SZO_REQUIRE(page_tokens == 16 || page_tokens == 32 || page_tokens == 64 || page_tokens == 128, SZO_ERR_UNSUPPORTED,
@@ -2029,8 +2033,7 @@ szo_status szo_model_enable_decode_kv8(szo_model_t* m, int32_t page_tokens, void
   const size_t bytes = static_cast<size_t>(c.n_layers) * 2 * pages * page_tokens * c.n_kv_heads * hd;
   m->kv8_pages = static_cast<int>(per_seq);
   const size_t scales = static_cast<size_t>(c.n_layers) * m->kv8_scale_floats() * sizeof(float);
-  // the most that szo_attention_kv8 asks for at these shapes: one partial tile of 256 rows per SM
-  const size_t ws = static_cast<size_t>(148) * 256 * (hd + 2) * sizeof(float);
+  const size_t ws = kv8_attention_ws(hd);
   uint8_t* codes = nullptr;
   SZO_TRY(dev_alloc(m, &codes, bytes));
   SZO_TRY(dev_alloc(m, &m->kv8_scales, scales));
@@ -2077,9 +2080,11 @@ szo_status szo_model_decode_share(szo_model_t* m, int32_t B, int32_t n, void* st
   const szo_model_config& c = m->cfg;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int hd = c.d_model / c.n_heads, G = c.n_heads / c.n_kv_heads, whole = n / m->kv8_page;
-  if (B > 1 && whole > 0) {
-    // the most that szo_attention_kv8_prefix asks for: any number of sequences, and of new tokens up to those that share nothing
-    size_t need = m->kv8_ws_bytes;
+  if (m->kv8_ws_fits.empty()) m->kv8_ws_fits.assign(static_cast<size_t>(c.max_batch) + 1, false);
+  if (B > 1 && whole > 0 && !m->kv8_ws_fits[B]) {
+    // the most that szo_attention_kv8_prefix asks for: any number of sequences, and of new tokens up to those that share nothing; these ask
+    // for what szo_attention_kv8 does and the groups' descriptions, a few words per sequence and row
+    size_t need = kv8_attention_ws(hd) + 4 * 256 + (c.max_batch + m->Mmax) * sizeof(int32_t);
     szo_kv8_cache cache{m->kv8_codes, m->kv8_codes, m->kv8_scales, static_cast<int64_t>(c.max_batch) * m->kv8_pages, m->kv8_page, c.n_kv_heads, hd};
     const szo_kv8_prefix prefix{m->kv8_group, m->kv8_group + 4, 1, B};
     for (int b = 1; b <= c.max_batch; ++b)
@@ -2092,6 +2097,7 @@ szo_status szo_model_decode_share(szo_model_t* m, int32_t B, int32_t n, void* st
       SZO_TRY(dev_alloc(m, reinterpret_cast<char**>(&m->kv8_ws), need));
       m->kv8_ws_bytes = need;
     }
+    m->kv8_ws_fits[B] = true;
   }
   const int64_t pages = static_cast<int64_t>(c.max_batch) * m->kv8_pages;
   shared_table_kernel<<<blocks_for(pages, 256), 256, 0, st>>>(m->kv8_table, pages, m->kv8_pages, B, whole);

@@ -88,6 +88,29 @@ def test_sharing_ends_and_protects_its_pages(B):
     m.close()
 
 
+def test_long_chunks_after_sharing(B, monkeypatch):
+    """Chunks of so many tokens that sharing gains nothing, at a length whose attention takes the most workspace."""
+    from paper_2406_02913_b200 import workloads as wl
+    monkeypatch.setitem(wl.MODEL_SHAPES, "tiny_one_kv_head", dict(wl.MODEL_SHAPES["tiny_gqa"], n_kv_heads=1, n_layers=1))
+    fx = DecoderFixture("tiny_one_kv_head", seed=8, mask="random", B=2, S=64)
+    toks = torch.from_numpy(wl.token_batch(512, 2, 4096, 8, wl.PURPOSE_MASK_BATCH, 0)).cuda()
+    got = []
+    for shared in (True, False):
+        m = make(B, fx, max_batch=2, max_seq=4096, loss_kind=B.LOSS_CLS2)
+        m.enable_decode(kv8_page_tokens=32)
+        prompt = toks[:1, :32].contiguous()
+        if shared:
+            m.decode_step(prompt, 0)
+            m.decode_share(2, 32)
+        else:
+            m.decode_step(prompt.expand(2, 32).contiguous(), 0)
+        got.append([m.decode_step(toks[:, 32:32 + n].contiguous(), 32).clone() for n in (2362, 300)])
+        assert B.device_status() == 0
+        m.close()
+    for x, y in zip(*got):
+        assert (x - y).abs().max() <= 4e-2 * y.abs().max()
+
+
 @pytest.mark.parametrize("name", ["tiny", "tiny_gqa", "tiny_opt", "tiny_lut", "small_gqa"])
 @pytest.mark.parametrize("kind", [0, 1])
 def test_token_losses_match_the_oracle_and_the_stored_logits(B, name, kind):
