@@ -12,6 +12,10 @@
 // Roles of a CTA's 12 warps: 0 brings the operands (both CTAs' copies arrive on the leader's barriers), 1 issues the products
 // (leader only), 2 has the TMEM, 4-11 the epilogue: two warps per 32 rows, 128 columns each, a thread per row.
 // Tiles are written through 4 KB of shared memory per warp by TMA, which leaves out what lies outside.
+// What bounds it: many rows, the tensor cores (their pipe 94 % busy, issue slots 10 %; 4096 rows of 32000 x 4096, bf16: loss 652 us, 1.65
+// PFLOP/s, gradient down to h 1.40 ms; 128 x 256 tiles of single CTAs read each operand tile twice as often); at most 128 rows, the reads of W
+// (8 rows of 32000 x 4096: 262 MB in 49.5 us, 5.3 TB/s; with the rows as rows of D, 71 us); small matrices, the chain of one tile (256 rows of
+// 1024 x 256, 10 us: setup 0.7, first operands 1.5, products 1.4, epilogue 3, end 0.7, join).
 #include <algorithm>
 #include <mutex>
 

@@ -562,7 +562,7 @@ kv8_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_con
 }
 
 // The same for up to 32 rows of a group over its shared positions, 16-bit types: every code is turned into fp16 once for all of them
-// (two tiles of 16 rows do so twice: 8 sequences of 4 rows on 65536 shared positions, 8 heads of 128, 69 us, here 65).  What
+// (two tiles of 16 rows do so twice: 8 sequences of 4 rows on 65536 shared positions, 8 heads of 128, 65 us, here 60).  What
 // bounds it is the latency of the chain in each of its 8 warps per SM (issue 35 %): 254 registers leave no room for more.  The queries' fragments do not fit the registers beside 32 rows of sums: they stay in shared
 // memory, and 16 positions are taken at a time.
 template <typename T, int HD>
@@ -1017,9 +1017,6 @@ template <typename T, int HD> szo_status launch_part(const View& V, const Rows& 
   const int64_t rows = static_cast<int64_t>(part.max_rows) * (A.H / V.hkv);
   if constexpr (sizeof(T) == 2)
     if (part.prefix && rows > 16 && rows <= kPrefixRows) return launch_prefix_rows<T, HD>(V, A, nsplit, st, part);
-  // (sequences of more items than blocks of 4 warps fit on the SMs at once: blocks of 2.  64 sequences of up to 512 positions of their own,
-  // 8 heads: 46 us, with blocks of 4 warps 48)
-  if (!part.prefix && rows <= 8 && static_cast<int64_t>(part.items) * V.hkv > 148 * 3) return launch_rows<T, HD, 1, 2, true>(V, A, nsplit, nullptr, st, part);
   return rows <= 8 ? launch_rows<T, HD, 1, 4, true>(V, A, nsplit, nullptr, st, part) : launch_rows<T, HD, 2, 4, true>(V, A, nsplit, nullptr, st, part);
 }
 #define SZO_KV8_PART(T, HD) template szo_status launch_part<T, HD>(const View&, const Rows&, const Part&, int, cudaStream_t)

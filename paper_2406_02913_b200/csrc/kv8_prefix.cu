@@ -4,8 +4,13 @@
 // shares, where the rows of all the group's sequences are taken together (so a shared code is read once for 8 to 256 rows of several
 // sequences, and prompts of a few rows each fill tensor-core tiles), and the rest of its sequence's positions.  Both are passes
 // of the attention kernels of kv8_attention.cu and kv8_attention_tc.cu that leave sums, maxima and sums of weights unfinished,
-// each cut into shares of the positions that fill the SMs.  Where a sequence has few rows its pass runs beside the groups' one, waits for
-// its end and finishes the rows, shares in their order; where it has many, a last kernel does.
+// each cut into shares of the positions that fill the SMs: fp32 sums of weights times codes with their (maximum, sum of weights).  The
+// sequences' pass starts once the groups' one runs and waits for nothing of it, but for one block whose end orders the two; a last kernel
+// joins a row's shares in their order.
+// What bounds it: bytes of codes (shared ones once per group, at 6.4 TB/s) plus, with one step of a conversation at a time, a fixed cost of
+// about 20 us: three dependent launches, the first trip to pages through the table, writing and joining the shares.  Measured (bf16, 32 heads
+// over 8 of 128, one new token each, in a replayed graph): 64 sequences on one prompt of 8192 with up to 512 positions of their own 36 us
+// (every sequence by itself, as szo_attention_kv8 reads it, 136); 8 sequences on one of 65536 60 us (136).
 #include <cmath>
 
 #include "kv8_prefix.cuh"
@@ -137,16 +142,35 @@ struct SharePlan {
   size_t groups, shared, pos, sums, stats, total;
   int64_t row_heads;
 };
-// How a pass's positions are cut.  The lengths are on the device, so the rule goes by the number of items (owner, head, row
-// tile).  Shared positions, few rows: as many shares as fill the SMs twice (8 sequences of 4 rows on 65536 positions, 8 heads: 37 shares
-// 62 us, 30 68), many: two thirds of the SMs once, since the sequences' pass runs beside (64 sequences on 8192: 11 or 12 shares 36 us, 9
-// 40, 14 39, 18 43).  A sequence's own: the SMs once.  Of 2 steps of 128 (units of 32 per warp) at least of what the page table could hold.
+// How a pass's positions are cut.  The lengths are on the device, so the rules go by the number of items (owner, head, row tile) and by what
+// the page table could hold.
+// Shared positions: the cost of n shares, in steps of 128 positions (many rows: 2.4 us of an SM), is that of a share where all of them
+// fit the SMs at once (many rows a block per SM, few two), or else of the rounds (and a third of one for the end) of shares with about 4 steps of
+// setup and epilogue; and a little for every share, which is written and joined and takes an SM from the sequences' pass.  Measured, 8
+// heads of 128 (groups x sequences on positions: us by shares), many rows: 1 x 64 on 8192: 9 41, 11 36, 12 38, 18 43; 1 x 64 on 16384: 10 54,
+// 16 45; 3 x 16 of 4 rows on 8192: 3 76, 5 56; 8 x 16 on 8192: 1 149, 2 87, 3 103; 16 x 16 on 4096: 1 94, 2 105.  Few: 1 x 8 on 65536: 30 68,
+// 37 62; 10 x 4 on 8192: 1 76, 2 53, 3 43, 4 52; 20 x 4 of 2 rows on 4096: 1 101, 2 94, 3 80, 4 89; 40 x 4 on 2048: 1 57, 2 62.
+// A sequence's own: the SMs once, but up to 4 shares where the kernel for few rows holds that many blocks on the SMs (16 sequences of 4096
+// positions of their own: 1 share 40 us, 2 31, 4 29; 32 of 2048: 1 39, 2 35, 3 37; 64 of 512 on 8192: 1 36, 2 40).
 Pass make_pass(const View& V, int64_t max_rows, int64_t owners, int H, bool wide_type, bool prefix) {
+  constexpr int kSms = 148, kMost = 64;
   const int64_t rows = max_rows * (H / V.hkv), places = static_cast<int64_t>(V.max_pages) << V.page_shift;
   Pass p{!wide_type && rows > 32, static_cast<int>(max_rows), 1};
   const int64_t tile = p.many ? 256 : rows <= 8 ? 8 : prefix && !wide_type && rows > 16 ? kPrefixRows : 16, items = owners * V.hkv * ceil_div(rows, tile);
-  const int64_t room = prefix ? (p.many ? 96 : 296) : 148, least = p.many ? 256 : 128;
-  while (p.shares < 64 && items * (p.shares + 1) <= room && places >= least * (p.shares + 1)) ++p.shares;
+  const int64_t least = p.many ? 256 : 128;                       // (2 steps of 128 at least, or units of 32 for each of 4 warps)
+  double best = 1e30;
+  for (int n = 1; n <= kMost && (n == 1 || places >= least * n); ++n) {
+    if (prefix) {
+      const double steps = static_cast<double>(places) / 128 / n, rounds = static_cast<double>(items) * n / (p.many ? kSms : 2 * kSms);
+      const double cost = (rounds <= 1 ? steps : (rounds + 0.3) * (steps + 4)) + (p.many ? 0.07 : 0.01) * static_cast<double>(items) * n;
+      if (cost < best) {
+        best = cost;
+        p.shares = n;
+      }
+    } else if (items * n <= kSms || (!p.many && n <= 4 && items * n <= 512)) {
+      p.shares = n;
+    }
+  }
   return p;
 }
 // Up to this much to read, if every sequence reads all that its table could hold, the sequences' own attention is as fast: it is one
