@@ -145,10 +145,11 @@ struct SharePlan {
 // How a pass's positions are cut.  The lengths are on the device, so the rules go by the number of items (owner, head, row tile) and by what
 // the page table could hold.
 // Shared positions: the cost of n shares, in steps of 128 positions (many rows: 2.4 us of an SM), is that of a share where all of them
-// fit the SMs at once (many rows a block per SM, few two), or else of the rounds (and a third of one for the end) of shares with about 4 steps of
-// setup and epilogue; and a little for every share, which is written and joined and takes an SM from the sequences' pass.  Measured, 8
+// fit the SMs at once (many rows a block per SM, few two), or else of the rounds, between whole ones (equal lengths) and parts, of shares with
+// about 4 steps of setup and epilogue; and a little for every share, which is written and joined and takes an SM from the sequences' pass.  Measured, 8
 // heads of 128 (groups x sequences on positions: us by shares), many rows: 1 x 64 on 8192: 9 41, 11 36, 12 38, 18 43; 1 x 64 on 16384: 10 54,
-// 16 45; 3 x 16 of 4 rows on 8192: 3 76, 5 56; 8 x 16 on 8192: 1 149, 2 87, 3 103; 16 x 16 on 4096: 1 94, 2 105.  Few: 1 x 8 on 65536: 30 68,
+// 16 45; 3 x 16 of 4 rows on 8192: 3 76, 5 56; 8 x 16 on 8192: 1 149, 2 87, 3 103; 16 x 16 on 4096: 1 94,
+// 2 105; 10 x 6 of 2 rows on 8192: 1 148, 2 129, 3 107; 20 x 8 of 2 rows on 4096: 1 138, 2 132, 3 135.  Few: 1 x 8 on 65536: 30 68,
 // 37 62; 10 x 4 on 8192: 1 76, 2 53, 3 43, 4 52; 20 x 4 of 2 rows on 4096: 1 101, 2 94, 3 80, 4 89; 40 x 4 on 2048: 1 57, 2 62.
 // A sequence's own: the SMs once, but up to 4 shares where the kernel for few rows holds that many blocks on the SMs (16 sequences of 4096
 // positions of their own: 1 share 40 us, 2 31, 4 29; 32 of 2048: 1 39, 2 35, 3 37; 64 of 512 on 8192: 1 36, 2 40).
@@ -162,7 +163,8 @@ Pass make_pass(const View& V, int64_t max_rows, int64_t owners, int H, bool wide
   for (int n = 1; n <= kMost && (n == 1 || places >= least * n); ++n) {
     if (prefix) {
       const double steps = static_cast<double>(places) / 128 / n, rounds = static_cast<double>(items) * n / (p.many ? kSms : 2 * kSms);
-      const double cost = (rounds <= 1 ? steps : (rounds + 0.3) * (steps + 4)) + (p.many ? 0.07 : 0.01) * static_cast<double>(items) * n;
+      const double time = rounds <= 1 ? steps : (0.5 * (std::ceil(rounds) + rounds) + 0.15) * (steps + 4);
+      const double cost = time + (!p.many ? 0.01 : rounds <= 1 ? 0.07 : 0.03) * static_cast<double>(items) * n;
       if (cost < best) {
         best = cost;
         p.shares = n;
@@ -176,6 +178,12 @@ Pass make_pass(const View& V, int64_t max_rows, int64_t owners, int H, bool wide
 // Up to this much to read, if every sequence reads all that its table could hold, the sequences' own attention is as fast: it is one
 // launch, and shared pages come from L2
 constexpr int64_t kDirectBytes = int64_t(96) << 20;
+// What a block's time per position is for `rows` rows of a key/value head (1: 8 rows, 26 ps with all SMs busy), in the kernel that takes them
+double row_units(int64_t rows, bool wide_type, bool prefix) {
+  if (rows <= 8) return 1.0;
+  if (!wide_type && rows > 32) return 4.9 * static_cast<double>(ceil_div(rows, 256));
+  return !wide_type && prefix && rows > 16 ? 3.4 : 1.6 * static_cast<double>(ceil_div(rows, 16));
+}
 SharePlan share_plan(const View& V, const Prefix& P, int H, int hd, bool wide_type) {
   SharePlan p = {};
   size_t at = 0;
@@ -189,6 +197,13 @@ SharePlan share_plan(const View& V, const Prefix& P, int H, int hd, bool wide_ty
   p.pos = take(static_cast<size_t>(V.rows) * sizeof(int32_t));
   p.direct = P.n_groups == 0 || P.max_seqs == 0 || static_cast<int64_t>(V.max_new) * (H / V.hkv) >= 256 ||
              (static_cast<int64_t>(V.batch) * V.max_pages << V.page_shift) * V.hkv * hd * 2 <= kDirectBytes;
+  // Where the prompts fill the SMs, blocks that read the same pages run close together and find them in L2: then rows taken together have to be
+  // cheaper than apart (us together / apart, 8 heads: 40 prompts x 4 sequences x 2 tokens on 2048 97 / 71, 20 x 4 x 2 on 4096 81 / 68, 30 x 2 x 4 on
+  // 8192 187 / 163; 20 x 4 x 1 on 4096 54 / 67; with fewer prompts 4 x 4 x 2 on 16384 59 / 68)
+  if (static_cast<int64_t>(P.n_groups) * V.hkv >= 148) {
+    const int64_t own = static_cast<int64_t>(V.max_new) * (H / V.hkv);
+    p.direct = p.direct || row_units(P.max_seqs * own, wide_type, true) >= 0.75 * P.max_seqs * row_units(own, wide_type, false);
+  }
   if (!p.direct) {
     const int64_t most = static_cast<int64_t>(P.max_seqs) * V.max_new;
     p.prefix = make_pass(V, most < V.rows ? most : V.rows, P.n_groups, H, wide_type, true);
@@ -253,8 +268,9 @@ size_t szo_attention_kv8_prefix_workspace_bytes(const szo_kv8_cache* cache, cons
   if (V.batch == 0 || V.max_new == 0 || V.rows == 0) return 0;
   // (for either kind of type: fp32 takes the kernel for few rows throughout, with other shares)
   const kv8::SharePlan a = kv8::share_plan(V, P, n_heads, cache->head_dim, false), b = kv8::share_plan(V, P, n_heads, cache->head_dim, true);
-  const size_t most = a.total > b.total ? a.total : b.total;
-  return most + (a.direct ? szo_attention_kv8_workspace_bytes(cache, batch, n_heads) : 0);
+  const size_t apart = a.direct || b.direct ? szo_attention_kv8_workspace_bytes(cache, batch, n_heads) : 0;
+  const size_t need_a = a.total + (a.direct ? apart : 0), need_b = b.total + (b.direct ? apart : 0);
+  return need_a > need_b ? need_a : need_b;
 }
 
 szo_status szo_attention_kv8_prefix(const szo_kv8_cache* cache, const szo_kv8_batch* batch, const szo_kv8_prefix* prefix, const void* q, int64_t q_stride,

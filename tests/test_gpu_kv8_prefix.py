@@ -173,6 +173,18 @@ def test_many_sequences(B, dt, group, count):
     assert B.device_status() == 0
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("new,most,hkv", [(1, 4, 4), (2, 4, 4), (2, 8, 4), (4, 2, 4), (1, 3, 1), (6, 3, 2), (18, 2, 4)])
+def test_many_prompts_of_few_sequences(B, dt, new, most, hkv):
+    """Prompts that fill the SMs by themselves: rows of a group that are cheaper together, and such that are not."""
+    sizes = [1 + (most - 1) * (g % 3 != 2) for g in range(40)]
+    lens = [49 + new + (7 * i) % 30 for i in range(sum(sizes))]
+    w = SharedWorld(B, sizes, [32 + 16 * (g % 2) for g in range(40)], lens, hkv, 16, 64, seed=33)
+    w.fill(lens)
+    check(B, w, lens, [new - (i % 4 == 3) for i in range(len(lens))], 4 * hkv, dt)
+    assert B.device_status() == 0
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("new,count", [(1, 3), (1, 40), (7, 20), (40, 9)])
 def test_sequences_of_no_group_and_batches_without_one(B, dt, new, count):
