@@ -382,7 +382,7 @@ szo_status szo_attention_kv8(const szo_kv8_cache* cache, const szo_kv8_batch* ba
  * own, a group with a skipped sequence, and every group where seqs does not ascend.  Results, arguments and errors otherwise as for
  * szo_attention_kv8, up to the order of sums (rows * n_heads below 2^31); rows at positions inside the shared part see what they see there.
  * Where a sequence's own rows fill the tensor cores' tiles (256 rows per key/value head), or all that the batch's tables could hold is
- * little (96 MB), sharing gains nothing and szo_attention_kv8 does the work.  workspace: szo_attention_kv8_prefix_workspace_bytes bytes (it
+ * little (96 MB), or prompts of few sequences fill the GPU by themselves, sharing gains nothing and szo_attention_kv8 does the work.  workspace: szo_attention_kv8_prefix_workspace_bytes bytes (it
  * depends on the shapes only: the output in fp32 once for each of the shares that the positions are cut into, two or a few with many rows,
  * dozens with few), contents irrelevant on entry; calls that may run at the same time need one
  * each. */
