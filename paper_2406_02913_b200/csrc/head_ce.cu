@@ -77,7 +77,8 @@ __global__ void __launch_bounds__(256) head_join_kernel(const float2* __restrict
     const float all = s * exp2f(m - tref) + exp2f(x - tref);
     total = all == 0.f ? -INFINITY : kLn2 * (tref + log2f(all));
     out = m - x > 64.f ? total - kLn2 * x : s == 0.f ? 0.f : log1pf(s * exp2f(m - x));
-    if (isnan(total)) out = total;
+    // (the target as far below everything as all else is: lse - x is the difference of two infinities)
+    if (isnan(total) || top == -INFINITY) out = __int_as_float(0x7fffffff);
   }
   if (isnan(total) || total == INFINITY) total = out = __int_as_float(0x7fffffff);
   loss[r] = out;

@@ -370,3 +370,27 @@ def test_agrees_with_the_log_probabilities_of_logits(B):
     x = (h.double() @ W.double().T).float()
     r = B.szo_token_logprobs(x, t.view(-1, 1))
     assert torch.allclose(got.lse, r.lse, rtol=0, atol=1e-4) and torch.allclose(got.loss, -r.logp[:, 0], rtol=0, atol=1e-4)
+
+
+@pytest.mark.parametrize("rows", [12, 200])
+def test_rows_whose_logits_are_all_minus_infinity(B, rows):
+    """log sum exp is -inf and the loss, a difference of two infinities, NaN; with a vocabulary of the target alone too.  Nothing of
+    them reaches a gradient."""
+    h, W, t, g = problem(rows, 400, 64, "bf16", 21, none=0.0)
+    W[:, 0] = -1e3
+    h[:, 0] = 0.0
+    dead = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    dead[[2, rows - 1]] = True
+    h[dead, 0] = 1e38
+    got = B.szo_head_ce(h, W, t)
+    assert (got.lse[dead] == -float("inf")).all() and got.loss[dead].isnan().all()
+    check_forward(B.HeadCe(got.loss[~dead], got.lse[~dead]), h[~dead], W, t[~dead], 1.0)
+    a = torch.randn(rows, device="cuda", generator=g)
+    dh, dW = B.szo_head_ce_bwd(h, W, t, got.lse, a)
+    assert (dh[dead] == 0).all()
+    wh, eh, wW, eW = backward_bounds(h[~dead], W, t[~dead], got.lse[~dead], a[~dead], None, 1.0, "bf16")
+    within(dh[~dead], wh, eh)
+    within(dW, wW, eW)
+    one = B.szo_head_ce(h, W[:1], torch.zeros_like(t))
+    assert (one.lse[dead] == -float("inf")).all() and one.loss[dead].isnan().all() and (one.loss[~dead] == 0).all()
+    assert B.device_status() == 0
