@@ -405,7 +405,7 @@ szo_status szo_attention_kv8_prefix(const szo_kv8_cache* cache, const szo_kv8_ba
  * h: dtype (SZO_BF16 or SZO_F16) [rows][d], W: the same dtype [vocab][d], rows h_stride / w_stride elements apart; d and the strides multiples
  * of 8.  Products are exact, sums fp32 in the tensor cores (whose additions truncate: some 3e-6 of a row's largest logits at d = 4096).  loss is formed from the other tokens' weights, so it keeps its relative precision
  * where the target has nearly all the probability.  A row whose logits hold a NaN or +inf has NaN results; one whose logits are all -inf has
- * lse -inf and loss NaN (a target alone of -inf: loss +inf). */
+ * lse -inf and loss NaN (a target alone of -inf: loss +inf).  Without a target the loss is 0 whatever the row holds. */
 size_t szo_head_ce_workspace_bytes(int64_t rows, int64_t vocab, int64_t d);
 szo_status szo_head_ce(const void* h, int64_t h_stride, const void* W, int64_t w_stride, szo_dtype dtype, int64_t rows, int64_t vocab,
                        int64_t d, float scale, const int32_t* targets, float* loss, float* lse, void* workspace, size_t workspace_bytes,

@@ -80,7 +80,10 @@ __global__ void __launch_bounds__(256) head_join_kernel(const float2* __restrict
     // (the target as far below everything as all else is: lse - x is the difference of two infinities)
     if (isnan(total) || top == -INFINITY) out = __int_as_float(0x7fffffff);
   }
-  if (isnan(total) || total == INFINITY) total = out = __int_as_float(0x7fffffff);
+  if (isnan(total) || total == INFINITY) {
+    total = __int_as_float(0x7fffffff);
+    if (t >= 0) out = total;                                      // (a row without a target may hold anything: no loss)
+  }
   loss[r] = out;
   if (lse != nullptr) lse[r] = total;
 }

@@ -394,3 +394,21 @@ def test_rows_whose_logits_are_all_minus_infinity(B, rows):
     one = B.szo_head_ce(h, W[:1], torch.zeros_like(t))
     assert (one.lse[dead] == -float("inf")).all() and one.loss[dead].isnan().all() and (one.loss[~dead] == 0).all()
     assert B.device_status() == 0
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("rows", [40, 300])
+def test_rows_without_a_target_have_no_loss_whatever_they_hold(B, dt, rows):
+    """A padding row's NaN or infinity stays in its lse: the losses' sum is that of the other rows."""
+    h, W, t, _ = problem(rows, 500, 64, dt, 22)
+    t[:4] = -1
+    none = t < 0
+    h[none, 3] = float("nan")
+    h[1], h[2, 5], h[3] = float("inf"), -float("inf"), 0.0
+    got = B.szo_head_ce(h, W, t)
+    assert (got.loss[none] == 0).all() and got.loss.isfinite().all()
+    odd = none.clone()
+    odd[3] = False                                        # (log of the vocabulary's size)
+    assert got.lse[odd].isnan().all()
+    check_forward(B.HeadCe(got.loss[~odd], got.lse[~odd]), h[~odd], W, t[~odd], 1.0)
+    assert B.device_status() == 0
