@@ -544,7 +544,8 @@ szo_status szo_model_enable_decode_kv8(szo_model_t* m, int32_t page_tokens, void
  * cache as their own.  Whole pages are shared and not copied, the rest of a last page is; the calls of szo_model_decode_step that follow
  * read the shared ones once for all (szo_attention_kv8_prefix).  They may not write positions below the shared pages' end
  * (SZO_ERR_INVALID_ARG).  B = 1 or n = 0 ends the sharing: other sequences than 0 then have their own pages again, with what they held
- * before.  Needs szo_model_enable_decode_kv8; may allocate. */
+ * before; positions behind the page that holds position n - 1 are a sequence's own throughout, so steps that were taken there while sharing
+ * have written them.  Needs szo_model_enable_decode_kv8; may allocate. */
 szo_status szo_model_decode_share(szo_model_t* m, int32_t B, int32_t n, void* stream);
 /* Next-token loss of every position of B sequences of S tokens, without logits being stored (szo_head_ce on the last hidden
  * states): loss fp32 [B*S] for targets int32 [B*S] (negative: none, loss 0; targets[b*S+s] is the token after position s), and lse

@@ -978,9 +978,10 @@ struct szo_model {
   double* d_scalars = nullptr;
   int64_t last_launches = 0;
   void *kcache = nullptr, *vcache = nullptr;     // [n_layers][max_batch][max_seq][n_kv_heads * head_dim], act dtype
-  // 8-bit cache (szo_model_enable_decode_kv8): sequence b owns the pages b * kv8_pages .. of every layer
-  uint8_t* kv8_codes = nullptr;                  // [n_layers][keys, values][max_batch * kv8_pages][n_kv_heads][kv8_page][head_dim]
-  float* kv8_scales = nullptr;                   // [n_layers] x kv8_scale_floats: [max_batch * kv8_pages][n_kv_heads][2]
+  // 8-bit cache (szo_model_enable_decode_kv8): sequence b owns the pages b * kv8_pages .. of every layer; behind them all each but the first
+  // has a page for its copy of the last part of a prompt that it shares
+  uint8_t* kv8_codes = nullptr;                  // [n_layers][keys, values][kv8_pool][n_kv_heads][kv8_page][head_dim]
+  float* kv8_scales = nullptr;                   // [n_layers] x kv8_scale_floats: [kv8_pool][n_kv_heads][2]
   int32_t *kv8_table = nullptr, *kv8_len = nullptr;    // [max_batch][kv8_pages]; [max_batch], set by every call
   void* kv8_ws = nullptr;
   size_t kv8_ws_bytes = 0;
@@ -990,8 +991,9 @@ struct szo_model {
   // one group of sequences, 0 and its end in the current call
   int kv8_sharers = 0, kv8_shared = 0;
   int32_t* kv8_group = nullptr;                  // [12]: the length at 0, the sequences at 4 (16-byte boundaries)
+  int64_t kv8_pool() const { return static_cast<int64_t>(cfg.max_batch) * kv8_pages + cfg.max_batch - 1; }      // pages of a layer
   int64_t kv8_scale_floats() const {             // of a layer; whole 16 bytes, on which every layer's scales have to start
-    return static_cast<int64_t>(round_up(static_cast<size_t>(cfg.max_batch) * kv8_pages * cfg.n_kv_heads * 2, 4));
+    return static_cast<int64_t>(round_up(static_cast<size_t>(kv8_pool()) * cfg.n_kv_heads * 2, 4));
   }
   float* h2 = nullptr;                           // [2][d_model]: second copy of the residual stream of a one- or two-row token step
   int sparse_dt = SZO_F32;                       // storage format of the sparse values (szo_model_set_sparse_storage)
@@ -1463,7 +1465,7 @@ szo_status run_decode_t(szo_model* m, const int32_t* tokens, int B, int Tn, cons
                                             Tn, H, Hkv, hd, 0, pos_dev));
         count_launch();
       }
-      const int64_t pages = static_cast<int64_t>(c.max_batch) * m->kv8_pages, bytes = pages * m->kv8_page * dkv;
+      const int64_t pages = m->kv8_pool(), bytes = pages * m->kv8_page * dkv;
       uint8_t* codes = m->kv8_codes + l * 2 * bytes;
       const szo_kv8_cache cache{codes, codes + bytes, m->kv8_scales + l * m->kv8_scale_floats(), pages, m->kv8_page, Hkv, hd};
       const szo_kv8_batch batch{m->kv8_table, m->kv8_len, nullptr, M, B, m->kv8_pages, Tn};
@@ -2029,9 +2031,9 @@ szo_status szo_model_enable_decode_kv8(szo_model_t* m, int32_t page_tokens, void
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int hd = c.d_model / c.n_heads;
   const int64_t per_seq = ceil_div(c.max_seq, page_tokens), pages = per_seq * c.max_batch;
-  SZO_REQUIRE(pages < (int64_t(1) << 31) / page_tokens / c.n_kv_heads, SZO_ERR_SHAPE, "max_batch * max_seq is too large for the 8-bit cache");
-  const size_t bytes = static_cast<size_t>(c.n_layers) * 2 * pages * page_tokens * c.n_kv_heads * hd;
+  SZO_REQUIRE(pages + c.max_batch <= (int64_t(1) << 31) / page_tokens / c.n_kv_heads, SZO_ERR_SHAPE, "max_batch * max_seq is too large for the 8-bit cache");
   m->kv8_pages = static_cast<int>(per_seq);
+  const size_t bytes = static_cast<size_t>(c.n_layers) * 2 * m->kv8_pool() * page_tokens * c.n_kv_heads * hd;
   const size_t scales = static_cast<size_t>(c.n_layers) * m->kv8_scale_floats() * sizeof(float);
   const size_t ws = kv8_attention_ws(hd);
   uint8_t* codes = nullptr;
@@ -2052,24 +2054,27 @@ szo_status szo_model_enable_decode_kv8(szo_model_t* m, int32_t page_tokens, void
   return SZO_OK;
 }
 
-// page_table[b][j] of every sequence: sequence 0's pages for the first `pages` places of sequences below `sharers`, else its own
-__global__ void shared_table_kernel(int32_t* __restrict__ table, int64_t n, int per_seq, int sharers, int pages) {
+// page_table[b][j] of every sequence: for sequences 1 .. sharers - 1 sequence 0's pages in the first `pages` places and (part) the page
+// behind the sequences' own in the next, else its own
+__global__ void shared_table_kernel(int32_t* __restrict__ table, int64_t n, int per_seq, int sharers, int pages, bool part) {
   const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
   if (i >= n) return;
   const int b = static_cast<int>(i / per_seq), j = static_cast<int>(i % per_seq);
-  table[i] = b < sharers && j < pages ? j : static_cast<int32_t>(i);
+  const bool shares = b > 0 && b < sharers;
+  table[i] = static_cast<int32_t>(shares && j < pages ? j : shares && part && j == pages ? n + b - 1 : i);
 }
-// Sequence 0's page `page` of every layer, codes and scales, to the same page of sequences 1 .. gridDim.y: grid (vectors, sequences, layers * 2)
-__global__ void copy_page_kernel(uint8_t* __restrict__ codes, int64_t kind_bytes, float* __restrict__ scales, int64_t scale_floats, int per_seq,
+// Sequence 0's page `page` of every layer, codes and scales, to pages first .. first + gridDim.y - 1: grid (vectors, sequences, layers * 2)
+__global__ void copy_page_kernel(uint8_t* __restrict__ codes, int64_t kind_bytes, float* __restrict__ scales, int64_t scale_floats, int64_t first,
                                  int page, int64_t page_bytes, int hkv) {
-  const int to = (static_cast<int>(blockIdx.y) + 1) * per_seq + page, kind = blockIdx.z & 1, layer = blockIdx.z >> 1;
+  const int64_t to = first + blockIdx.y;
+  const int kind = blockIdx.z & 1, layer = blockIdx.z >> 1;
   uint8_t* base = codes + blockIdx.z * kind_bytes;
   const int64_t i = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) * 16;
   if (i < page_bytes)
     *reinterpret_cast<uint4*>(base + to * page_bytes + i) = *reinterpret_cast<const uint4*>(base + static_cast<int64_t>(page) * page_bytes + i);
   float* sc = scales + layer * scale_floats;
   if (blockIdx.x == 0 && kind == 0)
-    for (int h = threadIdx.x; h < 2 * hkv; h += blockDim.x) sc[static_cast<int64_t>(to) * 2 * hkv + h] = sc[static_cast<int64_t>(page) * 2 * hkv + h];
+    for (int h = threadIdx.x; h < 2 * hkv; h += blockDim.x) sc[to * 2 * hkv + h] = sc[static_cast<int64_t>(page) * 2 * hkv + h];
 }
 
 szo_status szo_model_decode_share(szo_model_t* m, int32_t B, int32_t n, void* stream) {
@@ -2085,7 +2090,7 @@ szo_status szo_model_decode_share(szo_model_t* m, int32_t B, int32_t n, void* st
     // the most that szo_attention_kv8_prefix asks for: any number of sequences, and of new tokens up to those that share nothing; these ask
     // for what szo_attention_kv8 does and the groups' descriptions, a few words per sequence and row
     size_t need = kv8_attention_ws(hd) + 4 * 256 + (c.max_batch + m->Mmax) * sizeof(int32_t);
-    szo_kv8_cache cache{m->kv8_codes, m->kv8_codes, m->kv8_scales, static_cast<int64_t>(c.max_batch) * m->kv8_pages, m->kv8_page, c.n_kv_heads, hd};
+    szo_kv8_cache cache{m->kv8_codes, m->kv8_codes, m->kv8_scales, m->kv8_pool(), m->kv8_page, c.n_kv_heads, hd};
     const szo_kv8_prefix prefix{m->kv8_group, m->kv8_group + 4, 1, B};
     for (int b = 1; b <= c.max_batch; ++b)
       for (int T = 1; T <= 256 / G + 1 && T <= c.max_seq && static_cast<int64_t>(b) * T <= m->Mmax; ++T) {
@@ -2100,12 +2105,13 @@ szo_status szo_model_decode_share(szo_model_t* m, int32_t B, int32_t n, void* st
     m->kv8_ws_fits[B] = true;
   }
   const int64_t pages = static_cast<int64_t>(c.max_batch) * m->kv8_pages;
-  shared_table_kernel<<<blocks_for(pages, 256), 256, 0, st>>>(m->kv8_table, pages, m->kv8_pages, B, whole);
+  const bool part = n % m->kv8_page != 0;
+  shared_table_kernel<<<blocks_for(pages, 256), 256, 0, st>>>(m->kv8_table, pages, m->kv8_pages, B, whole, part);
   count_launch();
-  if (B > 1 && n % m->kv8_page != 0) {
+  if (B > 1 && part) {
     const int64_t bytes = static_cast<int64_t>(m->kv8_page) * c.n_kv_heads * hd;
-    copy_page_kernel<<<dim3(blocks_for(bytes / 16, 256), B - 1, 2 * c.n_layers), 256, 0, st>>>(m->kv8_codes, pages * bytes, m->kv8_scales,
-                                                                                           m->kv8_scale_floats(), m->kv8_pages, whole, bytes, c.n_kv_heads);
+    copy_page_kernel<<<dim3(blocks_for(bytes / 16, 256), B - 1, 2 * c.n_layers), 256, 0, st>>>(m->kv8_codes, m->kv8_pool() * bytes, m->kv8_scales,
+                                                                                           m->kv8_scale_floats(), pages, whole, bytes, c.n_kv_heads);
     count_launch();
   }
   set_i32_kernel<<<1, 1, 0, st>>>(m->kv8_group, whole * m->kv8_page);

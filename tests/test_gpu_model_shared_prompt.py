@@ -185,3 +185,28 @@ def test_scores_of_answers_to_one_prompt(B):
     assert torch.allclose(-lp.logp[:, 0], whole[:, 20], rtol=0.1, atol=0.2)
     assert B.device_status() == 0
     m.close()
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("page,n", [(16, 40), (16, 5), (32, 40), (16, 32)])
+def test_sequences_get_back_what_they_held(B, act, page, n):
+    """A part of a page that was taken over for the time of sharing is not lost: afterwards every sequence continues its own positions with
+    the logits that it had, to the bit."""
+    fx = DecoderFixture("tiny_gqa", seed=11, mask="random", B=4, S=64)
+    toks = torch.from_numpy(fx.batch(0)).cuda()
+    m = make(B, fx, act)
+    m.enable_decode(kv8_page_tokens=page)
+    m.decode_step(toks[:, :40].contiguous(), 0)
+    step = toks[:, 40:41].contiguous()
+    own = m.decode_step(step, 40).clone()
+    for sharers in (4, 3):
+        m.decode_share(sharers, n)
+        if n == 40:
+            shared = m.decode_step(step, 40)
+            assert not torch.allclose(shared[1], own[1], atol=1e-3) and not torch.allclose(shared[2], own[2], atol=1e-3)
+            if sharers == 3:                              # (the fourth has its own again)
+                assert (shared[3] - own[3]).abs().max() <= (2e-3 if act == "f32" else 4e-2) * own.abs().max()
+    m.decode_share(1, 0)
+    assert torch.equal(m.decode_step(step, 40), own)
+    assert B.device_status() == 0
+    m.close()
