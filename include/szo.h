@@ -414,7 +414,8 @@ szo_status szo_head_ce(const void* h, int64_t h_stride, const void* W, int64_t w
  *   G[r][j] = scale * ((a + d_lse[r]) p_j - a 1[j = t]),  p_j = exp(x[r][j] - lse[r]),  a = d_loss[r], 0 where t is outside [0, vocab)
  *   dh = G W      dtype [rows][d],  rows dh_stride apart (NULL: not wanted, as for dW)
  *   dW = G^T h    dtype [vocab][d], rows dw_stride apart; not added to what is there
- * G exists only for a piece of the vocabulary at a time, rounded to dtype (for SZO_F16 relative to the power of two of its row's
+ * G exists only for pieces of the vocabulary (three of some 64 MB at a time; above 8192 rows 24 KB per row, but dh alone of a vocabulary above
+ * 12288 goes over some thousand rows after the other), rounded to dtype (for SZO_F16 relative to the power of two of its row's
  * weights, so that small weights lose nothing); all sums are fp32 and each result is rounded once.  A row that weighs
  * nothing (no target and d_lse 0, or an lse of -inf) gives dh zeros and adds nothing to dW, whatever its h holds.  In dW of SZO_F16 a row whose
  * weight is 2^-j of the largest one's enters with h * 2^-j rounded to fp16, so elements of h below 2^(j-14) lose bits.

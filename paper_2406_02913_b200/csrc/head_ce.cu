@@ -243,17 +243,20 @@ Plan forward_plan(const Shape& s) {
   p.total = take.at;
   return p;
 }
-// Gradient.  G of a piece is about 64 MB (half of L2), and a piece 8192 to 65536 entries.  Many rows: one launch for all pieces, dh and dW
+// Gradient.  G of a piece is about 64 MB (half of L2), and a piece 4096 to 65536 entries: so up to 8192 rows three pieces' G stay below 200 MB, and
+// more rows take 24 KB each (32768 x 32000 x 4096, both gradients: least pieces of 2048 entries 24.0 ms, 4096 22.7, 8192 23.9: dh's sums are
+// written and read once per piece).  Many rows: one launch for all pieces, dh and dW
 // following G `lag` pieces behind, far enough that hardly a unit waits for one that runs beside it, and no SM for the end of a piece (4096 rows
 // of 32000 x 4096 in a launch per piece 1614 us, in one 1476); the sums of dh are kept in one place, piece after piece.  Few rows: a launch per
 // piece, since units that wait for others cost more than the end of a launch there (16 rows of 32000 x 4096 84 us, in one launch
 // 107, with dh so close behind G that it finds W in L2); the sums of the pieces are kept apart.
+constexpr int64_t kLeastPiece = 4096;
 Plan backward_plan(const Shape& s, bool dh, bool dw) {
   Plan p = {};
   Taker take;
   const bool is_few = few(s.rows);
   int64_t piece = (int64_t(64) << 20) / (2 * s.rows);
-  piece = piece < 8192 ? 8192 : piece > 65536 ? 65536 : piece;
+  piece = piece < kLeastPiece ? kLeastPiece : piece > 65536 ? 65536 : piece;
   if (piece > s.vocab) piece = s.vocab;
   p.piece = static_cast<int64_t>(round_up(static_cast<size_t>(piece), kTile));
   p.pieces = static_cast<int>(ceil_div(s.vocab, p.piece));
@@ -283,6 +286,13 @@ Plan backward_plan(const Shape& s, bool dh, bool dw) {
   if (dh) p.acc = take(static_cast<size_t>(p.sums) * s.rows * s.d * sizeof(float));
   p.total = take.at;
   return p;
+}
+// dh alone of more rows, where G is more than the pieces that are kept: up to 8192 of them at a time, in equal shares, which bounds the workspace
+// (65536 x 32000 x 4096: 320 MB and 29.0 ms, at once 2.5 GB and 31.4)
+int64_t rows_at_once(const Shape& s, bool dw) {
+  constexpr int64_t kMost = 8192;
+  if (dw || s.rows <= kMost || s.vocab <= 3 * kLeastPiece) return s.rows;
+  return static_cast<int64_t>(round_up(static_cast<size_t>(ceil_div(s.rows, ceil_div(s.rows, kMost))), kTile));
 }
 bool fits(int64_t rows, int64_t vocab, int64_t d) {
   constexpr int64_t kMost = 0x7fffff00, kTiles = 1 << 25;        // (tiles of a product, and blocks of a launch, are counted in 32 bits)
@@ -543,7 +553,10 @@ szo_status szo_head_ce(const void* h, int64_t h_stride, const void* W, int64_t w
 
 size_t szo_head_ce_bwd_workspace_bytes(int64_t rows, int64_t vocab, int64_t d, int32_t want_dh, int32_t want_dw) {
   if (!head::fits(rows, vocab, d) || rows == 0 || (!want_dh && !want_dw)) return 0;
-  return head::backward_plan({rows, vocab, d}, want_dh != 0, want_dw != 0).total;
+  const int64_t most = head::rows_at_once({rows, vocab, d}, want_dw != 0), last = rows - (ceil_div(rows, most) - 1) * most;
+  const size_t a = head::backward_plan({most, vocab, d}, want_dh != 0, want_dw != 0).total;
+  const size_t b = head::backward_plan({last, vocab, d}, want_dh != 0, want_dw != 0).total;      // (fewer rows may sum dh in more shares)
+  return a > b ? a : b;
 }
 
 szo_status szo_head_ce_bwd(const void* h, int64_t h_stride, const void* W, int64_t w_stride, szo_dtype dtype, int64_t rows, int64_t vocab, int64_t d,
@@ -564,14 +577,19 @@ szo_status szo_head_ce_bwd(const void* h, int64_t h_stride, const void* W, int64
   const size_t need = szo_head_ce_bwd_workspace_bytes(rows, vocab, d, dh != nullptr, dW != nullptr);
   SZO_REQUIRE(workspace && workspace_bytes >= need, SZO_ERR_WORKSPACE, "workspace: %zu bytes needed, %zu given", need,
               workspace ? workspace_bytes : size_t(0));
-  const head::Shape s{rows, vocab, d};
   auto* ws = static_cast<unsigned char*>(workspace);
   int32_t* status = device_status_word();
   SZO_REQUIRE(status != nullptr, SZO_ERR_CUDA, "no device status word (no CUDA device?)");
-  auto run = [&](auto zero) {
+  const int64_t most = head::rows_at_once({rows, vocab, d}, dW != nullptr);
+  auto run = [&](auto zero) -> szo_status {
     using T = decltype(zero);
-    return head::backward<T>(s, {static_cast<const T*>(h), h_stride, static_cast<const T*>(W), w_stride, scale, targets}, lse, d_loss, d_lse,
-                             static_cast<T*>(dh), dh_stride, static_cast<T*>(dW), dw_stride, ws, status, st);
+    for (int64_t r = 0; r < rows; r += most) {                    // (r is a multiple of 256: everything stays aligned)
+      const head::Shape s{rows - r < most ? rows - r : most, vocab, d};
+      SZO_TRY(head::backward<T>(s, {static_cast<const T*>(h) + r * h_stride, h_stride, static_cast<const T*>(W), w_stride, scale, targets + r}, lse + r,
+                                d_loss + r, d_lse != nullptr ? d_lse + r : nullptr, dh != nullptr ? static_cast<T*>(dh) + r * dh_stride : nullptr, dh_stride,
+                                static_cast<T*>(dW), dw_stride, ws, status, st));
+    }
+    return SZO_OK;
   };
   return dtype == SZO_BF16 ? run(__nv_bfloat16{}) : run(__half{});
 }

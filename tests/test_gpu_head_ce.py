@@ -412,3 +412,30 @@ def test_rows_without_a_target_have_no_loss_whatever_they_hold(B, dt, rows):
     assert got.lse[odd].isnan().all()
     check_forward(B.HeadCe(got.loss[~odd], got.lse[~odd]), h[~odd], W, t[~odd], 1.0)
     assert B.device_status() == 0
+
+
+@pytest.mark.parametrize("dt,rows,vocab,d", [("bf16", 17000, 12301, 64), ("f16", 9001, 13345, 136), ("bf16", 9000, 700, 72), ("f16", 33000, 12289, 72),
+                                             ("bf16", 8193, 16001, 264)])
+def test_many_rows(B, dt, rows, vocab, d):
+    """Pieces of the vocabulary at their shortest, with their buffers used again; dh alone of some thousand rows at a time (4352 and
+    3841 to four times 6656 and 6376), into a slice and with nothing around it touched."""
+    h, W, t, g = problem(rows, vocab, d, dt, seed=rows)
+    got = B.szo_head_ce(h, W, t)
+    check_forward(got, h, W, t, 1.0)
+    a, b = torch.randn(rows, device="cuda", generator=g), 0.2 * torch.randn(rows, device="cuda", generator=g)
+    dh, dW = B.szo_head_ce_bwd(h, W, t, got.lse, a, b)
+    wh, eh, wW, eW = backward_bounds(h, W, t, got.lse, a, b, 1.0, dt)
+    within(dh, wh, eh)
+    within(dW, wW, eW)
+    assert torch.equal(B.szo_head_ce_bwd(h, W, t, got.lse, a, b, need_dh=False)[1], dW)
+    wide = torch.full((rows + 2, d + 16), 7.0, dtype=DT[dt], device="cuda")
+    alone = B.szo_head_ce_bwd(h, W, t, got.lse, a, b, out_dh=wide[1:-1, 8:-8], need_dW=False)[0].clone()
+    within(alone, wh, eh)
+    wide[1:-1, 8:-8] = 7.0
+    assert (wide == 7).all()
+    L, n = B.lib(), B.lib().szo_head_ce_bwd_workspace_bytes(rows, vocab, d, 1, 0)
+    ws, out = torch.full((n + 16,), 0x7f, dtype=torch.uint8, device="cuda"), torch.empty_like(h)
+    B._check(L.szo_head_ce_bwd(h.data_ptr(), d, W.data_ptr(), d, 1 if dt == "bf16" else 2, rows, vocab, d, 1.0, t.data_ptr(), got.lse.data_ptr(), a.data_ptr(),
+                               b.data_ptr(), out.data_ptr(), d, None, 0, ws.data_ptr(), n, torch.cuda.current_stream().cuda_stream))
+    assert torch.equal(out, alone) and (ws[n:] == 0x7f).all()
+    assert B.device_status() == 0

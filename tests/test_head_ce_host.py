@@ -117,3 +117,18 @@ def test_the_gradient_s_formula_against_differences():
                 pair = [(x + s * step if x is h else h, x + s * step if x is W else W) for s in (1, -1)]
                 diff = (total(*pair[0]) - total(*pair[1])) / 2e-5
                 assert abs(diff - float(want[i, j])) < 1e-8 * 50        # third derivatives of order 1 times 1e-10, and 1e-16 / 1e-5
+
+
+@pytest.mark.parametrize("rows", [129, 4096, 5000, 8192, 8193, 16384, 65536, 300001])
+@pytest.mark.parametrize("vocab", [8192, 50272, 200000])
+def test_a_gradient_holds_three_pieces_of_g(B, rows, vocab):
+    """However many rows: pieces of 64 MB (rounded up to 256 entries), or of 4096 entries where that is more; for dh alone of a large
+    vocabulary 8192 rows at a time."""
+    d, L = 4096, B.lib()
+    others = 16 * rows + 8 * vocab + 4096                          # the rows' weights, counters
+
+    def bound(n):
+        # three pieces, and dh in fp32 (in up to 16 shares where there are few tiles)
+        return 3 * (max(64 << 20, 2 * 4096 * n) + 2 * 256 * n) + 4 * n * d * (16 if n < 1024 else 1)
+    assert L.szo_head_ce_bwd_workspace_bytes(rows, vocab, d, 1, 0) <= bound(rows if vocab == 8192 else min(rows, 8192)) + others
+    assert L.szo_head_ce_bwd_workspace_bytes(rows, vocab, d, 1, 1) <= bound(rows) + 2 * rows * d + others
