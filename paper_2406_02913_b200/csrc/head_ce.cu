@@ -17,7 +17,7 @@ namespace head {
 
 namespace {
 
-constexpr int kNoExponent = static_cast<int>(0x80808080u);       // (below every exponent; what a memset of 0x80 leaves)
+constexpr int kNoExponent = static_cast<int>(0x80808080u);       // (below every exponent)
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 template <typename T> __device__ __forceinline__ float widen(T x);
@@ -212,7 +212,7 @@ struct Plan {
   size_t total;
   int parts;                                                      // forward: of the vocabulary
   int64_t piece;                                                  // vocabulary entries of a piece of G
-  int pieces, lag, buffers;
+  int pieces, buffers;
   int dh_parts, sums;                                             // shares of dh's sum over a piece; sums kept apart in all
 };
 struct Taker {
@@ -246,8 +246,8 @@ Plan forward_plan(const Shape& s) {
 // Gradient.  G of a piece is about 64 MB (half of L2), and a piece 4096 to 65536 entries: so up to 8192 rows three pieces' G stay below 200 MB, and
 // more rows take 24 KB each (32768 x 32000 x 4096, both gradients: least pieces of 2048 entries 24.0 ms, 4096 22.7, 8192 23.9: dh's sums are
 // written and read once per piece).  Many rows: one launch for all pieces, dh and dW
-// following G `lag` pieces behind, far enough that hardly a unit waits for one that runs beside it, and no SM for the end of a piece (4096 rows
-// of 32000 x 4096 in a launch per piece 1614 us, in one 1476); the sums of dh are kept in one place, piece after piece.  Few rows: a launch per
+// following G a piece behind (of 256 units of logits at least, more than three for every pair of SMs), so that hardly a unit waits for one that
+// runs beside it, and no SM for the end of a piece (4096 rows of 32000 x 4096 in a launch per piece 1614 us, in one 1476); the sums of dh are kept in one place, piece after piece.  Few rows: a launch per
 // piece, since units that wait for others cost more than the end of a launch there (16 rows of 32000 x 4096 84 us, in one launch
 // 107, with dh so close behind G that it finds W in L2); the sums of the pieces are kept apart.
 constexpr int64_t kLeastPiece = 4096;
@@ -260,9 +260,7 @@ Plan backward_plan(const Shape& s, bool dh, bool dw) {
   if (piece > s.vocab) piece = s.vocab;
   p.piece = static_cast<int64_t>(round_up(static_cast<size_t>(piece), kTile));
   p.pieces = static_cast<int>(ceil_div(s.vocab, p.piece));
-  p.lag = is_few ? 1 : static_cast<int>(ceil_div(kPairs + kPairs / 4, tiles_of(s.rows) * ceil_div(p.piece, kTile)));
-  if (p.lag > p.pieces) p.lag = p.pieces;
-  p.buffers = p.lag + 2 < p.pieces ? p.lag + 2 : p.pieces;
+  p.buffers = p.pieces < 3 ? p.pieces : 3;                        // (written, read, and the one whose last readers may still run)
   p.info = take(static_cast<size_t>(s.rows) * sizeof(float4));
   p.exponent = take(sizeof(int32_t));
   p.counters = take(static_cast<size_t>(counters_of(p.pieces)) * sizeof(int32_t));
@@ -442,7 +440,6 @@ szo_status backward(const Shape& s, const Inputs<T>& in, const float* lse, const
   P.vocab = static_cast<int>(s.vocab);
   P.piece = static_cast<int>(p.piece);
   P.pieces = p.pieces;
-  P.lag = p.lag;
   P.buffers = p.buffers;
   P.targets = in.targets;
   P.info = info;
@@ -493,15 +490,15 @@ szo_status backward(const Shape& s, const Inputs<T>& in, const float* lse, const
     P.job[0].keep_from = static_cast<int>(s.vocab - kKept / (s.d * 2));
     P.job[1].keep_from = 0;
   }
-  const int steps = p.pieces + p.lag;
+  const int steps = p.pieces + 1;
   int64_t all = 0;                                                // (below 2^31: see fits)
   for (int i = 0; i < steps; ++i) {
-    const int64_t n = units(0, i) + units(1, i - p.lag) + units(2, i - p.lag);
+    const int64_t n = units(0, i) + units(1, i - 1) + units(2, i - 1);
     if (few(s.rows)) {
       P.step = i;
       P.units = static_cast<int>(n);
       P.idle = 0;
-      for (int k = 0; k < 3; ++k) P.idle |= units(k, k == 0 ? i : i - p.lag) == 0 ? 1 << k : 0;
+      for (int k = 0; k < 3; ++k) P.idle |= units(k, k == 0 ? i : i - 1) == 0 ? 1 << k : 0;
       SZO_TRY(launch_jobs<T>(P, true, true, st));
     }
     all += n;

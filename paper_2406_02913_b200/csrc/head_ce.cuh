@@ -41,12 +41,12 @@ struct Job {
   int m_band;                                  // tiles of m are taken in bands of m_band (0: all)
   Extent full, last;                           // over a piece, over the last one
 };
-// The units of work, in their order: for s = 0, 1, ..  job 0 of piece s, then jobs 1 and 2 of piece s - lag.  Jobs 1 and 2 read what job 0
+// The units of work, in their order: for s = 0, 1, ..  job 0 of piece s, then jobs 1 and 2 of piece s - 1.  Jobs 1 and 2 read what job 0
 // has written of their piece, in a ring of buffers.  A launch takes all steps s, its units handed out as they are asked for and waiting for
 // what they read (`counters`), or one step, its units dealt out in turn.
 struct Jobs {
   Job job[3];
-  int vocab, piece, pieces, lag, buffers;
+  int vocab, piece, pieces, buffers;
   int step, units;                             // the first step of the launch, and its units
   int idle;                                    // bit j: the launch has no units of job j (the ring need not hold its operands)
   int b_at, stage_bytes, stages;               // the ring of operands: B's place in a stage (set by launch_jobs)

@@ -194,7 +194,7 @@ template <bool kFew> struct Walk {
   __device__ __forceinline__ Unit seek(const Jobs& P, int u) {
     Unit r;
     while (true) {
-      r.i = j == 0 ? s : s - P.lag;
+      r.i = j == 0 ? s : s - 1;
       const int n = units_of(P, j, r.i);
       if (u < first + n) break;
       first += n;
