@@ -987,10 +987,10 @@ struct szo_model {
   size_t kv8_ws_bytes = 0;
   std::vector<bool> kv8_ws_fits;                 // by the number of sequences that share: kv8_ws is large enough
   int kv8_page = 0, kv8_pages = 0;
-  // sequences 0 .. kv8_sharers - 1 share their first kv8_shared positions (szo_model_decode_share); on the device: that number, and the
-  // one group of sequences, 0 and its end in the current call
+  // sequences 0 .. kv8_sharers - 1 share their first kv8_shared positions (szo_model_decode_share); on the device, where replayed steps find
+  // what holds by then: the positions, the one group of sequences, 0 and its end in the current call, and the sequences that share
   int kv8_sharers = 0, kv8_shared = 0;
-  int32_t* kv8_group = nullptr;                  // [12]: the length at 0, the sequences at 4 (16-byte boundaries)
+  int32_t* kv8_group = nullptr;                  // [12]: the length at 0, the sequences at 4 (16-byte boundaries), the sharers at 8
   int64_t kv8_pool() const { return static_cast<int64_t>(cfg.max_batch) * kv8_pages + cfg.max_batch - 1; }      // pages of a layer
   int64_t kv8_scale_floats() const {             // of a layer; whole 16 bytes, on which every layer's scales have to start
     return static_cast<int64_t>(round_up(static_cast<size_t>(kv8_pool()) * cfg.n_kv_heads * 2, 4));
@@ -2054,6 +2054,8 @@ szo_status szo_model_enable_decode_kv8(szo_model_t* m, int32_t page_tokens, void
   return SZO_OK;
 }
 
+// The group's end in a step: no more sequences than the step was laid out for, and than share now
+__global__ void group_end_kernel(int32_t* group, int most) { group[5] = min(most, group[8]); }
 // page_table[b][j] of every sequence: for sequences 1 .. sharers - 1 sequence 0's pages in the first `pages` places and (part) the page
 // behind the sequences' own in the next, else its own
 __global__ void shared_table_kernel(int32_t* __restrict__ table, int64_t n, int per_seq, int sharers, int pages, bool part) {
@@ -2114,12 +2116,13 @@ szo_status szo_model_decode_share(szo_model_t* m, int32_t B, int32_t n, void* st
                                                                                            m->kv8_scale_floats(), pages, whole, bytes, c.n_kv_heads);
     count_launch();
   }
-  set_i32_kernel<<<1, 1, 0, st>>>(m->kv8_group, whole * m->kv8_page);
-  set_i32_kernel<<<1, 1, 0, st>>>(m->kv8_group + 4, 0);
-  count_launch(2);
-  SZO_CHECK_LAUNCH("the kernels of szo_model_decode_share");
-  m->kv8_sharers = whole > 0 ? B : 0;
+  m->kv8_sharers = B > 1 && whole > 0 ? B : 0;
   m->kv8_shared = B > 1 ? whole * m->kv8_page : 0;
+  set_i32_kernel<<<1, 1, 0, st>>>(m->kv8_group, m->kv8_shared);
+  set_i32_kernel<<<1, 1, 0, st>>>(m->kv8_group + 4, 0);
+  set_i32_kernel<<<1, 1, 0, st>>>(m->kv8_group + 8, m->kv8_sharers);
+  count_launch(3);
+  SZO_CHECK_LAUNCH("the kernels of szo_model_decode_share");
   return SZO_OK;
 }
 
@@ -2177,7 +2180,7 @@ szo_status szo_model_decode_step(szo_model_t* m, const int32_t* tokens, int32_t 
     fill_i32_kernel<<<blocks_for(B, 256), 256, 0, st>>>(m->kv8_len, B, pos0 + T);
     count_launch();
     if (m->kv8_sharers > 1) {
-      set_i32_kernel<<<1, 1, 0, st>>>(m->kv8_group + 5, B < m->kv8_sharers ? B : m->kv8_sharers);
+      group_end_kernel<<<1, 1, 0, st>>>(m->kv8_group, B < m->kv8_sharers ? B : m->kv8_sharers);
       count_launch();
     }
   }

@@ -210,3 +210,31 @@ def test_sequences_get_back_what_they_held(B, act, page, n):
     assert torch.equal(m.decode_step(step, 40), own)
     assert B.device_status() == 0
     m.close()
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+def test_captured_steps_follow_the_sharing_of_their_replay(B, act):
+    """A step captured by its caller while four sequences share a prompt, replayed when two of them do, when none does and when the prompt is
+    another one: every time the logits of the same step made then."""
+    fx = DecoderFixture("tiny_gqa", seed=12, mask="random", B=4, S=64, n_layers=2)
+    toks = torch.from_numpy(fx.batch(0)).cuda()
+    m = make(B, fx, act, max_seq=131072, max_batch=4, loss_kind=B.LOSS_CLS2)      # (room: shared pages are read apart)
+    m.enable_decode(kv8_page_tokens=16)
+    m.decode_step(toks[:, :40].contiguous(), 0)
+    step, out = toks[:, 40:41].contiguous(), torch.empty(4, fx.shape["vocab"], device="cuda")
+    m.decode_share(4, 32)
+    m.decode_step(step, 40)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        m.decode_step(step, 40, logits=out)
+    seen = []
+    for sharers, n in ((4, 32), (2, 32), (1, 32), (3, 16), (4, 0), (4, 35)):
+        m.decode_share(sharers, n)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = m.decode_step(step, 40)
+        assert (out - want).abs().max() <= (2e-3 if act == "f32" else 4e-2) * want.abs().max(), (sharers, n)
+        seen.append(want)
+    assert (seen[0] - seen[2]).abs().max() > 0.1 * seen[0].abs().max()            # (whose pages are read does matter)
+    assert B.device_status() == 0
+    m.close()
