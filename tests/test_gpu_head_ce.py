@@ -439,3 +439,35 @@ def test_many_rows(B, dt, rows, vocab, d):
                                b.data_ptr(), out.data_ptr(), d, None, 0, ws.data_ptr(), n, torch.cuda.current_stream().cuda_stream))
     assert torch.equal(out, alone) and (ws[n:] == 0x7f).all()
     assert B.device_status() == 0
+
+
+@pytest.mark.parametrize("dt,rows,vocab,d", [("bf16", 17, 33001, 1032), ("f16", 17, 33001, 1032), ("bf16", 100, 70001, 520), ("bf16", 128, 8300, 4096)])
+def test_few_rows_of_a_large_matrix(B, dt, rows, vocab, d):
+    """W of more than 64 MB, whose last part the gradient keeps in L2 between its two readings: kept from within a tile on, over one piece of
+    G and over two."""
+    assert vocab * d * 2 > 64 << 20
+    h, W, t, g = problem(rows, vocab, d, dt, seed=rows + d)
+    t[0] = vocab - 1
+    lse = B.szo_head_ce(h, W, t).lse
+    a, b = torch.randn(rows, device="cuda", generator=g), 0.2 * torch.randn(rows, device="cuda", generator=g)
+    dh, dW = B.szo_head_ce_bwd(h, W, t, lse, a, b)
+    wh, eh, wW, eW = backward_bounds(h, W, t, lse, a, b, 1.0, dt)
+    within(dh, wh, eh)
+    within(dW, wW, eW)
+    assert torch.equal(B.szo_head_ce_bwd(h, W, t, lse, a, b, need_dW=False)[0], dh)
+    assert torch.equal(B.szo_head_ce_bwd(h, W, t, lse, a, b, need_dh=False)[1], dW)
+    assert B.device_status() == 0
+
+
+@pytest.mark.parametrize("dt,rows,vocab,d", [("bf16", 3137, 700, 8192), ("f16", 3400, 523, 8192), ("bf16", 3137, 10900, 8192), ("bf16", 1600, 300, 16392)])
+def test_rows_taken_in_bands(B, dt, rows, vocab, d):
+    """Hidden states of more than 48 MB go by in bands of row tiles (7 and 6 of 13; 7 of 14; the same over two pieces of G; 4 and 3 of 7)."""
+    h, W, t, g = problem(rows, vocab, d, dt, seed=rows + d)
+    got = B.szo_head_ce(h, W, t)
+    check_forward(got, h, W, t, 1.0)
+    a = torch.randn(rows, device="cuda", generator=g)
+    dh, dW = B.szo_head_ce_bwd(h, W, t, got.lse, a)
+    wh, eh, wW, eW = backward_bounds(h, W, t, got.lse, a, None, 1.0, dt)
+    within(dh, wh, eh)
+    within(dW, wW, eW)
+    assert B.device_status() == 0

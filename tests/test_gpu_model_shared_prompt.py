@@ -238,3 +238,56 @@ def test_captured_steps_follow_the_sharing_of_their_replay(B, act):
     assert (seen[0] - seen[2]).abs().max() > 0.1 * seen[0].abs().max()            # (whose pages are read does matter)
     assert B.device_status() == 0
     m.close()
+
+
+@pytest.mark.parametrize("dt,count,new", [("bf16", 12, 1), ("f16", 5, 3), ("bf16", 20, 9)])
+def test_attention_losses_and_gradient_of_answers_to_one_prompt(B, dt, count, new):
+    """The operators as they follow one another: answers attend to a prompt that they share, what comes out are the hidden states whose losses
+    are taken, and the gradient of these goes back to them; by themselves, and captured into one graph that then serves other contents."""
+    from tests import test_gpu_head_ce as head
+    H, hkv, d, page, prefix, vocab = 8, 2, 64, 32, 4000, 1203
+    g = torch.Generator("cuda").manual_seed(count)
+    lens, whole = [prefix + new + (37 * b) % 150 for b in range(count)], prefix // page
+    per = -(-(96 << 20) // (count * page * hkv * d * 2)) + 1      # (room: shared pages are read apart)
+    order = torch.randperm(whole + count * 8, device="cuda", generator=g).int()
+    table = torch.full((count, max(per, whole + 8)), -7, dtype=torch.int32, device="cuda")
+    table[:, :whole] = order[:whole]
+    table[:, whole:whole + 8] = order[whole:].view(count, 8)
+    codes = torch.randint(0, 256, (2, whole + count * 8, hkv, page, d), dtype=torch.uint8, device="cuda", generator=g)
+    codes[(codes & 127) == 127] = 3
+    scales = torch.exp2(torch.randint(-9, -6, (whole + count * 8, hkv, 2), device="cuda", generator=g).float())
+    cache, rows = B.Kv8Cache(codes, scales), count * new
+    batch = B.Kv8Batch(table, torch.tensor(lens, dtype=torch.int32, device="cuda"), rows)
+    shared = B.Kv8Prefix(torch.tensor([prefix], dtype=torch.int32, device="cuda"))
+    q = torch.randn(rows, H, d, device="cuda", generator=g).to(head.DT[dt])
+    W = (torch.randn(vocab, H * d, device="cuda", generator=g) / 8).to(head.DT[dt])
+    t = torch.randint(-1, vocab, (rows,), dtype=torch.int32, device="cuda", generator=g)
+    a = torch.randn(rows, device="cuda", generator=g)
+
+    def both():
+        o = B.szo_attention_kv8_prefix(cache, batch, shared, q)
+        r = B.szo_head_ce(o.view(rows, H * d), W, t)
+        return (o, r.loss, r.lse) + B.szo_head_ce_bwd(o.view(rows, H * d), W, t, r.lse, a)
+    o, loss, lse, dh, dW = first = both()
+    # (the bound of test_agrees_with_attention_that_shares_nothing: values up to 3.5, two results of the same kind)
+    logit = ((d + 8) * 2.0 ** -23 + 2.0 ** -20) * 6 * 3.5 * d ** 0.5
+    each = 3.5 * (2.0 ** -11 + 2 * logit + (max(lens) + 16) * 2.0 ** -23 + torch.finfo(o.dtype).eps / 2)
+    assert (B.szo_attention_kv8(cache, batch, q).double() - o.double()).abs().max() <= 2 * each
+    h = o.view(rows, H * d)
+    head.check_forward(B.HeadCe(loss, lse), h, W, t, 1.0)
+    wh, eh, wW, eW = head.backward_bounds(h, W, t, lse, a, None, 1.0, dt)
+    head.within(dh, wh, eh)
+    head.within(dW, wW, eW)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = both()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(first, captured))
+    q.neg_()
+    shared.length.fill_(prefix // 2)
+    t.copy_(t.flip(0))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(captured, both()))
+    assert B.device_status() == 0
