@@ -356,7 +356,8 @@ void sizes(Job* j, Kind kind, int vocab_dim, int64_t m, int64_t n, int64_t k, in
   j->full = extent(piece);
   j->last = extent(last);
 }
-// Tiles of m in equal bands whose part of A (16-bit) is at most 48 MB: it stays in L2 while B goes by
+// Tiles of m in equal bands whose part of A (16-bit) is at most 48 MB: it stays in L2 while B goes by (loss in bands / in one: 8192 rows of
+// 32000 x 4096 1.30 / 1.39 ms, 16384 2.8 to 3.0 / 3.7 to 3.8, 8192 of 50272 x 8192 5.1 / 5.9)
 int band_of(int64_t m, int64_t k) {
   const int64_t tiles = tiles_of(m), most = (int64_t(48) << 20) / (kTile * k * 2);
   if (tiles <= most || most < 1) return 0;

@@ -15,8 +15,8 @@
 //   warp 21          brings the codes by TMA, 64 positions of keys or values per slot of a small ring, and the pages' scales
 //                    (with the converting warps loading for themselves the latency of a step's loads showed: they have
 //                    no registers for a second set)
-// Measured: 2 sequences of 2048 new tokens at 8192 positions, 32 heads over 8 of 128, 526 us (875 TFLOP/s, 0.52 of the measured
-// burst rate of dense products, 0.63 of the sustained one).  A step of 128 positions takes 4500 cycles against 2048 for its
+// Measured: 2 sequences of 2048 new tokens at 8192 positions, 32 heads over 8 of 128, 508 us (906 TFLOP/s, 0.54 of the measured
+// burst rate of dense products, 0.65 of the sustained one).  A step of 128 positions takes 4500 cycles against 2048 for its
 // products: a row tile's scores wait 1400 for both tiles' products, its maxima take 700, their exchange 270, its weights 1850
 // (2048 for both tiles by the exponentials' rate), and the next products wait for them.  Copying and converting (1900 and
 // 3100 cycles a step, on their own warps) hide behind that.
